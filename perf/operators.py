@@ -166,14 +166,15 @@ def _random_bytes(g, rows, cols):
 
 
 def _pack(values):
-    """The codes (two to a byte, the even element in the low half, rows of whole blocks of 256) and scale bytes of a
-    matrix that a program has as 4-bit weights or kept activations."""
+    """The codes (two to a byte, the even element in the low half, rows filled up to a multiple of 256) and scale bytes
+    (rows filled up to a multiple of 16) of a matrix that a program has as 4-bit weights or kept activations."""
     rows, cols = values.shape
     wide = _up(cols, 256)
     t, byte, sign = _scaled(torch.nn.functional.pad(values.float(), (0, wide - cols)), False)
     code = _nearest_code(t) + 8 * sign
     code = code.to(torch.uint8).reshape(rows, wide // 2, 2)
-    return (code[..., 0] | code[..., 1] << 4).contiguous(), byte.to(torch.uint8).contiguous()
+    byte = torch.nn.functional.pad(byte.to(torch.uint8), (0, _up(wide // 32, 16) - wide // 32))
+    return (code[..., 0] | code[..., 1] << 4).contiguous(), byte.contiguous()
 
 
 def prepare(case, seed):
@@ -310,7 +311,8 @@ def _plain_unpack(packed, cols):
     rows = codes.shape[0]
     table = torch.tensor(GRID + tuple(-v for v in GRID), device="cuda")
     q = table[torch.stack((codes & 15, codes >> 4), -1).long()]
-    return (q.reshape(rows, -1, 32) * _scale_of(byte)[..., None]).reshape(rows, -1)[:, :cols]
+    q = q.reshape(rows, -1, 32)
+    return (q * _scale_of(byte)[:, :q.shape[1], None]).reshape(rows, -1)[:, :cols]
 
 
 def _plain_master(param, rho):
@@ -486,7 +488,7 @@ def _exact_unpack(packed, cols):
     power = torch.where(size < 2, 0, size // 2 - 1).double()                  # exponent and mantissa bits of a code
     value = torch.where(size < 2, size / 2, torch.exp2(power) * (1 + (size % 2) / 2)) * (1 - 2 * (nibbles // 8))
     scale = torch.exp2(byte.double() - 127).repeat_interleave(32, 1)
-    return (value * scale)[:, :cols]
+    return value[:, :cols] * scale[:, :cols]
 
 
 def _exact_norm(v, weight, bias, layer):
