@@ -60,7 +60,8 @@ typedef enum flashoptim_status {
     FLASHOPTIM_ERR_HIP = -4,         /* a HIP runtime call failed (see flashoptim_last_hip_error) */
     FLASHOPTIM_ERR_BAD_BLOB = -5,    /* checkpoint blob too small, or header/table mismatch   */
     FLASHOPTIM_ERR_SELFTEST = -6,    /* flashoptim_selftest found a failing check             */
-    FLASHOPTIM_ERR_LIST_TOO_LONG = -7 /* flashoptim_adamw_step_noalloc: more than 1024 non-empty tensors */
+    FLASHOPTIM_ERR_LIST_TOO_LONG = -7, /* flashoptim_adamw_step_noalloc: more than 1024 non-empty tensors */
+    FLASHOPTIM_ERR_WORKSPACE = -8    /* a workspace is smaller than the call needs */
 } flashoptim_status;
 
 /* Optimizer kinds (checkpoint entry points). */
@@ -307,6 +308,121 @@ int flashoptim_checkpoint_pack(int kind, const flashoptim_tensor* tensors, int64
 int flashoptim_checkpoint_unpack(int kind, const void* blob, int64_t blob_bytes,
                                  const flashoptim_tensor* tensors, int64_t n_tensors, int64_t* step_out,
                                  void* stream);
+
+/* ---- microscaled 4-bit matrices: the weights' low-precision form and the products on it -------------
+ * Around the step: the blocks of a model run on 4-bit copies of the weights that a step leaves, and hand back the
+ * gradients that the next one takes.
+ *
+ * A matrix of `rows` by `cols` values in 4 bits: consecutive blocks of 32 values of a row share one power of two.
+ *   codes:  [rows, 128 ceil(cols/256)] bytes, two codes to a byte, the even element in the low half.  A code is a sign
+ *           bit and an index into {0, 0.5, 1, 1.5, 2, 3, 4, 6} (one mantissa bit, two exponent bits).
+ *   scales: [rows, 16 ceil(cols/512)] bytes, one to a block: the block's values are its codes' times 2^(byte - 127);
+ *           byte 255 makes the whole block NaN.
+ * What lies behind column cols of a row is zero in both arrays (every call here writes it so, and the products count
+ * on it).  Both arrays 16-byte aligned and contiguous.
+ *
+ * Quantisation, by block, with E the exponent field of the FP32 value max|v| of the block:
+ *   to nearest:   byte = max(E - 2, 0); each v 2^(127 - byte) goes to the nearest of the eight magnitudes, ties to the
+ *                 even index, what is beyond 6 to 6.
+ *   stochastic (`rand` given): byte = max(E - 2, 0), one more where the mantissa of max|v| exceeds 1.5, so that
+ *                 nothing lies beyond 6; with a <= |v| 2^(127 - byte) < b between neighbouring magnitudes the value goes to b
+ *                 if 256 (|v| 2^(127 - byte) - a) / (b - a) > r + 1/2, r being the value's byte of `rand`.
+ *   A block with an infinity or a NaN gets byte 255 and codes 0.  All of it is exact: the same bits for the same
+ *   input on every path.
+ *
+ * flashoptim_matrix: a row-major matrix of BF16 or FP32 values whose rows begin `stride` elements apart (>= cols; any, and
+ * any alignment of a value, are valid; 16-byte aligned rows are fastest).  rows, cols < 2^31. */
+enum { FLASHOPTIM_BF16 = 0, FLASHOPTIM_FP32 = 1 };
+
+typedef struct flashoptim_matrix {
+    void*   data;
+    int64_t rows, cols, stride;
+    int32_t dtype;        /* FLASHOPTIM_BF16 or FLASHOPTIM_FP32 */
+} flashoptim_matrix;
+
+typedef struct flashoptim_mx4 {
+    uint8_t* codes;
+    uint8_t* scales;
+    int64_t  rows, cols;
+} flashoptim_mx4;
+
+/* quantize: `out` <- x in 4 bits along its rows; `out_t` <- the transpose of x (cols by rows) in 4 bits along ITS rows, from
+ *   the same pass over x.  Either may be NULL.  rho: NULL, or the [rows, cols] INT8 corrections (contiguous) of x, which is then
+ *   a contiguous BF16 matrix of split weights: what is quantised is the reconstructed FP32 weight.  rand: NULL, or [rows, cols]
+ *   random bytes (contiguous): stochastic rounding; out and out_t use the same byte of a value.
+ * dequantize: x <- the values that q stands for, in BF16 (exact) or FP32 (exact). */
+int flashoptim_mx4_quantize(const flashoptim_matrix* x, const int8_t* rho, const uint8_t* rand,
+                            const flashoptim_mx4* out, const flashoptim_mx4* out_t, void* stream);
+int flashoptim_mx4_dequantize(const flashoptim_mx4* q, const flashoptim_matrix* x, void* stream);
+
+/* Products.  Sums are FP32, rounded once to the type of the result; the order of a sum depends on the sizes alone, so a
+ * call's result is the same every time.  A product over zero terms is zero.
+ * matmul: c [m, n] <- a [m, k] b [n, k]^T.
+ * linear: y [m, n] <- Q(x) w^T with x [m, k] quantised to nearest along its rows and w [n, k]; if xt [k, m] is not NULL, Q(x^T) is
+ *   left there for the backward pass.  Up to 16 rows without xt are one launch, made for single tokens: the weights stream through
+ *   once.
+ * linear_backward: dx [m, k] <- Q(dy) wt^T and dw [n, k] <- Q(dy^T) xt^T, with dy [m, n] quantised along its rows and along
+ *   its columns in one pass (stochastically with `rand`), wt [k, n] the transposed weights in 4 bits (quantize's out_t) and xt [k, m].
+ *   dx or dw may be NULL, and with it wt or xt.  These are the gradients of the product of its quantised operands, the
+ *   quantisation itself counted as the identity, each with its operands in 4 bits along its own sum.
+ * workspace: DEVICE memory, 16-byte aligned, of at least the bytes that the *_workspace call returns for the same sizes (0: NULL will
+ *   do; negative: a status), and the call's until its work on `stream` is done.  (With `train` or rand nothing changes in size.) */
+int64_t flashoptim_mx4_matmul_workspace(int64_t m, int64_t n, int64_t k);
+int64_t flashoptim_mx4_linear_workspace(int64_t m, int64_t n, int64_t k);
+int64_t flashoptim_mx4_linear_backward_workspace(int64_t m, int64_t n, int64_t k);
+int flashoptim_mx4_matmul(const flashoptim_mx4* a, const flashoptim_mx4* b, const flashoptim_matrix* c, void* workspace,
+                          int64_t workspace_bytes, void* stream);
+int flashoptim_mx4_linear(const flashoptim_matrix* x, const flashoptim_mx4* w, const flashoptim_mx4* xt,
+                          const flashoptim_matrix* y, void* workspace, int64_t workspace_bytes, void* stream);
+int flashoptim_mx4_linear_backward(const flashoptim_matrix* dy, const uint8_t* rand, const flashoptim_mx4* wt,
+                                   const flashoptim_mx4* xt, const flashoptim_matrix* dx, const flashoptim_matrix* dw,
+                                   void* workspace, int64_t workspace_bytes, void* stream);
+
+/* ---- the norms before and after a block, with its gate and residual scale --------------------------------
+ * Between two blocks, in one pass over each row of the residual stream x [rows, cols]:
+ *   u = f, or norm(f) * post_weight + post_bias (post_norm)        f: the output of the block that ends
+ *   h = residual_scale * x + branch_scale * act(gate) * u
+ *   y = norm(h) * pre_weight + pre_bias                            y: the input of the block that begins
+ * norm(v) = (v - mean) / sqrt(mean((v - mean)^2) + eps); kind FLASHOPTIM_RMS_NORM takes 0 for the mean.  act is the identity or the
+ * sigmoid.  gate [g, cols] with g >= 1 dividing rows: row i of the result takes row i / (rows / g) of the gate (g = 1: a gate for
+ * each channel; g = rows: one for each value).  Sums and everything between loads and stores are FP32; y is formed from h before
+ * h is rounded.
+ * Left out: weights and biases (NULL: 1, 0; biases are for layer norms only), the gate (NULL: 1), the norm in front (y NULL), the branch (f NULL: h = x, not written;
+ * gate must be NULL).  x and h have one type, f, gate and y one type, which is BF16, or FP32 if x is FP32.  1 <= cols <= 16384.
+ * h may be x's own buffer, y f's.
+ * stats: NULL, or [4, rows] FP32 for the backward pass: mean and 1/sqrt(...) of the norm behind, of the norm in front (0 where
+ *   there is none). */
+enum { FLASHOPTIM_RMS_NORM = 0, FLASHOPTIM_LAYER_NORM = 1 };
+enum { FLASHOPTIM_GATE_LINEAR = 0, FLASHOPTIM_GATE_SIGMOID = 1 };
+
+typedef struct flashoptim_block_norm_spec {
+    int64_t cols;
+    int32_t kind, post_norm, gate_act;
+    int32_t param_dtype;                 /* of the four arrays below and of their gradients */
+    float   eps, residual_scale, branch_scale;
+    const void *post_weight, *post_bias, *pre_weight, *pre_bias;   /* [cols] each, or NULL */
+} flashoptim_block_norm_spec;
+
+int flashoptim_block_norm(const flashoptim_block_norm_spec* spec, const flashoptim_matrix* x, const flashoptim_matrix* f,
+                          const flashoptim_matrix* gate, const flashoptim_matrix* h, const flashoptim_matrix* y, float* stats,
+                          void* stream);
+
+/* The gradients of all of that.  h (x where there is no branch), f, gate and stats as the forward call read and left them; dy: of y
+ * (NULL if there was no norm in front); dh: what reaches h from elsewhere (NULL: nothing); not both NULL.
+ *   dx = residual_scale (dh + the gradient through the norm in front); df, dgate (summed over the rows that share a gate), and the
+ *   gradients of the four arrays, summed over all rows: of type param_dtype, [cols].
+ * Every output may be NULL: it is then not wanted.  dx has the type of h, df and dgate that of f.  dx may be dh's own buffer, df f's or dy's.
+ * Sums over rows have a fixed order.  workspace as above, for `gates` rows of gates (1 if there are none). */
+typedef struct flashoptim_block_norm_grads {
+    const flashoptim_matrix *dy, *dh;                                    /* in  */
+    const flashoptim_matrix *dx, *df, *dgate;                            /* out */
+    void *dpost_weight, *dpost_bias, *dpre_weight, *dpre_bias;           /* out */
+} flashoptim_block_norm_grads;
+
+int64_t flashoptim_block_norm_backward_workspace(const flashoptim_block_norm_spec* spec, int64_t rows, int64_t gates);
+int flashoptim_block_norm_backward(const flashoptim_block_norm_spec* spec, const flashoptim_matrix* h, const flashoptim_matrix* f,
+                                   const flashoptim_matrix* gate, const float* stats, const flashoptim_block_norm_grads* grads,
+                                   void* workspace, int64_t workspace_bytes, void* stream);
 
 /* ---- housekeeping --------------------------------------------------------------------
  * strerror: static string for a status.  last_hip_error: hipError_t value of the most recent

@@ -10,6 +10,9 @@ from .binding import (  # noqa: F401
     split_weights, reconstruct_weights, split_weights_i16, reconstruct_weights_i16, reconstruction_sweep, reconstruction_sweep_ex,
     quantize_momentum, dequantize_momentum, quantize_variance, dequantize_variance,
     quantize_state, dequantize_state, quantization_nmse, compress_state, decompress_state, stream_probe, step_launch_count,
+    Mx4Tensor, mx4_quantize, mx4_dequantize, mx4_matmul, mx4_linear, mx4_linear_backward,
+    mx4_matmul_workspace, mx4_linear_workspace, mx4_linear_backward_workspace,
+    BlockNorm, block_norm, block_norm_backward, block_norm_backward_workspace,
     checkpoint_size, checkpoint_pack, checkpoint_unpack,
     strerror, release_cache, version, selftest, faithful_rounding_stats, short_sqrt_state, ClockMonitor, EXPORTED_SYMBOLS, KIND,
 )

@@ -30,6 +30,9 @@ EXPORTED_SYMBOLS = [
     "flashoptim_quantize_state", "flashoptim_dequantize_state", "flashoptim_quantization_nmse",
     "flashoptim_compress_state", "flashoptim_decompress_state", "flashoptim_stream_probe",
     "flashoptim_adamw_step_noalloc", "flashoptim_shard_range",
+    "flashoptim_mx4_quantize", "flashoptim_mx4_dequantize", "flashoptim_mx4_matmul_workspace", "flashoptim_mx4_linear_workspace",
+    "flashoptim_mx4_linear_backward_workspace", "flashoptim_mx4_matmul", "flashoptim_mx4_linear", "flashoptim_mx4_linear_backward",
+    "flashoptim_block_norm", "flashoptim_block_norm_backward_workspace", "flashoptim_block_norm_backward",
 ]
 
 
@@ -65,6 +68,25 @@ class _SgdHp(C.Structure):
 
 class _LionHp(C.Structure):
     _fields_ = [("beta1", C.c_float), ("beta2", C.c_float)]
+
+
+class _Matrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("stride", C.c_int64), ("dtype", C.c_int32)]
+
+
+class _Mx4(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64)]
+
+
+class _BlockNormSpec(C.Structure):
+    _fields_ = [("cols", C.c_int64), ("kind", C.c_int32), ("post_norm", C.c_int32), ("gate_act", C.c_int32),
+                ("param_dtype", C.c_int32), ("eps", C.c_float), ("residual_scale", C.c_float), ("branch_scale", C.c_float),
+                ("post_weight", C.c_void_p), ("post_bias", C.c_void_p), ("pre_weight", C.c_void_p), ("pre_bias", C.c_void_p)]
+
+
+class _BlockNormGrads(C.Structure):
+    _fields_ = [(n, C.POINTER(_Matrix)) for n in ("dy", "dh", "dx", "df", "dgate")] + \
+               [(n, C.c_void_p) for n in ("dpost_weight", "dpost_bias", "dpre_weight", "dpre_bias")]
 
 
 def library_path():
@@ -110,10 +132,23 @@ def load_library():
     L.flashoptim_selftest.argtypes = [C.POINTER(i64), C.POINTER(i64), vp]
     L.flashoptim_faithful_rounding_stats.argtypes = [C.POINTER(i64), vp]
     L.flashoptim_clock_monitor.argtypes = [C.POINTER(C.c_uint64), i64, C.c_double, C.POINTER(C.c_double), vp]
+    mat, mx4, spec = C.POINTER(_Matrix), C.POINTER(_Mx4), C.POINTER(_BlockNormSpec)
+    L.flashoptim_mx4_quantize.argtypes = [mat, vp, vp, mx4, mx4, vp]
+    L.flashoptim_mx4_dequantize.argtypes = [mx4, mat, vp]
+    L.flashoptim_mx4_matmul.argtypes = [mx4, mx4, mat, vp, i64, vp]
+    L.flashoptim_mx4_linear.argtypes = [mat, mx4, mx4, mat, vp, i64, vp]
+    L.flashoptim_mx4_linear_backward.argtypes = [mat, vp, mx4, mx4, mat, mat, vp, i64, vp]
+    L.flashoptim_block_norm.argtypes = [spec, mat, mat, mat, mat, mat, vp, vp]
+    L.flashoptim_block_norm_backward.argtypes = [spec, mat, mat, mat, vp, C.POINTER(_BlockNormGrads), vp, i64, vp]
+    L.flashoptim_block_norm_backward_workspace.argtypes = [spec, i64, i64]
+    for name in ("flashoptim_mx4_matmul_workspace", "flashoptim_mx4_linear_workspace", "flashoptim_mx4_linear_backward_workspace"):
+        getattr(L, name).argtypes = [i64, i64, i64]
     L.flashoptim_strerror.argtypes = [i32]
     L.flashoptim_strerror.restype = C.c_char_p
     for name in EXPORTED_SYMBOLS:
-        if name not in ("flashoptim_checkpoint_size", "flashoptim_strerror"):
+        if name.endswith("_workspace"):
+            getattr(L, name).restype = i64
+        elif name not in ("flashoptim_checkpoint_size", "flashoptim_strerror"):
             getattr(L, name).restype = i32
     _lib = L
     return L
@@ -428,6 +463,181 @@ def checkpoint_unpack(kind, blob, tensors, stream=None):
                                                        tl.array, tl.n, C.byref(step), _stream(stream)),
            "flashoptim_checkpoint_unpack")
     return int(step.value)
+
+
+_DTYPE = {torch.bfloat16: 0, torch.float32: 1}
+
+
+def _matrix(t, name):
+    """A flashoptim_matrix of a two-dimensional tensor with neighbouring columns, whose rows may lie apart; None for None."""
+    if t is None:
+        return None
+    dtype = _DTYPE.get(t.dtype)
+    if dtype is None or t.dim() != 2:
+        raise ValueError(f"{name}: a matrix of bfloat16 or float32 values, not {t.dim()}-dimensional {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: not on the GPU")
+    rows, cols = t.shape
+    stride, step = t.stride()
+    if cols > 1 and step != 1:
+        raise ValueError(f"{name}: the values of a row must be neighbours in memory")
+    return _Matrix(t.data_ptr(), rows, cols, stride if rows > 1 else cols, dtype)
+
+
+def _bytes_like(t, x, dtype, name):
+    """The pointer of a contiguous one-byte companion of matrix x, None for None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.shape != x.shape or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{name}: contiguous {dtype} of the matrix's shape on the GPU")
+    return t.data_ptr()
+
+
+def _workspace(t):
+    if t is None:
+        return None, 0
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("workspace: contiguous memory on the GPU")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+class Mx4Tensor:
+    """A matrix of rows by cols values in microscaled 4 bits: `codes` [rows, 128 ceil(cols/256)] and `scales`
+    [rows, 16 ceil(cols/512)], both uint8, laid out as flashoptim.h describes.  `buffers`: a (codes, scales) pair to use
+    instead of new ones."""
+
+    def __init__(self, rows, cols, device="cuda", buffers=None):
+        self.rows, self.cols = int(rows), int(cols)
+        shapes = ((self.rows, 128 * -(-self.cols // 256)), (self.rows, 16 * -(-self.cols // 512)))
+        if buffers is None:
+            buffers = [torch.zeros(s, dtype=torch.uint8, device=device) for s in shapes]
+        for t, s in zip(buffers, shapes):
+            if t.dtype != torch.uint8 or tuple(t.shape) != s or not t.is_contiguous():
+                raise ValueError(f"a {self.rows} by {self.cols} matrix in 4 bits takes contiguous uint8 of shapes {shapes}")
+        self.codes, self.scales = buffers
+        self.on_gpu = self.codes.is_cuda and self.scales.is_cuda
+        self.desc = _Mx4(self.codes.data_ptr(), self.scales.data_ptr(), self.rows, self.cols)
+
+
+def _mx4(q):
+    if q is None:
+        return None
+    if not q.on_gpu:
+        raise ValueError("a matrix in 4 bits that is not on the GPU")
+    return q.desc
+
+
+def mx4_quantize(x, out=None, out_t=None, rho=None, rand=None, stream=None):
+    """out <- x, out_t <- the transpose of x, each in 4 bits along its own rows (Mx4Tensor; either may be None).  rho: x holds
+    BF16 weights with these INT8 corrections.  rand: random bytes for stochastic rounding."""
+    _check(load_library().flashoptim_mx4_quantize(_matrix(x, "x"), _bytes_like(rho, x, torch.int8, "rho"),
+                                                  _bytes_like(rand, x, torch.uint8, "rand"), _mx4(out), _mx4(out_t),
+                                                  _stream_handle(stream)), "flashoptim_mx4_quantize")
+
+
+def mx4_dequantize(q, out, stream=None):
+    _check(load_library().flashoptim_mx4_dequantize(_mx4(q), _matrix(out, "out"), _stream_handle(stream)),
+           "flashoptim_mx4_dequantize")
+
+
+def _size(r, where):
+    if r < 0:
+        raise FlashOptimError(int(r), where)
+    return int(r)
+
+
+def mx4_matmul_workspace(m, n, k):
+    """Bytes of workspace of mx4_matmul for an m by n result of sums over k terms."""
+    return _size(load_library().flashoptim_mx4_matmul_workspace(m, n, k), "flashoptim_mx4_matmul_workspace")
+
+
+def mx4_linear_workspace(m, n, k):
+    return _size(load_library().flashoptim_mx4_linear_workspace(m, n, k), "flashoptim_mx4_linear_workspace")
+
+
+def mx4_linear_backward_workspace(m, n, k):
+    return _size(load_library().flashoptim_mx4_linear_backward_workspace(m, n, k), "flashoptim_mx4_linear_backward_workspace")
+
+
+def mx4_matmul(a, b, out, workspace=None, stream=None):
+    """out [m, n] <- a [m, k] b [n, k]^T, both Mx4Tensor."""
+    ws, size = _workspace(workspace)
+    _check(load_library().flashoptim_mx4_matmul(_mx4(a), _mx4(b), _matrix(out, "out"), ws, size, _stream_handle(stream)),
+           "flashoptim_mx4_matmul")
+
+
+def mx4_linear(x, w, out, xt=None, workspace=None, stream=None):
+    """out [m, n] <- Q(x) w^T with x [m, k] quantised on the way, w an Mx4Tensor [n, k]; xt: Mx4Tensor [k, m] for Q(x^T)."""
+    ws, size = _workspace(workspace)
+    _check(load_library().flashoptim_mx4_linear(_matrix(x, "x"), _mx4(w), _mx4(xt), _matrix(out, "out"), ws, size,
+                                                _stream_handle(stream)), "flashoptim_mx4_linear")
+
+
+def mx4_linear_backward(dy, wt, xt, dx, dw, rand=None, workspace=None, stream=None):
+    """dx [m, k] <- Q(dy) wt^T and dw [n, k] <- Q(dy^T) xt^T, with wt [k, n] and xt [k, m] Mx4Tensor; a pair (wt, dx) or (xt, dw)
+    may be None."""
+    ws, size = _workspace(workspace)
+    _check(load_library().flashoptim_mx4_linear_backward(_matrix(dy, "dy"), _bytes_like(rand, dy, torch.uint8, "rand"), _mx4(wt),
+                                                         _mx4(xt), _matrix(dx, "dx"), _matrix(dw, "dw"), ws, size,
+                                                         _stream_handle(stream)), "flashoptim_mx4_linear_backward")
+
+
+class BlockNorm:
+    """The norms between two blocks of `cols` channels: which there are, their weights and scales (flashoptim_block_norm_spec).  The
+    weights and biases are BF16 or FP32, all of one type."""
+
+    def __init__(self, cols, kind="rms", eps=1e-5, post_norm=False, gate_act="linear", residual_scale=1.0, branch_scale=1.0,
+                 post_weight=None, post_bias=None, pre_weight=None, pre_bias=None):
+        self.params = dict(post_weight=post_weight, post_bias=post_bias, pre_weight=pre_weight, pre_bias=pre_bias)
+        given = [t for t in self.params.values() if t is not None]
+        self.param_dtype = given[0].dtype if given else torch.bfloat16
+        for name, t in self.params.items():
+            self.check_param(t, cols, name)
+        self.cols = int(cols)
+        self.desc = _BlockNormSpec(self.cols, {"rms": 0, "layer": 1}.get(kind, -1), int(post_norm), {"linear": 0, "sigmoid": 1}.get(gate_act, -1),
+                                   _DTYPE[self.param_dtype], eps, residual_scale, branch_scale,
+                                   *(_ptr(t) for t in self.params.values()))
+
+    def check_param(self, t, cols, name):
+        if t is None:
+            return
+        if t.dtype not in _DTYPE or t.dtype != self.param_dtype or t.numel() != cols or not t.is_contiguous() or not t.is_cuda:
+            raise ValueError(f"{name}: {cols} contiguous values on the GPU, bfloat16 or float32, one type for all weights and biases")
+
+
+def _check_stats(stats, rows):
+    if stats is not None and (stats.dtype != torch.float32 or stats.numel() != 4 * rows or not stats.is_contiguous()):
+        raise ValueError("stats: contiguous float32 of shape (4, rows)")
+    if stats is not None and not stats.is_cuda:
+        raise ValueError("stats: not on the GPU")
+    return _ptr(stats)
+
+
+def block_norm(spec, x, f=None, gate=None, h=None, y=None, stats=None, stream=None):
+    """h <- residual_scale x + branch_scale act(gate) u, u = f or its norm; y <- the norm of h (of x without f); stats [4, rows] for
+    the backward pass."""
+    _check(load_library().flashoptim_block_norm(spec.desc, _matrix(x, "x"), _matrix(f, "f"), _matrix(gate, "gate"), _matrix(h, "h"),
+                                                _matrix(y, "y"), _check_stats(stats, x.shape[0]), _stream_handle(stream)),
+           "flashoptim_block_norm")
+
+
+def block_norm_backward_workspace(spec, rows, gates=1):
+    return _size(load_library().flashoptim_block_norm_backward_workspace(spec.desc, rows, gates),
+                 "flashoptim_block_norm_backward_workspace")
+
+
+def block_norm_backward(spec, h, stats, f=None, gate=None, dy=None, dh=None, dx=None, df=None, dgate=None, dpost_weight=None,
+                        dpost_bias=None, dpre_weight=None, dpre_bias=None, workspace=None, stream=None):
+    """The gradients of block_norm that are not None, from dy and dh (either may be None); h is x where there is no branch."""
+    ws, size = _workspace(workspace)
+    sums = dict(dpost_weight=dpost_weight, dpost_bias=dpost_bias, dpre_weight=dpre_weight, dpre_bias=dpre_bias)
+    for name, t in sums.items():
+        spec.check_param(t, spec.cols, name)
+    mats = [_matrix(t, n) for t, n in ((dy, "dy"), (dh, "dh"), (dx, "dx"), (df, "df"), (dgate, "dgate"))]
+    grads = _BlockNormGrads(*(None if m is None else C.pointer(m) for m in mats), *(_ptr(t) for t in sums.values()))
+    _check(load_library().flashoptim_block_norm_backward(spec.desc, _matrix(h, "h"), _matrix(f, "f"), _matrix(gate, "gate"),
+                                                         _check_stats(stats, h.shape[0]), grads, ws, size, _stream_handle(stream)),
+           "flashoptim_block_norm_backward")
 
 
 def faithful_rounding_stats(stream=None):

@@ -21,6 +21,7 @@
 
 #include "flashoptim.h"
 #include "flashoptim_device.h"
+#include "flashoptim_host.h"
 
 namespace {
 
@@ -920,6 +921,11 @@ __global__ __launch_bounds__(256) void noalloc_fill_coarse(const TensorDev* tabl
 
 }  // namespace
 
+int fo::hip_status(hipError_t e) {
+    FO_HIP(e);
+    return FLASHOPTIM_OK;
+}
+
 extern "C" {
 
 // 255 * sqrt(1 / rbc2), evaluated in double and handed to the kernels as two floats.
@@ -1446,6 +1452,7 @@ const char* flashoptim_strerror(int status) {
         case FLASHOPTIM_ERR_BAD_BLOB: return "checkpoint blob too small or does not match the tensor list";
         case FLASHOPTIM_ERR_SELFTEST: return "device self-test found a hardware operation outside its documented error bound";
         case FLASHOPTIM_ERR_LIST_TOO_LONG: return "list has more tensors than the entry point without allocation holds (1024)";
+        case FLASHOPTIM_ERR_WORKSPACE: return "workspace is smaller than the call needs";
         default: return "unknown status";
     }
 }

@@ -1,0 +1,605 @@
+// Microscaled 4-bit matrices on gfx950: quantisation from BF16, FP32 or split weights (along rows, along columns, or both from one
+// pass), the way back, and the products of a linear layer and its gradients on the matrix cores' scaled 4-bit instructions.
+//
+// The arithmetic of a block of 32 values: max|v| has the exponent field E, the block's scale is 2^(E - 2 - 127), so that the
+// largest magnitude lies in [4, 8) on the grid {0, 0.5, 1, 1.5, 2, 3, 4, 6}.  The scaling is exact, so a code is decided by comparing
+// exact numbers: v_cvt_scalef32_pk_fp4_f32 does that to nearest, ties to even, for scale bytes down to 0 and for subnormal values
+// (every one of the 2^20 pairs of a check over all of these agreed); the stochastic rounding compares exactly in FP32.
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include <string.h>
+
+#include <type_traits>
+
+#include "flashoptim.h"
+#include "flashoptim_host.h"
+
+namespace {
+
+using i32x4 = int __attribute__((ext_vector_type(4)));
+using i32x8 = int __attribute__((ext_vector_type(8)));
+using f32x4 = float __attribute__((ext_vector_type(4)));
+
+constexpr int kBlock = 32;                  // values that share a scale
+constexpr int kSegment = 256;               // a row of codes is filled up to a multiple of this many values
+constexpr int kSegmentBytes = kSegment / 2;
+
+inline int64_t up(int64_t n, int64_t unit) { return (n + unit - 1) / unit; }
+
+// A 4-bit matrix as a kernel takes it.
+struct Mx4 {
+    uint8_t* codes;
+    uint8_t* scales;
+    uint32_t rows, cols;
+    uint32_t segments;      // of 256 values to a row: 128 bytes of codes, 8 of scales
+    uint32_t scale_pitch;   // bytes
+};
+Mx4 to_dev(const flashoptim_mx4& m) {
+    return {m.codes, m.scales, (uint32_t)m.rows, (uint32_t)m.cols, (uint32_t)up(m.cols, kSegment), (uint32_t)(16 * up(m.cols, 2 * kSegment))};
+}
+
+enum SourceKind { kBf16, kFp32, kSplit };
+struct Source {
+    const void* data;
+    const int8_t* rho;       // kSplit
+    const uint8_t* rand;     // stochastic rounding
+    int64_t stride;
+    uint32_t rows, cols;
+};
+
+template <typename T>
+__device__ __forceinline__ T load_as(const void* p) {       // any alignment: the hardware takes global accesses at any byte
+    T v;
+    __builtin_memcpy(&v, p, sizeof(T));
+    return v;
+}
+template <typename T>
+__device__ __forceinline__ void store_as(void* p, T v) {
+    __builtin_memcpy(p, &v, sizeof(T));
+}
+
+__device__ __forceinline__ float bf16_value(uint32_t bits) { return __uint_as_float(bits << 16); }
+
+// theta' + (rho / 127) ULP(theta') / 2 (Section 3.1, Eq. 2), as the optimizer step reconstructs it.
+__device__ __forceinline__ float master_weight(uint32_t bits, int rho) {
+    const float base = bf16_value(bits), r = (float)rho;
+    const int e = (int)(bits >> 7) & 255;
+    const float q = fmaf(r, 0x1.020408p-7f, r * 0x1.020408p-35f);        // rho / 127, correctly rounded for every byte
+    return e == 255 ? base : base + __builtin_amdgcn_ldexpf(q, max(e, 1) - 135);
+}
+
+// Eight consecutive values of a row, 0 behind its end.
+template <int SRC>
+__device__ __forceinline__ void load8(float (&v)[8], const Source& s, uint32_t row, uint32_t col) {
+    const int64_t at = (int64_t)row * s.stride + col;
+    const int64_t at_rho = (int64_t)row * s.cols + col;
+    const uint32_t left = col < s.cols ? s.cols - col : 0;
+    if constexpr (SRC == kFp32) {
+        const float* p = (const float*)s.data + at;
+        if (left >= 8) {
+            const f32x4 a = load_as<f32x4>(p), b = load_as<f32x4>(p + 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = i < (int)left ? p[i] : 0.0f;
+        }
+    } else {
+        const uint16_t* p = (const uint16_t*)s.data + at;
+        uint32_t bits[8];
+        uint64_t rho = 0;
+        if (left >= 8) {
+            const i32x4 a = load_as<i32x4>(p);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { bits[2 * i] = (uint32_t)a[i] & 0xffffu; bits[2 * i + 1] = (uint32_t)a[i] >> 16; }
+            if constexpr (SRC == kSplit) rho = load_as<uint64_t>(s.rho + at_rho);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                bits[i] = i < (int)left ? p[i] : 0u;
+                if constexpr (SRC == kSplit) rho |= i < (int)left ? (uint64_t)(uint8_t)s.rho[at_rho + i] << (8 * i) : 0;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (SRC == kSplit) v[i] = master_weight(bits[i], (int)(int8_t)(rho >> (8 * i)));
+            else v[i] = bf16_value(bits[i]);
+        }
+    }
+}
+__device__ __forceinline__ uint64_t load_rand8(const Source& s, uint32_t row, uint32_t col) {
+    const uint8_t* p = s.rand + (int64_t)row * s.cols + col;
+    const uint32_t left = col < s.cols ? s.cols - col : 0;
+    if (left >= 8) return load_as<uint64_t>(p);
+    uint64_t r = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r |= i < (int)left ? (uint64_t)p[i] << (8 * i) : 0;
+    return r;
+}
+
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// The scale byte of a block whose largest magnitude has these bits.
+template <bool RANDOM>
+__device__ __forceinline__ uint32_t scale_byte(uint32_t largest) {
+    int byte = (int)(largest >> 23) - 2;
+    if (RANDOM && (largest & 0x7fffffu) > 0x400000u) ++byte;
+    return largest >= 0x7f800000u ? 255u : (uint32_t)max(byte, 0);
+}
+
+// One stochastically rounded code: t = |v| 2^(127 - byte) <= 6 lies on a stretch of the grid with steps of 1/2, 1 or 2.
+__device__ __forceinline__ uint32_t random_code(float v, float up_scale, uint32_t r) {
+    const float t = fabsf(v) * up_scale;
+    const bool fine = t < 2.0f, mid = t < 4.0f;
+    const float y = t * (fine ? 2.0f : mid ? 1.0f : 0.5f), low = floorf(y);
+    const uint32_t more = (y - low) * 256.0f > (float)r + 0.5f ? 1u : 0u;
+    return (uint32_t)low + (fine ? 0u : mid ? 2u : 4u) + more + ((__float_as_uint(v) >> 31) << 3);
+}
+
+// Eight codes, the first in the lowest bits.
+template <bool RANDOM>
+__device__ __forceinline__ uint32_t codes8(const float* v, uint32_t byte, uint64_t r) {
+    if constexpr (RANDOM) {
+        const float up_scale = __uint_as_float((254u - (byte == 255u ? 0u : byte)) << 23);
+        uint32_t c = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c |= random_code(v[i], up_scale, (uint32_t)(r >> (8 * i)) & 255u) << (4 * i);
+        return byte == 255u ? 0u : c;
+    } else {
+        const float scale = __uint_as_float(byte << 23);
+        uint32_t c = 0;
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0], v[1], scale, 0);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], scale, 1);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], scale, 2);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], scale, 3);
+        return byte == 255u ? 0u : c;
+    }
+}
+
+// The largest of a value over the four lanes of a quad.
+__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
+    v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xb1, 0xf, 0xf, true));   // quad_perm [1,0,3,2]
+    return max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4e, 0xf, 0xf, true));   // quad_perm [2,3,0,1]
+}
+
+// Codes and scale of the eight values that this lane has of its quad's block.
+template <bool RANDOM>
+__device__ __forceinline__ uint32_t quad_codes(const float (&v)[8], uint64_t r, uint32_t* byte) {
+    uint32_t largest = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) largest = max(largest, magnitude(v[i]));
+    *byte = scale_byte<RANDOM>(quad_max(largest));
+    return codes8<RANDOM>(v, *byte, r);
+}
+
+// ------------------------------------------------------------------------------------------------ along rows --
+
+// Half a wavefront handles a segment of 256 values: eight to a lane, a block to a quad.
+template <int SRC, bool RANDOM>
+__global__ __launch_bounds__(256) void quantize_rows(Source s, Mx4 out, uint32_t total) {
+    const uint32_t unit = blockIdx.x * 8 + threadIdx.x / 32, lane = threadIdx.x % 32;
+    if (unit >= total) return;
+    const uint32_t row = unit / out.segments, seg = unit - row * out.segments;
+    const uint32_t col = seg * kSegment + lane * 8;
+    float v[8];
+    load8<SRC>(v, s, row, col);
+    const uint64_t r = RANDOM ? load_rand8(s, row, col) : 0;
+    uint32_t byte;
+    const uint32_t c = quad_codes<RANDOM>(v, r, &byte);
+    store_as(out.codes + ((int64_t)row * out.segments + seg) * kSegmentBytes + lane * 4, c);
+    uint8_t* scales = out.scales + (int64_t)row * out.scale_pitch + seg * 8;
+    if (lane % 4 == 0) scales[lane / 4] = (uint8_t)byte;
+    if (seg + 1 == out.segments && (out.segments & 1) && lane < 8) scales[8 + lane] = 0;
+}
+
+// ---------------------------------------------------------------------------------- along columns, or both ways --
+
+// A workgroup handles 128 by 128 values: the rows as above, and through LDS the columns.  The grid covers rows and columns up to whole
+// segments, so that what lies behind the matrix's end is written as zeros in both layouts.
+constexpr int kTile = 128;
+
+template <int SRC, bool RANDOM>
+__global__ __launch_bounds__(256) void quantize_both(Source s, Mx4 out, Mx4 out_t, bool rows_too) {
+    using Cell = typename std::conditional<SRC == kBf16, uint16_t, float>::type;
+    __shared__ Cell tile[kTile][kTile];
+    __shared__ uint8_t rands[RANDOM ? kTile : 1][kTile];
+    const uint32_t row0 = blockIdx.y * kTile, col0 = blockIdx.x * kTile;
+    const uint32_t lane = threadIdx.x % 16, line = threadIdx.x / 16;
+    const uint32_t col = col0 + lane * 8;
+#pragma unroll
+    for (int i = 0; i < kTile / 16; ++i) {
+        const uint32_t row = row0 + i * 16 + line;
+        float v[8];
+        uint64_t r = 0;
+        if (row < s.rows) {
+            load8<SRC>(v, s, row, col);
+            if (RANDOM) r = load_rand8(s, row, col);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+        }
+        Cell* cell = &tile[i * 16 + line][lane * 8];
+        if constexpr (SRC == kBf16) {
+            i32x4 w;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = (int)((__float_as_uint(v[2 * j]) >> 16) | (__float_as_uint(v[2 * j + 1]) & 0xffff0000u));
+            *(i32x4*)cell = w;
+        } else {
+            *(f32x4*)cell = f32x4{v[0], v[1], v[2], v[3]};
+            *(f32x4*)(cell + 4) = f32x4{v[4], v[5], v[6], v[7]};
+        }
+        if constexpr (RANDOM) *(uint64_t*)&rands[i * 16 + line][lane * 8] = r;
+        if (rows_too && row < s.rows) {
+            uint32_t byte;
+            const uint32_t c = quad_codes<RANDOM>(v, r, &byte);
+            if (col < out.segments * kSegment) {
+                store_as(out.codes + (int64_t)row * out.segments * kSegmentBytes + col / 2, c);
+                if (lane % 4 == 0) out.scales[(int64_t)row * out.scale_pitch + col / kBlock] = (uint8_t)byte;
+            }
+        }
+    }
+    if (rows_too && col0 + kTile == out.segments * kSegment && (out.segments & 1)) {       // the row's scales behind the last segment
+        const uint32_t row = row0 + threadIdx.x / 2;
+        if (row < s.rows) store_as(out.scales + (int64_t)row * out.scale_pitch + out.segments * 8 + threadIdx.x % 2 * 4, 0u);
+    }
+    __syncthreads();
+    // a wavefront takes 32 of the rows, a lane two columns of them
+    const uint32_t wave = threadIdx.x / 64, pair = threadIdx.x % 64;
+    const uint32_t at_row = row0 + wave * kBlock;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t c = SRC == kBf16 ? pair * 2 + h : pair + 64 * h, col_t = col0 + c;
+        float v[kBlock];
+        uint32_t largest = 0;
+#pragma unroll
+        for (int i = 0; i < kBlock; ++i) {
+            if constexpr (SRC == kBf16) {
+                const uint32_t w = *(const uint32_t*)&tile[wave * kBlock + i][pair * 2];
+                v[i] = __uint_as_float(h ? w & 0xffff0000u : w << 16);
+            } else {
+                v[i] = tile[wave * kBlock + i][c];
+            }
+            largest = max(largest, magnitude(v[i]));
+        }
+        const uint32_t byte = scale_byte<RANDOM>(largest);
+        i32x4 codes;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint64_t r = 0;
+            if constexpr (RANDOM) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) r |= (uint64_t)rands[wave * kBlock + j * 8 + i][c] << (8 * i);
+            }
+            codes[j] = (int)codes8<RANDOM>(v + 8 * j, byte, r);
+        }
+        if (col_t < s.cols && at_row < out_t.segments * kSegment) {
+            store_as(out_t.codes + (int64_t)col_t * out_t.segments * kSegmentBytes + at_row / 2, codes);
+            out_t.scales[(int64_t)col_t * out_t.scale_pitch + at_row / kBlock] = (uint8_t)byte;
+        }
+        if (col_t < s.cols && (out_t.segments & 1) && row0 + kTile == out_t.segments * kSegment)
+            out_t.scales[(int64_t)col_t * out_t.scale_pitch + out_t.segments * 8 + wave] = 0,
+            out_t.scales[(int64_t)col_t * out_t.scale_pitch + out_t.segments * 8 + 4 + wave] = 0;
+    }
+}
+
+// --------------------------------------------------------------------------------------------------- the way back --
+
+__device__ __forceinline__ float code_value(uint32_t code, float scale) {
+    // magnitude index 2 e + m: m / 2 for e = 0, (1 + m / 2) 2^(e - 1) else: as a float the exponent field e + 126 and the top mantissa
+    // bit m, of which 0 and 1 (that is 0 and 1/2) are no such numbers
+    const uint32_t i = code & 7u;
+    const float v = i < 2 ? 0.5f * (float)i : __uint_as_float((i << 22) + (126u << 23));
+    return __uint_as_float(__float_as_uint(v * scale) | (code & 8u) << 28);
+}
+
+template <bool FP32>
+__global__ __launch_bounds__(256) void dequantize_rows(Mx4 q, void* data, int64_t stride, uint32_t total) {
+    const uint32_t unit = blockIdx.x * 8 + threadIdx.x / 32, lane = threadIdx.x % 32;
+    if (unit >= total) return;
+    const uint32_t row = unit / q.segments, seg = unit - row * q.segments;
+    const uint32_t col = seg * kSegment + lane * 8;
+    if (col >= q.cols) return;
+    const uint32_t c = load_as<uint32_t>(q.codes + ((int64_t)row * q.segments + seg) * kSegmentBytes + lane * 4);
+    const uint32_t byte = q.scales[(int64_t)row * q.scale_pitch + seg * 8 + lane / 4];
+    const float scale = __uint_as_float(byte == 0 ? 0x00400000u : byte == 255 ? 0x7fc00000u : byte << 23);
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = code_value(c >> (4 * i), scale);
+    const uint32_t left = q.cols - col;
+    if constexpr (FP32) {
+        float* p = (float*)data + (int64_t)row * stride + col;
+        if (left >= 8) {
+            store_as(p, f32x4{v[0], v[1], v[2], v[3]});
+            store_as(p + 4, f32x4{v[4], v[5], v[6], v[7]});
+        } else {
+            for (uint32_t i = 0; i < 8; ++i) if (i < left) p[i] = v[i];
+        }
+    } else {                     // two significant bits and an exponent of at least -128: exact in BF16
+        uint16_t* p = (uint16_t*)data + (int64_t)row * stride + col;
+        if (left >= 8) {
+            i32x4 w;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = (int)((__float_as_uint(v[2 * j]) >> 16) | (__float_as_uint(v[2 * j + 1]) & 0xffff0000u));
+            store_as(p, w);
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) if (i < left) p[i] = (uint16_t)(__float_as_uint(v[i]) >> 16);
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------- products --
+//
+// c[i][j] = sum over k of a[i][k] b[j][k].  The matrix instruction takes 16 rows of each operand and 128 terms: lane l has row l % 16
+// and, of four blocks of 32 terms, number l / 16.  Which blocks of the sum these are is ours to choose, as long as both operands agree: a
+// segment of 256 terms is two instructions s = 0, 1, and quarter q of the lanes takes block 2 q + s, so that a lane's 32 bytes of
+// codes and its two scale bytes are contiguous.  The instruction's rows are b's, its columns a's: a lane then holds four neighbouring
+// values of a row of c.
+
+__device__ __forceinline__ f32x4 mfma(i32x4 p, i32x4 q, f32x4 acc, int p_scale, int q_scale, int s) {
+    const i32x8 pw = {p[0], p[1], p[2], p[3], 0, 0, 0, 0}, qw = {q[0], q[1], q[2], q[3], 0, 0, 0, 0};
+    return s == 0 ? __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(pw, qw, acc, 4, 4, 0, p_scale, 0, q_scale)
+                  : __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(pw, qw, acc, 4, 4, 1, p_scale, 1, q_scale);
+}
+
+struct Result {
+    void* data;
+    int64_t stride;
+    uint32_t rows, cols;
+};
+
+template <bool FP32>
+__device__ __forceinline__ void store_result4(const Result& c, uint32_t row, uint32_t col, f32x4 v) {
+    if (row >= c.rows || col >= c.cols) return;
+    const uint32_t left = c.cols - col;
+    if constexpr (FP32) {
+        float* p = (float*)c.data + (int64_t)row * c.stride + col;
+        if (left >= 4) store_as(p, v);
+        else for (uint32_t i = 0; i < 4; ++i) if (i < left) p[i] = v[i];
+    } else {
+        using bf16x4 = __bf16 __attribute__((ext_vector_type(4)));
+        const bf16x4 w = __builtin_convertvector(v, bf16x4);
+        __bf16* p = (__bf16*)c.data + (int64_t)row * c.stride + col;
+        if (left >= 4) store_as(p, w);
+        else for (uint32_t i = 0; i < 4; ++i) if (i < left) p[i] = w[i];
+    }
+}
+
+// A workgroup makes 16 columns by 16 rows of c; its wavefronts share out the segments of the sum and are added up through LDS.
+template <bool FP32, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void product_small(Mx4 b, Mx4 a, Result c) {
+    __shared__ f32x4 part[WAVES][64];
+    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64, q = lane / 16;
+    const uint32_t b_row = min(blockIdx.x * 16 + lane % 16, b.rows - 1), a_row = min(blockIdx.y * 16 + lane % 16, a.rows - 1);
+    const uint8_t* pb = b.codes + (int64_t)b_row * b.segments * kSegmentBytes + q * 32;
+    const uint8_t* pa = a.codes + (int64_t)a_row * a.segments * kSegmentBytes + q * 32;
+    const uint8_t* sb = b.scales + (int64_t)b_row * b.scale_pitch + q * 2;
+    const uint8_t* sa = a.scales + (int64_t)a_row * a.scale_pitch + q * 2;
+    f32x4 acc = {};
+    for (uint32_t seg = wave; seg < b.segments; seg += WAVES) {
+        i32x4 wb[2], wa[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            wb[s] = load_as<i32x4>(pb + (int64_t)seg * kSegmentBytes + s * 16);
+            wa[s] = load_as<i32x4>(pa + (int64_t)seg * kSegmentBytes + s * 16);
+        }
+        const int xb = load_as<uint16_t>(sb + seg * 8), xa = load_as<uint16_t>(sa + seg * 8);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) acc = mfma(wb[s], wa[s], acc, xb, xa, s);
+    }
+    part[wave][lane] = acc;
+    __syncthreads();
+    if (wave == 0) {
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) acc += part[w][lane];
+        store_result4<FP32>(c, blockIdx.y * 16 + lane % 16, blockIdx.x * 16 + q * 4, acc);
+    }
+}
+
+__global__ __launch_bounds__(256) void fill_zero(Result c, int bytes) {
+    const uint32_t col = blockIdx.x * 256 + threadIdx.x;
+    if (col >= c.cols) return;
+    for (uint32_t row = blockIdx.y; row < c.rows; row += gridDim.y) {
+        if (bytes == 4) ((float*)c.data)[(int64_t)row * c.stride + col] = 0.0f;
+        else ((uint16_t*)c.data)[(int64_t)row * c.stride + col] = 0;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------ host --
+
+int check_mx4(const flashoptim_mx4* m) {
+    if (!m || m->rows < 0 || m->cols < 0) return FLASHOPTIM_ERR_INVALID_ARG;
+    if (m->rows >= ((int64_t)1 << 31) || m->cols >= ((int64_t)1 << 31)) return FLASHOPTIM_ERR_NUMEL_RANGE;
+    // half a wavefront to a segment: a launch stays below 2^32 lanes
+    if (m->rows > 0 && up(m->cols, kSegment) >= ((int64_t)1 << 27) / m->rows) return FLASHOPTIM_ERR_NUMEL_RANGE;
+    if (m->rows == 0 || m->cols == 0) return FLASHOPTIM_OK;
+    if (!m->codes || !m->scales) return FLASHOPTIM_ERR_INVALID_ARG;
+    if (!fo::aligned_to(m->codes, 16) || !fo::aligned_to(m->scales, 16)) return FLASHOPTIM_ERR_MISALIGNED;
+    return FLASHOPTIM_OK;
+}
+
+template <int SRC, bool RANDOM>
+int launch_quantize(const Source& s, const flashoptim_mx4* out, const flashoptim_mx4* out_t, hipStream_t stream) {
+    if (!out_t) {
+        const Mx4 o = to_dev(*out);
+        const uint32_t total = o.rows * o.segments;
+        hipLaunchKernelGGL((quantize_rows<SRC, RANDOM>), dim3((total + 7) / 8), dim3(256), 0, stream, s, o, total);
+    } else {
+        const Mx4 t = to_dev(*out_t), o = out ? to_dev(*out) : Mx4{};
+        const dim3 grid((unsigned)(up(s.cols, kSegment) * (kSegment / kTile)), (unsigned)(up(s.rows, kSegment) * (kSegment / kTile)));
+        hipLaunchKernelGGL((quantize_both<SRC, RANDOM>), grid, dim3(256), 0, stream, s, o, t, out != nullptr);
+    }
+    return fo::hip_status(hipGetLastError());
+}
+
+template <int SRC>
+int launch_quantize(const Source& s, const flashoptim_mx4* out, const flashoptim_mx4* out_t, hipStream_t stream) {
+    return s.rand ? launch_quantize<SRC, true>(s, out, out_t, stream) : launch_quantize<SRC, false>(s, out, out_t, stream);
+}
+
+// All arguments checked.
+int quantize(const flashoptim_matrix& x, const int8_t* rho, const uint8_t* rand, const flashoptim_mx4* out, const flashoptim_mx4* out_t,
+             hipStream_t stream) {
+    if (x.rows == 0 || x.cols == 0) return FLASHOPTIM_OK;
+    const Source s = {x.data, rho, rand, x.stride, (uint32_t)x.rows, (uint32_t)x.cols};
+    if (rho) return launch_quantize<kSplit>(s, out, out_t, stream);
+    return x.dtype == FLASHOPTIM_FP32 ? launch_quantize<kFp32>(s, out, out_t, stream) : launch_quantize<kBf16>(s, out, out_t, stream);
+}
+
+int product(const flashoptim_mx4& a, const flashoptim_mx4& b, const flashoptim_matrix& c, void* workspace, hipStream_t stream) {
+    (void)workspace;
+    if (c.rows == 0 || c.cols == 0) return FLASHOPTIM_OK;
+    const Result r = {c.data, c.stride, (uint32_t)c.rows, (uint32_t)c.cols};
+    const bool fp32 = c.dtype == FLASHOPTIM_FP32;
+    if (a.cols == 0) {
+        hipLaunchKernelGGL(fill_zero, dim3((unsigned)up(c.cols, 256), (unsigned)(c.rows < 1024 ? c.rows : 1024)), dim3(256), 0, stream, r, fp32 ? 4 : 2);
+        return fo::hip_status(hipGetLastError());
+    }
+    const dim3 grid((unsigned)up(c.cols, 16), (unsigned)up(c.rows, 16));
+    if (fp32) hipLaunchKernelGGL((product_small<true, 8>), grid, dim3(512), 0, stream, to_dev(b), to_dev(a), r);
+    else hipLaunchKernelGGL((product_small<false, 8>), grid, dim3(512), 0, stream, to_dev(b), to_dev(a), r);
+    return fo::hip_status(hipGetLastError());
+}
+
+// Codes and scales of a matrix in a workspace.
+int64_t mx4_bytes(int64_t rows, int64_t cols) { return rows * (up(cols, kSegment) * kSegmentBytes + 16 * up(cols, 2 * kSegment)); }
+int64_t align16(int64_t n) { return up(n, 16) * 16; }
+flashoptim_mx4 carve(uint8_t*& at, int64_t rows, int64_t cols) {
+    flashoptim_mx4 m = {at, at + rows * up(cols, kSegment) * kSegmentBytes, rows, cols};
+    at += align16(mx4_bytes(rows, cols));
+    return m;
+}
+
+int64_t check_sizes(int64_t m, int64_t n, int64_t k) {
+    if (m < 0 || n < 0 || k < 0) return FLASHOPTIM_ERR_INVALID_ARG;
+    const int64_t most = (int64_t)1 << 31;
+    if (m >= most || n >= most || k >= most) return FLASHOPTIM_ERR_NUMEL_RANGE;
+    const int64_t sizes[3] = {m, n, k};
+    for (int i = 0; i < 3; ++i)
+        for (int j = 0; j < 3; ++j)
+            if (sizes[i] > 0 && up(sizes[j], kSegment) >= ((int64_t)1 << 27) / sizes[i]) return FLASHOPTIM_ERR_NUMEL_RANGE;
+    return FLASHOPTIM_OK;
+}
+int64_t product_bytes(int64_t m, int64_t n, int64_t k) {
+    (void)m; (void)n; (void)k;
+    return 0;
+}
+
+int check_workspace(const void* workspace, int64_t bytes, int64_t need) {
+    if (need < 0) return (int)need;
+    if (need == 0) return FLASHOPTIM_OK;
+    if (!workspace) return FLASHOPTIM_ERR_INVALID_ARG;
+    if (bytes < need) return FLASHOPTIM_ERR_WORKSPACE;
+    return fo::aligned_to(workspace, 16) ? FLASHOPTIM_OK : FLASHOPTIM_ERR_MISALIGNED;
+}
+
+#define FO_TRY(expr)                          \
+    do {                                      \
+        const int rc_ = (int)(expr);          \
+        if (rc_ != FLASHOPTIM_OK) return rc_; \
+    } while (0)
+
+}  // namespace
+
+extern "C" {
+
+int flashoptim_mx4_quantize(const flashoptim_matrix* x, const int8_t* rho, const uint8_t* rand, const flashoptim_mx4* out,
+                            const flashoptim_mx4* out_t, void* stream) {
+    FO_TRY(fo::check_matrix(x));
+    if (!out && !out_t) return FLASHOPTIM_ERR_INVALID_ARG;
+    if (rho && x->dtype != FLASHOPTIM_BF16) return FLASHOPTIM_ERR_INVALID_ARG;
+    if (out) FO_TRY(check_mx4(out));
+    if (out_t) FO_TRY(check_mx4(out_t));
+    if (out && (out->rows != x->rows || out->cols != x->cols)) return FLASHOPTIM_ERR_INVALID_ARG;
+    if (out_t && (out_t->rows != x->cols || out_t->cols != x->rows)) return FLASHOPTIM_ERR_INVALID_ARG;
+    if (out_t && up(x->rows, kSegment) * (kSegment / kTile) > 65535) return FLASHOPTIM_ERR_NUMEL_RANGE;
+    return quantize(*x, rho, rand, out, out_t, (hipStream_t)stream);
+}
+
+int flashoptim_mx4_dequantize(const flashoptim_mx4* q, const flashoptim_matrix* x, void* stream) {
+    FO_TRY(check_mx4(q));
+    FO_TRY(fo::check_matrix(x));
+    if (q->rows != x->rows || q->cols != x->cols) return FLASHOPTIM_ERR_INVALID_ARG;
+    if (x->rows == 0 || x->cols == 0) return FLASHOPTIM_OK;
+    const Mx4 m = to_dev(*q);
+    const uint32_t total = m.rows * m.segments;
+    if (x->dtype == FLASHOPTIM_FP32) hipLaunchKernelGGL(dequantize_rows<true>, dim3((total + 7) / 8), dim3(256), 0, (hipStream_t)stream, m, x->data, x->stride, total);
+    else hipLaunchKernelGGL(dequantize_rows<false>, dim3((total + 7) / 8), dim3(256), 0, (hipStream_t)stream, m, x->data, x->stride, total);
+    return fo::hip_status(hipGetLastError());
+}
+
+int64_t flashoptim_mx4_matmul_workspace(int64_t m, int64_t n, int64_t k) {
+    FO_TRY(check_sizes(m, n, k));
+    return product_bytes(m, n, k);
+}
+
+int64_t flashoptim_mx4_linear_workspace(int64_t m, int64_t n, int64_t k) {
+    FO_TRY(check_sizes(m, n, k));
+    return align16(mx4_bytes(m, k)) + product_bytes(m, n, k);
+}
+
+int64_t flashoptim_mx4_linear_backward_workspace(int64_t m, int64_t n, int64_t k) {
+    FO_TRY(check_sizes(m, n, k));
+    const int64_t dx = product_bytes(m, k, n), dw = product_bytes(n, k, m);
+    return align16(mx4_bytes(m, n)) + align16(mx4_bytes(n, m)) + (dx > dw ? dx : dw);
+}
+
+int flashoptim_mx4_matmul(const flashoptim_mx4* a, const flashoptim_mx4* b, const flashoptim_matrix* c, void* workspace,
+                          int64_t workspace_bytes, void* stream) {
+    FO_TRY(check_mx4(a));
+    FO_TRY(check_mx4(b));
+    FO_TRY(fo::check_matrix(c));
+    if (a->cols != b->cols || c->rows != a->rows || c->cols != b->rows) return FLASHOPTIM_ERR_INVALID_ARG;
+    FO_TRY(check_sizes(a->rows, b->rows, a->cols));
+    FO_TRY(check_workspace(workspace, workspace_bytes, product_bytes(a->rows, b->rows, a->cols)));
+    return product(*a, *b, *c, workspace, (hipStream_t)stream);
+}
+
+int flashoptim_mx4_linear(const flashoptim_matrix* x, const flashoptim_mx4* w, const flashoptim_mx4* xt, const flashoptim_matrix* y,
+                          void* workspace, int64_t workspace_bytes, void* stream) {
+    FO_TRY(fo::check_matrix(x));
+    FO_TRY(check_mx4(w));
+    FO_TRY(fo::check_matrix(y));
+    if (xt) FO_TRY(check_mx4(xt));
+    if (w->cols != x->cols || y->rows != x->rows || y->cols != w->rows) return FLASHOPTIM_ERR_INVALID_ARG;
+    if (xt && (xt->rows != x->cols || xt->cols != x->rows)) return FLASHOPTIM_ERR_INVALID_ARG;
+    if (xt && up(x->rows, kSegment) * (kSegment / kTile) > 65535) return FLASHOPTIM_ERR_NUMEL_RANGE;
+    FO_TRY(check_workspace(workspace, workspace_bytes, flashoptim_mx4_linear_workspace(x->rows, w->rows, x->cols)));
+    uint8_t* at = (uint8_t*)workspace;
+    const flashoptim_mx4 q = carve(at, x->rows, x->cols);
+    FO_TRY(quantize(*x, nullptr, nullptr, &q, xt, (hipStream_t)stream));
+    return product(q, *w, *y, at, (hipStream_t)stream);
+}
+
+int flashoptim_mx4_linear_backward(const flashoptim_matrix* dy, const uint8_t* rand, const flashoptim_mx4* wt, const flashoptim_mx4* xt,
+                                   const flashoptim_matrix* dx, const flashoptim_matrix* dw, void* workspace, int64_t workspace_bytes,
+                                   void* stream) {
+    FO_TRY(fo::check_matrix(dy));
+    if (!dx && !dw) return FLASHOPTIM_ERR_INVALID_ARG;
+    const int64_t m = dy->rows, n = dy->cols;
+    int64_t k = 0;
+    if (dx) {
+        FO_TRY(check_mx4(wt));
+        FO_TRY(fo::check_matrix(dx));
+        k = dx->cols;
+        if (dx->rows != m || wt->rows != k || wt->cols != n) return FLASHOPTIM_ERR_INVALID_ARG;
+    }
+    if (dw) {
+        FO_TRY(check_mx4(xt));
+        FO_TRY(fo::check_matrix(dw));
+        if (dx && dw->cols != k) return FLASHOPTIM_ERR_INVALID_ARG;
+        k = dw->cols;
+        if (dw->rows != n || xt->rows != k || xt->cols != m) return FLASHOPTIM_ERR_INVALID_ARG;
+        if (up(m, kSegment) * (kSegment / kTile) > 65535) return FLASHOPTIM_ERR_NUMEL_RANGE;
+    }
+    FO_TRY(check_workspace(workspace, workspace_bytes, flashoptim_mx4_linear_backward_workspace(m, n, k)));
+    uint8_t* at = (uint8_t*)workspace;
+    const flashoptim_mx4 q = carve(at, m, n), qt = carve(at, n, m);
+    FO_TRY(quantize(*dy, nullptr, rand, dx ? &q : nullptr, dw ? &qt : nullptr, (hipStream_t)stream));
+    if (dx) FO_TRY(product(q, *wt, *dx, at, (hipStream_t)stream));
+    if (dw) FO_TRY(product(qt, *xt, *dw, at, (hipStream_t)stream));
+    return FLASHOPTIM_OK;
+}
+
+}  // extern "C"

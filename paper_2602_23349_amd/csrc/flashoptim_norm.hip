@@ -1,0 +1,658 @@
+// The norms before and after a block with its gate and residual scale, and their gradients, for gfx950.
+//
+// Forward, by row: u = f or norm(f) w + b;  h = a x + c act(gate) u;  y = norm(h) w' + b'.  Backward, with hat(v) = (v - mean) rstd:
+//   dH = dh + rstd (g - hat(h) mean(g hat(h)) [- mean(g]),  g = dy w'           (the bracket: layer norms only)
+//   dx = a dH,  dgate = sum c dH u act',  du = c dH act,  df = the same through the norm behind
+//   dw' = sum dy hat(h),  db' = sum dy,  dw = sum du hat(f),  db = sum du       (over rows)
+// Bound: HBM.  A row is loaded once, kept in FP32 registers through all its sums, and stored once.
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "flashoptim.h"
+#include "flashoptim_host.h"
+
+namespace {
+
+using i32x4 = int __attribute__((ext_vector_type(4)));
+using f32x4 = float __attribute__((ext_vector_type(4)));
+using f32x8 = float __attribute__((ext_vector_type(8)));
+using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
+
+template <typename T>
+__device__ __forceinline__ T load_as(const void* p) {       // any alignment: the hardware takes global accesses at any byte
+    T v;
+    __builtin_memcpy(&v, p, sizeof(T));
+    return v;
+}
+template <typename T>
+__device__ __forceinline__ void store_as(void* p, T v) {
+    __builtin_memcpy(p, &v, sizeof(T));
+}
+
+// A matrix as a kernel takes it; data NULL: left out.
+struct Rows {
+    char* data;
+    int64_t stride;      // values
+};
+Rows to_dev(const flashoptim_matrix* m) { return m ? Rows{(char*)m->data, m->rows > 1 ? m->stride : 0} : Rows{nullptr, 0}; }
+
+// Eight values from `at` on, of which `left` exist (the others: 0).
+__device__ __forceinline__ f32x8 load8(const void* p, bool fp32, int64_t at, int left) {
+    f32x8 v = {};
+    if (fp32) {
+        const float* f = (const float*)p + at;
+        if (left >= 8) {
+            const f32x4 a = load_as<f32x4>(f), b = load_as<f32x4>(f + 4);
+            v = f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) if (i < left) v[i] = f[i];
+        }
+    } else {
+        const uint16_t* f = (const uint16_t*)p + at;
+        if (left >= 8) {
+            const i32x4 w = load_as<i32x4>(f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[2 * i] = __uint_as_float((uint32_t)w[i] << 16);
+                v[2 * i + 1] = __uint_as_float((uint32_t)w[i] & 0xffff0000u);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) if (i < left) v[i] = __uint_as_float((uint32_t)f[i] << 16);
+        }
+    }
+    return v;
+}
+__device__ __forceinline__ void store8(void* p, bool fp32, int64_t at, int left, f32x8 v) {
+    if (fp32) {
+        float* f = (float*)p + at;
+        if (left >= 8) {
+            store_as(f, f32x4{v[0], v[1], v[2], v[3]});
+            store_as(f + 4, f32x4{v[4], v[5], v[6], v[7]});
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) if (i < left) f[i] = v[i];
+        }
+    } else {
+        __bf16* f = (__bf16*)p + at;
+        const bf16x8 w = __builtin_convertvector(v, bf16x8);
+        if (left >= 8) store_as(f, w);
+        else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) if (i < left) f[i] = w[i];
+        }
+    }
+}
+
+// The sum over a wavefront, in every lane, in a fixed order.
+__device__ __forceinline__ float wave_sum(float v) {
+#define FO_ADD(ctrl, rows) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl, rows, 0xf, false))
+    FO_ADD(0x111, 0xf);      // row_shr 1, 2, 4, 8: lane 15 of each row of 16 has the row's sum
+    FO_ADD(0x112, 0xf);
+    FO_ADD(0x114, 0xf);
+    FO_ADD(0x118, 0xf);
+    FO_ADD(0x142, 0xa);      // row_bcast 15, into the second and the fourth row
+    FO_ADD(0x143, 0xc);      // row_bcast 31, into the upper half
+#undef FO_ADD
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
+// Sums over the lanes that share a row.  With more than one wavefront through LDS: the two halves of `part` alternate, so that one barrier
+// lies between a half's readers and its next writers.
+template <int LANES>
+struct RowSums {
+    static constexpr int kWaves = LANES / 64;
+    f32x4* part;             // [2][kWaves], the first two of each in use
+    int turn;
+    __device__ __forceinline__ void sum2(float& a, float& b) {
+        a = wave_sum(a);
+        b = wave_sum(b);
+        if constexpr (kWaves > 1) {
+            f32x4* p = part + turn * kWaves;
+            turn ^= 1;
+            if (threadIdx.x % 64 == 0) p[threadIdx.x / 64] = f32x4{a, b, 0.0f, 0.0f};
+            __syncthreads();
+            a = b = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) { a += p[w][0]; b += p[w][1]; }
+        }
+    }
+    __device__ __forceinline__ float sum(float a) {
+        float none = 0.0f;
+        sum2(a, none);
+        return a;
+    }
+};
+
+__device__ __forceinline__ float sigmoid(float v) { return 1.0f / (1.0f + __expf(-v)); }
+
+struct NormArgs {
+    Rows x, f, gate, h, y;
+    const void *post_weight, *post_bias, *pre_weight, *pre_bias;
+    float* stats;
+    uint32_t rows, rows_per_gate;
+    int32_t cols;
+    float eps, residual_scale, branch_scale, inv_cols;
+    uint8_t layer, post_norm, sigmoid, param_fp32;
+};
+
+// Mean and 1/sqrt(mean square distance + eps) of the row whose values the lanes have.
+template <int LANES, int CHUNKS>
+__device__ __forceinline__ void moments(RowSums<LANES>& sums, const f32x8 (&v)[CHUNKS], const int (&left)[CHUNKS], const NormArgs& a, float* mean,
+                                        float* rstd) {
+    *mean = 0.0f;
+    if (a.layer) {
+        float s = 0.0f;
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s += v[j][i];
+        *mean = sums.sum(s) * a.inv_cols;
+    }
+    float s = 0.0f;
+#pragma unroll
+    for (int j = 0; j < CHUNKS; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float d = i < left[j] ? v[j][i] - *mean : 0.0f;
+            s = fmaf(d, d, s);
+        }
+    *rstd = 1.0f / sqrtf(fmaf(sums.sum(s), a.inv_cols, a.eps));
+}
+
+template <int CHUNKS>
+__device__ __forceinline__ void affine(f32x8 (&v)[CHUNKS], const int (&left)[CHUNKS], const int (&col)[CHUNKS], const NormArgs& a, const void* weight,
+                                       const void* bias, float mean, float rstd) {
+#pragma unroll
+    for (int j = 0; j < CHUNKS; ++j) {
+        v[j] = (v[j] - mean) * rstd;
+        if (weight) v[j] *= load8(weight, a.param_fp32, col[j], left[j]);
+        if (bias) v[j] += load8(bias, a.param_fp32, col[j], left[j]);
+    }
+}
+
+// LANES lanes to a row, each CHUNKS times eight neighbouring values.
+template <bool STREAM_FP32, bool BRANCH_FP32, int LANES, int CHUNKS>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_rows(NormArgs a) {
+    constexpr int kLines = LANES < 256 ? 256 / LANES : 1;
+    __shared__ f32x4 part[2 * (LANES / 64)];
+    const uint32_t row = blockIdx.x * kLines + (kLines > 1 ? threadIdx.x / LANES : 0);
+    const int lane = threadIdx.x % LANES;
+    if (kLines > 1 && row >= a.rows) return;
+    RowSums<LANES> sums = {part, 0};
+    int col[CHUNKS], left[CHUNKS];
+    f32x8 h[CHUNKS], u[CHUNKS];
+#pragma unroll
+    for (int j = 0; j < CHUNKS; ++j) {
+        col[j] = (j * LANES + lane) * 8;
+        left[j] = a.cols - col[j];
+        h[j] = load8(a.x.data, STREAM_FP32, (int64_t)row * a.x.stride + col[j], left[j]);
+    }
+    float post_mean = 0.0f, post_rstd = 0.0f, pre_mean = 0.0f, pre_rstd = 0.0f;
+    if (a.f.data) {
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j) u[j] = load8(a.f.data, BRANCH_FP32, (int64_t)row * a.f.stride + col[j], left[j]);
+        if (a.post_norm) {
+            moments(sums, u, left, a, &post_mean, &post_rstd);
+            affine(u, left, col, a, a.post_weight, a.post_bias, post_mean, post_rstd);
+        }
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j) {
+            if (a.gate.data) {
+                f32x8 g = load8(a.gate.data, BRANCH_FP32, (int64_t)(row / a.rows_per_gate) * a.gate.stride + col[j], left[j]);
+                if (a.sigmoid) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) g[i] = sigmoid(g[i]);
+                }
+                u[j] *= g;
+            }
+            h[j] = a.residual_scale * h[j] + a.branch_scale * u[j];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[j][i] = i < left[j] ? h[j][i] : 0.0f;      // (a bias, or an infinite scale, behind the row's end)
+            store8(a.h.data, STREAM_FP32, (int64_t)row * a.h.stride + col[j], left[j], h[j]);
+        }
+    }
+    if (a.y.data) {
+        moments(sums, h, left, a, &pre_mean, &pre_rstd);
+        affine(h, left, col, a, a.pre_weight, a.pre_bias, pre_mean, pre_rstd);
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j) store8(a.y.data, BRANCH_FP32, (int64_t)row * a.y.stride + col[j], left[j], h[j]);
+    }
+    if (a.stats && lane == 0) {
+        const int64_t rows = a.rows;
+        a.stats[row] = post_mean;
+        a.stats[rows + row] = post_rstd;
+        a.stats[2 * rows + row] = pre_mean;
+        a.stats[3 * rows + row] = pre_rstd;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------- backward --
+
+// Sums over rows are formed in two stages of fixed order: a workgroup adds up the rows of its part in registers and leaves one row
+// of sums for each kind of them; sum_parts adds up the parts.  Of a gate that serves many rows no part crosses the boundary
+// (units are then rows); of one that serves few a part takes whole groups (units are groups), and their sums are complete.
+enum Sum { kPreWeight, kPreBias, kPostWeight, kPostBias, kGate, kSums };
+
+struct GradArgs {
+    Rows h, f, gate, dy, dh, dx, df, dgate;
+    const void *post_weight, *post_bias, *pre_weight;
+    const float* stats;
+    float* part;                 // [kind in use][parts][cols]
+    int32_t slot[kSums];         // which kind in use, or -1
+    uint32_t rows, rows_per_gate, parts;
+    uint32_t unit_rows, part_units, units_per_group;      // (units_per_group: units that parts may not reach beyond)
+    uint32_t parts_per_group;
+    int32_t cols;
+    float residual_scale, branch_scale, inv_cols;
+    uint8_t post_norm, sigmoid, param_fp32, gate_done;      // gate_done: a unit's sums of the gate are complete
+};
+
+template <bool STREAM_FP32, bool BRANCH_FP32, int LANES, int CHUNKS, bool LAYER, bool BRANCH>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_gradients(GradArgs a) {
+    constexpr int kLines = LANES < 256 ? 256 / LANES : 1;
+    __shared__ f32x4 part_sums[2 * (LANES / 64)];
+    __shared__ float joined[kLines > 1 ? kLines : 1][kLines > 1 ? LANES * 8 * CHUNKS : 1];
+    const int line = kLines > 1 ? threadIdx.x / LANES : 0, lane = threadIdx.x % LANES;
+    RowSums<LANES> sums = {part_sums, 0};
+    int col[CHUNKS], left[CHUNKS];
+#pragma unroll
+    for (int j = 0; j < CHUNKS; ++j) {
+        col[j] = (j * LANES + lane) * 8;
+        left[j] = a.cols - col[j];
+    }
+    f32x8 acc[kSums][CHUNKS] = {};
+    const uint32_t group = blockIdx.x / a.parts_per_group, in_group = blockIdx.x - group * a.parts_per_group;
+    const uint32_t begin = group * a.units_per_group + in_group * a.part_units;
+    const uint32_t end = min(begin + a.part_units, min((group + 1) * a.units_per_group, (a.rows + a.unit_rows - 1) / a.unit_rows));
+    for (uint32_t unit = begin + line; unit < end; unit += kLines) {
+        for (uint32_t row = unit * a.unit_rows; row < unit * a.unit_rows + a.unit_rows; ++row) {
+            f32x8 total[CHUNKS];
+#pragma unroll
+            for (int j = 0; j < CHUNKS; ++j)
+                total[j] = a.dh.data ? load8(a.dh.data, STREAM_FP32, (int64_t)row * a.dh.stride + col[j], left[j]) : f32x8{};
+            const int64_t rows = a.rows;
+            if (a.dy.data) {
+                const float mean = a.stats[2 * rows + row], rstd = a.stats[3 * rows + row];
+                f32x8 hat[CHUNKS], g[CHUNKS];
+                float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+                for (int j = 0; j < CHUNKS; ++j) {
+                    hat[j] = (load8(a.h.data, STREAM_FP32, (int64_t)row * a.h.stride + col[j], left[j]) - mean) * rstd;
+                    g[j] = load8(a.dy.data, BRANCH_FP32, (int64_t)row * a.dy.stride + col[j], left[j]);
+                    acc[kPreWeight][j] += g[j] * hat[j];
+                    if (LAYER) acc[kPreBias][j] += g[j];
+                    if (a.pre_weight) g[j] *= load8(a.pre_weight, a.param_fp32, col[j], left[j]);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        s0 = fmaf(g[j][i], hat[j][i], s0);
+                        if (LAYER) s1 += g[j][i];
+                    }
+                }
+                sums.sum2(s0, s1);
+                s0 *= a.inv_cols;
+                s1 *= a.inv_cols;
+#pragma unroll
+                for (int j = 0; j < CHUNKS; ++j) total[j] += rstd * (g[j] - hat[j] * s0 - (LAYER ? s1 : 0.0f));
+            }
+            if (a.dx.data) {
+#pragma unroll
+                for (int j = 0; j < CHUNKS; ++j)
+                    store8(a.dx.data, STREAM_FP32, (int64_t)row * a.dx.stride + col[j], left[j], BRANCH ? a.residual_scale * total[j] : total[j]);
+            }
+            if constexpr (BRANCH) {
+                const float mean = a.post_norm ? a.stats[row] : 0.0f, rstd = a.post_norm ? a.stats[rows + row] : 1.0f;
+                f32x8 hat[CHUNKS];
+                float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+                for (int j = 0; j < CHUNKS; ++j) {
+                    hat[j] = (load8(a.f.data, BRANCH_FP32, (int64_t)row * a.f.stride + col[j], left[j]) - mean) * rstd;
+                    f32x8 du = a.branch_scale * total[j];
+                    if (a.gate.data) {
+                        f32x8 act = load8(a.gate.data, BRANCH_FP32, (int64_t)(row / a.rows_per_gate) * a.gate.stride + col[j], left[j]);
+                        f32x8 u = hat[j];
+                        if (a.post_weight) u *= load8(a.post_weight, a.param_fp32, col[j], left[j]);
+                        if (a.post_bias) u += load8(a.post_bias, a.param_fp32, col[j], left[j]);
+                        u *= du;
+                        if (a.sigmoid) {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                act[i] = sigmoid(act[i]);
+                                u[i] *= act[i] * (1.0f - act[i]);
+                            }
+                        }
+                        acc[kGate][j] += u;
+                        du *= act;
+                    }
+                    if (a.post_norm) {
+                        acc[kPostWeight][j] += du * hat[j];
+                        if (LAYER) acc[kPostBias][j] += du;
+                        if (a.post_weight) du *= load8(a.post_weight, a.param_fp32, col[j], left[j]);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            s0 += i < left[j] ? du[i] * hat[j][i] : 0.0f;
+                            if (LAYER) s1 += i < left[j] ? du[i] : 0.0f;
+                        }
+                    }
+                    total[j] = du;
+                }
+                if (a.post_norm) {
+                    sums.sum2(s0, s1);
+                    s0 *= a.inv_cols;
+                    s1 *= a.inv_cols;
+                }
+                if (a.df.data) {
+#pragma unroll
+                    for (int j = 0; j < CHUNKS; ++j) {
+                        if (a.post_norm) total[j] = rstd * (total[j] - hat[j] * s0 - (LAYER ? s1 : 0.0f));
+                        store8(a.df.data, BRANCH_FP32, (int64_t)row * a.df.stride + col[j], left[j], total[j]);
+                    }
+                }
+            }
+        }
+        if (BRANCH && a.gate_done && a.dgate.data) {
+#pragma unroll
+            for (int j = 0; j < CHUNKS; ++j) {
+                store8(a.dgate.data, BRANCH_FP32, (int64_t)unit * a.dgate.stride + col[j], left[j], acc[kGate][j]);
+                acc[kGate][j] = f32x8{};
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kSums; ++k) {
+        if (a.slot[k] < 0 || (!BRANCH && k >= kPostWeight) || (!LAYER && (k == kPreBias || k == kPostBias))) continue;
+        float* out = a.part + ((int64_t)a.slot[k] * a.parts + blockIdx.x) * a.cols;
+        if constexpr (kLines > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < CHUNKS; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) joined[line][(j * 8 + i) * LANES + lane] = acc[k][j][i];
+            __syncthreads();
+            if (line == 0) {
+#pragma unroll
+                for (int j = 0; j < CHUNKS; ++j) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+#pragma unroll
+                        for (int l = 1; l < kLines; ++l) acc[k][j][i] += joined[l][(j * 8 + i) * LANES + lane];
+                    store8(out, true, col[j], left[j], acc[k][j]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < CHUNKS; ++j) store8(out, true, col[j], left[j], acc[k][j]);
+        }
+    }
+}
+
+// out[group][col] = the sum of part[group * parts .. (group + 1) * parts)[col].  One entry for each kind of sum.
+struct PartSum {
+    const float* part;
+    void* out;
+    int64_t stride;
+    uint32_t parts, groups;
+    int32_t fp32;
+};
+struct PartSums {
+    PartSum of[kSums];
+    int32_t cols;
+};
+
+__global__ __launch_bounds__(256) void sum_parts(PartSums p) {
+    __shared__ float joined[4][64];
+    const PartSum& s = p.of[blockIdx.z];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = blockIdx.x * 64 + lane;
+    for (uint32_t group = blockIdx.y; group < s.groups; group += gridDim.y) {
+        float v = 0.0f;
+        if (col < p.cols) {
+            const float* at = s.part + ((int64_t)group * s.parts) * p.cols + col;
+            for (uint32_t i = wave; i < s.parts; i += 4) v += at[(int64_t)i * p.cols];
+        }
+        __syncthreads();
+        joined[wave][lane] = v;
+        __syncthreads();
+        if (wave == 0 && col < p.cols) {
+            v = ((joined[0][lane] + joined[1][lane]) + joined[2][lane]) + joined[3][lane];
+            const int64_t at = (int64_t)group * s.stride + col;
+            if (s.fp32) ((float*)s.out)[at] = v;
+            else ((__bf16*)s.out)[at] = (__bf16)v;
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------ host --
+
+constexpr int64_t kMaxCols = 16384;
+
+int check_spec(const flashoptim_block_norm_spec* s) {
+    if (!s || s->cols < 1 || s->kind < 0 || s->kind > 1 || s->post_norm < 0 || s->post_norm > 1 || s->gate_act < 0 || s->gate_act > 1 ||
+        (s->param_dtype != FLASHOPTIM_BF16 && s->param_dtype != FLASHOPTIM_FP32) || !(s->eps >= 0.0f))
+        return FLASHOPTIM_ERR_INVALID_ARG;
+    if (s->kind == FLASHOPTIM_RMS_NORM && (s->post_bias || s->pre_bias)) return FLASHOPTIM_ERR_INVALID_ARG;
+    if (s->cols > kMaxCols) return FLASHOPTIM_ERR_NUMEL_RANGE;
+    const uintptr_t unit = (uintptr_t)fo::elem_bytes(s->param_dtype);
+    for (const void* p : {s->post_weight, s->post_bias, s->pre_weight, s->pre_bias})
+        if (!fo::aligned_to(p, unit)) return FLASHOPTIM_ERR_MISALIGNED;
+    return FLASHOPTIM_OK;
+}
+
+// A matrix that may be left out: rows by cols, of this type if it is there.
+int check_rows(const flashoptim_matrix* m, int64_t rows, int64_t cols, int dtype) {
+    if (!m) return FLASHOPTIM_OK;
+    const int rc = fo::check_matrix(m);
+    if (rc != FLASHOPTIM_OK) return rc;
+    return m->rows == rows && m->cols == cols && m->dtype == dtype ? FLASHOPTIM_OK : FLASHOPTIM_ERR_INVALID_ARG;
+}
+
+#define FO_TRY(expr)                          \
+    do {                                      \
+        const int rc_ = (int)(expr);          \
+        if (rc_ != FLASHOPTIM_OK) return rc_; \
+    } while (0)
+
+// The gate's rows, 0 without a gate.
+int check_gate(const flashoptim_matrix* gate, int64_t rows, int64_t cols, int dtype, int64_t* rows_per_gate) {
+    *rows_per_gate = rows > 0 ? rows : 1;
+    if (!gate) return FLASHOPTIM_OK;
+    FO_TRY(check_rows(gate, gate->rows, cols, dtype));
+    if (gate->rows < 1 || rows % gate->rows != 0) return FLASHOPTIM_ERR_INVALID_ARG;
+    if (rows > 0) *rows_per_gate = rows / gate->rows;
+    return FLASHOPTIM_OK;
+}
+
+// Calls launch(lanes, chunks) as integral constants with the shape for rows of this many values.
+template <int LANES, int CHUNKS>
+struct Shape { static constexpr int kLanes = LANES, kChunks = CHUNKS; };
+template <typename F>
+void with_shape(int64_t cols, F launch) {
+    if (cols <= 512) launch(Shape<64, 1>{});
+    else if (cols <= 1024) launch(Shape<64, 2>{});
+    else if (cols <= 2048) launch(Shape<256, 1>{});
+    else if (cols <= 4096) launch(Shape<256, 2>{});
+    else if (cols <= 8192) launch(Shape<512, 2>{});
+    else launch(Shape<1024, 2>{});
+}
+inline int lines_of(int64_t cols) { return cols <= 1024 ? 4 : 1; }
+
+inline int64_t up(int64_t n, int64_t unit) { return (n + unit - 1) / unit; }
+
+// How the rows of a backward call are cut into parts.
+struct Parts {
+    int64_t unit_rows, part_units, units_per_group, parts_per_group, parts;
+    bool gate_done;
+};
+Parts cut(int64_t rows, int64_t gates, int64_t cols) {
+    const int64_t rows_per_gate = rows / gates;
+    const int64_t least = lines_of(cols);
+    int64_t part_rows = up(rows, 512);
+    if (part_rows < least) part_rows = least;
+    Parts p;
+    if (gates == 1 || rows_per_gate >= part_rows) {
+        p.unit_rows = 1;
+        p.part_units = part_rows;
+        p.units_per_group = rows_per_gate;
+        p.parts_per_group = up(rows_per_gate, part_rows);
+        p.parts = gates * p.parts_per_group;
+        p.gate_done = false;
+    } else {
+        p.unit_rows = rows_per_gate;
+        p.part_units = up(part_rows, rows_per_gate);
+        p.units_per_group = gates;
+        p.parts_per_group = p.parts = up(gates, p.part_units);
+        p.gate_done = true;
+    }
+    return p;
+}
+
+// Which sums a call wants, at most (workspace) or of this call.
+int64_t part_bytes(const flashoptim_block_norm_spec* spec, int64_t rows, int64_t gates) {
+    if (rows == 0) return 0;
+    const int64_t kinds = spec->kind == FLASHOPTIM_LAYER_NORM ? 5 : 3;
+    return kinds * cut(rows, gates, spec->cols).parts * spec->cols * 4;
+}
+
+}  // namespace
+
+extern "C" {
+
+int flashoptim_block_norm(const flashoptim_block_norm_spec* spec, const flashoptim_matrix* x, const flashoptim_matrix* f,
+                          const flashoptim_matrix* gate, const flashoptim_matrix* h, const flashoptim_matrix* y, float* stats,
+                          void* stream) {
+    FO_TRY(check_spec(spec));
+    FO_TRY(fo::check_matrix(x));
+    const int64_t rows = x->rows;
+    if (x->cols != spec->cols || (!f && !y) || (!f) != (!h) || (gate && !f)) return FLASHOPTIM_ERR_INVALID_ARG;
+    const int branch_type = f ? f->dtype : y->dtype;
+    if (branch_type == FLASHOPTIM_FP32 && x->dtype != FLASHOPTIM_FP32) return FLASHOPTIM_ERR_INVALID_ARG;
+    FO_TRY(check_rows(f, rows, spec->cols, branch_type));
+    FO_TRY(check_rows(h, rows, spec->cols, x->dtype));
+    FO_TRY(check_rows(y, rows, spec->cols, branch_type));
+    int64_t rows_per_gate;
+    FO_TRY(check_gate(gate, rows, spec->cols, branch_type, &rows_per_gate));
+    if (!fo::aligned_to(stats, 4)) return FLASHOPTIM_ERR_MISALIGNED;
+    if (rows == 0) return FLASHOPTIM_OK;
+    NormArgs a = {};
+    a.x = to_dev(x); a.f = to_dev(f); a.gate = to_dev(gate); a.h = to_dev(h); a.y = to_dev(y);
+    a.post_weight = spec->post_weight; a.post_bias = spec->post_bias; a.pre_weight = spec->pre_weight; a.pre_bias = spec->pre_bias;
+    a.stats = stats;
+    a.rows = (uint32_t)rows; a.rows_per_gate = (uint32_t)rows_per_gate; a.cols = (int32_t)spec->cols;
+    a.eps = spec->eps; a.residual_scale = spec->residual_scale; a.branch_scale = spec->branch_scale;
+    a.inv_cols = (float)(1.0 / (double)spec->cols);
+    a.layer = spec->kind == FLASHOPTIM_LAYER_NORM; a.post_norm = f && spec->post_norm; a.sigmoid = spec->gate_act == FLASHOPTIM_GATE_SIGMOID;
+    a.param_fp32 = spec->param_dtype == FLASHOPTIM_FP32;
+    const bool sf = x->dtype == FLASHOPTIM_FP32, bf = branch_type == FLASHOPTIM_FP32;
+    with_shape(spec->cols, [&](auto shape) {
+        constexpr int L = decltype(shape)::kLanes, C = decltype(shape)::kChunks, T = L < 256 ? 256 : L;
+        const dim3 grid((unsigned)up(rows, T / L)), block(T);
+        if (bf) hipLaunchKernelGGL((norm_rows<true, true, L, C>), grid, block, 0, (hipStream_t)stream, a);
+        else if (sf) hipLaunchKernelGGL((norm_rows<true, false, L, C>), grid, block, 0, (hipStream_t)stream, a);
+        else hipLaunchKernelGGL((norm_rows<false, false, L, C>), grid, block, 0, (hipStream_t)stream, a);
+    });
+    return fo::hip_status(hipGetLastError());
+}
+
+int64_t flashoptim_block_norm_backward_workspace(const flashoptim_block_norm_spec* spec, int64_t rows, int64_t gates) {
+    FO_TRY(check_spec(spec));
+    if (rows < 0 || gates < 1 || rows % gates != 0) return FLASHOPTIM_ERR_INVALID_ARG;
+    if (rows >= ((int64_t)1 << 31)) return FLASHOPTIM_ERR_NUMEL_RANGE;
+    return part_bytes(spec, rows, gates);
+}
+
+int flashoptim_block_norm_backward(const flashoptim_block_norm_spec* spec, const flashoptim_matrix* h, const flashoptim_matrix* f,
+                                   const flashoptim_matrix* gate, const float* stats, const flashoptim_block_norm_grads* grads,
+                                   void* workspace, int64_t workspace_bytes, void* stream) {
+    FO_TRY(check_spec(spec));
+    FO_TRY(fo::check_matrix(h));
+    if (!grads || (!grads->dy && !grads->dh)) return FLASHOPTIM_ERR_INVALID_ARG;
+    const int64_t rows = h->rows, cols = spec->cols;
+    const flashoptim_block_norm_grads& g = *grads;
+    const bool post_norm = f && spec->post_norm, layer = spec->kind == FLASHOPTIM_LAYER_NORM;
+    if (h->cols != cols || (!f && (gate || g.df)) || (!gate && g.dgate)) return FLASHOPTIM_ERR_INVALID_ARG;
+    const int branch_type = f ? f->dtype : g.dy ? g.dy->dtype : h->dtype;
+    if (branch_type == FLASHOPTIM_FP32 && h->dtype != FLASHOPTIM_FP32) return FLASHOPTIM_ERR_INVALID_ARG;
+    FO_TRY(check_rows(f, rows, cols, branch_type));
+    FO_TRY(check_rows(g.dy, rows, cols, branch_type));
+    FO_TRY(check_rows(g.dh, rows, cols, h->dtype));
+    FO_TRY(check_rows(g.dx, rows, cols, h->dtype));
+    FO_TRY(check_rows(g.df, rows, cols, branch_type));
+    int64_t rows_per_gate;
+    FO_TRY(check_gate(gate, rows, cols, branch_type, &rows_per_gate));
+    if (gate) FO_TRY(check_rows(g.dgate, gate->rows, cols, branch_type));
+    // a gradient of what is not there
+    if ((!g.dy && (g.dpre_weight || g.dpre_bias)) || (!post_norm && (g.dpost_weight || g.dpost_bias)) ||
+        (!layer && (g.dpre_bias || g.dpost_bias)))
+        return FLASHOPTIM_ERR_INVALID_ARG;
+    if ((g.dy || post_norm) && rows > 0 && !stats) return FLASHOPTIM_ERR_INVALID_ARG;
+    const uintptr_t unit = (uintptr_t)fo::elem_bytes(spec->param_dtype);
+    void* const outs[kSums] = {g.dpre_weight, g.dpre_bias, g.dpost_weight, g.dpost_bias, g.dgate ? g.dgate->data : nullptr};
+    for (int k = 0; k < kGate; ++k)
+        if (!fo::aligned_to(outs[k], unit)) return FLASHOPTIM_ERR_MISALIGNED;
+    const int64_t gates = gate ? gate->rows : 1;
+    const int64_t need = part_bytes(spec, rows, gates);
+    if (need > 0 && !workspace) return FLASHOPTIM_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return FLASHOPTIM_ERR_WORKSPACE;
+    if (!fo::aligned_to(workspace, 16) || !fo::aligned_to(stats, 4)) return FLASHOPTIM_ERR_MISALIGNED;
+
+    PartSums p = {};
+    p.cols = (int32_t)cols;
+    int kinds = 0;
+    const Parts c = rows > 0 ? cut(rows, gates, cols) : Parts{1, 1, 1, 1, 0, false};
+    GradArgs a = {};
+    for (int k = 0; k < kSums; ++k) {
+        a.slot[k] = -1;
+        if (!outs[k] || (k == kGate && c.gate_done)) continue;
+        a.slot[k] = kinds;
+        PartSum& s = p.of[kinds];
+        s.part = (const float*)workspace + (int64_t)kinds * c.parts * cols;
+        s.out = outs[k];
+        s.groups = k == kGate ? (uint32_t)gates : 1u;
+        s.parts = k == kGate ? (uint32_t)c.parts_per_group : (uint32_t)c.parts;
+        s.stride = k == kGate ? (gates > 1 ? g.dgate->stride : 0) : 0;
+        if (rows == 0) s.parts = 0;
+        s.fp32 = k == kGate ? branch_type == FLASHOPTIM_FP32 : spec->param_dtype == FLASHOPTIM_FP32;
+        ++kinds;
+    }
+    if (rows > 0) {
+        a.h = to_dev(h); a.f = to_dev(f); a.gate = to_dev(gate);
+        a.dy = to_dev(g.dy); a.dh = to_dev(g.dh); a.dx = to_dev(g.dx); a.df = to_dev(g.df); a.dgate = to_dev(g.dgate);
+        a.post_weight = post_norm ? spec->post_weight : nullptr; a.post_bias = post_norm ? spec->post_bias : nullptr;
+        a.pre_weight = spec->pre_weight;
+        a.stats = stats; a.part = (float*)workspace;
+        a.rows = (uint32_t)rows; a.rows_per_gate = (uint32_t)rows_per_gate; a.parts = (uint32_t)c.parts;
+        a.unit_rows = (uint32_t)c.unit_rows; a.part_units = (uint32_t)c.part_units; a.units_per_group = (uint32_t)c.units_per_group;
+        a.parts_per_group = (uint32_t)c.parts_per_group;
+        a.cols = (int32_t)cols;
+        a.residual_scale = spec->residual_scale; a.branch_scale = spec->branch_scale; a.inv_cols = (float)(1.0 / (double)cols);
+        a.post_norm = post_norm; a.sigmoid = spec->gate_act == FLASHOPTIM_GATE_SIGMOID; a.param_fp32 = spec->param_dtype == FLASHOPTIM_FP32;
+        a.gate_done = c.gate_done;
+        const bool sf = h->dtype == FLASHOPTIM_FP32, bf = branch_type == FLASHOPTIM_FP32;
+        with_shape(cols, [&](auto shape) {
+            constexpr int L = decltype(shape)::kLanes, C = decltype(shape)::kChunks, T = L < 256 ? 256 : L;
+            const dim3 grid((unsigned)c.parts), block(T);
+            auto launch = [&](auto layer_c, auto branch_c) {
+                constexpr bool LN = decltype(layer_c)::value, BR = decltype(branch_c)::value;
+                if (bf) hipLaunchKernelGGL((norm_gradients<true, true, L, C, LN, BR>), grid, block, 0, (hipStream_t)stream, a);
+                else if (sf) hipLaunchKernelGGL((norm_gradients<true, false, L, C, LN, BR>), grid, block, 0, (hipStream_t)stream, a);
+                else hipLaunchKernelGGL((norm_gradients<false, false, L, C, LN, BR>), grid, block, 0, (hipStream_t)stream, a);
+            };
+            using Yes = std::true_type;
+            using No = std::false_type;
+            if (layer) { if (f) launch(Yes{}, Yes{}); else launch(Yes{}, No{}); }
+            else { if (f) launch(No{}, Yes{}); else launch(No{}, No{}); }
+        });
+        FO_TRY(fo::hip_status(hipGetLastError()));
+    }
+    if (kinds) {
+        const unsigned groups = a.slot[kGate] >= 0 ? (unsigned)(gates < 1024 ? gates : 1024) : 1u;
+        hipLaunchKernelGGL(sum_parts, dim3((unsigned)up(cols, 64), groups, (unsigned)kinds), dim3(256), 0, (hipStream_t)stream, p);
+        FO_TRY(fo::hip_status(hipGetLastError()));
+    }
+    return FLASHOPTIM_OK;
+}
+
+}  // extern "C"
