@@ -397,6 +397,141 @@ __global__ __launch_bounds__(64 * WAVES) void product_small(Mx4 b, Mx4 a, Result
     }
 }
 
+// Large products: a workgroup makes BP columns by BQ rows of c.  A step takes a segment of 256 terms: 128 bytes of codes and 8 of scales
+// of each row come to LDS straight from memory (no registers in between), for the next step while the matrix cores work on this one.
+// A wavefront makes BP / WP by BQ / WQ values in tiles of 32 by 32, whose instruction takes 64 terms: half h of its lanes takes blocks
+// 4 h .. 4 h + 3 of the segment in four turns, so that a lane's four scales are one word.
+// In LDS, a row's 128 bytes are eight pieces of 16; piece c of row r lies at c ^ (r / 2 % 8), so that the 64 lanes of a read, 32 rows
+// of the same piece in each half, spread evenly over the banks.  A copy to LDS writes consecutive lanes to consecutive places, so the lanes
+// ask memory for their pieces in that order.
+using f32x16 = float __attribute__((ext_vector_type(16)));
+
+template <int ROWS>
+struct Stage {
+    uint8_t codes[ROWS * kSegmentBytes];
+    uint8_t scales[ROWS * 8];
+};
+
+#define FO_LDS(p) ((__attribute__((address_space(3))) void*)(p))
+
+constexpr int64_t kMaxTiledTerms = (int64_t)1 << 23;      // 256 rows of codes stay below 2^31 bytes, which a lane's offset reaches
+
+// `bytes` bytes from p on as a buffer; addresses into it are a lane's 32-bit offset and a scalar one.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const uint8_t* p, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, (int)bytes, 0x00020000);
+}
+
+__device__ __forceinline__ int swizzle(int row) { return row >> 1 & 7; }
+
+// What a wavefront copies of ROWS rows: the lane's places in them.  Behind the matrix's last row a copy takes that row again.
+template <int ROWS, int WAVES>
+struct Copier {
+    static constexpr int kCodes = ROWS / 8 / WAVES, kScales = ROWS / 32 / WAVES;      // copies of 64 times 16, and 4, bytes
+    static_assert(kCodes * 8 * WAVES == ROWS && kScales * 32 * WAVES == ROWS, "every wavefront copies as much");
+    __amdgpu_buffer_rsrc_t codes, scales;      // from the tile's first row on
+    uint32_t code_at[kCodes], scale_at[kScales];
+    int wave;
+    __device__ __forceinline__ Copier(const Mx4& m, uint32_t row0, int wave, int lane) : wave(wave) {
+        const uint32_t last = min(m.rows - 1 - row0, (uint32_t)ROWS - 1), pitch = m.segments * kSegmentBytes;
+        codes = buffer_of(m.codes + (int64_t)row0 * pitch, (last + 1) * pitch);
+        scales = buffer_of(m.scales + (int64_t)row0 * m.scale_pitch, (last + 1) * m.scale_pitch);
+#pragma unroll
+        for (int i = 0; i < kCodes; ++i) {
+            const int row = (wave * kCodes + i) * 8 + lane / 8;
+            code_at[i] = min((uint32_t)row, last) * pitch + (uint32_t)((lane % 8 ^ swizzle(row)) * 16);
+        }
+#pragma unroll
+        for (int i = 0; i < kScales; ++i) {
+            const int row = (wave * kScales + i) * 32 + lane / 2;
+            scale_at[i] = min((uint32_t)row, last) * m.scale_pitch + (uint32_t)(lane % 2 * 4);
+        }
+    }
+    __device__ __forceinline__ void copy(Stage<ROWS>& to, uint32_t seg) const {
+#pragma unroll
+        for (int i = 0; i < kCodes; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(codes, FO_LDS(to.codes + (wave * kCodes + i) * 1024), 16, (int)code_at[i], (int)(seg * kSegmentBytes), 0, 0);
+#pragma unroll
+        for (int i = 0; i < kScales; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(scales, FO_LDS(to.scales + (wave * kScales + i) * 256), 4, (int)scale_at[i], (int)(seg * 8), 0, 0);
+    }
+};
+
+template <int ROWS>
+__device__ __forceinline__ i32x4 piece(const Stage<ROWS>& s, int row, int c) {
+    return *(const i32x4*)(s.codes + row * kSegmentBytes + (c ^ swizzle(row)) * 16);
+}
+
+template <int TURN>
+__device__ __forceinline__ f32x16 mfma32(i32x4 p, i32x4 q, f32x16 acc, int p_scale, int q_scale) {
+    const i32x8 pw = {p[0], p[1], p[2], p[3], 0, 0, 0, 0}, qw = {q[0], q[1], q[2], q[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(pw, qw, acc, 4, 4, TURN, p_scale, TURN, q_scale);
+}
+
+template <int TURN, int BP, int BQ, int TP, int TQ>
+__device__ __forceinline__ void turn(const Stage<BP>& p, const Stage<BQ>& q, int p0, int q0, int h, const int (&p_scale)[TP], const int (&q_scale)[TQ],
+                                     f32x16 (&acc)[TP][TQ]) {
+    i32x4 pw[TP], qw[TQ];
+#pragma unroll
+    for (int i = 0; i < TP; ++i) pw[i] = piece(p, p0 + 32 * i, 4 * h + TURN);
+#pragma unroll
+    for (int j = 0; j < TQ; ++j) qw[j] = piece(q, q0 + 32 * j, 4 * h + TURN);
+#pragma unroll
+    for (int i = 0; i < TP; ++i)
+#pragma unroll
+        for (int j = 0; j < TQ; ++j) acc[i][j] = mfma32<TURN>(pw[i], qw[j], acc[i][j], p_scale[i], q_scale[j]);
+}
+
+template <bool FP32, int BP, int BQ, int WP, int WQ, int RESIDENT>
+__global__ __launch_bounds__(64 * WP * WQ, RESIDENT) void product_tiles(Mx4 b, Mx4 a, Result c, uint32_t p_tiles, uint32_t q_tiles) {
+    constexpr int kWaves = WP * WQ, TP = BP / WP / 32, TQ = BQ / WQ / 32;
+    __shared__ Stage<BP> p_stage0, p_stage1;
+    __shared__ Stage<BQ> q_stage0, q_stage1;
+    // consecutive workgroups run on different XCDs: each XCD takes a stretch of the tiles, in columns of eight, whose rows it then has in its L2
+    const uint32_t tiles = p_tiles * q_tiles, xcd = blockIdx.x % 8, at = blockIdx.x / 8;
+    const uint32_t tile = xcd * (tiles / 8) + min(xcd, tiles % 8) + at;
+    constexpr uint32_t kGroup = 8;
+    const uint32_t group = tile / (kGroup * p_tiles), in_group = tile - group * kGroup * p_tiles;
+    const uint32_t height = min(kGroup, q_tiles - group * kGroup);
+    const uint32_t p_tile = in_group / height, q_tile = group * kGroup + in_group - p_tile * height;
+
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+    const Copier<BP, kWaves> p_copy(b, p_tile * BP, wave, lane);
+    const Copier<BQ, kWaves> q_copy(a, q_tile * BQ, wave, lane);
+    const int h = lane / 32, p0 = wave / WQ * (BP / WP) + lane % 32, q0 = wave % WQ * (BQ / WQ) + lane % 32;
+    f32x16 acc[TP][TQ] = {};
+    auto step = [&](const Stage<BP>& p, const Stage<BQ>& q, Stage<BP>& p_next, Stage<BQ>& q_next, uint32_t seg) {
+        __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0): this wavefront's copies of the segment have landed
+        __builtin_amdgcn_s_barrier();            // all have, and nobody reads the other stage any more
+        if (seg + 1 < b.segments) {
+            p_copy.copy(p_next, seg + 1);
+            q_copy.copy(q_next, seg + 1);
+        }
+        int p_scale[TP], q_scale[TQ];
+#pragma unroll
+        for (int i = 0; i < TP; ++i) p_scale[i] = *(const int*)(p.scales + (p0 + 32 * i) * 8 + h * 4);
+#pragma unroll
+        for (int j = 0; j < TQ; ++j) q_scale[j] = *(const int*)(q.scales + (q0 + 32 * j) * 8 + h * 4);
+        turn<0, BP, BQ, TP, TQ>(p, q, p0, q0, h, p_scale, q_scale, acc);
+        turn<1, BP, BQ, TP, TQ>(p, q, p0, q0, h, p_scale, q_scale, acc);
+        turn<2, BP, BQ, TP, TQ>(p, q, p0, q0, h, p_scale, q_scale, acc);
+        turn<3, BP, BQ, TP, TQ>(p, q, p0, q0, h, p_scale, q_scale, acc);
+    };
+    p_copy.copy(p_stage0, 0);
+    q_copy.copy(q_stage0, 0);
+    for (uint32_t seg = 0; seg < b.segments; seg += 2) {
+        step(p_stage0, q_stage0, p_stage1, q_stage1, seg);
+        if (seg + 1 < b.segments) step(p_stage1, q_stage1, p_stage0, q_stage0, seg + 1);
+    }
+#pragma unroll
+    for (int i = 0; i < TP; ++i)
+#pragma unroll
+        for (int j = 0; j < TQ; ++j)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                store_result4<FP32>(c, q_tile * BQ + q0 + 32 * j, p_tile * BP + (p0 - lane % 32) + 32 * i + 8 * g + 4 * h,
+                                    f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]});
+}
+
 __global__ __launch_bounds__(256) void fill_zero(Result c, int bytes) {
     const uint32_t col = blockIdx.x * 256 + threadIdx.x;
     if (col >= c.cols) return;
@@ -454,6 +589,20 @@ int product(const flashoptim_mx4& a, const flashoptim_mx4& b, const flashoptim_m
     const bool fp32 = c.dtype == FLASHOPTIM_FP32;
     if (a.cols == 0) {
         hipLaunchKernelGGL(fill_zero, dim3((unsigned)up(c.cols, 256), (unsigned)(c.rows < 1024 ? c.rows : 1024)), dim3(256), 0, stream, r, fp32 ? 4 : 2);
+        return fo::hip_status(hipGetLastError());
+    }
+    if (c.rows > 16 && c.cols > 16 && a.cols <= kMaxTiledTerms) {
+        auto tiles = [&](auto kernel, int bp, int bq, int threads) {
+            const uint32_t pt = (uint32_t)up(c.cols, bp), qt = (uint32_t)up(c.rows, bq);
+            hipLaunchKernelGGL(kernel, dim3(pt * qt), dim3(threads), 0, stream, to_dev(b), to_dev(a), r, pt, qt);
+        };
+        if (up(c.cols, 256) * up(c.rows, 256) >= 256) {
+            if (fp32) tiles(product_tiles<true, 256, 256, 2, 4, 2>, 256, 256, 512);
+            else tiles(product_tiles<false, 256, 256, 2, 4, 2>, 256, 256, 512);
+        } else {
+            if (fp32) tiles(product_tiles<true, 128, 128, 2, 2, 2>, 128, 128, 256);
+            else tiles(product_tiles<false, 128, 128, 2, 2, 2>, 128, 128, 256);
+        }
         return fo::hip_status(hipGetLastError());
     }
     const dim3 grid((unsigned)up(c.cols, 16), (unsigned)up(c.rows, 16));
