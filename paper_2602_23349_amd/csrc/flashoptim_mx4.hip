@@ -12,6 +12,7 @@
 
 #include <type_traits>
 
+
 #include "flashoptim.h"
 #include "flashoptim_host.h"
 
@@ -397,44 +398,73 @@ __global__ __launch_bounds__(64 * WAVES) void product_small(Mx4 b, Mx4 a, Result
     }
 }
 
-// Large products: a workgroup makes BP columns by BQ rows of c.  A step takes a segment of 256 terms: 128 bytes of codes and 8 of scales
-// of each row come to LDS straight from memory (no registers in between), for the next step while the matrix cores work on this one.
-// A wavefront makes BP / WP by BQ / WQ values in tiles of 32 by 32, whose instruction takes 64 terms: half h of its lanes takes blocks
-// 4 h .. 4 h + 3 of the segment in four turns, so that a lane's four scales are one word.
-// In LDS, a row's 128 bytes are eight pieces of 16; piece c of row r lies at c ^ (r / 2 % 8), so that the 64 lanes of a read, 32 rows
-// of the same piece in each half, spread evenly over the banks.  A copy to LDS writes consecutive lanes to consecutive places, so the lanes
-// ask memory for their pieces in that order.
+// Large products: a workgroup makes BP columns by BQ rows of c.  A step takes a segment of 256 terms, 128 bytes of codes of each row,
+// which come to LDS straight from memory (no registers in between) while the matrix cores work on the segment before.  A wavefront makes
+// BP / WP by BQ / WQ values in tiles of 32 by 32, whose instruction takes 64 terms: half h of its lanes takes blocks 4 h .. 4 h + 3 of the
+// segment in four turns, so that a lane's four scales are one word.
+//
+// What bounds it: the matrix cores and the package's power.  8192 x 8192 x 8192: 266 us, 4.1 PFLOP/s; with all codes zero, which
+// costs less power, 207 us, 5.3 PFLOP/s.  What it took, for 8192 x 8192 x 8192:
+//   * scales for 1024 terms at a time instead of 256 (a copy's rows pass the memory pipe one after the other, and 8 bytes of a row take it
+//     as long as 128): 305 -> 300 us, and with 128 by 128 tiles 357 -> 296;
+//   * the next segment's copies go out one by one between the products (together, all wavefronts of a workgroup queue up in front of the memory
+//     pipe before their first product): 300 -> 266;
+//   * steps of 128 terms, with four stages: 287 (64-byte pieces of rows).  Wavefronts of 128 by 128 values, one to a SIMD: 273.
+// The tile of 256 by 256 fills the LDS (160 KB), so that one workgroup is resident on a compute unit.
 using f32x16 = float __attribute__((ext_vector_type(16)));
 
+constexpr int kScaleTerms = 1024, kScaleBytes = kScaleTerms / kBlock, kScaleSteps = kScaleTerms / kSegment;
 template <int ROWS>
 struct Stage {
     uint8_t codes[ROWS * kSegmentBytes];
-    uint8_t scales[ROWS * 8];
 };
-
-#define FO_LDS(p) ((__attribute__((address_space(3))) void*)(p))
+template <int ROWS>
+struct Scales {
+    uint8_t bytes[ROWS * kScaleBytes];
+};
+// In LDS, a row's codes are eight pieces of 16 bytes; piece c of row r lies at c ^ swizzle(r), so that the 64 lanes of a read, 32 rows
+// of the same piece in each half, spread evenly over the banks; its scales are two.  A copy to LDS writes consecutive lanes to
+// consecutive places, so the lanes ask memory for their pieces in that order.
+__device__ __forceinline__ int swizzle(int row) { return row >> 1 & 7; }
+__device__ __forceinline__ int scale_swizzle(int row) { return row >> 3 & 1; }
 
 constexpr int64_t kMaxTiledTerms = (int64_t)1 << 23;      // 256 rows of codes stay below 2^31 bytes, which a lane's offset reaches
 
+#define FO_LDS(p) ((__attribute__((address_space(3))) void*)(p))
+
 // `bytes` bytes from p on as a buffer; addresses into it are a lane's 32-bit offset and a scalar one.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const uint8_t* p, uint32_t bytes) {
-    return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, (int)bytes, 0x00020000);
+__device__ __forceinline__ i32x4 buffer_of(const uint8_t* p, uint32_t bytes) {
+    const uint64_t at = (uint64_t)p;
+    return i32x4{__builtin_amdgcn_readfirstlane((int)(uint32_t)at), __builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32)),
+                 __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000};
 }
 
-__device__ __forceinline__ int swizzle(int row) { return row >> 1 & 7; }
+// Copies 16 bytes for each lane from the buffer to LDS, consecutive lanes to consecutive places from `to` on; from an empty buffer, nothing is
+// fetched.  It has no result in registers, so that written as assembly it is safe; written with the builtin, the compiler has every later read
+// of LDS wait for it, whichever stage it reads.  What waits for it is wait_copies.  (s_nop: m0 is to be set one cycle
+// ahead.  The compiler sets m0 right ahead of its own uses, and has none in these kernels.)
+__device__ __forceinline__ void copy_to_lds(i32x4 buffer, uint32_t lane_offset, uint32_t offset, void* to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"((uint32_t)(uintptr_t)FO_LDS(to)), "v"(lane_offset), "s"(buffer),
+                 "s"(offset) : "memory");
+}
+// Waits until this wavefront's copies have landed and its reads of LDS have come back.
+__device__ __forceinline__ void wait_copies() { __builtin_amdgcn_s_waitcnt(0x0070); }
 
 // What a wavefront copies of ROWS rows: the lane's places in them.  Behind the matrix's last row a copy takes that row again.
 template <int ROWS, int WAVES>
 struct Copier {
-    static constexpr int kCodes = ROWS / 8 / WAVES, kScales = ROWS / 32 / WAVES;      // copies of 64 times 16, and 4, bytes
-    static_assert(kCodes * 8 * WAVES == ROWS && kScales * 32 * WAVES == ROWS, "every wavefront copies as much");
-    __amdgpu_buffer_rsrc_t codes, scales;      // from the tile's first row on
+    static constexpr int kCodes = ROWS * kSegmentBytes / 1024 / WAVES, kScales = ROWS * kScaleBytes / 1024 / WAVES;      // copies of 1024 bytes
+    static_assert(kCodes * 1024 * WAVES == ROWS * kSegmentBytes && kScales * 1024 * WAVES == ROWS * kScaleBytes, "every wavefront copies as much");
+    const uint8_t *codes, *scales;      // from the tile's first row on
+    uint32_t code_bytes, scale_bytes;
     uint32_t code_at[kCodes], scale_at[kScales];
     int wave;
     __device__ __forceinline__ Copier(const Mx4& m, uint32_t row0, int wave, int lane) : wave(wave) {
         const uint32_t last = min(m.rows - 1 - row0, (uint32_t)ROWS - 1), pitch = m.segments * kSegmentBytes;
-        codes = buffer_of(m.codes + (int64_t)row0 * pitch, (last + 1) * pitch);
-        scales = buffer_of(m.scales + (int64_t)row0 * m.scale_pitch, (last + 1) * m.scale_pitch);
+        codes = m.codes + (int64_t)row0 * pitch;
+        scales = m.scales + (int64_t)row0 * m.scale_pitch;
+        code_bytes = (last + 1) * pitch;
+        scale_bytes = (last + 1) * m.scale_pitch;
 #pragma unroll
         for (int i = 0; i < kCodes; ++i) {
             const int row = (wave * kCodes + i) * 8 + lane / 8;
@@ -443,22 +473,28 @@ struct Copier {
 #pragma unroll
         for (int i = 0; i < kScales; ++i) {
             const int row = (wave * kScales + i) * 32 + lane / 2;
-            scale_at[i] = min((uint32_t)row, last) * m.scale_pitch + (uint32_t)(lane % 2 * 4);
+            scale_at[i] = min((uint32_t)row, last) * m.scale_pitch + (uint32_t)((lane % 2 ^ scale_swizzle(row)) * 16);
         }
     }
-    __device__ __forceinline__ void copy(Stage<ROWS>& to, uint32_t seg) const {
+    __device__ __forceinline__ i32x4 buffer(bool there) const { return buffer_of(codes, there ? code_bytes : 0); }
+    __device__ __forceinline__ void copy_codes(i32x4 buffer, Stage<ROWS>& to, uint32_t step, int i) const {
+        copy_to_lds(buffer, code_at[i], step * kSegmentBytes, to.codes + (wave * kCodes + i) * 1024);
+    }
+    __device__ __forceinline__ void copy_scales(Scales<ROWS>& to, uint32_t group, bool there) const {
+        const i32x4 buffer = buffer_of(scales, there ? scale_bytes : 0);
 #pragma unroll
-        for (int i = 0; i < kCodes; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(codes, FO_LDS(to.codes + (wave * kCodes + i) * 1024), 16, (int)code_at[i], (int)(seg * kSegmentBytes), 0, 0);
-#pragma unroll
-        for (int i = 0; i < kScales; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(scales, FO_LDS(to.scales + (wave * kScales + i) * 256), 4, (int)scale_at[i], (int)(seg * 8), 0, 0);
+        for (int i = 0; i < kScales; ++i) copy_to_lds(buffer, scale_at[i], group * kScaleBytes, to.bytes + (wave * kScales + i) * 1024);
     }
 };
 
 template <int ROWS>
 __device__ __forceinline__ i32x4 piece(const Stage<ROWS>& s, int row, int c) {
     return *(const i32x4*)(s.codes + row * kSegmentBytes + (c ^ swizzle(row)) * 16);
+}
+// The scales of half h of the row's blocks in the step-th segment of the 1024 terms: the lowest byte is the first one's.
+template <int ROWS>
+__device__ __forceinline__ int scales_of(const Scales<ROWS>& s, int row, int step, int h) {
+    return *(const int*)(s.bytes + row * kScaleBytes + ((step * 8 + h * 4) ^ scale_swizzle(row) * 16));
 }
 
 template <int TURN>
@@ -468,60 +504,93 @@ __device__ __forceinline__ f32x16 mfma32(i32x4 p, i32x4 q, f32x16 acc, int p_sca
 }
 
 template <int TURN, int BP, int BQ, int TP, int TQ>
-__device__ __forceinline__ void turn(const Stage<BP>& p, const Stage<BQ>& q, int p0, int q0, int h, const int (&p_scale)[TP], const int (&q_scale)[TQ],
-                                     f32x16 (&acc)[TP][TQ]) {
-    i32x4 pw[TP], qw[TQ];
+__device__ __forceinline__ void read_turn(const Stage<BP>& p, const Stage<BQ>& q, int p0, int q0, int h, i32x4 (&pw)[TP], i32x4 (&qw)[TQ]) {
 #pragma unroll
     for (int i = 0; i < TP; ++i) pw[i] = piece(p, p0 + 32 * i, 4 * h + TURN);
 #pragma unroll
     for (int j = 0; j < TQ; ++j) qw[j] = piece(q, q0 + 32 * j, 4 * h + TURN);
+    __builtin_amdgcn_sched_barrier(0);
+}
+template <int TURN, int TP, int TQ, typename F>
+__device__ __forceinline__ void multiply_turn(const i32x4 (&pw)[TP], const i32x4 (&qw)[TQ], const int (&p_scale)[TP], const int (&q_scale)[TQ],
+                                              f32x16 (&acc)[TP][TQ], F behind) {
 #pragma unroll
     for (int i = 0; i < TP; ++i)
 #pragma unroll
-        for (int j = 0; j < TQ; ++j) acc[i][j] = mfma32<TURN>(pw[i], qw[j], acc[i][j], p_scale[i], q_scale[j]);
+        for (int j = 0; j < TQ; ++j) {
+            acc[i][j] = mfma32<TURN>(pw[i], qw[j], acc[i][j], p_scale[i], q_scale[j]);
+            behind((TURN * TP + i) * TQ + j);
+        }
+    __builtin_amdgcn_sched_barrier(0);
 }
 
 template <bool FP32, int BP, int BQ, int WP, int WQ, int RESIDENT>
 __global__ __launch_bounds__(64 * WP * WQ, RESIDENT) void product_tiles(Mx4 b, Mx4 a, Result c, uint32_t p_tiles, uint32_t q_tiles) {
     constexpr int kWaves = WP * WQ, TP = BP / WP / 32, TQ = BQ / WQ / 32;
-    __shared__ Stage<BP> p_stage0, p_stage1;
-    __shared__ Stage<BQ> q_stage0, q_stage1;
+    __shared__ Stage<BP> p_stage[2];
+    __shared__ Stage<BQ> q_stage[2];
+    __shared__ Scales<BP> p_scales[2];
+    __shared__ Scales<BQ> q_scales[2];
     // consecutive workgroups run on different XCDs: each XCD takes a stretch of the tiles, in columns of eight, whose rows it then has in its L2
     const uint32_t tiles = p_tiles * q_tiles, xcd = blockIdx.x % 8, at = blockIdx.x / 8;
     const uint32_t tile = xcd * (tiles / 8) + min(xcd, tiles % 8) + at;
-    constexpr uint32_t kGroup = 8;
-    const uint32_t group = tile / (kGroup * p_tiles), in_group = tile - group * kGroup * p_tiles;
-    const uint32_t height = min(kGroup, q_tiles - group * kGroup);
-    const uint32_t p_tile = in_group / height, q_tile = group * kGroup + in_group - p_tile * height;
+    constexpr uint32_t kColumn = 8;
+    const uint32_t column = tile / (kColumn * p_tiles), in_column = tile - column * kColumn * p_tiles;
+    const uint32_t height = min(kColumn, q_tiles - column * kColumn);
+    const uint32_t p_tile = in_column / height, q_tile = column * kColumn + in_column - p_tile * height;
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
     const Copier<BP, kWaves> p_copy(b, p_tile * BP, wave, lane);
     const Copier<BQ, kWaves> q_copy(a, q_tile * BQ, wave, lane);
     const int h = lane / 32, p0 = wave / WQ * (BP / WP) + lane % 32, q0 = wave % WQ * (BQ / WQ) + lane % 32;
+    const uint32_t steps = b.segments;
     f32x16 acc[TP][TQ] = {};
-    auto step = [&](const Stage<BP>& p, const Stage<BQ>& q, Stage<BP>& p_next, Stage<BQ>& q_next, uint32_t seg) {
-        __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0): this wavefront's copies of the segment have landed
-        __builtin_amdgcn_s_barrier();            // all have, and nobody reads the other stage any more
-        if (seg + 1 < b.segments) {
-            p_copy.copy(p_next, seg + 1);
-            q_copy.copy(q_next, seg + 1);
+    auto copy = [&](i32x4 p_buffer, i32x4 q_buffer, uint32_t step, int i) {
+        if (i < p_copy.kCodes) p_copy.copy_codes(p_buffer, p_stage[step % 2], step, i);
+        else q_copy.copy_codes(q_buffer, q_stage[step % 2], step, i - p_copy.kCodes);
+    };
+    constexpr int kCopies = p_copy.kCodes + q_copy.kCodes;
+    constexpr int kEvery = TP * TQ * 2 / kCopies > 0 ? TP * TQ * 2 / kCopies : 1;      // products to a copy: all in the first half of a step
+    static_assert(kEvery * kCopies <= TP * TQ * 4, "every copy has its product");
+    p_copy.copy_scales(p_scales[0], 0, true);
+    q_copy.copy_scales(q_scales[0], 0, true);
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) copy(p_copy.buffer(true), q_copy.buffer(true), 0, i);
+    for (uint32_t t = 0; t < steps; ++t) {
+        // this wavefront's copies for step t have landed; behind the barrier all have, and nobody reads the stage of step t - 1 any more
+        wait_copies();
+        __builtin_amdgcn_s_barrier();
+        const uint32_t group = t / kScaleSteps, in_group = t % kScaleSteps;
+        if (in_group == 0) {
+            p_copy.copy_scales(p_scales[group % 2 ^ 1], group + 1, t + kScaleSteps < steps);
+            q_copy.copy_scales(q_scales[group % 2 ^ 1], group + 1, t + kScaleSteps < steps);
         }
+        const i32x4 p_buffer = p_copy.buffer(t + 1 < steps), q_buffer = q_copy.buffer(t + 1 < steps);
+        auto behind = [&](int product) {
+            if (product % kEvery != 0 || product / kEvery >= kCopies) return;
+            __builtin_amdgcn_sched_barrier(0);
+            copy(p_buffer, q_buffer, t + 1, product / kEvery);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        const Stage<BP>& p = p_stage[t % 2];
+        const Stage<BQ>& q = q_stage[t % 2];
         int p_scale[TP], q_scale[TQ];
 #pragma unroll
-        for (int i = 0; i < TP; ++i) p_scale[i] = *(const int*)(p.scales + (p0 + 32 * i) * 8 + h * 4);
+        for (int i = 0; i < TP; ++i) p_scale[i] = scales_of(p_scales[group % 2], p0 + 32 * i, (int)in_group, h);
 #pragma unroll
-        for (int j = 0; j < TQ; ++j) q_scale[j] = *(const int*)(q.scales + (q0 + 32 * j) * 8 + h * 4);
-        turn<0, BP, BQ, TP, TQ>(p, q, p0, q0, h, p_scale, q_scale, acc);
-        turn<1, BP, BQ, TP, TQ>(p, q, p0, q0, h, p_scale, q_scale, acc);
-        turn<2, BP, BQ, TP, TQ>(p, q, p0, q0, h, p_scale, q_scale, acc);
-        turn<3, BP, BQ, TP, TQ>(p, q, p0, q0, h, p_scale, q_scale, acc);
-    };
-    p_copy.copy(p_stage0, 0);
-    q_copy.copy(q_stage0, 0);
-    for (uint32_t seg = 0; seg < b.segments; seg += 2) {
-        step(p_stage0, q_stage0, p_stage1, q_stage1, seg);
-        if (seg + 1 < b.segments) step(p_stage1, q_stage1, p_stage0, q_stage0, seg + 1);
+        for (int j = 0; j < TQ; ++j) q_scale[j] = scales_of(q_scales[group % 2], q0 + 32 * j, (int)in_group, h);
+        // the pieces of a turn are read ahead of the products of the turn before
+        i32x4 pw[2][TP], qw[2][TQ];
+        read_turn<0, BP, BQ, TP, TQ>(p, q, p0, q0, h, pw[0], qw[0]);
+        read_turn<1, BP, BQ, TP, TQ>(p, q, p0, q0, h, pw[1], qw[1]);
+        multiply_turn<0>(pw[0], qw[0], p_scale, q_scale, acc, behind);
+        read_turn<2, BP, BQ, TP, TQ>(p, q, p0, q0, h, pw[0], qw[0]);
+        multiply_turn<1>(pw[1], qw[1], p_scale, q_scale, acc, behind);
+        read_turn<3, BP, BQ, TP, TQ>(p, q, p0, q0, h, pw[1], qw[1]);
+        multiply_turn<2>(pw[0], qw[0], p_scale, q_scale, acc, behind);
+        multiply_turn<3>(pw[1], qw[1], p_scale, q_scale, acc, behind);
     }
+    wait_copies();
 #pragma unroll
     for (int i = 0; i < TP; ++i)
 #pragma unroll
@@ -597,8 +666,8 @@ int product(const flashoptim_mx4& a, const flashoptim_mx4& b, const flashoptim_m
             hipLaunchKernelGGL(kernel, dim3(pt * qt), dim3(threads), 0, stream, to_dev(b), to_dev(a), r, pt, qt);
         };
         if (up(c.cols, 256) * up(c.rows, 256) >= 256) {
-            if (fp32) tiles(product_tiles<true, 256, 256, 2, 4, 2>, 256, 256, 512);
-            else tiles(product_tiles<false, 256, 256, 2, 4, 2>, 256, 256, 512);
+            if (fp32) tiles(product_tiles<true, 256, 256, 4, 2, 2>, 256, 256, 512);
+            else tiles(product_tiles<false, 256, 256, 4, 2, 2>, 256, 256, 512);
         } else {
             if (fp32) tiles(product_tiles<true, 128, 128, 2, 2, 2>, 128, 128, 256);
             else tiles(product_tiles<false, 128, 128, 2, 2, 2>, 128, 128, 256);
