@@ -39,51 +39,91 @@ struct Rows {
 };
 Rows to_dev(const flashoptim_matrix* m) { return m ? Rows{(char*)m->data, m->rows > 1 ? m->stride : 0} : Rows{nullptr, 0}; }
 
-// Eight values from `at` on, of which `left` exist (the others: 0).
-__device__ __forceinline__ f32x8 load8(const void* p, bool fp32, int64_t at, int left) {
-    f32x8 v = {};
-    if (fp32) {
-        const float* f = (const float*)p + at;
-        if (left >= 8) {
-            const f32x4 a = load_as<f32x4>(f), b = load_as<f32x4>(f + 4);
-            v = f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-        } else {
+// Eight values as they lie in memory, so that loads can be issued well ahead of their first use.  `fp32` is a constant for the matrices and the
+// same for all lanes for the weights.
+struct Raw {
+    i32x4 a, b;      // BF16: b unused
+};
+// The eight neighbouring columns that a lane loads, and which of them, first .. last - 1, are its own.  Every lane loads eight that exist: the
+// last one of a ragged row the row's last eight, some of which are its neighbour's; those behind it the same, none of them theirs.  So a
+// load is never a case distinction, which would wait for each of its loads before the next.  (Rows of fewer than eight: lane 0 alone,
+// one by one.)
+struct Place {
+    int col, first, last;
+    __device__ __forceinline__ Place() = default;
+    __device__ __forceinline__ Place(int at, int cols) {
+        col = cols < 8 ? 0 : min(at, cols - 8);
+        first = min(at - col, 8);
+        last = cols < 8 ? cols : 8;
+    }
+    __device__ __forceinline__ bool whole() const { return first == 0 && last == 8; }
+    __device__ __forceinline__ bool has(int i) const { return i >= first && i < last; }
+    __device__ __forceinline__ f32x8 mask(f32x8 v) const {
+        if (!whole()) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) if (i < left) v[i] = f[i];
+            for (int i = 0; i < 8; ++i) v[i] = has(i) ? v[i] : 0.0f;
         }
-    } else {
-        const uint16_t* f = (const uint16_t*)p + at;
-        if (left >= 8) {
-            const i32x4 w = load_as<i32x4>(f);
+        return v;
+    }
+};
+
+// `row`: where the row begins, in values.
+__device__ __forceinline__ Raw load8(const void* p, bool fp32, int64_t row, const Place& at) {
+    Raw r = {};
+    if (fp32) {
+        const int* f = (const int*)p + row + at.col;
+        if (at.last == 8) {
+            r.a = load_as<i32x4>(f);
+            r.b = load_as<i32x4>(f + 4);
+        } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                v[2 * i] = __uint_as_float((uint32_t)w[i] << 16);
-                v[2 * i + 1] = __uint_as_float((uint32_t)w[i] & 0xffff0000u);
+                r.a[i] = f[min(i, at.last - 1)];
+                r.b[i] = f[min(i + 4, at.last - 1)];
             }
+        }
+    } else {
+        const uint16_t* f = (const uint16_t*)p + row + at.col;
+        if (at.last == 8) {
+            r.a = load_as<i32x4>(f);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) if (i < left) v[i] = __uint_as_float((uint32_t)f[i] << 16);
+            for (int i = 0; i < 8; ++i) r.a[i / 2] |= (int)((uint32_t)f[min(i, at.last - 1)] << (16 * (i % 2)));
+        }
+    }
+    return r;
+}
+__device__ __forceinline__ f32x8 values(const Raw& r, bool fp32) {
+    f32x8 v;
+    if (fp32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[i] = __int_as_float(r.a[i]); v[4 + i] = __int_as_float(r.b[i]); }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = __uint_as_float((uint32_t)r.a[i] << 16);
+            v[2 * i + 1] = __uint_as_float((uint32_t)r.a[i] & 0xffff0000u);
         }
     }
     return v;
 }
-__device__ __forceinline__ void store8(void* p, bool fp32, int64_t at, int left, f32x8 v) {
+__device__ __forceinline__ void store8(void* p, bool fp32, int64_t row, const Place& at, f32x8 v) {
     if (fp32) {
-        float* f = (float*)p + at;
-        if (left >= 8) {
+        float* f = (float*)p + row + at.col;
+        if (at.whole()) {
             store_as(f, f32x4{v[0], v[1], v[2], v[3]});
             store_as(f + 4, f32x4{v[4], v[5], v[6], v[7]});
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) if (i < left) f[i] = v[i];
+            for (int i = 0; i < 8; ++i) if (at.has(i)) f[i] = v[i];
         }
     } else {
-        __bf16* f = (__bf16*)p + at;
+        __bf16* f = (__bf16*)p + row + at.col;
         const bf16x8 w = __builtin_convertvector(v, bf16x8);
-        if (left >= 8) store_as(f, w);
+        if (at.whole()) store_as(f, w);
         else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) if (i < left) f[i] = w[i];
+            for (int i = 0; i < 8; ++i) if (at.has(i)) f[i] = w[i];
         }
     }
 }
@@ -128,6 +168,9 @@ struct RowSums {
     }
 };
 
+// Rows that a workgroup handles side by side: where a wavefront has a row to itself, four (they need no barrier).
+constexpr int lines_of(int lanes) { return lanes == 64 ? 4 : 1; }
+
 __device__ __forceinline__ float sigmoid(float v) { return 1.0f / (1.0f + __expf(-v)); }
 
 struct NormArgs {
@@ -140,9 +183,9 @@ struct NormArgs {
     uint8_t layer, post_norm, sigmoid, param_fp32;
 };
 
-// Mean and 1/sqrt(mean square distance + eps) of the row whose values the lanes have.
+// Mean and 1/sqrt(mean square distance + eps) of the row whose values the lanes have (0 where a lane has none).
 template <int LANES, int CHUNKS>
-__device__ __forceinline__ void moments(RowSums<LANES>& sums, const f32x8 (&v)[CHUNKS], const int (&left)[CHUNKS], const NormArgs& a, float* mean,
+__device__ __forceinline__ void moments(RowSums<LANES>& sums, const f32x8 (&v)[CHUNKS], const Place (&at)[CHUNKS], const NormArgs& a, float* mean,
                                         float* rstd) {
     *mean = 0.0f;
     if (a.layer) {
@@ -155,72 +198,88 @@ __device__ __forceinline__ void moments(RowSums<LANES>& sums, const f32x8 (&v)[C
     }
     float s = 0.0f;
 #pragma unroll
-    for (int j = 0; j < CHUNKS; ++j)
+    for (int j = 0; j < CHUNKS; ++j) {
+        const f32x8 d = at[j].mask(v[j] - *mean);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float d = i < left[j] ? v[j][i] - *mean : 0.0f;
-            s = fmaf(d, d, s);
-        }
+        for (int i = 0; i < 8; ++i) s = fmaf(d[i], d[i], s);
+    }
     *rstd = 1.0f / sqrtf(fmaf(sums.sum(s), a.inv_cols, a.eps));
 }
 
 template <int CHUNKS>
-__device__ __forceinline__ void affine(f32x8 (&v)[CHUNKS], const int (&left)[CHUNKS], const int (&col)[CHUNKS], const NormArgs& a, const void* weight,
-                                       const void* bias, float mean, float rstd) {
+struct Params {
+    Raw weight[CHUNKS], bias[CHUNKS];
+    __device__ __forceinline__ void load(const void* w, const void* b, bool fp32, const Place (&at)[CHUNKS]) {
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j) {
+            if (w) weight[j] = load8(w, fp32, 0, at[j]);
+            if (b) bias[j] = load8(b, fp32, 0, at[j]);
+        }
+    }
+};
+
+template <int CHUNKS>
+__device__ __forceinline__ void affine(f32x8 (&v)[CHUNKS], const Params<CHUNKS>& p, bool weight, bool bias, bool fp32, float mean, float rstd) {
 #pragma unroll
     for (int j = 0; j < CHUNKS; ++j) {
         v[j] = (v[j] - mean) * rstd;
-        if (weight) v[j] *= load8(weight, a.param_fp32, col[j], left[j]);
-        if (bias) v[j] += load8(bias, a.param_fp32, col[j], left[j]);
+        if (weight) v[j] *= values(p.weight[j], fp32);
+        if (bias) v[j] += values(p.bias[j], fp32);
     }
 }
 
-// LANES lanes to a row, each CHUNKS times eight neighbouring values.
+// LANES lanes to a row, each CHUNKS times eight neighbouring values.  All that a row reads is asked for at once: a single row, whose time is
+// latency, waits for memory once.
 template <bool STREAM_FP32, bool BRANCH_FP32, int LANES, int CHUNKS>
-__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_rows(NormArgs a) {
-    constexpr int kLines = LANES < 256 ? 256 / LANES : 1;
+__global__ __launch_bounds__(LANES * lines_of(LANES)) void norm_rows(NormArgs a) {
+    constexpr int kLines = lines_of(LANES);
     __shared__ f32x4 part[2 * (LANES / 64)];
     const uint32_t row = blockIdx.x * kLines + (kLines > 1 ? threadIdx.x / LANES : 0);
     const int lane = threadIdx.x % LANES;
     if (kLines > 1 && row >= a.rows) return;
     RowSums<LANES> sums = {part, 0};
-    int col[CHUNKS], left[CHUNKS];
-    f32x8 h[CHUNKS], u[CHUNKS];
+    Place at[CHUNKS];
+    Raw x[CHUNKS], f[CHUNKS], gate[CHUNKS];
+    Params<CHUNKS> post, pre;
 #pragma unroll
     for (int j = 0; j < CHUNKS; ++j) {
-        col[j] = (j * LANES + lane) * 8;
-        left[j] = a.cols - col[j];
-        h[j] = load8(a.x.data, STREAM_FP32, (int64_t)row * a.x.stride + col[j], left[j]);
+        at[j] = Place((j * LANES + lane) * 8, a.cols);
+        if (a.f.data) f[j] = load8(a.f.data, BRANCH_FP32, (int64_t)row * a.f.stride, at[j]);
+        x[j] = load8(a.x.data, STREAM_FP32, (int64_t)row * a.x.stride, at[j]);
+        if (a.gate.data) gate[j] = load8(a.gate.data, BRANCH_FP32, (int64_t)(row / a.rows_per_gate) * a.gate.stride, at[j]);
     }
+    post.load(a.post_weight, a.post_bias, a.param_fp32, at);
+    pre.load(a.pre_weight, a.pre_bias, a.param_fp32, at);
     float post_mean = 0.0f, post_rstd = 0.0f, pre_mean = 0.0f, pre_rstd = 0.0f;
+    f32x8 h[CHUNKS], u[CHUNKS];
+#pragma unroll
+    for (int j = 0; j < CHUNKS; ++j) h[j] = at[j].mask(values(x[j], STREAM_FP32));
     if (a.f.data) {
 #pragma unroll
-        for (int j = 0; j < CHUNKS; ++j) u[j] = load8(a.f.data, BRANCH_FP32, (int64_t)row * a.f.stride + col[j], left[j]);
+        for (int j = 0; j < CHUNKS; ++j) u[j] = at[j].mask(values(f[j], BRANCH_FP32));
         if (a.post_norm) {
-            moments(sums, u, left, a, &post_mean, &post_rstd);
-            affine(u, left, col, a, a.post_weight, a.post_bias, post_mean, post_rstd);
+            moments(sums, u, at, a, &post_mean, &post_rstd);
+            affine(u, post, a.post_weight, a.post_bias, a.param_fp32, post_mean, post_rstd);
         }
 #pragma unroll
         for (int j = 0; j < CHUNKS; ++j) {
             if (a.gate.data) {
-                f32x8 g = load8(a.gate.data, BRANCH_FP32, (int64_t)(row / a.rows_per_gate) * a.gate.stride + col[j], left[j]);
+                f32x8 g = values(gate[j], BRANCH_FP32);
                 if (a.sigmoid) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) g[i] = sigmoid(g[i]);
                 }
                 u[j] *= g;
             }
-            h[j] = a.residual_scale * h[j] + a.branch_scale * u[j];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) h[j][i] = i < left[j] ? h[j][i] : 0.0f;      // (a bias, or an infinite scale, behind the row's end)
-            store8(a.h.data, STREAM_FP32, (int64_t)row * a.h.stride + col[j], left[j], h[j]);
+            h[j] = at[j].mask(a.residual_scale * h[j] + a.branch_scale * u[j]);
+            store8(a.h.data, STREAM_FP32, (int64_t)row * a.h.stride, at[j], h[j]);
         }
     }
     if (a.y.data) {
-        moments(sums, h, left, a, &pre_mean, &pre_rstd);
-        affine(h, left, col, a, a.pre_weight, a.pre_bias, pre_mean, pre_rstd);
+        moments(sums, h, at, a, &pre_mean, &pre_rstd);
+        affine(h, pre, a.pre_weight, a.pre_bias, a.param_fp32, pre_mean, pre_rstd);
 #pragma unroll
-        for (int j = 0; j < CHUNKS; ++j) store8(a.y.data, BRANCH_FP32, (int64_t)row * a.y.stride + col[j], left[j], h[j]);
+        for (int j = 0; j < CHUNKS; ++j) store8(a.y.data, BRANCH_FP32, (int64_t)row * a.y.stride, at[j], h[j]);
     }
     if (a.stats && lane == 0) {
         const int64_t rows = a.rows;
@@ -252,115 +311,157 @@ struct GradArgs {
     uint8_t post_norm, sigmoid, param_fp32, gate_done;      // gate_done: a unit's sums of the gate are complete
 };
 
+// What a row reads.
+template <int CHUNKS>
+struct RowData {
+    Raw h[CHUNKS], dy[CHUNKS], dh[CHUNKS], f[CHUNKS], gate[CHUNKS];
+    float post_mean, post_rstd, pre_mean, pre_rstd;
+};
+
 template <bool STREAM_FP32, bool BRANCH_FP32, int LANES, int CHUNKS, bool LAYER, bool BRANCH>
-__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_gradients(GradArgs a) {
-    constexpr int kLines = LANES < 256 ? 256 / LANES : 1;
+__global__ __launch_bounds__(LANES * lines_of(LANES)) void norm_gradients(GradArgs a) {
+    constexpr int kLines = lines_of(LANES);
     __shared__ f32x4 part_sums[2 * (LANES / 64)];
     __shared__ float joined[kLines > 1 ? kLines : 1][kLines > 1 ? LANES * 8 * CHUNKS : 1];
     const int line = kLines > 1 ? threadIdx.x / LANES : 0, lane = threadIdx.x % LANES;
     RowSums<LANES> sums = {part_sums, 0};
-    int col[CHUNKS], left[CHUNKS];
+    Place at[CHUNKS];
 #pragma unroll
     for (int j = 0; j < CHUNKS; ++j) {
-        col[j] = (j * LANES + lane) * 8;
-        left[j] = a.cols - col[j];
+        at[j] = Place((j * LANES + lane) * 8, a.cols);
     }
+    Params<CHUNKS> post, pre;
+    pre.load(a.pre_weight, nullptr, a.param_fp32, at);
+    if constexpr (BRANCH) post.load(a.post_weight, a.post_bias, a.param_fp32, at);
+    auto load = [&](RowData<CHUNKS>& d, uint32_t row) {
+        const int64_t rows = a.rows;
+        if (a.dy.data) {
+            d.pre_mean = a.stats[2 * rows + row];
+            d.pre_rstd = a.stats[3 * rows + row];
+        }
+        if (BRANCH && a.post_norm) {
+            d.post_mean = a.stats[row];
+            d.post_rstd = a.stats[rows + row];
+        }
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j) {
+            if (a.dy.data) {
+                d.h[j] = load8(a.h.data, STREAM_FP32, (int64_t)row * a.h.stride, at[j]);
+                d.dy[j] = load8(a.dy.data, BRANCH_FP32, (int64_t)row * a.dy.stride, at[j]);
+            }
+            if (a.dh.data) d.dh[j] = load8(a.dh.data, STREAM_FP32, (int64_t)row * a.dh.stride, at[j]);
+            if constexpr (BRANCH) {
+                d.f[j] = load8(a.f.data, BRANCH_FP32, (int64_t)row * a.f.stride, at[j]);
+                if (a.gate.data) d.gate[j] = load8(a.gate.data, BRANCH_FP32, (int64_t)(row / a.rows_per_gate) * a.gate.stride, at[j]);
+            }
+        }
+    };
     f32x8 acc[kSums][CHUNKS] = {};
     const uint32_t group = blockIdx.x / a.parts_per_group, in_group = blockIdx.x - group * a.parts_per_group;
     const uint32_t begin = group * a.units_per_group + in_group * a.part_units;
     const uint32_t end = min(begin + a.part_units, min((group + 1) * a.units_per_group, (a.rows + a.unit_rows - 1) / a.unit_rows));
-    for (uint32_t unit = begin + line; unit < end; unit += kLines) {
-        for (uint32_t row = unit * a.unit_rows; row < unit * a.unit_rows + a.unit_rows; ++row) {
-            f32x8 total[CHUNKS];
+    uint32_t unit = begin + line, row = unit * a.unit_rows;
+    constexpr bool kAhead = CHUNKS < 4;      // (the widest rows leave no registers for it)
+    RowData<CHUNKS> d, next;
+    if (unit < end) load(d, row);
+    while (unit < end) {
+        // the next row is on its way while this one goes through its sums
+        uint32_t next_row = row + 1, next_unit = unit;
+        if (next_row == (unit + 1) * a.unit_rows) {
+            next_unit = unit + kLines;
+            next_row = next_unit * a.unit_rows;
+        }
+        if (kAhead && next_unit < end) load(next, next_row);
+        f32x8 total[CHUNKS];
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j) total[j] = a.dh.data ? values(d.dh[j], STREAM_FP32) : f32x8{};
+        if (a.dy.data) {
+            f32x8 hat[CHUNKS], g[CHUNKS];
+            float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+            for (int j = 0; j < CHUNKS; ++j) {
+                hat[j] = (values(d.h[j], STREAM_FP32) - d.pre_mean) * d.pre_rstd;
+                g[j] = at[j].mask(values(d.dy[j], BRANCH_FP32));
+                acc[kPreWeight][j] += g[j] * hat[j];
+                if (LAYER) acc[kPreBias][j] += g[j];
+                if (a.pre_weight) g[j] *= values(pre.weight[j], a.param_fp32);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    s0 = fmaf(g[j][i], hat[j][i], s0);
+                    if (LAYER) s1 += g[j][i];
+                }
+            }
+            sums.sum2(s0, s1);
+            s0 *= a.inv_cols;
+            s1 *= a.inv_cols;
+#pragma unroll
+            for (int j = 0; j < CHUNKS; ++j) total[j] += d.pre_rstd * (g[j] - hat[j] * s0 - (LAYER ? s1 : 0.0f));
+        }
+        if (a.dx.data) {
 #pragma unroll
             for (int j = 0; j < CHUNKS; ++j)
-                total[j] = a.dh.data ? load8(a.dh.data, STREAM_FP32, (int64_t)row * a.dh.stride + col[j], left[j]) : f32x8{};
-            const int64_t rows = a.rows;
-            if (a.dy.data) {
-                const float mean = a.stats[2 * rows + row], rstd = a.stats[3 * rows + row];
-                f32x8 hat[CHUNKS], g[CHUNKS];
-                float s0 = 0.0f, s1 = 0.0f;
+                store8(a.dx.data, STREAM_FP32, (int64_t)row * a.dx.stride, at[j], BRANCH ? a.residual_scale * total[j] : total[j]);
+        }
+        if constexpr (BRANCH) {
+            const float mean = a.post_norm ? d.post_mean : 0.0f, rstd = a.post_norm ? d.post_rstd : 1.0f;
+            f32x8 hat[CHUNKS];
+            float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
-                for (int j = 0; j < CHUNKS; ++j) {
-                    hat[j] = (load8(a.h.data, STREAM_FP32, (int64_t)row * a.h.stride + col[j], left[j]) - mean) * rstd;
-                    g[j] = load8(a.dy.data, BRANCH_FP32, (int64_t)row * a.dy.stride + col[j], left[j]);
-                    acc[kPreWeight][j] += g[j] * hat[j];
-                    if (LAYER) acc[kPreBias][j] += g[j];
-                    if (a.pre_weight) g[j] *= load8(a.pre_weight, a.param_fp32, col[j], left[j]);
+            for (int j = 0; j < CHUNKS; ++j) {
+                hat[j] = (values(d.f[j], BRANCH_FP32) - mean) * rstd;
+                f32x8 du = a.branch_scale * total[j];
+                if (a.gate.data) {
+                    f32x8 act = values(d.gate[j], BRANCH_FP32), u = hat[j];
+                    if (a.post_weight) u *= values(post.weight[j], a.param_fp32);
+                    if (a.post_bias) u += values(post.bias[j], a.param_fp32);
+                    u *= du;
+                    if (a.sigmoid) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            act[i] = sigmoid(act[i]);
+                            u[i] *= act[i] * (1.0f - act[i]);
+                        }
+                    }
+                    acc[kGate][j] += u;
+                    du *= act;
+                }
+                if (a.post_norm) {
+                    acc[kPostWeight][j] += du * hat[j];
+                    if (LAYER) acc[kPostBias][j] += du;
+                    if (a.post_weight) du *= values(post.weight[j], a.param_fp32);
+                    const f32x8 own = at[j].mask(du);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        s0 = fmaf(g[j][i], hat[j][i], s0);
-                        if (LAYER) s1 += g[j][i];
+                        s0 = fmaf(own[i], hat[j][i], s0);
+                        if (LAYER) s1 += own[i];
                     }
                 }
+                total[j] = du;
+            }
+            if (a.post_norm) {
                 sums.sum2(s0, s1);
                 s0 *= a.inv_cols;
                 s1 *= a.inv_cols;
-#pragma unroll
-                for (int j = 0; j < CHUNKS; ++j) total[j] += rstd * (g[j] - hat[j] * s0 - (LAYER ? s1 : 0.0f));
             }
-            if (a.dx.data) {
-#pragma unroll
-                for (int j = 0; j < CHUNKS; ++j)
-                    store8(a.dx.data, STREAM_FP32, (int64_t)row * a.dx.stride + col[j], left[j], BRANCH ? a.residual_scale * total[j] : total[j]);
-            }
-            if constexpr (BRANCH) {
-                const float mean = a.post_norm ? a.stats[row] : 0.0f, rstd = a.post_norm ? a.stats[rows + row] : 1.0f;
-                f32x8 hat[CHUNKS];
-                float s0 = 0.0f, s1 = 0.0f;
+            if (a.df.data) {
 #pragma unroll
                 for (int j = 0; j < CHUNKS; ++j) {
-                    hat[j] = (load8(a.f.data, BRANCH_FP32, (int64_t)row * a.f.stride + col[j], left[j]) - mean) * rstd;
-                    f32x8 du = a.branch_scale * total[j];
-                    if (a.gate.data) {
-                        f32x8 act = load8(a.gate.data, BRANCH_FP32, (int64_t)(row / a.rows_per_gate) * a.gate.stride + col[j], left[j]);
-                        f32x8 u = hat[j];
-                        if (a.post_weight) u *= load8(a.post_weight, a.param_fp32, col[j], left[j]);
-                        if (a.post_bias) u += load8(a.post_bias, a.param_fp32, col[j], left[j]);
-                        u *= du;
-                        if (a.sigmoid) {
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                act[i] = sigmoid(act[i]);
-                                u[i] *= act[i] * (1.0f - act[i]);
-                            }
-                        }
-                        acc[kGate][j] += u;
-                        du *= act;
-                    }
-                    if (a.post_norm) {
-                        acc[kPostWeight][j] += du * hat[j];
-                        if (LAYER) acc[kPostBias][j] += du;
-                        if (a.post_weight) du *= load8(a.post_weight, a.param_fp32, col[j], left[j]);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            s0 += i < left[j] ? du[i] * hat[j][i] : 0.0f;
-                            if (LAYER) s1 += i < left[j] ? du[i] : 0.0f;
-                        }
-                    }
-                    total[j] = du;
+                    if (a.post_norm) total[j] = rstd * (total[j] - hat[j] * s0 - (LAYER ? s1 : 0.0f));
+                    store8(a.df.data, BRANCH_FP32, (int64_t)row * a.df.stride, at[j], total[j]);
                 }
-                if (a.post_norm) {
-                    sums.sum2(s0, s1);
-                    s0 *= a.inv_cols;
-                    s1 *= a.inv_cols;
-                }
-                if (a.df.data) {
+            }
+            if (next_unit != unit && a.gate_done && a.dgate.data) {
 #pragma unroll
-                    for (int j = 0; j < CHUNKS; ++j) {
-                        if (a.post_norm) total[j] = rstd * (total[j] - hat[j] * s0 - (LAYER ? s1 : 0.0f));
-                        store8(a.df.data, BRANCH_FP32, (int64_t)row * a.df.stride + col[j], left[j], total[j]);
-                    }
+                for (int j = 0; j < CHUNKS; ++j) {
+                    store8(a.dgate.data, BRANCH_FP32, (int64_t)unit * a.dgate.stride, at[j], acc[kGate][j]);
+                    acc[kGate][j] = f32x8{};
                 }
             }
         }
-        if (BRANCH && a.gate_done && a.dgate.data) {
-#pragma unroll
-            for (int j = 0; j < CHUNKS; ++j) {
-                store8(a.dgate.data, BRANCH_FP32, (int64_t)unit * a.dgate.stride + col[j], left[j], acc[kGate][j]);
-                acc[kGate][j] = f32x8{};
-            }
-        }
+        row = next_row;
+        unit = next_unit;
+        if (kAhead) d = next;
+        else if (unit < end) load(d, row);
     }
 #pragma unroll
     for (int k = 0; k < kSums; ++k) {
@@ -380,12 +481,12 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_gradients(Grad
                     for (int i = 0; i < 8; ++i)
 #pragma unroll
                         for (int l = 1; l < kLines; ++l) acc[k][j][i] += joined[l][(j * 8 + i) * LANES + lane];
-                    store8(out, true, col[j], left[j], acc[k][j]);
+                    store8(out, true, 0, at[j], acc[k][j]);
                 }
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < CHUNKS; ++j) store8(out, true, col[j], left[j], acc[k][j]);
+            for (int j = 0; j < CHUNKS; ++j) store8(out, true, 0, at[j], acc[k][j]);
         }
     }
 }
@@ -403,21 +504,30 @@ struct PartSums {
     int32_t cols;
 };
 
-__global__ __launch_bounds__(256) void sum_parts(PartSums p) {
-    __shared__ float joined[4][64];
+// A wavefront of the 16 adds up every 16th part, eight loads on their way at a time.
+constexpr int kSumWaves = 16;
+__global__ __launch_bounds__(64 * kSumWaves) void sum_parts(PartSums p) {
+    __shared__ float joined[kSumWaves][64];
     const PartSum& s = p.of[blockIdx.z];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = blockIdx.x * 64 + lane;
     for (uint32_t group = blockIdx.y; group < s.groups; group += gridDim.y) {
         float v = 0.0f;
         if (col < p.cols) {
             const float* at = s.part + ((int64_t)group * s.parts) * p.cols + col;
-            for (uint32_t i = wave; i < s.parts; i += 4) v += at[(int64_t)i * p.cols];
+            for (uint32_t i = wave; i < s.parts; i += 8 * kSumWaves) {
+                float w[8];
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j) w[j] = i + j * kSumWaves < s.parts ? at[(int64_t)(i + j * kSumWaves) * p.cols] : 0.0f;
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j) v += w[j];
+            }
         }
         __syncthreads();
         joined[wave][lane] = v;
         __syncthreads();
         if (wave == 0 && col < p.cols) {
-            v = ((joined[0][lane] + joined[1][lane]) + joined[2][lane]) + joined[3][lane];
+#pragma unroll
+            for (int w = 1; w < kSumWaves; ++w) v += joined[w][lane];
             const int64_t at = (int64_t)group * s.stride + col;
             if (s.fp32) ((float*)s.out)[at] = v;
             else ((__bf16*)s.out)[at] = (__bf16)v;
@@ -468,16 +578,17 @@ int check_gate(const flashoptim_matrix* gate, int64_t rows, int64_t cols, int dt
 // Calls launch(lanes, chunks) as integral constants with the shape for rows of this many values.
 template <int LANES, int CHUNKS>
 struct Shape { static constexpr int kLanes = LANES, kChunks = CHUNKS; };
+// Eight values to a lane as far as 512 lanes reach.  The backward pass keeps up to five sums a value, for which 1024 lanes, of 128 registers each,
+// have no room: it takes 512 lanes with 16 or 32 values.
 template <typename F>
 void with_shape(int64_t cols, F launch) {
     if (cols <= 512) launch(Shape<64, 1>{});
-    else if (cols <= 1024) launch(Shape<64, 2>{});
+    else if (cols <= 1024) launch(Shape<128, 1>{});
     else if (cols <= 2048) launch(Shape<256, 1>{});
-    else if (cols <= 4096) launch(Shape<256, 2>{});
+    else if (cols <= 4096) launch(Shape<512, 1>{});
     else if (cols <= 8192) launch(Shape<512, 2>{});
-    else launch(Shape<1024, 2>{});
+    else launch(Shape<512, 4>{});
 }
-inline int lines_of(int64_t cols) { return cols <= 1024 ? 4 : 1; }
 
 inline int64_t up(int64_t n, int64_t unit) { return (n + unit - 1) / unit; }
 
@@ -488,8 +599,10 @@ struct Parts {
 };
 Parts cut(int64_t rows, int64_t gates, int64_t cols) {
     const int64_t rows_per_gate = rows / gates;
-    const int64_t least = lines_of(cols);
-    int64_t part_rows = up(rows, 512);
+    // As many parts as there are compute units times what one holds of them, from 1024 of 128 lanes to 256 of 512 (us, 256 / 512 / 1024 / 1536 parts: 16384
+    // rows of 1024 values 116 / 74 / 48 / 47, 8192 of 4096 98 / 99 / 106 / 121, 4096 of 2048, layer norms, 42 / 33 / 41 / 47).
+    const int64_t least = cols <= 512 ? lines_of(64) : 2, most = cols <= 512 ? 512 : cols <= 1024 ? 1024 : cols <= 2048 ? 512 : 256;
+    int64_t part_rows = up(rows, most);
     if (part_rows < least) part_rows = least;
     Parts p;
     if (gates == 1 || rows_per_gate >= part_rows) {
@@ -547,7 +660,7 @@ int flashoptim_block_norm(const flashoptim_block_norm_spec* spec, const flashopt
     a.param_fp32 = spec->param_dtype == FLASHOPTIM_FP32;
     const bool sf = x->dtype == FLASHOPTIM_FP32, bf = branch_type == FLASHOPTIM_FP32;
     with_shape(spec->cols, [&](auto shape) {
-        constexpr int L = decltype(shape)::kLanes, C = decltype(shape)::kChunks, T = L < 256 ? 256 : L;
+        constexpr int L = decltype(shape)::kLanes, C = decltype(shape)::kChunks, T = L * lines_of(L);
         const dim3 grid((unsigned)up(rows, T / L)), block(T);
         if (bf) hipLaunchKernelGGL((norm_rows<true, true, L, C>), grid, block, 0, (hipStream_t)stream, a);
         else if (sf) hipLaunchKernelGGL((norm_rows<true, false, L, C>), grid, block, 0, (hipStream_t)stream, a);
@@ -632,7 +745,7 @@ int flashoptim_block_norm_backward(const flashoptim_block_norm_spec* spec, const
         a.gate_done = c.gate_done;
         const bool sf = h->dtype == FLASHOPTIM_FP32, bf = branch_type == FLASHOPTIM_FP32;
         with_shape(cols, [&](auto shape) {
-            constexpr int L = decltype(shape)::kLanes, C = decltype(shape)::kChunks, T = L < 256 ? 256 : L;
+            constexpr int L = decltype(shape)::kLanes, C = decltype(shape)::kChunks, T = L * lines_of(L);
             const dim3 grid((unsigned)c.parts), block(T);
             auto launch = [&](auto layer_c, auto branch_c) {
                 constexpr bool LN = decltype(layer_c)::value, BR = decltype(branch_c)::value;
@@ -649,7 +762,7 @@ int flashoptim_block_norm_backward(const flashoptim_block_norm_spec* spec, const
     }
     if (kinds) {
         const unsigned groups = a.slot[kGate] >= 0 ? (unsigned)(gates < 1024 ? gates : 1024) : 1u;
-        hipLaunchKernelGGL(sum_parts, dim3((unsigned)up(cols, 64), groups, (unsigned)kinds), dim3(256), 0, (hipStream_t)stream, p);
+        hipLaunchKernelGGL(sum_parts, dim3((unsigned)up(cols, 64), groups, (unsigned)kinds), dim3(64 * kSumWaves), 0, (hipStream_t)stream, p);
         FO_TRY(fo::hip_status(hipGetLastError()));
     }
     return FLASHOPTIM_OK;
