@@ -154,6 +154,26 @@ def load_library():
     return L
 
 
+_fast = None
+
+
+def _marshal():
+    """The module that turns tensors into the C ABI's matrices (csrc/marshal.cpp), with this library's entry points bound to it."""
+    global _fast
+    if _fast is None:
+        try:
+            from . import _marshal as fast
+        except ImportError as e:
+            raise RuntimeError("_marshal.so is missing: build it with `python paper_2602_23349_amd/build.py`") from e
+        lib = load_library()
+        names = [n for n in EXPORTED_SYMBOLS if n.startswith(("flashoptim_mx4_", "flashoptim_block_norm"))]
+        fast.bind({n: C.cast(getattr(lib, n), C.c_void_p).value for n in names}, torch._C._cuda_getCurrentRawStream,
+                  torch._C._cuda_getDevice)
+        torch.cuda.init()
+        _fast = fast
+    return _fast
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -468,37 +488,9 @@ def checkpoint_unpack(kind, blob, tensors, stream=None):
 _DTYPE = {torch.bfloat16: 0, torch.float32: 1}
 
 
-def _matrix(t, name):
-    """A flashoptim_matrix of a two-dimensional tensor with neighbouring columns, whose rows may lie apart; None for None."""
-    if t is None:
-        return None
-    dtype = _DTYPE.get(t.dtype)
-    if dtype is None or t.dim() != 2:
-        raise ValueError(f"{name}: a matrix of bfloat16 or float32 values, not {t.dim()}-dimensional {t.dtype}")
-    if not t.is_cuda:
-        raise ValueError(f"{name}: not on the GPU")
-    rows, cols = t.shape
-    stride, step = t.stride()
-    if cols > 1 and step != 1:
-        raise ValueError(f"{name}: the values of a row must be neighbours in memory")
-    return _Matrix(t.data_ptr(), rows, cols, stride if rows > 1 else cols, dtype)
-
-
-def _bytes_like(t, x, dtype, name):
-    """The pointer of a contiguous one-byte companion of matrix x, None for None."""
-    if t is None:
-        return None
-    if t.dtype != dtype or t.shape != x.shape or not t.is_contiguous() or not t.is_cuda:
-        raise ValueError(f"{name}: contiguous {dtype} of the matrix's shape on the GPU")
-    return t.data_ptr()
-
-
-def _workspace(t):
-    if t is None:
-        return None, 0
-    if not t.is_cuda or not t.is_contiguous():
-        raise ValueError("workspace: contiguous memory on the GPU")
-    return t.data_ptr(), t.numel() * t.element_size()
+def _handle(stream):
+    """What csrc/marshal.cpp takes for a stream: None is the current one."""
+    return None if stream is None else _stream_handle(stream)
 
 
 class Mx4Tensor:
@@ -515,29 +507,23 @@ class Mx4Tensor:
             if t.dtype != torch.uint8 or tuple(t.shape) != s or not t.is_contiguous():
                 raise ValueError(f"a {self.rows} by {self.cols} matrix in 4 bits takes contiguous uint8 of shapes {shapes}")
         self.codes, self.scales = buffers
-        self.on_gpu = self.codes.is_cuda and self.scales.is_cuda
         self.desc = _Mx4(self.codes.data_ptr(), self.scales.data_ptr(), self.rows, self.cols)
-
-
-def _mx4(q):
-    if q is None:
-        return None
-    if not q.on_gpu:
-        raise ValueError("a matrix in 4 bits that is not on the GPU")
-    return q.desc
+        self.address = C.addressof(self.desc) if self.codes.is_cuda and self.scales.is_cuda else -1
 
 
 def mx4_quantize(x, out=None, out_t=None, rho=None, rand=None, stream=None):
     """out <- x, out_t <- the transpose of x, each in 4 bits along its own rows (Mx4Tensor; either may be None).  rho: x holds
     BF16 weights with these INT8 corrections.  rand: random bytes for stochastic rounding."""
-    _check(load_library().flashoptim_mx4_quantize(_matrix(x, "x"), _bytes_like(rho, x, torch.int8, "rho"),
-                                                  _bytes_like(rand, x, torch.uint8, "rand"), _mx4(out), _mx4(out_t),
-                                                  _stream_handle(stream)), "flashoptim_mx4_quantize")
+    status = (_fast or _marshal()).quantize(x, None if out is None else out.address, None if out_t is None else out_t.address, rho, rand,
+                                            _handle(stream))
+    if status:
+        raise FlashOptimError(status, "flashoptim_mx4_quantize")
 
 
 def mx4_dequantize(q, out, stream=None):
-    _check(load_library().flashoptim_mx4_dequantize(_mx4(q), _matrix(out, "out"), _stream_handle(stream)),
-           "flashoptim_mx4_dequantize")
+    status = (_fast or _marshal()).dequantize(q.address, out, _handle(stream))
+    if status:
+        raise FlashOptimError(status, "flashoptim_mx4_dequantize")
 
 
 def _size(r, where):
@@ -561,25 +547,25 @@ def mx4_linear_backward_workspace(m, n, k):
 
 def mx4_matmul(a, b, out, workspace=None, stream=None):
     """out [m, n] <- a [m, k] b [n, k]^T, both Mx4Tensor."""
-    ws, size = _workspace(workspace)
-    _check(load_library().flashoptim_mx4_matmul(_mx4(a), _mx4(b), _matrix(out, "out"), ws, size, _stream_handle(stream)),
-           "flashoptim_mx4_matmul")
+    status = (_fast or _marshal()).matmul(a.address, b.address, out, workspace, _handle(stream))
+    if status:
+        raise FlashOptimError(status, "flashoptim_mx4_matmul")
 
 
 def mx4_linear(x, w, out, xt=None, workspace=None, stream=None):
     """out [m, n] <- Q(x) w^T with x [m, k] quantised on the way, w an Mx4Tensor [n, k]; xt: Mx4Tensor [k, m] for Q(x^T)."""
-    ws, size = _workspace(workspace)
-    _check(load_library().flashoptim_mx4_linear(_matrix(x, "x"), _mx4(w), _mx4(xt), _matrix(out, "out"), ws, size,
-                                                _stream_handle(stream)), "flashoptim_mx4_linear")
+    status = (_fast or _marshal()).linear(x, w.address, None if xt is None else xt.address, out, workspace, _handle(stream))
+    if status:
+        raise FlashOptimError(status, "flashoptim_mx4_linear")
 
 
 def mx4_linear_backward(dy, wt, xt, dx, dw, rand=None, workspace=None, stream=None):
     """dx [m, k] <- Q(dy) wt^T and dw [n, k] <- Q(dy^T) xt^T, with wt [k, n] and xt [k, m] Mx4Tensor; a pair (wt, dx) or (xt, dw)
     may be None."""
-    ws, size = _workspace(workspace)
-    _check(load_library().flashoptim_mx4_linear_backward(_matrix(dy, "dy"), _bytes_like(rand, dy, torch.uint8, "rand"), _mx4(wt),
-                                                         _mx4(xt), _matrix(dx, "dx"), _matrix(dw, "dw"), ws, size,
-                                                         _stream_handle(stream)), "flashoptim_mx4_linear_backward")
+    status = (_fast or _marshal()).linear_backward(dy, rand, None if wt is None else wt.address, None if xt is None else xt.address, dx, dw,
+                                                   workspace, _handle(stream))
+    if status:
+        raise FlashOptimError(status, "flashoptim_mx4_linear_backward")
 
 
 class BlockNorm:
@@ -590,35 +576,23 @@ class BlockNorm:
                  post_weight=None, post_bias=None, pre_weight=None, pre_bias=None):
         self.params = dict(post_weight=post_weight, post_bias=post_bias, pre_weight=pre_weight, pre_bias=pre_bias)
         given = [t for t in self.params.values() if t is not None]
-        self.param_dtype = given[0].dtype if given else torch.bfloat16
+        dtype = given[0].dtype if given else torch.bfloat16
         for name, t in self.params.items():
-            self.check_param(t, cols, name)
+            if t is not None and (t.dtype not in _DTYPE or t.dtype != dtype or t.numel() != cols or not t.is_contiguous() or not t.is_cuda):
+                raise ValueError(f"{name}: {cols} contiguous values on the GPU, bfloat16 or float32, one type for all weights and biases")
         self.cols = int(cols)
-        self.desc = _BlockNormSpec(self.cols, {"rms": 0, "layer": 1}.get(kind, -1), int(post_norm), {"linear": 0, "sigmoid": 1}.get(gate_act, -1),
-                                   _DTYPE[self.param_dtype], eps, residual_scale, branch_scale,
+        self.desc = _BlockNormSpec(self.cols, {"rms": 0, "layer": 1}.get(kind, -1), int(post_norm),
+                                   {"linear": 0, "sigmoid": 1}.get(gate_act, -1), _DTYPE[dtype], eps, residual_scale, branch_scale,
                                    *(_ptr(t) for t in self.params.values()))
-
-    def check_param(self, t, cols, name):
-        if t is None:
-            return
-        if t.dtype not in _DTYPE or t.dtype != self.param_dtype or t.numel() != cols or not t.is_contiguous() or not t.is_cuda:
-            raise ValueError(f"{name}: {cols} contiguous values on the GPU, bfloat16 or float32, one type for all weights and biases")
-
-
-def _check_stats(stats, rows):
-    if stats is not None and (stats.dtype != torch.float32 or stats.numel() != 4 * rows or not stats.is_contiguous()):
-        raise ValueError("stats: contiguous float32 of shape (4, rows)")
-    if stats is not None and not stats.is_cuda:
-        raise ValueError("stats: not on the GPU")
-    return _ptr(stats)
+        self.address = C.addressof(self.desc)
 
 
 def block_norm(spec, x, f=None, gate=None, h=None, y=None, stats=None, stream=None):
     """h <- residual_scale x + branch_scale act(gate) u, u = f or its norm; y <- the norm of h (of x without f); stats [4, rows] for
     the backward pass."""
-    _check(load_library().flashoptim_block_norm(spec.desc, _matrix(x, "x"), _matrix(f, "f"), _matrix(gate, "gate"), _matrix(h, "h"),
-                                                _matrix(y, "y"), _check_stats(stats, x.shape[0]), _stream_handle(stream)),
-           "flashoptim_block_norm")
+    status = (_fast or _marshal()).norm(spec.address, x, f, gate, h, y, stats, _handle(stream))
+    if status:
+        raise FlashOptimError(status, "flashoptim_block_norm")
 
 
 def block_norm_backward_workspace(spec, rows, gates=1):
@@ -629,15 +603,10 @@ def block_norm_backward_workspace(spec, rows, gates=1):
 def block_norm_backward(spec, h, stats, f=None, gate=None, dy=None, dh=None, dx=None, df=None, dgate=None, dpost_weight=None,
                         dpost_bias=None, dpre_weight=None, dpre_bias=None, workspace=None, stream=None):
     """The gradients of block_norm that are not None, from dy and dh (either may be None); h is x where there is no branch."""
-    ws, size = _workspace(workspace)
-    sums = dict(dpost_weight=dpost_weight, dpost_bias=dpost_bias, dpre_weight=dpre_weight, dpre_bias=dpre_bias)
-    for name, t in sums.items():
-        spec.check_param(t, spec.cols, name)
-    mats = [_matrix(t, n) for t, n in ((dy, "dy"), (dh, "dh"), (dx, "dx"), (df, "df"), (dgate, "dgate"))]
-    grads = _BlockNormGrads(*(None if m is None else C.pointer(m) for m in mats), *(_ptr(t) for t in sums.values()))
-    _check(load_library().flashoptim_block_norm_backward(spec.desc, _matrix(h, "h"), _matrix(f, "f"), _matrix(gate, "gate"),
-                                                         _check_stats(stats, h.shape[0]), grads, ws, size, _stream_handle(stream)),
-           "flashoptim_block_norm_backward")
+    status = (_fast or _marshal()).norm_backward(spec.address, h, stats, f, gate, dy, dh, dx, df, dgate, dpost_weight, dpost_bias,
+                                                 dpre_weight, dpre_bias, workspace, _handle(stream))
+    if status:
+        raise FlashOptimError(status, "flashoptim_block_norm_backward")
 
 
 def faithful_rounding_stats(stream=None):

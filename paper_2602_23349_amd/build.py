@@ -1,15 +1,19 @@
-"""Builds the FlashOptim HIP library for gfx950 in-tree: paper_2602_23349_amd/libflashoptim.so."""
+"""Builds in-tree the FlashOptim HIP library for gfx950, paper_2602_23349_amd/libflashoptim.so, and the module that marshals
+torch tensors for it, paper_2602_23349_amd/_marshal.so."""
 import concurrent.futures
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libflashoptim.so")
+MARSHAL = os.path.join(HERE, "_marshal.so")
+MARSHAL_SOURCES = [os.path.join(CSRC, "marshal.cpp"), os.path.join(ROOT, "include", "flashoptim.h")]
 SOURCES = [os.path.join(CSRC, n) for n in ("flashoptim_kernels.hip", "flashoptim_api.hip", "flashoptim_mx4.hip", "flashoptim_norm.hip")]
 HEADERS = [os.path.join(CSRC, "flashoptim_device.h"), os.path.join(CSRC, "flashoptim_launch.h"), os.path.join(CSRC, "flashoptim_host.h"),
            os.path.join(ROOT, "include", "flashoptim.h")]
@@ -31,23 +35,46 @@ def hipcc() -> str:
     raise RuntimeError("hipcc not found")
 
 
-def stale() -> bool:
-    if not os.path.exists(LIB):
+def older(built, sources) -> bool:
+    if not os.path.exists(built):
         return True
-    t = os.path.getmtime(LIB)
-    return any(os.path.getmtime(p) > t for p in SOURCES + HEADERS + [os.path.abspath(__file__)])     # (this file: the flags)
+    t = os.path.getmtime(built)
+    return any(os.path.getmtime(p) > t for p in sources + [os.path.abspath(__file__)])     # (this file: the flags)
+
+
+def stale() -> bool:
+    return older(LIB, SOURCES + HEADERS)
+
+
+def marshal_command() -> list:
+    """Host code against torch's headers, by the host compiler; the library's entry points are bound at run time."""
+    import torch
+    from torch.utils import cpp_extension
+    libs = cpp_extension.library_paths()
+    return (["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-w", "-fvisibility=hidden",
+             f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I" + os.path.join(ROOT, "include"),
+             "-I" + sysconfig.get_paths()["include"]] + ["-I" + d for d in cpp_extension.include_paths()] +
+            [MARSHAL_SOURCES[0], "-o", MARSHAL] + [a for d in libs for a in ("-L" + d, "-Wl,-rpath," + d)] +
+            ["-lc10", "-ltorch_cpu", "-ltorch_python"])
 
 
 def build(force: bool = True) -> str:
-    if not force and not stale():
-        return LIB
+    with concurrent.futures.ThreadPoolExecutor(2) as pool:
+        marshal = pool.submit(run, marshal_command()) if force or older(MARSHAL, MARSHAL_SOURCES) else None
+        if force or stale():
+            build_library()
+        if marshal:
+            marshal.result()
+    return LIB
+
+
+def build_library() -> None:
     with tempfile.TemporaryDirectory() as tmp, concurrent.futures.ThreadPoolExecutor(4) as pool:
         objects = [os.path.join(tmp, os.path.basename(src) + ".o") for src in SOURCES]
         compiled = pool.map(lambda p: run([hipcc()] + FLAGS + ["-c", p[0], "-o", p[1]]), zip(SOURCES, objects))
         out = "".join(compiled) + run([hipcc(), "--offload-arch=gfx950", "-fPIC", "-shared"] + objects + ["-o", LIB])
     if out.strip():
         print(out, file=sys.stderr)
-    return LIB
 
 
 def run(cmd) -> str:
@@ -55,7 +82,7 @@ def run(cmd) -> str:
     # the host pass warns that it does not know the packed-fp32-ops feature: harmless
     out = "\n".join(l for l in r.stdout.splitlines() if "packed-fp32-ops" not in l)
     if r.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + out)
+        raise RuntimeError(f"{os.path.basename(cmd[0])} failed:\n" + out)
     return out
 
 
