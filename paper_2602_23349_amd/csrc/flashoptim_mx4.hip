@@ -70,53 +70,67 @@ __device__ __forceinline__ float master_weight(uint32_t bits, int rho) {
     return e == 255 ? base : base + __builtin_amdgcn_ldexpf(q, max(e, 1) - 135);
 }
 
-// Eight consecutive values of a row, 0 behind its end.
+// Eight consecutive values of a row as they lie in memory, with their corrections and random bytes.
+struct Eight {
+    i32x4 a, b;      // (b: FP32 only)
+    uint64_t rho, rand;
+};
 template <int SRC>
-__device__ __forceinline__ void load8(float (&v)[8], const Source& s, uint32_t row, uint32_t col) {
-    const int64_t at = (int64_t)row * s.stride + col;
-    const int64_t at_rho = (int64_t)row * s.cols + col;
-    const uint32_t left = col < s.cols ? s.cols - col : 0;
+__device__ __forceinline__ void load_whole(Eight& e, const Source& s, uint32_t row, uint32_t col) {
+    const int64_t at = (int64_t)row * s.stride + col, packed = (int64_t)row * s.cols + col;
     if constexpr (SRC == kFp32) {
-        const float* p = (const float*)s.data + at;
-        if (left >= 8) {
-            const f32x4 a = load_as<f32x4>(p), b = load_as<f32x4>(p + 4);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = i < (int)left ? p[i] : 0.0f;
-        }
+        e.a = load_as<i32x4>((const float*)s.data + at);
+        e.b = load_as<i32x4>((const float*)s.data + at + 4);
     } else {
-        const uint16_t* p = (const uint16_t*)s.data + at;
-        uint32_t bits[8];
-        uint64_t rho = 0;
-        if (left >= 8) {
-            const i32x4 a = load_as<i32x4>(p);
+        e.a = load_as<i32x4>((const uint16_t*)s.data + at);
+    }
+    if constexpr (SRC == kSplit) e.rho = load_as<uint64_t>(s.rho + packed);
+    if (s.rand) e.rand = load_as<uint64_t>(s.rand + packed);
+}
+template <int SRC>
+__device__ __forceinline__ void unpack(float (&v)[8], const Eight& e) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { bits[2 * i] = (uint32_t)a[i] & 0xffffu; bits[2 * i + 1] = (uint32_t)a[i] >> 16; }
-            if constexpr (SRC == kSplit) rho = load_as<uint64_t>(s.rho + at_rho);
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (SRC == kFp32) {
+            v[i] = __int_as_float(i < 4 ? e.a[i] : e.b[i - 4]);
         } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                bits[i] = i < (int)left ? p[i] : 0u;
-                if constexpr (SRC == kSplit) rho |= i < (int)left ? (uint64_t)(uint8_t)s.rho[at_rho + i] << (8 * i) : 0;
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if constexpr (SRC == kSplit) v[i] = master_weight(bits[i], (int)(int8_t)(rho >> (8 * i)));
-            else v[i] = bf16_value(bits[i]);
+            const uint32_t bits = i % 2 ? (uint32_t)e.a[i / 2] >> 16 : (uint32_t)e.a[i / 2] & 0xffffu;
+            if constexpr (SRC == kSplit) v[i] = master_weight(bits, (int)(int8_t)(e.rho >> (8 * i)));
+            else v[i] = bf16_value(bits);
         }
     }
 }
-__device__ __forceinline__ uint64_t load_rand8(const Source& s, uint32_t row, uint32_t col) {
-    const uint8_t* p = s.rand + (int64_t)row * s.cols + col;
+// The same where the row may end within the eight or before them: 0 behind its end.  What is not there is loaded from the last place that
+// is: a load that is made only if it is there would wait for the one before.
+template <int SRC>
+__device__ __forceinline__ void load8(float (&v)[8], uint64_t& rand, const Source& s, uint32_t row, uint32_t col) {
     const uint32_t left = col < s.cols ? s.cols - col : 0;
-    if (left >= 8) return load_as<uint64_t>(p);
-    uint64_t r = 0;
+    Eight e = {};
+    if (left >= 8) {
+        load_whole<SRC>(e, s, row, col);
+    } else if (left > 0) {
+        const int last = (int)left - 1;
+        const int64_t at = (int64_t)row * s.stride + col, packed = (int64_t)row * s.cols + col;
+        uint32_t w[8];
+        uint8_t rho[8], r[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r |= i < (int)left ? (uint64_t)p[i] << (8 * i) : 0;
-    return r;
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (SRC == kFp32) w[i] = ((const uint32_t*)s.data)[at + min(i, last)];
+            else w[i] = ((const uint16_t*)s.data)[at + min(i, last)];
+            if constexpr (SRC == kSplit) rho[i] = (uint8_t)s.rho[packed + min(i, last)];
+            if (s.rand) r[i] = s.rand[packed + min(i, last)];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (i > last) continue;
+            if constexpr (SRC == kFp32) { if (i < 4) e.a[i] = (int)w[i]; else e.b[i - 4] = (int)w[i]; }
+            else e.a[i / 2] |= (int)(w[i] << (16 * (i % 2)));
+            if constexpr (SRC == kSplit) e.rho |= (uint64_t)rho[i] << (8 * i);
+            if (s.rand) e.rand |= (uint64_t)r[i] << (8 * i);
+        }
+    }
+    rand = e.rand;
+    unpack<SRC>(v, e);
 }
 
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
@@ -129,23 +143,28 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t largest) {
     return largest >= 0x7f800000u ? 255u : (uint32_t)max(byte, 0);
 }
 
-// One stochastically rounded code: t = |v| 2^(127 - byte) <= 6 lies on a stretch of the grid with steps of 1/2, 1 or 2.
+// One stochastically rounded code of a value whose random byte is r.  With t = |v| 2^(127 - byte) <= 6, from 1 on the grid's codes are the upper bits of
+// t's own representation (one mantissa bit), the 22 below them the share (t - a) / (b - a) in units of 2^-22: what is added carries into the
+// code exactly if the share exceeds (r + 1/2) / 256.  Below 1, where the grid goes on in steps of 1/2, 2^23 t takes that place, rounded up to a whole
+// number, which leaves the comparison with whole numbers as it is; of a BF16 value, 1 + t has the same bits (it is exact, or t too small to
+// be rounded up).
+template <bool BF16>
 __device__ __forceinline__ uint32_t random_code(float v, float up_scale, uint32_t r) {
     const float t = fabsf(v) * up_scale;
-    const bool fine = t < 2.0f, mid = t < 4.0f;
-    const float y = t * (fine ? 2.0f : mid ? 1.0f : 0.5f), low = floorf(y);
-    const uint32_t more = (y - low) * 256.0f > (float)r + 0.5f ? 1u : 0u;
-    return (uint32_t)low + (fine ? 0u : mid ? 2u : 4u) + more + ((__float_as_uint(v) >> 31) << 3);
+    const uint32_t above = __float_as_uint(t) - (252u << 22);
+    const uint32_t below = BF16 ? __float_as_uint(1.0f + t) - (254u << 22) : (uint32_t)ceilf(t * 0x1p23f);
+    const uint32_t place = t < 1.0f ? below : above;
+    return ((place + (0x3fffffu - 0x2000u) - (r << 14)) >> 22) | (__float_as_uint(v) >> 31) << 3;
 }
 
 // Eight codes, the first in the lowest bits.
-template <bool RANDOM>
+template <bool RANDOM, bool BF16 = false>
 __device__ __forceinline__ uint32_t codes8(const float* v, uint32_t byte, uint64_t r) {
     if constexpr (RANDOM) {
         const float up_scale = __uint_as_float((254u - (byte == 255u ? 0u : byte)) << 23);
         uint32_t c = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) c |= random_code(v[i], up_scale, (uint32_t)(r >> (8 * i)) & 255u) << (4 * i);
+        for (int i = 0; i < 8; ++i) c |= random_code<BF16>(v[i], up_scale, (uint32_t)(r >> (8 * i)) & 255u) << (4 * i);
         return byte == 255u ? 0u : c;
     } else {
         const float scale = __uint_as_float(byte << 23);
@@ -165,13 +184,35 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t v) {
 }
 
 // Codes and scale of the eight values that this lane has of its quad's block.
-template <bool RANDOM>
+template <bool RANDOM, bool BF16 = false>
 __device__ __forceinline__ uint32_t quad_codes(const float (&v)[8], uint64_t r, uint32_t* byte) {
     uint32_t largest = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) largest = max(largest, magnitude(v[i]));
     *byte = scale_byte<RANDOM>(quad_max(largest));
-    return codes8<RANDOM>(v, *byte, r);
+    return codes8<RANDOM, BF16>(v, *byte, r);
+}
+
+// The same from eight BF16 values as they lie in memory, without unpacking them.
+__device__ __forceinline__ uint32_t quad_codes_bf16(i32x4 w, uint32_t* byte) {
+    using u16x2 = unsigned short __attribute__((ext_vector_type(2)));
+    using bf16x2 = __bf16 __attribute__((ext_vector_type(2)));
+    u16x2 largest = {};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int m = w[i] & 0x7fff7fff;
+        largest = __builtin_elementwise_max(largest, __builtin_bit_cast(u16x2, m));
+    }
+    *byte = scale_byte<false>(quad_max((uint32_t)max(largest[0], largest[1]) << 16));
+    const float scale = __uint_as_float(*byte << 23);
+    bf16x2 v[4];      // (by memcpy: a bit cast of a vector's element takes its first)
+    __builtin_memcpy(v, &w, 16);
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, v[0], scale, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, v[1], scale, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, v[2], scale, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, v[3], scale, 3);
+    return *byte == 255u ? 0u : c;
 }
 
 // ------------------------------------------------------------------------------------------------ along rows --
@@ -184,10 +225,10 @@ __global__ __launch_bounds__(256) void quantize_rows(Source s, Mx4 out, uint32_t
     const uint32_t row = unit / out.segments, seg = unit - row * out.segments;
     const uint32_t col = seg * kSegment + lane * 8;
     float v[8];
-    load8<SRC>(v, s, row, col);
-    const uint64_t r = RANDOM ? load_rand8(s, row, col) : 0;
+    uint64_t r = 0;
+    load8<SRC>(v, r, s, row, col);
     uint32_t byte;
-    const uint32_t c = quad_codes<RANDOM>(v, r, &byte);
+    const uint32_t c = quad_codes<RANDOM, SRC == kBf16>(v, r, &byte);
     store_as(out.codes + ((int64_t)row * out.segments + seg) * kSegmentBytes + lane * 4, c);
     uint8_t* scales = out.scales + (int64_t)row * out.scale_pitch + seg * 8;
     if (lane % 4 == 0) scales[lane / 4] = (uint8_t)byte;
@@ -196,29 +237,43 @@ __global__ __launch_bounds__(256) void quantize_rows(Source s, Mx4 out, uint32_t
 
 // ---------------------------------------------------------------------------------- along columns, or both ways --
 
-// A workgroup handles 128 by 128 values: the rows as above, and through LDS the columns.  The grid covers rows and columns up to whole
-// segments, so that what lies behind the matrix's end is written as zeros in both layouts.
-constexpr int kTile = 128;
+// A workgroup handles ROWS by 128 values: the rows as above, and through LDS the columns.  The grid covers rows and columns up to whole
+// segments, so that what lies behind the matrix's end is written as zeros in both layouts.  All loads of a tile are on their way together:
+// where a tile reaches beyond the matrix, its lanes load from its last row, or a row's first values, and drop them.
+// Bound: HBM.  Neighbouring tiles of one column are neighbours on one XCD, whose L2 puts their 32 or 64 bytes of a row of out_t together.
+constexpr int kTileCols = 128;
 
-template <int SRC, bool RANDOM>
-__global__ __launch_bounds__(256) void quantize_both(Source s, Mx4 out, Mx4 out_t, bool rows_too) {
+template <int SRC, bool RANDOM, int ROWS>
+__global__ __launch_bounds__(256) void quantize_both(Source s, Mx4 out, Mx4 out_t, bool rows_too, uint32_t row_tiles, uint32_t tiles) {
     using Cell = typename std::conditional<SRC == kBf16, uint16_t, float>::type;
-    __shared__ Cell tile[kTile][kTile];
-    __shared__ uint8_t rands[RANDOM ? kTile : 1][kTile];
-    const uint32_t row0 = blockIdx.y * kTile, col0 = blockIdx.x * kTile;
+    constexpr int kPasses = ROWS / 16;
+    __shared__ Cell tile[ROWS][kTileCols];
+    __shared__ uint8_t rands[RANDOM ? ROWS : 1][kTileCols];
+    const uint32_t xcd = blockIdx.x % 8, at = xcd * (tiles / 8) + min(xcd, tiles % 8) + blockIdx.x / 8;
+    const uint32_t row0 = at % row_tiles * ROWS, col0 = at / row_tiles * kTileCols;
     const uint32_t lane = threadIdx.x % 16, line = threadIdx.x / 16;
     const uint32_t col = col0 + lane * 8;
+    const bool ragged = s.cols % 8 != 0 && col0 + kTileCols > s.cols;      // a row ends within some lane's eight values
+    Eight e[kPasses];
+    if (!ragged) {
 #pragma unroll
-    for (int i = 0; i < kTile / 16; ++i) {
+        for (int i = 0; i < kPasses; ++i) load_whole<SRC>(e[i], s, min(row0 + i * 16 + line, s.rows - 1), col < s.cols ? col : 0);
+    }
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
         const uint32_t row = row0 + i * 16 + line;
         float v[8];
         uint64_t r = 0;
-        if (row < s.rows) {
-            load8<SRC>(v, s, row, col);
-            if (RANDOM) r = load_rand8(s, row, col);
+        if (ragged) {
+            if (row < s.rows) load8<SRC>(v, r, s, row, col);
         } else {
+            unpack<SRC>(v, e[i]);
+            r = e[i].rand;
+        }
+        if (row >= s.rows || col >= s.cols) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+            r = 0;
         }
         Cell* cell = &tile[i * 16 + line][lane * 8];
         if constexpr (SRC == kBf16) {
@@ -233,34 +288,28 @@ __global__ __launch_bounds__(256) void quantize_both(Source s, Mx4 out, Mx4 out_
         if constexpr (RANDOM) *(uint64_t*)&rands[i * 16 + line][lane * 8] = r;
         if (rows_too && row < s.rows) {
             uint32_t byte;
-            const uint32_t c = quad_codes<RANDOM>(v, r, &byte);
+            const uint32_t c = quad_codes<RANDOM, SRC == kBf16>(v, r, &byte);
             if (col < out.segments * kSegment) {
                 store_as(out.codes + (int64_t)row * out.segments * kSegmentBytes + col / 2, c);
                 if (lane % 4 == 0) out.scales[(int64_t)row * out.scale_pitch + col / kBlock] = (uint8_t)byte;
             }
         }
     }
-    if (rows_too && col0 + kTile == out.segments * kSegment && (out.segments & 1)) {       // the row's scales behind the last segment
+    if (rows_too && col0 + kTileCols == out.segments * kSegment && (out.segments & 1)) {       // the row's scales behind the last segment
         const uint32_t row = row0 + threadIdx.x / 2;
-        if (row < s.rows) store_as(out.scales + (int64_t)row * out.scale_pitch + out.segments * 8 + threadIdx.x % 2 * 4, 0u);
+        if (threadIdx.x < 2 * ROWS && row < s.rows) store_as(out.scales + (int64_t)row * out.scale_pitch + out.segments * 8 + threadIdx.x % 2 * 4, 0u);
     }
     __syncthreads();
-    // a wavefront takes 32 of the rows, a lane two columns of them
-    const uint32_t wave = threadIdx.x / 64, pair = threadIdx.x % 64;
-    const uint32_t at_row = row0 + wave * kBlock;
+    // a lane takes 32 rows of a column
+    const uint32_t c = threadIdx.x % kTileCols, col_t = col0 + c;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const uint32_t c = SRC == kBf16 ? pair * 2 + h : pair + 64 * h, col_t = col0 + c;
+    for (uint32_t block = threadIdx.x / kTileCols; block < ROWS / kBlock; block += 256 / kTileCols) {
         float v[kBlock];
         uint32_t largest = 0;
 #pragma unroll
         for (int i = 0; i < kBlock; ++i) {
-            if constexpr (SRC == kBf16) {
-                const uint32_t w = *(const uint32_t*)&tile[wave * kBlock + i][pair * 2];
-                v[i] = __uint_as_float(h ? w & 0xffff0000u : w << 16);
-            } else {
-                v[i] = tile[wave * kBlock + i][c];
-            }
+            if constexpr (SRC == kBf16) v[i] = bf16_value(tile[block * kBlock + i][c]);
+            else v[i] = tile[block * kBlock + i][c];
             largest = max(largest, magnitude(v[i]));
         }
         const uint32_t byte = scale_byte<RANDOM>(largest);
@@ -270,17 +319,17 @@ __global__ __launch_bounds__(256) void quantize_both(Source s, Mx4 out, Mx4 out_
             uint64_t r = 0;
             if constexpr (RANDOM) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) r |= (uint64_t)rands[wave * kBlock + j * 8 + i][c] << (8 * i);
+                for (int i = 0; i < 8; ++i) r |= (uint64_t)rands[block * kBlock + j * 8 + i][c] << (8 * i);
             }
-            codes[j] = (int)codes8<RANDOM>(v + 8 * j, byte, r);
+            codes[j] = (int)codes8<RANDOM, SRC == kBf16>(v + 8 * j, byte, r);
         }
+        const uint32_t at_row = row0 + block * kBlock;
         if (col_t < s.cols && at_row < out_t.segments * kSegment) {
             store_as(out_t.codes + (int64_t)col_t * out_t.segments * kSegmentBytes + at_row / 2, codes);
-            out_t.scales[(int64_t)col_t * out_t.scale_pitch + at_row / kBlock] = (uint8_t)byte;
+            uint8_t* scales = out_t.scales + (int64_t)col_t * out_t.scale_pitch;
+            scales[at_row / kBlock] = (uint8_t)byte;
+            if (at_row + kSegment >= out_t.segments * kSegment && (out_t.segments & 1)) scales[at_row / kBlock + 8] = 0;      // behind the last segment
         }
-        if (col_t < s.cols && (out_t.segments & 1) && row0 + kTile == out_t.segments * kSegment)
-            out_t.scales[(int64_t)col_t * out_t.scale_pitch + out_t.segments * 8 + wave] = 0,
-            out_t.scales[(int64_t)col_t * out_t.scale_pitch + out_t.segments * 8 + 4 + wave] = 0;
     }
 }
 
@@ -369,10 +418,11 @@ __device__ __forceinline__ void store_result4(const Result& c, uint32_t row, uin
 
 // A workgroup makes 16 columns by 16 rows of c; its wavefronts share out the segments of the sum and are added up through LDS.
 template <bool FP32, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void product_small(Mx4 b, Mx4 a, Result c) {
+__global__ __launch_bounds__(64 * WAVES) void product_small(Mx4 b, Mx4 a, Result c, uint32_t p_tiles) {
     __shared__ f32x4 part[WAVES][64];
     const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64, q = lane / 16;
-    const uint32_t b_row = min(blockIdx.x * 16 + lane % 16, b.rows - 1), a_row = min(blockIdx.y * 16 + lane % 16, a.rows - 1);
+    const uint32_t q_tile = blockIdx.x / p_tiles, p_tile = blockIdx.x - q_tile * p_tiles;
+    const uint32_t b_row = min(p_tile * 16 + lane % 16, b.rows - 1), a_row = min(q_tile * 16 + lane % 16, a.rows - 1);
     const uint8_t* pb = b.codes + (int64_t)b_row * b.segments * kSegmentBytes + q * 32;
     const uint8_t* pa = a.codes + (int64_t)a_row * a.segments * kSegmentBytes + q * 32;
     const uint8_t* sb = b.scales + (int64_t)b_row * b.scale_pitch + q * 2;
@@ -394,7 +444,7 @@ __global__ __launch_bounds__(64 * WAVES) void product_small(Mx4 b, Mx4 a, Result
     if (wave == 0) {
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) acc += part[w][lane];
-        store_result4<FP32>(c, blockIdx.y * 16 + lane % 16, blockIdx.x * 16 + q * 4, acc);
+        store_result4<FP32>(c, q_tile * 16 + lane % 16, p_tile * 16 + q * 4, acc);
     }
 }
 
@@ -447,14 +497,19 @@ __device__ __forceinline__ void copy_to_lds(i32x4 buffer, uint32_t lane_offset, 
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"((uint32_t)(uintptr_t)FO_LDS(to)), "v"(lane_offset), "s"(buffer),
                  "s"(offset) : "memory");
 }
-// Waits until this wavefront's copies have landed and its reads of LDS have come back.
-__device__ __forceinline__ void wait_copies() { __builtin_amdgcn_s_waitcnt(0x0070); }
+// Waits until all but the last `VM` of this wavefront's copies have landed and its reads of LDS have come back.
+template <int VM>
+__device__ __forceinline__ void wait_copies() {
+    static_assert(VM < 64, "six bits");
+    __builtin_amdgcn_s_waitcnt((VM & 15) | (VM >> 4) << 14 | 0x0070);
+}
 
 // What a wavefront copies of ROWS rows: the lane's places in them.  Behind the matrix's last row a copy takes that row again.
 template <int ROWS, int WAVES>
 struct Copier {
-    static constexpr int kCodes = ROWS * kSegmentBytes / 1024 / WAVES, kScales = ROWS * kScaleBytes / 1024 / WAVES;      // copies of 1024 bytes
-    static_assert(kCodes * 1024 * WAVES == ROWS * kSegmentBytes && kScales * 1024 * WAVES == ROWS * kScaleBytes, "every wavefront copies as much");
+    // Copies of 1024 bytes.  All wavefronts make as many, so that they can count alike: where there are fewer of scales than wavefronts, some twice.
+    static constexpr int kCodes = ROWS * kSegmentBytes / 1024 / WAVES, kAllScales = ROWS * kScaleBytes / 1024, kScales = (kAllScales + WAVES - 1) / WAVES;
+    static_assert(kCodes * 1024 * WAVES == ROWS * kSegmentBytes && (kAllScales % WAVES == 0 || WAVES % kAllScales == 0), "every wavefront copies as much");
     const uint8_t *codes, *scales;      // from the tile's first row on
     uint32_t code_bytes, scale_bytes;
     uint32_t code_at[kCodes], scale_at[kScales];
@@ -472,7 +527,7 @@ struct Copier {
         }
 #pragma unroll
         for (int i = 0; i < kScales; ++i) {
-            const int row = (wave * kScales + i) * 32 + lane / 2;
+            const int row = (wave * kScales + i) % kAllScales * 32 + lane / 2;
             scale_at[i] = min((uint32_t)row, last) * m.scale_pitch + (uint32_t)((lane % 2 ^ scale_swizzle(row)) * 16);
         }
     }
@@ -483,7 +538,7 @@ struct Copier {
     __device__ __forceinline__ void copy_scales(Scales<ROWS>& to, uint32_t group, bool there) const {
         const i32x4 buffer = buffer_of(scales, there ? scale_bytes : 0);
 #pragma unroll
-        for (int i = 0; i < kScales; ++i) copy_to_lds(buffer, scale_at[i], group * kScaleBytes, to.bytes + (wave * kScales + i) * 1024);
+        for (int i = 0; i < kScales; ++i) copy_to_lds(buffer, scale_at[i], group * kScaleBytes, to.bytes + (wave * kScales + i) % kAllScales * 1024);
     }
 };
 
@@ -524,11 +579,11 @@ __device__ __forceinline__ void multiply_turn(const i32x4 (&pw)[TP], const i32x4
     __builtin_amdgcn_sched_barrier(0);
 }
 
-template <bool FP32, int BP, int BQ, int WP, int WQ, int RESIDENT>
+template <bool FP32, int BP, int BQ, int WP, int WQ, int STAGES, int RESIDENT>
 __global__ __launch_bounds__(64 * WP * WQ, RESIDENT) void product_tiles(Mx4 b, Mx4 a, Result c, uint32_t p_tiles, uint32_t q_tiles) {
     constexpr int kWaves = WP * WQ, TP = BP / WP / 32, TQ = BQ / WQ / 32;
-    __shared__ Stage<BP> p_stage[2];
-    __shared__ Stage<BQ> q_stage[2];
+    __shared__ Stage<BP> p_stage[STAGES];
+    __shared__ Stage<BQ> q_stage[STAGES];
     __shared__ Scales<BP> p_scales[2];
     __shared__ Scales<BQ> q_scales[2];
     // consecutive workgroups run on different XCDs: each XCD takes a stretch of the tiles, in columns of eight, whose rows it then has in its L2
@@ -546,8 +601,8 @@ __global__ __launch_bounds__(64 * WP * WQ, RESIDENT) void product_tiles(Mx4 b, M
     const uint32_t steps = b.segments;
     f32x16 acc[TP][TQ] = {};
     auto copy = [&](i32x4 p_buffer, i32x4 q_buffer, uint32_t step, int i) {
-        if (i < p_copy.kCodes) p_copy.copy_codes(p_buffer, p_stage[step % 2], step, i);
-        else q_copy.copy_codes(q_buffer, q_stage[step % 2], step, i - p_copy.kCodes);
+        if (i < p_copy.kCodes) p_copy.copy_codes(p_buffer, p_stage[step % STAGES], step, i);
+        else q_copy.copy_codes(q_buffer, q_stage[step % STAGES], step, i - p_copy.kCodes);
     };
     constexpr int kCopies = p_copy.kCodes + q_copy.kCodes;
     constexpr int kEvery = TP * TQ * 2 / kCopies > 0 ? TP * TQ * 2 / kCopies : 1;      // products to a copy: all in the first half of a step
@@ -555,25 +610,27 @@ __global__ __launch_bounds__(64 * WP * WQ, RESIDENT) void product_tiles(Mx4 b, M
     p_copy.copy_scales(p_scales[0], 0, true);
     q_copy.copy_scales(q_scales[0], 0, true);
 #pragma unroll
-    for (int i = 0; i < kCopies; ++i) copy(p_copy.buffer(true), q_copy.buffer(true), 0, i);
+    for (int j = 0; j < STAGES - 1; ++j)
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) copy(p_copy.buffer(j < steps), q_copy.buffer(j < steps), j, i);
     for (uint32_t t = 0; t < steps; ++t) {
         // this wavefront's copies for step t have landed; behind the barrier all have, and nobody reads the stage of step t - 1 any more
-        wait_copies();
+        wait_copies<(STAGES - 2) * kCopies>();
         __builtin_amdgcn_s_barrier();
-        const uint32_t group = t / kScaleSteps, in_group = t % kScaleSteps;
+        const uint32_t group = t / kScaleSteps, in_group = t % kScaleSteps, next = t + STAGES - 1;
         if (in_group == 0) {
             p_copy.copy_scales(p_scales[group % 2 ^ 1], group + 1, t + kScaleSteps < steps);
             q_copy.copy_scales(q_scales[group % 2 ^ 1], group + 1, t + kScaleSteps < steps);
         }
-        const i32x4 p_buffer = p_copy.buffer(t + 1 < steps), q_buffer = q_copy.buffer(t + 1 < steps);
+        const i32x4 p_buffer = p_copy.buffer(next < steps), q_buffer = q_copy.buffer(next < steps);
         auto behind = [&](int product) {
             if (product % kEvery != 0 || product / kEvery >= kCopies) return;
             __builtin_amdgcn_sched_barrier(0);
-            copy(p_buffer, q_buffer, t + 1, product / kEvery);
+            copy(p_buffer, q_buffer, next, product / kEvery);
             __builtin_amdgcn_sched_barrier(0);
         };
-        const Stage<BP>& p = p_stage[t % 2];
-        const Stage<BQ>& q = q_stage[t % 2];
+        const Stage<BP>& p = p_stage[t % STAGES];
+        const Stage<BQ>& q = q_stage[t % STAGES];
         int p_scale[TP], q_scale[TQ];
 #pragma unroll
         for (int i = 0; i < TP; ++i) p_scale[i] = scales_of(p_scales[group % 2], p0 + 32 * i, (int)in_group, h);
@@ -590,7 +647,7 @@ __global__ __launch_bounds__(64 * WP * WQ, RESIDENT) void product_tiles(Mx4 b, M
         multiply_turn<2>(pw[0], qw[0], p_scale, q_scale, acc, behind);
         multiply_turn<3>(pw[1], qw[1], p_scale, q_scale, acc, behind);
     }
-    wait_copies();
+    wait_copies<0>();
 #pragma unroll
     for (int i = 0; i < TP; ++i)
 #pragma unroll
@@ -599,6 +656,144 @@ __global__ __launch_bounds__(64 * WP * WQ, RESIDENT) void product_tiles(Mx4 b, M
             for (int g = 0; g < 4; ++g)
                 store_result4<FP32>(c, q_tile * BQ + q0 + 32 * j, p_tile * BP + (p0 - lane % 32) + 32 * i + 8 * g + 4 * h,
                                     f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]});
+}
+
+// ------------------------------------------------------------------------------------------- linear, for single tokens --
+//
+// y = Q(x) w^T for at most 16 rows of x, in one launch.  A workgroup makes 16 TILES columns.  It asks for x and its first weights, quantises x, all of
+// it, into LDS (eight values to a lane, as in quantize_rows), and multiplies; its wavefronts share out the segments of the sum and are added up
+// through LDS.  Every workgroup quantises x again: 8 rows of 4096 values are 240 instructions to a lane of 512, under the latency of the weights.
+// (With every lane quantising the blocks that it multiplies, without LDS, the loads of x, 16 bytes from each of 32 lines, took longer than the
+// weights: 8 rows on 14336 by 4096 weights 16.6 us.)
+// Bound: the weights' bytes, and for few of them the latency of one pass through memory.
+struct Few {
+    Source x;
+    Mx4 w;
+    Result y;
+    uint32_t code_pitch, scale_pitch;      // of x in LDS
+    uint32_t units_magic;                  // item / units = the upper half of item times this, for all items there can be
+};
+
+template <int SRC, bool FP32, int WAVES, int TILES>
+__global__ __launch_bounds__(64 * WAVES) void linear_small(Few a) {
+    extern __shared__ __align__(16) uint8_t lds[];
+    constexpr int kAhead = 2;      // segments of a wavefront's weights that are on their way at a time
+    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64, q = lane / 16, x_row = lane % 16;
+    const uint32_t segments = a.w.segments;
+    const uint8_t *codes[TILES], *scales[TILES];
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+        const uint32_t row = min((blockIdx.x * TILES + i) * 16 + lane % 16, a.w.rows - 1);
+        codes[i] = a.w.codes + (int64_t)row * segments * kSegmentBytes + q * 32;
+        scales[i] = a.w.scales + (int64_t)row * a.w.scale_pitch + q * 2;
+    }
+    struct Weights {
+        i32x4 codes[kAhead][TILES][2];
+        int scales[kAhead][TILES];
+    } now, next;
+    auto load = [&](Weights& to, uint32_t seg) {
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            if (seg + j * WAVES >= segments) continue;
+#pragma unroll
+            for (int i = 0; i < TILES; ++i) {
+                const uint32_t at = (seg + j * WAVES) * kSegmentBytes;
+                to.codes[j][i][0] = load_as<i32x4>(codes[i] + at);
+                to.codes[j][i][1] = load_as<i32x4>(codes[i] + at + 16);
+                to.scales[j][i] = load_as<uint16_t>(scales[i] + (seg + j * WAVES) * 8);
+            }
+        }
+    };
+    uint8_t* const x_codes = lds;
+    uint8_t* const x_scales = lds + a.x.rows * a.code_pitch;
+    const uint32_t units = segments * (kSegment / 8), total = units * a.x.rows;      // of eight values: to a row, of all
+    auto store = [&](uint32_t c, uint32_t byte, uint32_t row, uint32_t unit) {
+        *(uint32_t*)(x_codes + row * a.code_pitch + unit * 4) = c;
+        if (unit % 4 == 0) x_scales[row * a.scale_pitch + unit / 4] = (uint8_t)byte;
+    };
+    // The first units of x are asked for ahead of the weights: they come back in this order, and are quantised while the weights are on their way.
+    // No load is made by a case distinction, which would wait for it: a unit behind the row's end loads the row's first values.
+    auto quantize = [&](auto batch) {
+        constexpr int kBatch = decltype(batch)::value, kWords = SRC == kFp32 ? 2 : 1;
+        i32x4 raw[kBatch][kWords];
+        auto ask = [&](uint32_t at) {
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                const uint32_t item = min(at + j * 64 * WAVES, total - 1), row = __umulhi(item, a.units_magic), col = (item - row * units) * 8;
+                const int64_t from = (int64_t)row * a.x.stride + (col < a.x.cols ? col : 0);
+#pragma unroll
+                for (int i = 0; i < kWords; ++i) raw[j][i] = load_as<i32x4>((const uint8_t*)a.x.data + from * (SRC == kFp32 ? 4 : 2) + 16 * i);
+            }
+        };
+        ask(threadIdx.x);
+        load(now, wave);
+        for (uint32_t at = threadIdx.x; at < total; at += 64 * WAVES * kBatch) {
+            if (at != threadIdx.x) ask(at);
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                const uint32_t item = at + j * 64 * WAVES, row = __umulhi(item, a.units_magic), unit = item - row * units;
+                if (item >= total) continue;
+                uint32_t byte, c;
+                if constexpr (SRC == kFp32) {
+                    float v[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = unit * 8 < a.x.cols ? __int_as_float(raw[j][i / 4][i % 4]) : 0.0f;
+                    c = quad_codes<false>(v, 0, &byte);
+                } else {
+                    c = quad_codes_bf16(unit * 8 < a.x.cols ? raw[j][0] : i32x4{}, &byte);
+                }
+                store(c, byte, row, unit);
+            }
+        }
+    };
+    if (a.x.cols % 8 == 0) {
+        if (total <= 64 * WAVES) quantize(std::integral_constant<int, 1>{});
+        else quantize(std::integral_constant<int, 4>{});
+    } else {
+        load(now, wave);
+        for (uint32_t item = threadIdx.x; item < total; item += 64 * WAVES) {
+            const uint32_t row = __umulhi(item, a.units_magic), unit = item - row * units;
+            float v[8];
+            uint64_t r = 0;
+            load8<SRC>(v, r, a.x, row, unit * 8);
+            uint32_t byte;
+            const uint32_t c = quad_codes<false>(v, 0, &byte);
+            store(c, byte, row, unit);
+        }
+    }
+    __syncthreads();
+    f32x4 acc[TILES] = {};
+    for (uint32_t seg = wave; seg < segments; seg += kAhead * WAVES) {
+        if (seg + kAhead * WAVES < segments) load(next, seg + kAhead * WAVES);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const uint32_t at = seg + j * WAVES;
+            if (at >= segments) continue;
+            i32x4 x[2] = {};
+            int x_scale = 0;
+            if (x_row < a.x.rows) {
+                x[0] = *(const i32x4*)(x_codes + x_row * a.code_pitch + at * kSegmentBytes + q * 32);
+                x[1] = *(const i32x4*)(x_codes + x_row * a.code_pitch + at * kSegmentBytes + q * 32 + 16);
+                x_scale = *(const uint16_t*)(x_scales + x_row * a.scale_pitch + at * 8 + q * 2);
+            }
+#pragma unroll
+            for (int i = 0; i < TILES; ++i)
+#pragma unroll
+                for (int s = 0; s < 2; ++s) acc[i] = mfma(now.codes[j][i][s], x[s], acc[i], now.scales[j][i], x_scale, s);
+        }
+        now = next;
+    }
+    __syncthreads();
+    f32x4* const part = (f32x4*)lds;      // [wave][tile][lane], over x
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) part[(wave * TILES + i) * 64 + lane] = acc[i];
+    __syncthreads();
+    if (wave < TILES) {
+        f32x4 sum = part[wave * 64 + lane];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) sum += part[(w * TILES + wave) * 64 + lane];
+        store_result4<FP32>(a.y, lane % 16, (blockIdx.x * TILES + wave) * 16 + q * 4, sum);
+    }
 }
 
 __global__ __launch_bounds__(256) void fill_zero(Result c, int bytes) {
@@ -631,8 +826,15 @@ int launch_quantize(const Source& s, const flashoptim_mx4* out, const flashoptim
         hipLaunchKernelGGL((quantize_rows<SRC, RANDOM>), dim3((total + 7) / 8), dim3(256), 0, stream, s, o, total);
     } else {
         const Mx4 t = to_dev(*out_t), o = out ? to_dev(*out) : Mx4{};
-        const dim3 grid((unsigned)(up(s.cols, kSegment) * (kSegment / kTile)), (unsigned)(up(s.rows, kSegment) * (kSegment / kTile)));
-        hipLaunchKernelGGL((quantize_both<SRC, RANDOM>), grid, dim3(256), 0, stream, s, o, t, out != nullptr);
+        auto launch = [&](auto rows) {
+            constexpr int R = decltype(rows)::value;
+            const uint32_t row_tiles = t.segments * (kSegment / R), tiles = row_tiles * (uint32_t)up(s.cols, kSegment) * (kSegment / kTileCols);
+            hipLaunchKernelGGL((quantize_both<SRC, RANDOM, R>), dim3(tiles), dim3(256), 0, stream, s, o, t, out != nullptr, row_tiles, tiles);
+        };
+        // Rows of a tile, in us with 32 / 64 / 128: BF16, 1024 x 2304 4.4 / 4.8 / 6.1, 8192 x 4096 25.2 / 24.2 / 26.2, 14336 x 4096 38.7 / 36.5 / 38.4,
+        // stochastic 68 / 61 / 68; split weights, 1001 x 768 4.0 / 4.8 / 6.9, 14336 x 4096 45.2 / 45.4 / 56.4.
+        if ((int64_t)s.rows * s.cols < ((int64_t)1 << 25)) launch(std::integral_constant<int, 32>{});
+        else launch(std::integral_constant<int, 64>{});
     }
     return fo::hip_status(hipGetLastError());
 }
@@ -651,8 +853,44 @@ int quantize(const flashoptim_matrix& x, const int8_t* rho, const uint8_t* rand,
     return x.dtype == FLASHOPTIM_FP32 ? launch_quantize<kFp32>(s, out, out_t, stream) : launch_quantize<kBf16>(s, out, out_t, stream);
 }
 
-int product(const flashoptim_mx4& a, const flashoptim_mx4& b, const flashoptim_matrix& c, void* workspace, hipStream_t stream) {
-    (void)workspace;
+// Calls launch with the number of wavefronts that share out a sum over this many segments.
+template <typename F>
+void with_waves(int64_t segments, F launch) {
+    if (segments <= 4) launch(std::integral_constant<int, 4>{});
+    else if (segments <= 16) launch(std::integral_constant<int, 8>{});
+    else launch(std::integral_constant<int, 16>{});
+}
+
+// How a product of m by n sums over k terms is made: by the largest tiles of which there are enough.  In us, with tiles of 16 (the wavefronts of a
+// workgroup share out the sum) / 64 / 128 / 256:
+//   kTiny while they are at most 256 tiles: 33 x 64 x 7600 (m, n, k) 6.1 / 9.6 / 16 / 39, 200 x 200 x 14000 11.1 / 16.2 / 28 / 71, 40 x 500 x 300
+//     2.4 / 3.1 / 4.0 / 6.2; 90 x 950 x 950, 360 of them, 3.5 / 3.6, 600 x 600 x 600, 1444, 5.2 / 3.5;
+//   kTile256 from 192 tiles on, three quarters of the compute units: 3000 x 4096 x 4096 - / 53 / 39.5 / 36.1; with 128 of them, 2048 x 4096 x 4096,
+//     - / 37 / 26.6 / 32.7;
+//   kTile64 up to 512 tiles, which is two for each compute unit: 512 x 4096 x 4096 86 / 10.4 / 12.1, 2304 x 768 x 1024 - / 5.2 / 6.2, 768 x 768 x 8000 49 /
+//     10.8 / 19.8; kTile128 beyond: 1001 x 2304 x 768, 576 of them, - / 7.0 / 6.2, 1024 x 4096 x 4096 - / 19.5 / 15.7, 8192 x 768 x 768 - / 12.1 / 9.9.
+// Sums split over workgroups and joined by another launch: 768 x 768 x 8000 in two 13.5, in four 16.2.
+enum Shape { kTiny, kTile64, kTile128, kTile256 };
+Shape product_shape(int64_t m, int64_t n, int64_t k) {
+    if (m <= 16 || n <= 16 || k > kMaxTiledTerms) return kTiny;
+    if (up(m, 16) * up(n, 16) <= 256) return kTiny;
+    if (up(m, 256) * up(n, 256) >= 192) return kTile256;
+    return m > 64 && n > 64 && up(m, 64) * up(n, 64) > 512 ? kTile128 : kTile64;
+}
+
+template <bool FP32>
+int launch_tiles(Shape shape, const Mx4& a, const Mx4& b, const Result& c, hipStream_t stream) {
+    auto launch = [&](auto kernel, int edge, int threads) {
+        const uint32_t pt = (uint32_t)up(c.cols, edge), qt = (uint32_t)up(c.rows, edge);
+        hipLaunchKernelGGL(kernel, dim3(pt * qt), dim3(threads), 0, stream, b, a, c, pt, qt);
+    };
+    if (shape == kTile256) launch(product_tiles<FP32, 256, 256, 4, 2, 2, 2>, 256, 512);
+    else if (shape == kTile128) launch(product_tiles<FP32, 128, 128, 2, 2, 2, 2>, 128, 256);
+    else launch(product_tiles<FP32, 64, 64, 2, 2, 4, 2>, 64, 256);
+    return fo::hip_status(hipGetLastError());
+}
+
+int product(const flashoptim_mx4& a, const flashoptim_mx4& b, const flashoptim_matrix& c, hipStream_t stream) {
     if (c.rows == 0 || c.cols == 0) return FLASHOPTIM_OK;
     const Result r = {c.data, c.stride, (uint32_t)c.rows, (uint32_t)c.cols};
     const bool fp32 = c.dtype == FLASHOPTIM_FP32;
@@ -660,23 +898,53 @@ int product(const flashoptim_mx4& a, const flashoptim_mx4& b, const flashoptim_m
         hipLaunchKernelGGL(fill_zero, dim3((unsigned)up(c.cols, 256), (unsigned)(c.rows < 1024 ? c.rows : 1024)), dim3(256), 0, stream, r, fp32 ? 4 : 2);
         return fo::hip_status(hipGetLastError());
     }
-    if (c.rows > 16 && c.cols > 16 && a.cols <= kMaxTiledTerms) {
-        auto tiles = [&](auto kernel, int bp, int bq, int threads) {
-            const uint32_t pt = (uint32_t)up(c.cols, bp), qt = (uint32_t)up(c.rows, bq);
-            hipLaunchKernelGGL(kernel, dim3(pt * qt), dim3(threads), 0, stream, to_dev(b), to_dev(a), r, pt, qt);
+    const Shape shape = product_shape(c.rows, c.cols, a.cols);
+    if (shape != kTiny)
+        return fp32 ? launch_tiles<true>(shape, to_dev(a), to_dev(b), r, stream) : launch_tiles<false>(shape, to_dev(a), to_dev(b), r, stream);
+    const uint32_t pt = (uint32_t)up(c.cols, 16), qt = (uint32_t)up(c.rows, 16);
+    auto launch = [&](auto waves) {
+        constexpr int W = decltype(waves)::value;
+        if (fp32) hipLaunchKernelGGL((product_small<true, W>), dim3(pt * qt), dim3(64 * W), 0, stream, to_dev(b), to_dev(a), r, pt);
+        else hipLaunchKernelGGL((product_small<false, W>), dim3(pt * qt), dim3(64 * W), 0, stream, to_dev(b), to_dev(a), r, pt);
+    };
+    with_waves(up(a.cols, kSegment), launch);
+    return fo::hip_status(hipGetLastError());
+}
+
+// Whether x is quantised by every workgroup of linear_small, or once by a launch of its own: by the number of values, filled up to whole segments.
+// One launch / two, us: 4096 x 4096 (n, k) with 1 row 4.4 / 6.2, 8 rows 6.1 / 7.0, 16 rows 8.0 / 7.4; 4096 x 14336 4 rows 11.4 / 12.5, 8 rows 14.3 / 13.8;
+// 8192 x 2048 16 rows 6.1 / 7.4.
+constexpr int64_t kFewRows = 16, kFewValues = 57344;
+
+// What linear_small keeps of x in LDS: rows of codes begin 16 bytes apart in the banks.
+int64_t few_code_pitch(int64_t k) { return up(k, kSegment) * kSegmentBytes + 16; }
+int64_t few_scale_pitch(int64_t k) { return up(k, kSegment) * 8 + 8; }
+// Exact for items and units below 2^16 (there are at most 2^13 units of eight).
+uint32_t few_units_magic(int64_t k) { return (uint32_t)(((uint64_t)1 << 32) / (uint64_t)(up(k, kSegment) * (kSegment / 8)) + 1); }
+bool takes_few_rows(int64_t m, int64_t n, int64_t k) {
+    return m >= 1 && m <= kFewRows && n >= 1 && k >= 1 && m * up(k, kSegment) * kSegment <= kFewValues;
+}
+
+int linear_few_rows(const flashoptim_matrix& x, const flashoptim_mx4& w, const flashoptim_matrix& y, hipStream_t stream) {
+    const Few a = {{x.data, nullptr, nullptr, x.stride, (uint32_t)x.rows, (uint32_t)x.cols}, to_dev(w), {y.data, y.stride, (uint32_t)y.rows, (uint32_t)y.cols},
+                   (uint32_t)few_code_pitch(x.cols), (uint32_t)few_scale_pitch(x.cols), few_units_magic(x.cols)};
+    const bool fp32 = y.dtype == FLASHOPTIM_FP32, x_fp32 = x.dtype == FLASHOPTIM_FP32;
+    const int64_t x_bytes = x.rows * (few_code_pitch(x.cols) + few_scale_pitch(x.cols));
+    with_waves(up(x.cols, kSegment), [&](auto waves) {
+        auto launch = [&](auto tiles) {
+            constexpr int W = decltype(waves)::value, T = decltype(tiles)::value;
+            const int64_t part_bytes = W * T * 1024;
+            const dim3 grid((unsigned)up(y.cols, 16 * T));
+            const unsigned bytes = (unsigned)(x_bytes > part_bytes ? x_bytes : part_bytes);
+            auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * W), bytes, stream, a); };
+            if (x_fp32) { if (fp32) go(linear_small<kFp32, true, W, T>); else go(linear_small<kFp32, false, W, T>); }
+            else { if (fp32) go(linear_small<kBf16, true, W, T>); else go(linear_small<kBf16, false, W, T>); }
         };
-        if (up(c.cols, 256) * up(c.rows, 256) >= 256) {
-            if (fp32) tiles(product_tiles<true, 256, 256, 4, 2, 2>, 256, 256, 512);
-            else tiles(product_tiles<false, 256, 256, 4, 2, 2>, 256, 256, 512);
-        } else {
-            if (fp32) tiles(product_tiles<true, 128, 128, 2, 2, 2>, 128, 128, 256);
-            else tiles(product_tiles<false, 128, 128, 2, 2, 2>, 128, 128, 256);
-        }
-        return fo::hip_status(hipGetLastError());
-    }
-    const dim3 grid((unsigned)up(c.cols, 16), (unsigned)up(c.rows, 16));
-    if (fp32) hipLaunchKernelGGL((product_small<true, 8>), grid, dim3(512), 0, stream, to_dev(b), to_dev(a), r);
-    else hipLaunchKernelGGL((product_small<false, 8>), grid, dim3(512), 0, stream, to_dev(b), to_dev(a), r);
+        // two tiles to a workgroup, which halves the work on x, where that leaves one for every compute unit (14336 x 4096: 1 row 9.2 us, with two 9.6; 8
+        // rows 13.3, 11.7)
+        if (x.rows < 4 || up(y.cols, 16) < 512) launch(std::integral_constant<int, 1>{});
+        else launch(std::integral_constant<int, 2>{});
+    });
     return fo::hip_status(hipGetLastError());
 }
 
@@ -698,10 +966,6 @@ int64_t check_sizes(int64_t m, int64_t n, int64_t k) {
         for (int j = 0; j < 3; ++j)
             if (sizes[i] > 0 && up(sizes[j], kSegment) >= ((int64_t)1 << 27) / sizes[i]) return FLASHOPTIM_ERR_NUMEL_RANGE;
     return FLASHOPTIM_OK;
-}
-int64_t product_bytes(int64_t m, int64_t n, int64_t k) {
-    (void)m; (void)n; (void)k;
-    return 0;
 }
 
 int check_workspace(const void* workspace, int64_t bytes, int64_t need) {
@@ -731,7 +995,6 @@ int flashoptim_mx4_quantize(const flashoptim_matrix* x, const int8_t* rho, const
     if (out_t) FO_TRY(check_mx4(out_t));
     if (out && (out->rows != x->rows || out->cols != x->cols)) return FLASHOPTIM_ERR_INVALID_ARG;
     if (out_t && (out_t->rows != x->cols || out_t->cols != x->rows)) return FLASHOPTIM_ERR_INVALID_ARG;
-    if (out_t && up(x->rows, kSegment) * (kSegment / kTile) > 65535) return FLASHOPTIM_ERR_NUMEL_RANGE;
     return quantize(*x, rho, rand, out, out_t, (hipStream_t)stream);
 }
 
@@ -749,18 +1012,17 @@ int flashoptim_mx4_dequantize(const flashoptim_mx4* q, const flashoptim_matrix* 
 
 int64_t flashoptim_mx4_matmul_workspace(int64_t m, int64_t n, int64_t k) {
     FO_TRY(check_sizes(m, n, k));
-    return product_bytes(m, n, k);
+    return 0;
 }
 
 int64_t flashoptim_mx4_linear_workspace(int64_t m, int64_t n, int64_t k) {
     FO_TRY(check_sizes(m, n, k));
-    return align16(mx4_bytes(m, k)) + product_bytes(m, n, k);
+    return align16(mx4_bytes(m, k));
 }
 
 int64_t flashoptim_mx4_linear_backward_workspace(int64_t m, int64_t n, int64_t k) {
     FO_TRY(check_sizes(m, n, k));
-    const int64_t dx = product_bytes(m, k, n), dw = product_bytes(n, k, m);
-    return align16(mx4_bytes(m, n)) + align16(mx4_bytes(n, m)) + (dx > dw ? dx : dw);
+    return align16(mx4_bytes(m, n)) + align16(mx4_bytes(n, m));
 }
 
 int flashoptim_mx4_matmul(const flashoptim_mx4* a, const flashoptim_mx4* b, const flashoptim_matrix* c, void* workspace,
@@ -770,8 +1032,8 @@ int flashoptim_mx4_matmul(const flashoptim_mx4* a, const flashoptim_mx4* b, cons
     FO_TRY(fo::check_matrix(c));
     if (a->cols != b->cols || c->rows != a->rows || c->cols != b->rows) return FLASHOPTIM_ERR_INVALID_ARG;
     FO_TRY(check_sizes(a->rows, b->rows, a->cols));
-    FO_TRY(check_workspace(workspace, workspace_bytes, product_bytes(a->rows, b->rows, a->cols)));
-    return product(*a, *b, *c, workspace, (hipStream_t)stream);
+    FO_TRY(check_workspace(workspace, workspace_bytes, 0));
+    return product(*a, *b, *c, (hipStream_t)stream);
 }
 
 int flashoptim_mx4_linear(const flashoptim_matrix* x, const flashoptim_mx4* w, const flashoptim_mx4* xt, const flashoptim_matrix* y,
@@ -782,12 +1044,12 @@ int flashoptim_mx4_linear(const flashoptim_matrix* x, const flashoptim_mx4* w, c
     if (xt) FO_TRY(check_mx4(xt));
     if (w->cols != x->cols || y->rows != x->rows || y->cols != w->rows) return FLASHOPTIM_ERR_INVALID_ARG;
     if (xt && (xt->rows != x->cols || xt->cols != x->rows)) return FLASHOPTIM_ERR_INVALID_ARG;
-    if (xt && up(x->rows, kSegment) * (kSegment / kTile) > 65535) return FLASHOPTIM_ERR_NUMEL_RANGE;
     FO_TRY(check_workspace(workspace, workspace_bytes, flashoptim_mx4_linear_workspace(x->rows, w->rows, x->cols)));
+    if (!xt && takes_few_rows(x->rows, y->cols, x->cols)) return linear_few_rows(*x, *w, *y, (hipStream_t)stream);
     uint8_t* at = (uint8_t*)workspace;
     const flashoptim_mx4 q = carve(at, x->rows, x->cols);
     FO_TRY(quantize(*x, nullptr, nullptr, &q, xt, (hipStream_t)stream));
-    return product(q, *w, *y, at, (hipStream_t)stream);
+    return product(q, *w, *y, (hipStream_t)stream);
 }
 
 int flashoptim_mx4_linear_backward(const flashoptim_matrix* dy, const uint8_t* rand, const flashoptim_mx4* wt, const flashoptim_mx4* xt,
@@ -809,14 +1071,13 @@ int flashoptim_mx4_linear_backward(const flashoptim_matrix* dy, const uint8_t* r
         if (dx && dw->cols != k) return FLASHOPTIM_ERR_INVALID_ARG;
         k = dw->cols;
         if (dw->rows != n || xt->rows != k || xt->cols != m) return FLASHOPTIM_ERR_INVALID_ARG;
-        if (up(m, kSegment) * (kSegment / kTile) > 65535) return FLASHOPTIM_ERR_NUMEL_RANGE;
     }
     FO_TRY(check_workspace(workspace, workspace_bytes, flashoptim_mx4_linear_backward_workspace(m, n, k)));
     uint8_t* at = (uint8_t*)workspace;
     const flashoptim_mx4 q = carve(at, m, n), qt = carve(at, n, m);
     FO_TRY(quantize(*dy, nullptr, rand, dx ? &q : nullptr, dw ? &qt : nullptr, (hipStream_t)stream));
-    if (dx) FO_TRY(product(q, *wt, *dx, at, (hipStream_t)stream));
-    if (dw) FO_TRY(product(qt, *xt, *dw, at, (hipStream_t)stream));
+    if (dx) FO_TRY(product(q, *wt, *dx, (hipStream_t)stream));
+    if (dw) FO_TRY(product(qt, *xt, *dw, (hipStream_t)stream));
     return FLASHOPTIM_OK;
 }
 
