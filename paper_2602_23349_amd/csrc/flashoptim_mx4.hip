@@ -55,6 +55,12 @@ __device__ __forceinline__ T load_as(const void* p) {       // any alignment: th
     __builtin_memcpy(&v, p, sizeof(T));
     return v;
 }
+// The same of data that this kernel reads once: it leaves the caches to what is read again.
+template <typename T, int ALIGN>
+__device__ __forceinline__ T load_once(const void* p) {
+    typedef T Unaligned __attribute__((aligned(ALIGN)));
+    return __builtin_nontemporal_load((const Unaligned*)p);
+}
 template <typename T>
 __device__ __forceinline__ void store_as(void* p, T v) {
     __builtin_memcpy(p, &v, sizeof(T));
@@ -79,13 +85,13 @@ template <int SRC>
 __device__ __forceinline__ void load_whole(Eight& e, const Source& s, uint32_t row, uint32_t col) {
     const int64_t at = (int64_t)row * s.stride + col, packed = (int64_t)row * s.cols + col;
     if constexpr (SRC == kFp32) {
-        e.a = load_as<i32x4>((const float*)s.data + at);
-        e.b = load_as<i32x4>((const float*)s.data + at + 4);
+        e.a = load_once<i32x4, 4>((const float*)s.data + at);
+        e.b = load_once<i32x4, 4>((const float*)s.data + at + 4);
     } else {
-        e.a = load_as<i32x4>((const uint16_t*)s.data + at);
+        e.a = load_once<i32x4, 2>((const uint16_t*)s.data + at);
     }
-    if constexpr (SRC == kSplit) e.rho = load_as<uint64_t>(s.rho + packed);
-    if (s.rand) e.rand = load_as<uint64_t>(s.rand + packed);
+    if constexpr (SRC == kSplit) e.rho = load_once<uint64_t, 1>(s.rho + packed);
+    if (s.rand) e.rand = load_once<uint64_t, 1>(s.rand + packed);
 }
 template <int SRC>
 __device__ __forceinline__ void unpack(float (&v)[8], const Eight& e) {
@@ -240,7 +246,9 @@ __global__ __launch_bounds__(256) void quantize_rows(Source s, Mx4 out, uint32_t
 // A workgroup handles ROWS by 128 values: the rows as above, and through LDS the columns.  The grid covers rows and columns up to whole
 // segments, so that what lies behind the matrix's end is written as zeros in both layouts.  All loads of a tile are on their way together:
 // where a tile reaches beyond the matrix, its lanes load from its last row, or a row's first values, and drop them.
-// Bound: HBM.  Neighbouring tiles of one column are neighbours on one XCD, whose L2 puts their 32 or 64 bytes of a row of out_t together.
+// Bound: HBM.  An XCD goes through its tiles in bands of 1024 rows, down each column of a band: its L2 then puts the tiles' 16 or 32 bytes of a row of
+// out_t together, and a band's rows of out, 64 bytes from each tile, while they are there.  In us, down whole columns / in bands / and with x read
+// past the caches: 14336 x 4096 split weights from memory 63 / 57 / 54, BF16 55 / 48 / 45, along the rows 66 and 53.
 constexpr int kTileCols = 128;
 
 template <int SRC, bool RANDOM, int ROWS>
@@ -250,7 +258,10 @@ __global__ __launch_bounds__(256) void quantize_both(Source s, Mx4 out, Mx4 out_
     __shared__ Cell tile[ROWS][kTileCols];
     __shared__ uint8_t rands[RANDOM ? ROWS : 1][kTileCols];
     const uint32_t xcd = blockIdx.x % 8, at = xcd * (tiles / 8) + min(xcd, tiles % 8) + blockIdx.x / 8;
-    const uint32_t row0 = at % row_tiles * ROWS, col0 = at / row_tiles * kTileCols;
+    constexpr uint32_t kBand = 1024 / ROWS;
+    const uint32_t col_tiles = tiles / row_tiles, band = at / (kBand * col_tiles), in_band = at - band * kBand * col_tiles;
+    const uint32_t height = min(kBand, row_tiles - band * kBand);
+    const uint32_t row0 = (band * kBand + in_band % height) * ROWS, col0 = in_band / height * kTileCols;
     const uint32_t lane = threadIdx.x % 16, line = threadIdx.x / 16;
     const uint32_t col = col0 + lane * 8;
     const bool ragged = s.cols % 8 != 0 && col0 + kTileCols > s.cols;      // a row ends within some lane's eight values
