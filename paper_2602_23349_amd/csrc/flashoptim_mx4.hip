@@ -21,6 +21,7 @@ namespace {
 using i32x4 = int __attribute__((ext_vector_type(4)));
 using i32x8 = int __attribute__((ext_vector_type(8)));
 using f32x4 = float __attribute__((ext_vector_type(4)));
+using bf16x4 = __bf16 __attribute__((ext_vector_type(4)));
 
 constexpr int kBlock = 32;                  // values that share a scale
 constexpr int kSegment = 256;               // a row of codes is filled up to a multiple of this many values
@@ -419,11 +420,27 @@ __device__ __forceinline__ void store_result4(const Result& c, uint32_t row, uin
         if (left >= 4) store_as(p, v);
         else for (uint32_t i = 0; i < 4; ++i) if (i < left) p[i] = v[i];
     } else {
-        using bf16x4 = __bf16 __attribute__((ext_vector_type(4)));
         const bf16x4 w = __builtin_convertvector(v, bf16x4);
         __bf16* p = (__bf16*)c.data + (int64_t)row * c.stride + col;
         if (left >= 4) store_as(p, w);
         else for (uint32_t i = 0; i < 4; ++i) if (i < left) p[i] = w[i];
+    }
+}
+
+// 16 bytes of a row of c.
+template <bool FP32>
+__device__ __forceinline__ void store_result16(const Result& c, uint32_t row, uint32_t col, i32x4 v) {
+    if (row >= c.rows || col >= c.cols) return;
+    uint8_t* p = (uint8_t*)c.data + ((int64_t)row * c.stride + col) * (FP32 ? 4 : 2);
+    const uint32_t left = c.cols - col;
+    if (left >= (FP32 ? 4 : 8)) {
+        store_as(p, v);
+    } else if constexpr (FP32) {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) if (i < left) ((int*)p)[i] = v[i];
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) if (i < left) ((uint16_t*)p)[i] = (uint16_t)((uint32_t)v[i / 2] >> (16 * (i % 2)));
     }
 }
 
@@ -593,10 +610,17 @@ __device__ __forceinline__ void multiply_turn(const i32x4 (&pw)[TP], const i32x4
 template <bool FP32, int BP, int BQ, int WP, int WQ, int STAGES, int RESIDENT>
 __global__ __launch_bounds__(64 * WP * WQ, RESIDENT) void product_tiles(Mx4 b, Mx4 a, Result c, uint32_t p_tiles, uint32_t q_tiles) {
     constexpr int kWaves = WP * WQ, TP = BP / WP / 32, TQ = BQ / WQ / 32;
-    __shared__ Stage<BP> p_stage[STAGES];
-    __shared__ Stage<BQ> q_stage[STAGES];
-    __shared__ Scales<BP> p_scales[2];
-    __shared__ Scales<BQ> q_scales[2];
+    struct Lds {
+        Stage<BP> p_stage[STAGES];
+        Stage<BQ> q_stage[STAGES];
+        Scales<BP> p_scales[2];
+        Scales<BQ> q_scales[2];
+    };
+    __shared__ __align__(16) Lds lds;
+    auto& p_stage = lds.p_stage;
+    auto& q_stage = lds.q_stage;
+    auto& p_scales = lds.p_scales;
+    auto& q_scales = lds.q_scales;
     // consecutive workgroups run on different XCDs: each XCD takes a stretch of the tiles, in columns of eight, whose rows it then has in its L2
     const uint32_t tiles = p_tiles * q_tiles, xcd = blockIdx.x % 8, at = blockIdx.x / 8;
     const uint32_t tile = xcd * (tiles / 8) + min(xcd, tiles % 8) + at;
@@ -659,14 +683,31 @@ __global__ __launch_bounds__(64 * WP * WQ, RESIDENT) void product_tiles(Mx4 b, M
         multiply_turn<3>(pw[1], qw[1], p_scale, q_scale, acc, behind);
     }
     wait_copies<0>();
+    __builtin_amdgcn_s_barrier();
+    // Out through LDS, 32 rows of c at a time, so that a wavefront's stores are whole pieces of rows: a lane has four neighbouring columns of 32 rows, and
+    // stores of those, 16 bytes of each row, would take the memory pipe as long as the products (8192 x 14336 x 4096: 285 us -> ZZZ).
+    constexpr int kValue = FP32 ? 4 : 2, kRow = BP / WP * kValue, kPitch = kRow + 16, kLanes = kRow / 16, kRows = 64 / kLanes;
+    static_assert(kWaves * 32 * kPitch <= (int)sizeof(Lds), "a slab for each wavefront");
+    uint8_t* const slab = (uint8_t*)&lds + wave * 32 * kPitch;
+    const uint32_t col = p_tile * BP + wave / WQ * (BP / WP) + lane % kLanes * (16 / kValue);
 #pragma unroll
-    for (int i = 0; i < TP; ++i)
+    for (int j = 0; j < TQ; ++j) {
 #pragma unroll
-        for (int j = 0; j < TQ; ++j)
+        for (int i = 0; i < TP; ++i)
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
-                store_result4<FP32>(c, q_tile * BQ + q0 + 32 * j, p_tile * BP + (p0 - lane % 32) + 32 * i + 8 * g + 4 * h,
-                                    f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]});
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+                uint8_t* at = slab + lane % 32 * kPitch + (32 * i + 8 * g + 4 * h) * kValue;
+                if constexpr (FP32) *(f32x4*)at = v;
+                else *(bf16x4*)at = __builtin_convertvector(v, bf16x4);
+            }
+#pragma unroll
+        for (int r = 0; r < 32; r += kRows) {
+            const uint32_t row = q_tile * BQ + wave % WQ * (BQ / WQ) + 32 * j + r + lane / kLanes;
+            const i32x4 v = *(const i32x4*)(slab + (r + lane / kLanes) * kPitch + lane % kLanes * 16);
+            store_result16<FP32>(c, row, col, v);
+        }
+    }
 }
 
 // ------------------------------------------------------------------------------------------- linear, for single tokens --

@@ -42,54 +42,52 @@ Rows to_dev(const flashoptim_matrix* m) { return m ? Rows{(char*)m->data, m->row
 // Eight values as they lie in memory, so that loads can be issued well ahead of their first use.  `fp32` is a constant for the matrices and the
 // same for all lanes for the weights.
 struct Raw {
-    i32x4 a, b;      // BF16: b unused
+    i32x4 a, b;      // BF16: all in a
 };
-// The eight neighbouring columns that a lane loads, and which of them, first .. last - 1, are its own.  Every lane loads eight that exist: the
-// last one of a ragged row the row's last eight, some of which are its neighbour's; those behind it the same, none of them theirs.  So a
-// load is never a case distinction, which would wait for each of its loads before the next.  (Rows of fewer than eight: lane 0 alone,
-// one by one.)
+// The eight neighbouring columns that a lane loads, and which of them, from `first` on, are its own.  Every lane loads eight that exist: the last
+// one of a ragged row the row's last eight, some of which are its neighbour's; those behind it the same, none of them theirs.  So a load is
+// never a case distinction, at whose end the compiler has each wait for its data before the next is made (as such: 100 rows of 768,
+// backward, 11.5 us of kernel time, without YYY).  Rows of fewer than eight columns have kernels of their own (NARROW), in which lane 0 takes them
+// one by one.
+template <bool NARROW>
 struct Place {
     int col, first, last;
     __device__ __forceinline__ Place() = default;
     __device__ __forceinline__ Place(int at, int cols) {
-        col = cols < 8 ? 0 : min(at, cols - 8);
+        col = NARROW ? 0 : min(at, cols - 8);
         first = min(at - col, 8);
-        last = cols < 8 ? cols : 8;
+        last = NARROW ? cols : 8;
     }
-    __device__ __forceinline__ bool whole() const { return first == 0 && last == 8; }
-    __device__ __forceinline__ bool has(int i) const { return i >= first && i < last; }
+    __device__ __forceinline__ bool whole() const { return !NARROW && first == 0; }
     __device__ __forceinline__ f32x8 mask(f32x8 v) const {
         if (!whole()) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = has(i) ? v[i] : 0.0f;
+            for (int i = 0; i < 8; ++i) v[i] = i >= first && i < last ? v[i] : 0.0f;
         }
         return v;
     }
 };
 
 // `row`: where the row begins, in values.
-__device__ __forceinline__ Raw load8(const void* p, bool fp32, int64_t row, const Place& at) {
+template <bool NARROW>
+__device__ __forceinline__ Raw load8(const void* p, bool fp32, int64_t row, const Place<NARROW>& at) {
     Raw r = {};
-    if (fp32) {
-        const int* f = (const int*)p + row + at.col;
-        if (at.last == 8) {
-            r.a = load_as<i32x4>(f);
-            r.b = load_as<i32x4>(f + 4);
-        } else {
+    if constexpr (NARROW) {
+        uint32_t w[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                r.a[i] = f[min(i, at.last - 1)];
-                r.b[i] = f[min(i + 4, at.last - 1)];
-            }
+        for (int i = 0; i < 8; ++i) {
+            const int64_t from = row + min(i, at.last - 1);
+            w[i] = fp32 ? ((const uint32_t*)p)[from] : (uint32_t)((const uint16_t*)p)[from];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (fp32) { if (i < 4) r.a[i] = (int)w[i]; else r.b[i - 4] = (int)w[i]; }
+            else r.a[i / 2] |= (int)(w[i] << (16 * (i % 2)));
         }
     } else {
-        const uint16_t* f = (const uint16_t*)p + row + at.col;
-        if (at.last == 8) {
-            r.a = load_as<i32x4>(f);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) r.a[i / 2] |= (int)((uint32_t)f[min(i, at.last - 1)] << (16 * (i % 2)));
-        }
+        const char* f = (const char*)p + (row + at.col) * (fp32 ? 4 : 2);
+        r.a = load_as<i32x4>(f);
+        r.b = load_as<i32x4>(f + (fp32 ? 16 : 0));      // (of BF16 matrices, where fp32 is a constant, left out)
     }
     return r;
 }
@@ -107,7 +105,8 @@ __device__ __forceinline__ f32x8 values(const Raw& r, bool fp32) {
     }
     return v;
 }
-__device__ __forceinline__ void store8(void* p, bool fp32, int64_t row, const Place& at, f32x8 v) {
+template <bool NARROW>
+__device__ __forceinline__ void store8(void* p, bool fp32, int64_t row, const Place<NARROW>& at, f32x8 v) {
     if (fp32) {
         float* f = (float*)p + row + at.col;
         if (at.whole()) {
@@ -115,7 +114,7 @@ __device__ __forceinline__ void store8(void* p, bool fp32, int64_t row, const Pl
             store_as(f + 4, f32x4{v[4], v[5], v[6], v[7]});
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) if (at.has(i)) f[i] = v[i];
+            for (int i = 0; i < 8; ++i) if (i >= at.first && i < at.last) f[i] = v[i];
         }
     } else {
         __bf16* f = (__bf16*)p + row + at.col;
@@ -123,7 +122,7 @@ __device__ __forceinline__ void store8(void* p, bool fp32, int64_t row, const Pl
         if (at.whole()) store_as(f, w);
         else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) if (at.has(i)) f[i] = w[i];
+            for (int i = 0; i < 8; ++i) if (i >= at.first && i < at.last) f[i] = w[i];
         }
     }
 }
@@ -168,10 +167,15 @@ struct RowSums {
     }
 };
 
+// Has a kernel's arguments in scalar registers from here on.  Left to itself the compiler loads each where a path first needs it, one wait after the
+// other: a dozen of them ahead of the first row.
+#define FO_ROWS(r) "s"((r).data), "s"((r).stride)
+
 // Rows that a workgroup handles side by side: where a wavefront has a row to itself, four (they need no barrier).
 constexpr int lines_of(int lanes) { return lanes == 64 ? 4 : 1; }
 
-__device__ __forceinline__ float sigmoid(float v) { return 1.0f / (1.0f + __expf(-v)); }
+// (The hardware's exponential and reciprocal, within a few units of the last place, where the sums around it are off by dozens.)
+__device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -0x1.715476p+0f)); }
 
 struct NormArgs {
     Rows x, f, gate, h, y;
@@ -184,8 +188,8 @@ struct NormArgs {
 };
 
 // Mean and 1/sqrt(mean square distance + eps) of the row whose values the lanes have (0 where a lane has none).
-template <int LANES, int CHUNKS>
-__device__ __forceinline__ void moments(RowSums<LANES>& sums, const f32x8 (&v)[CHUNKS], const Place (&at)[CHUNKS], const NormArgs& a, float* mean,
+template <int LANES, int CHUNKS, bool NARROW>
+__device__ __forceinline__ void moments(RowSums<LANES>& sums, const f32x8 (&v)[CHUNKS], const Place<NARROW> (&at)[CHUNKS], const NormArgs& a, float* mean,
                                         float* rstd) {
     *mean = 0.0f;
     if (a.layer) {
@@ -209,7 +213,8 @@ __device__ __forceinline__ void moments(RowSums<LANES>& sums, const f32x8 (&v)[C
 template <int CHUNKS>
 struct Params {
     Raw weight[CHUNKS], bias[CHUNKS];
-    __device__ __forceinline__ void load(const void* w, const void* b, bool fp32, const Place (&at)[CHUNKS]) {
+    template <bool NARROW>
+    __device__ __forceinline__ void load(const void* w, const void* b, bool fp32, const Place<NARROW> (&at)[CHUNKS]) {
 #pragma unroll
         for (int j = 0; j < CHUNKS; ++j) {
             if (w) weight[j] = load8(w, fp32, 0, at[j]);
@@ -230,7 +235,7 @@ __device__ __forceinline__ void affine(f32x8 (&v)[CHUNKS], const Params<CHUNKS>&
 
 // LANES lanes to a row, each CHUNKS times eight neighbouring values.  All that a row reads is asked for at once: a single row, whose time is
 // latency, waits for memory once.
-template <bool STREAM_FP32, bool BRANCH_FP32, int LANES, int CHUNKS>
+template <bool STREAM_FP32, bool BRANCH_FP32, int LANES, int CHUNKS, bool NARROW>
 __global__ __launch_bounds__(LANES * lines_of(LANES)) void norm_rows(NormArgs a) {
     constexpr int kLines = lines_of(LANES);
     __shared__ f32x4 part[2 * (LANES / 64)];
@@ -238,12 +243,12 @@ __global__ __launch_bounds__(LANES * lines_of(LANES)) void norm_rows(NormArgs a)
     const int lane = threadIdx.x % LANES;
     if (kLines > 1 && row >= a.rows) return;
     RowSums<LANES> sums = {part, 0};
-    Place at[CHUNKS];
+    Place<NARROW> at[CHUNKS];
     Raw x[CHUNKS], f[CHUNKS], gate[CHUNKS];
     Params<CHUNKS> post, pre;
 #pragma unroll
     for (int j = 0; j < CHUNKS; ++j) {
-        at[j] = Place((j * LANES + lane) * 8, a.cols);
+        at[j] = Place<NARROW>((j * LANES + lane) * 8, a.cols);
         if (a.f.data) f[j] = load8(a.f.data, BRANCH_FP32, (int64_t)row * a.f.stride, at[j]);
         x[j] = load8(a.x.data, STREAM_FP32, (int64_t)row * a.x.stride, at[j]);
         if (a.gate.data) gate[j] = load8(a.gate.data, BRANCH_FP32, (int64_t)(row / a.rows_per_gate) * a.gate.stride, at[j]);
@@ -318,17 +323,20 @@ struct RowData {
     float post_mean, post_rstd, pre_mean, pre_rstd;
 };
 
-template <bool STREAM_FP32, bool BRANCH_FP32, int LANES, int CHUNKS, bool LAYER, bool BRANCH>
+template <bool STREAM_FP32, bool BRANCH_FP32, int LANES, int CHUNKS, bool NARROW, bool LAYER, bool BRANCH>
 __global__ __launch_bounds__(LANES * lines_of(LANES)) void norm_gradients(GradArgs a) {
     constexpr int kLines = lines_of(LANES);
     __shared__ f32x4 part_sums[2 * (LANES / 64)];
     __shared__ float joined[kLines > 1 ? kLines : 1][kLines > 1 ? LANES * 8 * CHUNKS : 1];
+    asm volatile("" ::FO_ROWS(a.h), FO_ROWS(a.f), FO_ROWS(a.gate), FO_ROWS(a.dy), FO_ROWS(a.dh), FO_ROWS(a.dx), FO_ROWS(a.df), "s"(a.post_weight),
+                 "s"(a.post_bias), "s"(a.pre_weight), "s"(a.stats), "s"(a.rows), "s"(a.rows_per_gate), "s"(a.unit_rows), "s"(a.part_units),
+                 "s"(a.units_per_group), "s"(a.parts_per_group), "s"(a.cols), "s"(a.residual_scale));
     const int line = kLines > 1 ? threadIdx.x / LANES : 0, lane = threadIdx.x % LANES;
     RowSums<LANES> sums = {part_sums, 0};
-    Place at[CHUNKS];
+    Place<NARROW> at[CHUNKS];
 #pragma unroll
     for (int j = 0; j < CHUNKS; ++j) {
-        at[j] = Place((j * LANES + lane) * 8, a.cols);
+        at[j] = Place<NARROW>((j * LANES + lane) * 8, a.cols);
     }
     Params<CHUNKS> post, pre;
     pre.load(a.pre_weight, nullptr, a.param_fp32, at);
@@ -504,7 +512,7 @@ struct PartSums {
     int32_t cols;
 };
 
-// A wavefront of the 16 adds up every 16th part, eight loads on their way at a time.
+// A wavefront of the 16 adds up every 16th part, sixteen loads on their way at a time.
 constexpr int kSumWaves = 16;
 __global__ __launch_bounds__(64 * kSumWaves) void sum_parts(PartSums p) {
     __shared__ float joined[kSumWaves][64];
@@ -514,12 +522,12 @@ __global__ __launch_bounds__(64 * kSumWaves) void sum_parts(PartSums p) {
         float v = 0.0f;
         if (col < p.cols) {
             const float* at = s.part + ((int64_t)group * s.parts) * p.cols + col;
-            for (uint32_t i = wave; i < s.parts; i += 8 * kSumWaves) {
-                float w[8];
+            for (uint32_t i = wave; i < s.parts; i += 16 * kSumWaves) {
+                float w[16];
 #pragma unroll
-                for (uint32_t j = 0; j < 8; ++j) w[j] = i + j * kSumWaves < s.parts ? at[(int64_t)(i + j * kSumWaves) * p.cols] : 0.0f;
+                for (uint32_t j = 0; j < 16; ++j) w[j] = i + j * kSumWaves < s.parts ? at[(int64_t)(i + j * kSumWaves) * p.cols] : 0.0f;
 #pragma unroll
-                for (uint32_t j = 0; j < 8; ++j) v += w[j];
+                for (uint32_t j = 0; j < 16; ++j) v += w[j];
             }
         }
         __syncthreads();
@@ -576,13 +584,17 @@ int check_gate(const flashoptim_matrix* gate, int64_t rows, int64_t cols, int dt
 }
 
 // Calls launch(lanes, chunks) as integral constants with the shape for rows of this many values.
-template <int LANES, int CHUNKS>
-struct Shape { static constexpr int kLanes = LANES, kChunks = CHUNKS; };
+template <int LANES, int CHUNKS, bool NARROW = false>
+struct Shape {
+    static constexpr int kLanes = LANES, kChunks = CHUNKS;
+    static constexpr bool kNarrow = NARROW;
+};
 // Eight values to a lane as far as 512 lanes reach.  The backward pass keeps up to five sums a value, for which 1024 lanes, of 128 registers each,
 // have no room: it takes 512 lanes with 16 or 32 values.
 template <typename F>
 void with_shape(int64_t cols, F launch) {
-    if (cols <= 512) launch(Shape<64, 1>{});
+    if (cols < 8) launch(Shape<64, 1, true>{});
+    else if (cols <= 512) launch(Shape<64, 1>{});
     else if (cols <= 1024) launch(Shape<128, 1>{});
     else if (cols <= 2048) launch(Shape<256, 1>{});
     else if (cols <= 4096) launch(Shape<512, 1>{});
@@ -661,10 +673,11 @@ int flashoptim_block_norm(const flashoptim_block_norm_spec* spec, const flashopt
     const bool sf = x->dtype == FLASHOPTIM_FP32, bf = branch_type == FLASHOPTIM_FP32;
     with_shape(spec->cols, [&](auto shape) {
         constexpr int L = decltype(shape)::kLanes, C = decltype(shape)::kChunks, T = L * lines_of(L);
+        constexpr bool N = decltype(shape)::kNarrow;
         const dim3 grid((unsigned)up(rows, T / L)), block(T);
-        if (bf) hipLaunchKernelGGL((norm_rows<true, true, L, C>), grid, block, 0, (hipStream_t)stream, a);
-        else if (sf) hipLaunchKernelGGL((norm_rows<true, false, L, C>), grid, block, 0, (hipStream_t)stream, a);
-        else hipLaunchKernelGGL((norm_rows<false, false, L, C>), grid, block, 0, (hipStream_t)stream, a);
+        if (bf) hipLaunchKernelGGL((norm_rows<true, true, L, C, N>), grid, block, 0, (hipStream_t)stream, a);
+        else if (sf) hipLaunchKernelGGL((norm_rows<true, false, L, C, N>), grid, block, 0, (hipStream_t)stream, a);
+        else hipLaunchKernelGGL((norm_rows<false, false, L, C, N>), grid, block, 0, (hipStream_t)stream, a);
     });
     return fo::hip_status(hipGetLastError());
 }
@@ -746,12 +759,13 @@ int flashoptim_block_norm_backward(const flashoptim_block_norm_spec* spec, const
         const bool sf = h->dtype == FLASHOPTIM_FP32, bf = branch_type == FLASHOPTIM_FP32;
         with_shape(cols, [&](auto shape) {
             constexpr int L = decltype(shape)::kLanes, C = decltype(shape)::kChunks, T = L * lines_of(L);
+        constexpr bool N = decltype(shape)::kNarrow;
             const dim3 grid((unsigned)c.parts), block(T);
             auto launch = [&](auto layer_c, auto branch_c) {
                 constexpr bool LN = decltype(layer_c)::value, BR = decltype(branch_c)::value;
-                if (bf) hipLaunchKernelGGL((norm_gradients<true, true, L, C, LN, BR>), grid, block, 0, (hipStream_t)stream, a);
-                else if (sf) hipLaunchKernelGGL((norm_gradients<true, false, L, C, LN, BR>), grid, block, 0, (hipStream_t)stream, a);
-                else hipLaunchKernelGGL((norm_gradients<false, false, L, C, LN, BR>), grid, block, 0, (hipStream_t)stream, a);
+                if (bf) hipLaunchKernelGGL((norm_gradients<true, true, L, C, N, LN, BR>), grid, block, 0, (hipStream_t)stream, a);
+                else if (sf) hipLaunchKernelGGL((norm_gradients<true, false, L, C, N, LN, BR>), grid, block, 0, (hipStream_t)stream, a);
+                else hipLaunchKernelGGL((norm_gradients<false, false, L, C, N, LN, BR>), grid, block, 0, (hipStream_t)stream, a);
             };
             using Yes = std::true_type;
             using No = std::false_type;
