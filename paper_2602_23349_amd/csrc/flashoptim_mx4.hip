@@ -685,7 +685,7 @@ __global__ __launch_bounds__(64 * WP * WQ, RESIDENT) void product_tiles(Mx4 b, M
     wait_copies<0>();
     __builtin_amdgcn_s_barrier();
     // Out through LDS, 32 rows of c at a time, so that a wavefront's stores are whole pieces of rows: a lane has four neighbouring columns of 32 rows, and
-    // stores of those, 16 bytes of each row, would take the memory pipe as long as the products (8192 x 14336 x 4096: 285 us -> ZZZ).
+    // stores of those, 16 bytes of each row, would take the memory pipe as long as the products (8192 x 14336 x 4096: 285 us, and 230 so).
     constexpr int kValue = FP32 ? 4 : 2, kRow = BP / WP * kValue, kPitch = kRow + 16, kLanes = kRow / 16, kRows = 64 / kLanes;
     static_assert(kWaves * 32 * kPitch <= (int)sizeof(Lds), "a slab for each wavefront");
     uint8_t* const slab = (uint8_t*)&lds + wave * 32 * kPitch;
@@ -726,6 +726,26 @@ struct Few {
     uint32_t units_magic;                  // item / units = the upper half of item times this, for all items there can be
 };
 
+// The last `left` of eight values in the place of the first, 0 behind them; all 0 for left <= 0.
+__device__ __forceinline__ void move_down(float (&v)[8], int left) {
+    const int by = left > 0 ? 8 - left : 8;
+#pragma unroll
+    for (int step = 8; step >= 1; step /= 2)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = by & step ? (i + step < 8 ? v[i + step] : 0.0f) : v[i];
+}
+__device__ __forceinline__ i32x4 move_down(i32x4 w, int left) {
+    const int by = left > 0 ? 8 - left : 8;
+    if (by & 8) w = i32x4{};
+    if (by & 4) w = i32x4{w[2], w[3], 0, 0};
+    if (by & 2) w = i32x4{w[1], w[2], w[3], 0};
+    if (by & 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = (int)((uint32_t)w[i] >> 16 | (i < 3 ? (uint32_t)w[i + 1] << 16 : 0u));
+    }
+    return w;
+}
+
 template <int SRC, bool FP32, int WAVES, int TILES>
 __global__ __launch_bounds__(64 * WAVES) void linear_small(Few a) {
     extern __shared__ __align__(16) uint8_t lds[];
@@ -764,15 +784,16 @@ __global__ __launch_bounds__(64 * WAVES) void linear_small(Few a) {
         if (unit % 4 == 0) x_scales[row * a.scale_pitch + unit / 4] = (uint8_t)byte;
     };
     // The first units of x are asked for ahead of the weights: they come back in this order, and are quantised while the weights are on their way.
-    // No load is made by a case distinction, which would wait for it: a unit behind the row's end loads the row's first values.
+    // No load is made by a case distinction, which would wait for it: a unit that the row ends in, or before, loads the row's last eight values, which
+    // are then moved down to where they belong.
     auto quantize = [&](auto batch) {
         constexpr int kBatch = decltype(batch)::value, kWords = SRC == kFp32 ? 2 : 1;
         i32x4 raw[kBatch][kWords];
         auto ask = [&](uint32_t at) {
 #pragma unroll
             for (int j = 0; j < kBatch; ++j) {
-                const uint32_t item = min(at + j * 64 * WAVES, total - 1), row = __umulhi(item, a.units_magic), col = (item - row * units) * 8;
-                const int64_t from = (int64_t)row * a.x.stride + (col < a.x.cols ? col : 0);
+                const uint32_t item = min(at + j * 64 * WAVES, total - 1), row = __umulhi(item, a.units_magic);
+                const int64_t from = (int64_t)row * a.x.stride + min((item - row * units) * 8, a.x.cols - 8);
 #pragma unroll
                 for (int i = 0; i < kWords; ++i) raw[j][i] = load_as<i32x4>((const uint8_t*)a.x.data + from * (SRC == kFp32 ? 4 : 2) + 16 * i);
             }
@@ -785,20 +806,23 @@ __global__ __launch_bounds__(64 * WAVES) void linear_small(Few a) {
             for (int j = 0; j < kBatch; ++j) {
                 const uint32_t item = at + j * 64 * WAVES, row = __umulhi(item, a.units_magic), unit = item - row * units;
                 if (item >= total) continue;
+                const int left = (int)a.x.cols - (int)unit * 8;
                 uint32_t byte, c;
                 if constexpr (SRC == kFp32) {
                     float v[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = unit * 8 < a.x.cols ? __int_as_float(raw[j][i / 4][i % 4]) : 0.0f;
+                    for (int i = 0; i < 8; ++i) v[i] = __int_as_float(raw[j][i / 4][i % 4]);
+                    if (left < 8) move_down(v, left);
                     c = quad_codes<false>(v, 0, &byte);
                 } else {
-                    c = quad_codes_bf16(unit * 8 < a.x.cols ? raw[j][0] : i32x4{}, &byte);
+                    if (left < 8) raw[j][0] = move_down(raw[j][0], left);
+                    c = quad_codes_bf16(raw[j][0], &byte);
                 }
                 store(c, byte, row, unit);
             }
         }
     };
-    if (a.x.cols % 8 == 0) {
+    if (a.x.cols >= 8) {
         if (total <= 64 * WAVES) quantize(std::integral_constant<int, 1>{});
         else quantize(std::integral_constant<int, 4>{});
     } else {
@@ -924,8 +948,7 @@ void with_waves(int64_t segments, F launch) {
 // Sums split over workgroups and joined by another launch: 768 x 768 x 8000 in two 13.5, in four 16.2.
 enum Shape { kTiny, kTile64, kTile128, kTile256 };
 Shape product_shape(int64_t m, int64_t n, int64_t k) {
-    if (m <= 16 || n <= 16 || k > kMaxTiledTerms) return kTiny;
-    if (up(m, 16) * up(n, 16) <= 256) return kTiny;
+    if (k > kMaxTiledTerms || up(m, 16) * up(n, 16) <= 256) return kTiny;
     if (up(m, 256) * up(n, 256) >= 192) return kTile256;
     return m > 64 && n > 64 && up(m, 64) * up(n, 64) > 512 ? kTile128 : kTile64;
 }
@@ -963,18 +986,38 @@ int product(const flashoptim_mx4& a, const flashoptim_mx4& b, const flashoptim_m
     return fo::hip_status(hipGetLastError());
 }
 
-// Whether x is quantised by every workgroup of linear_small, or once by a launch of its own: by the number of values, filled up to whole segments.
-// One launch / two, us: 4096 x 4096 (n, k) with 1 row 4.4 / 6.2, 8 rows 6.1 / 7.0, 16 rows 8.0 / 7.4; 4096 x 14336 4 rows 11.4 / 12.5, 8 rows 14.3 / 13.8;
-// 8192 x 2048 16 rows 6.1 / 7.4.
-constexpr int64_t kFewRows = 16, kFewValues = 57344;
+constexpr int64_t kFewRows = 16;
+
+// How linear_small goes about it: tiles of 16 columns to a workgroup, and wavefronts.  In us:
+//   two tiles where one each would be more than one workgroup for each compute unit: 6000 x 6000 (n, k), 375 tiles, 1 row 8.4 with one, 8.0 with two, 16
+//     rows 17.6, 12.5; 14336 x 4096 1 row 10.2, 9.2, 8 rows 14.1, 11.8; 8192 x 2048 1 row 4.4, 4.6, 16 rows 7.0, 6.2;
+//   16 wavefronts where there is no more than one workgroup for each compute unit, and many segments or rows: 4096 x 4096 with 8 / 16, 1 row 4.3 / 4.5, 16 rows
+//     8.0 / 6.9; 6000 x 6000 as above 8.4 / 8.0 and 14.4 / 12.5; 14336 x 4096 9.2 / 11.4;
+//   4 for up to four segments and few rows: 12000 x 500 with 4 / 8, 1 row 3.9 / 4.0, 16 rows 4.8 / 4.4.
+struct FewPlan {
+    int tiles, waves;
+    int64_t workgroups;
+};
+FewPlan plan_few(int64_t m, int64_t n, int64_t k) {
+    const int64_t tiles = up(n, 16), segments = up(k, kSegment);
+    FewPlan p = {tiles > 256 ? 2 : 1, 8, 0};
+    p.workgroups = up(tiles, p.tiles);
+    if (segments <= 4) p.waves = m >= 8 ? 8 : 4;
+    else if (p.workgroups <= 256 && (m >= 4 || segments > 16)) p.waves = 16;
+    return p;
+}
+// Whether x is quantised by every workgroup of linear_small, or once by a launch of its own: by the work on x that a compute unit then has.  One launch /
+// two, us: 4096 x 4096 with 1 row 4.4 / 6.5, 16 rows 6.9 / 7.8; 4096 x 14336 4 rows 11.4 / 12.2, 8 rows 14.3 / 13.5; 14336 x 4096 8 rows 11.8 / 11.3, 16 rows
+// 15.0 / 11.3; 6000 x 6000 16 rows 12.5 / 13.6.
+constexpr int64_t kFewValues = 98304;
 
 // What linear_small keeps of x in LDS: rows of codes begin 16 bytes apart in the banks.
 int64_t few_code_pitch(int64_t k) { return up(k, kSegment) * kSegmentBytes + 16; }
 int64_t few_scale_pitch(int64_t k) { return up(k, kSegment) * 8 + 8; }
-// Exact for items and units below 2^16 (there are at most 2^13 units of eight).
+// Exact for items and units below 2^16 (there are at most 12288 units of eight).
 uint32_t few_units_magic(int64_t k) { return (uint32_t)(((uint64_t)1 << 32) / (uint64_t)(up(k, kSegment) * (kSegment / 8)) + 1); }
 bool takes_few_rows(int64_t m, int64_t n, int64_t k) {
-    return m >= 1 && m <= kFewRows && n >= 1 && k >= 1 && m * up(k, kSegment) * kSegment <= kFewValues;
+    return m >= 1 && m <= kFewRows && n >= 1 && k >= 1 && m * up(k, kSegment) * kSegment * up(plan_few(m, n, k).workgroups, 256) <= kFewValues;
 }
 
 int linear_few_rows(const flashoptim_matrix& x, const flashoptim_mx4& w, const flashoptim_matrix& y, hipStream_t stream) {
@@ -982,21 +1025,22 @@ int linear_few_rows(const flashoptim_matrix& x, const flashoptim_mx4& w, const f
                    (uint32_t)few_code_pitch(x.cols), (uint32_t)few_scale_pitch(x.cols), few_units_magic(x.cols)};
     const bool fp32 = y.dtype == FLASHOPTIM_FP32, x_fp32 = x.dtype == FLASHOPTIM_FP32;
     const int64_t x_bytes = x.rows * (few_code_pitch(x.cols) + few_scale_pitch(x.cols));
-    with_waves(up(x.cols, kSegment), [&](auto waves) {
-        auto launch = [&](auto tiles) {
-            constexpr int W = decltype(waves)::value, T = decltype(tiles)::value;
-            const int64_t part_bytes = W * T * 1024;
-            const dim3 grid((unsigned)up(y.cols, 16 * T));
-            const unsigned bytes = (unsigned)(x_bytes > part_bytes ? x_bytes : part_bytes);
-            auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * W), bytes, stream, a); };
-            if (x_fp32) { if (fp32) go(linear_small<kFp32, true, W, T>); else go(linear_small<kFp32, false, W, T>); }
-            else { if (fp32) go(linear_small<kBf16, true, W, T>); else go(linear_small<kBf16, false, W, T>); }
-        };
-        // two tiles to a workgroup, which halves the work on x, where that leaves one for every compute unit (14336 x 4096: 1 row 9.2 us, with two 9.6; 8
-        // rows 13.3, 11.7)
-        if (x.rows < 4 || up(y.cols, 16) < 512) launch(std::integral_constant<int, 1>{});
-        else launch(std::integral_constant<int, 2>{});
-    });
+    const FewPlan p = plan_few(x.rows, y.cols, x.cols);
+    auto launch = [&](auto waves, auto tiles) {
+        constexpr int W = decltype(waves)::value, T = decltype(tiles)::value;
+        const int64_t part_bytes = W * T * 1024;
+        const unsigned bytes = (unsigned)(x_bytes > part_bytes ? x_bytes : part_bytes);
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)p.workgroups), dim3(64 * W), bytes, stream, a); };
+        if (x_fp32) { if (fp32) go(linear_small<kFp32, true, W, T>); else go(linear_small<kFp32, false, W, T>); }
+        else { if (fp32) go(linear_small<kBf16, true, W, T>); else go(linear_small<kBf16, false, W, T>); }
+    };
+    auto with_tiles = [&](auto waves) {
+        if (p.tiles == 1) launch(waves, std::integral_constant<int, 1>{});
+        else launch(waves, std::integral_constant<int, 2>{});
+    };
+    if (p.waves == 4) with_tiles(std::integral_constant<int, 4>{});
+    else if (p.waves == 8) with_tiles(std::integral_constant<int, 8>{});
+    else with_tiles(std::integral_constant<int, 16>{});
     return fo::hip_status(hipGetLastError());
 }
 
