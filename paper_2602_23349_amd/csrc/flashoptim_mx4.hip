@@ -532,6 +532,13 @@ __device__ __forceinline__ void wait_copies() {
     __builtin_amdgcn_s_waitcnt((VM & 15) | (VM >> 4) << 14 | 0x0070);
 }
 
+// A barrier for what lies in LDS, which the waits around it have settled: the compiler, which does not know of the copies, moves no access across.
+__device__ __forceinline__ void meet() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 // What a wavefront copies of ROWS rows: the lane's places in them.  Behind the matrix's last row a copy takes that row again.
 template <int ROWS, int WAVES>
 struct Copier {
@@ -668,7 +675,7 @@ __global__ __launch_bounds__(64 * WP * WQ, RESIDENT) void product_tiles(Products
     for (uint32_t t = 0; t < steps; ++t) {
         // this wavefront's copies for step t have landed; behind the barrier all have, and nobody reads the stage of step t - 1 any more
         wait_copies<(STAGES - 2) * kCopies>();
-        __builtin_amdgcn_s_barrier();
+        meet();
         const uint32_t group = t / kScaleSteps, in_group = t % kScaleSteps, next = t + STAGES - 1;
         if (in_group == 0) {
             p_copy.copy_scales(p_scales[group % 2 ^ 1], group + 1, t + kScaleSteps < steps);
@@ -700,7 +707,7 @@ __global__ __launch_bounds__(64 * WP * WQ, RESIDENT) void product_tiles(Products
         multiply_turn<3>(pw[1], qw[1], p_scale, q_scale, acc, behind);
     }
     wait_copies<0>();
-    __builtin_amdgcn_s_barrier();
+    meet();
     // Out through LDS, 32 rows of c at a time, so that a wavefront's stores are whole pieces of rows: a lane has four neighbouring columns of 32 rows, and
     // stores of those, 16 bytes of each row, would take the memory pipe as long as the products (8192 x 14336 x 4096: 285 us, and 230 so).
     constexpr int kValue = FP32 ? 4 : 2, kRow = BP / WP * kValue, kPitch = kRow + 16, kLanes = kRow / 16, kRows = 64 / kLanes;

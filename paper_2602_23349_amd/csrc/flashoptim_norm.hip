@@ -338,10 +338,20 @@ __global__ __launch_bounds__(LANES * lines_of(LANES)) void norm_gradients(GradAr
     for (int j = 0; j < CHUNKS; ++j) {
         at[j] = Place<NARROW>((j * LANES + lane) * 8, a.cols);
     }
-    Params<CHUNKS> post, pre;
-    pre.load(a.pre_weight, nullptr, a.param_fp32, at);
-    if constexpr (BRANCH) post.load(a.post_weight, a.post_bias, a.param_fp32, at);
-    auto load = [&](RowData<CHUNKS>& d, uint32_t row) {
+    // What a row reads is held from its loads on, and the next row's with it.  Of rows of more than 4096 values that takes more registers than there
+    // are, by what they hold: their weights, then all that is theirs, are read again where they are needed, from the L2.  us with all of it held
+    // (spilled), the weights read again, all read again, for 4096 rows of 8192 of a branch: RMS in BF16 98, 126, 100; RMS on an FP32 stream 239, 159,
+    // 193; layer in BF16 266, 138, 188; layer on an FP32 stream 609, 234, 202; 2000 rows of 12000, RMS in BF16: 1120, -, 179.
+    constexpr bool kNarrow = CHUNKS == 1 || (CHUNKS == 2 && !BRANCH);
+    constexpr bool kHold = kNarrow || (CHUNKS == 2 && (LAYER ? !STREAM_FP32 : !BRANCH_FP32));
+    constexpr bool kHoldParams = kNarrow || (CHUNKS == 2 && !LAYER && !STREAM_FP32);
+    Params<kHoldParams ? CHUNKS : 1> post, pre;
+    if constexpr (kHoldParams) {
+        pre.load(a.pre_weight, nullptr, a.param_fp32, at);
+        if constexpr (BRANCH) post.load(a.post_weight, a.post_bias, a.param_fp32, at);
+    }
+    RowData<kHold ? CHUNKS : 1> d, next;
+    auto load = [&](RowData<kHold ? CHUNKS : 1>& d, uint32_t row) {
         const int64_t rows = a.rows;
         if (a.dy.data) {
             d.pre_mean = a.stats[2 * rows + row];
@@ -351,26 +361,35 @@ __global__ __launch_bounds__(LANES * lines_of(LANES)) void norm_gradients(GradAr
             d.post_mean = a.stats[row];
             d.post_rstd = a.stats[rows + row];
         }
+        if constexpr (kHold) {
 #pragma unroll
-        for (int j = 0; j < CHUNKS; ++j) {
-            if (a.dy.data) {
-                d.h[j] = load8(a.h.data, STREAM_FP32, (int64_t)row * a.h.stride, at[j]);
-                d.dy[j] = load8(a.dy.data, BRANCH_FP32, (int64_t)row * a.dy.stride, at[j]);
-            }
-            if (a.dh.data) d.dh[j] = load8(a.dh.data, STREAM_FP32, (int64_t)row * a.dh.stride, at[j]);
-            if constexpr (BRANCH) {
-                d.f[j] = load8(a.f.data, BRANCH_FP32, (int64_t)row * a.f.stride, at[j]);
-                if (a.gate.data) d.gate[j] = load8(a.gate.data, BRANCH_FP32, (int64_t)(row / a.rows_per_gate) * a.gate.stride, at[j]);
+            for (int j = 0; j < CHUNKS; ++j) {
+                if (a.dy.data) {
+                    d.h[j] = load8(a.h.data, STREAM_FP32, (int64_t)row * a.h.stride, at[j]);
+                    d.dy[j] = load8(a.dy.data, BRANCH_FP32, (int64_t)row * a.dy.stride, at[j]);
+                }
+                if (a.dh.data) d.dh[j] = load8(a.dh.data, STREAM_FP32, (int64_t)row * a.dh.stride, at[j]);
+                if constexpr (BRANCH) {
+                    d.f[j] = load8(a.f.data, BRANCH_FP32, (int64_t)row * a.f.stride, at[j]);
+                    if (a.gate.data) d.gate[j] = load8(a.gate.data, BRANCH_FP32, (int64_t)(row / a.rows_per_gate) * a.gate.stride, at[j]);
+                }
             }
         }
+    };
+    // Chunk j of matrix m, held as `held`, of row `row`; and of a weight or bias.
+    auto chunk = [&](const Rows& m, const Raw* held, bool fp32, uint32_t row, int j) {
+        if constexpr (kHold) return values(held[j], fp32);
+        else return values(load8(m.data, fp32, (int64_t)row * m.stride, at[j]), fp32);
+    };
+    auto param = [&](const void* p, const Raw* held, int j) {
+        if constexpr (kHoldParams) return values(held[j], a.param_fp32);
+        else return values(load8(p, a.param_fp32, 0, at[j]), a.param_fp32);
     };
     f32x8 acc[kSums][CHUNKS] = {};
     const uint32_t group = blockIdx.x / a.parts_per_group, in_group = blockIdx.x - group * a.parts_per_group;
     const uint32_t begin = group * a.units_per_group + in_group * a.part_units;
     const uint32_t end = min(begin + a.part_units, min((group + 1) * a.units_per_group, (a.rows + a.unit_rows - 1) / a.unit_rows));
     uint32_t unit = begin + line, row = unit * a.unit_rows;
-    constexpr bool kAhead = CHUNKS < 4;      // (the widest rows leave no registers for it)
-    RowData<CHUNKS> d, next;
     if (unit < end) load(d, row);
     while (unit < end) {
         // the next row is on its way while this one goes through its sums
@@ -379,50 +398,58 @@ __global__ __launch_bounds__(LANES * lines_of(LANES)) void norm_gradients(GradAr
             next_unit = unit + kLines;
             next_row = next_unit * a.unit_rows;
         }
-        if (kAhead && next_unit < end) load(next, next_row);
-        f32x8 total[CHUNKS];
-#pragma unroll
-        for (int j = 0; j < CHUNKS; ++j) total[j] = a.dh.data ? values(d.dh[j], STREAM_FP32) : f32x8{};
+        if (next_unit < end) load(next, next_row);
+        auto pre_hat = [&](int j) { return (chunk(a.h, d.h, STREAM_FP32, row, j) - d.pre_mean) * d.pre_rstd; };
+        auto pre_grad = [&](int j) { return at[j].mask(chunk(a.dy, d.dy, BRANCH_FP32, row, j)); };
+        float pre_s0 = 0.0f, pre_s1 = 0.0f;
+        f32x8 kept_hat, kept_g, kept_post;
         if (a.dy.data) {
-            f32x8 hat[CHUNKS], g[CHUNKS];
-            float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
             for (int j = 0; j < CHUNKS; ++j) {
-                hat[j] = (values(d.h[j], STREAM_FP32) - d.pre_mean) * d.pre_rstd;
-                g[j] = at[j].mask(values(d.dy[j], BRANCH_FP32));
-                acc[kPreWeight][j] += g[j] * hat[j];
-                if (LAYER) acc[kPreBias][j] += g[j];
-                if (a.pre_weight) g[j] *= values(pre.weight[j], a.param_fp32);
+                const f32x8 hat = pre_hat(j);
+                f32x8 g = pre_grad(j);
+                acc[kPreWeight][j] += g * hat;
+                if (LAYER) acc[kPreBias][j] += g;
+                if (a.pre_weight) g *= param(a.pre_weight, pre.weight, j);
+                kept_hat = hat;
+                kept_g = g;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    s0 = fmaf(g[j][i], hat[j][i], s0);
-                    if (LAYER) s1 += g[j][i];
+                    pre_s0 = fmaf(g[i], hat[i], pre_s0);
+                    if (LAYER) pre_s1 += g[i];
                 }
             }
-            sums.sum2(s0, s1);
-            s0 *= a.inv_cols;
-            s1 *= a.inv_cols;
-#pragma unroll
-            for (int j = 0; j < CHUNKS; ++j) total[j] += d.pre_rstd * (g[j] - hat[j] * s0 - (LAYER ? s1 : 0.0f));
+            sums.sum2(pre_s0, pre_s1);
+            pre_s0 *= a.inv_cols;
+            pre_s1 *= a.inv_cols;
         }
-        if (a.dx.data) {
+        const float mean = BRANCH && a.post_norm ? d.post_mean : 0.0f, rstd = BRANCH && a.post_norm ? d.post_rstd : 1.0f;
+        auto post_hat = [&](int j) { return (chunk(a.f, d.f, BRANCH_FP32, row, j) - mean) * rstd; };
+        f32x8 du[CHUNKS];
+        float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
-            for (int j = 0; j < CHUNKS; ++j)
-                store8(a.dx.data, STREAM_FP32, (int64_t)row * a.dx.stride, at[j], BRANCH ? a.residual_scale * total[j] : total[j]);
-        }
-        if constexpr (BRANCH) {
-            const float mean = a.post_norm ? d.post_mean : 0.0f, rstd = a.post_norm ? d.post_rstd : 1.0f;
-            f32x8 hat[CHUNKS];
-            float s0 = 0.0f, s1 = 0.0f;
-#pragma unroll
-            for (int j = 0; j < CHUNKS; ++j) {
-                hat[j] = (values(d.f[j], BRANCH_FP32) - mean) * rstd;
-                f32x8 du = a.branch_scale * total[j];
+        for (int j = 0; j < CHUNKS; ++j) {
+            f32x8 total = a.dh.data ? chunk(a.dh, d.dh, STREAM_FP32, row, j) : f32x8{};
+            if (a.dy.data) {
+                f32x8 hat = kept_hat, g = kept_g;
+                if constexpr (CHUNKS > 1) {
+                    hat = pre_hat(j);
+                    g = pre_grad(j);
+                    if (a.pre_weight) g *= param(a.pre_weight, pre.weight, j);
+                }
+                total += d.pre_rstd * (g - hat * pre_s0 - (LAYER ? pre_s1 : 0.0f));
+            }
+            if constexpr (BRANCH) {
+                const f32x8 hat = kept_post = post_hat(j);
+                du[j] = a.branch_scale * total;
                 if (a.gate.data) {
-                    f32x8 act = values(d.gate[j], BRANCH_FP32), u = hat[j];
-                    if (a.post_weight) u *= values(post.weight[j], a.param_fp32);
-                    if (a.post_bias) u += values(post.bias[j], a.param_fp32);
-                    u *= du;
+                    const Rows gate_row = {a.gate.data, 0};
+                    f32x8 act = kHold ? chunk(gate_row, d.gate, BRANCH_FP32, 0, j)
+                                      : values(load8(a.gate.data, BRANCH_FP32, (int64_t)(row / a.rows_per_gate) * a.gate.stride, at[j]), BRANCH_FP32);
+                    f32x8 u = hat;
+                    if (a.post_weight) u *= param(a.post_weight, post.weight, j);
+                    if (a.post_bias) u += param(a.post_bias, post.bias, j);
+                    u *= du[j];
                     if (a.sigmoid) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
@@ -431,21 +458,23 @@ __global__ __launch_bounds__(LANES * lines_of(LANES)) void norm_gradients(GradAr
                         }
                     }
                     acc[kGate][j] += u;
-                    du *= act;
+                    du[j] *= act;
                 }
                 if (a.post_norm) {
-                    acc[kPostWeight][j] += du * hat[j];
-                    if (LAYER) acc[kPostBias][j] += du;
-                    if (a.post_weight) du *= values(post.weight[j], a.param_fp32);
-                    const f32x8 own = at[j].mask(du);
+                    acc[kPostWeight][j] += du[j] * hat;
+                    if (LAYER) acc[kPostBias][j] += du[j];
+                    if (a.post_weight) du[j] *= param(a.post_weight, post.weight, j);
+                    const f32x8 own = at[j].mask(du[j]);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        s0 = fmaf(own[i], hat[j][i], s0);
+                        s0 = fmaf(own[i], hat[i], s0);
                         if (LAYER) s1 += own[i];
                     }
                 }
-                total[j] = du;
             }
+            if (a.dx.data) store8(a.dx.data, STREAM_FP32, (int64_t)row * a.dx.stride, at[j], BRANCH ? a.residual_scale * total : total);
+        }
+        if constexpr (BRANCH) {
             if (a.post_norm) {
                 sums.sum2(s0, s1);
                 s0 *= a.inv_cols;
@@ -454,8 +483,8 @@ __global__ __launch_bounds__(LANES * lines_of(LANES)) void norm_gradients(GradAr
             if (a.df.data) {
 #pragma unroll
                 for (int j = 0; j < CHUNKS; ++j) {
-                    if (a.post_norm) total[j] = rstd * (total[j] - hat[j] * s0 - (LAYER ? s1 : 0.0f));
-                    store8(a.df.data, BRANCH_FP32, (int64_t)row * a.df.stride, at[j], total[j]);
+                    if (a.post_norm) du[j] = rstd * (du[j] - (CHUNKS == 1 ? kept_post : post_hat(j)) * s0 - (LAYER ? s1 : 0.0f));
+                    store8(a.df.data, BRANCH_FP32, (int64_t)row * a.df.stride, at[j], du[j]);
                 }
             }
             if (next_unit != unit && a.gate_done && a.dgate.data) {
@@ -466,10 +495,9 @@ __global__ __launch_bounds__(LANES * lines_of(LANES)) void norm_gradients(GradAr
                 }
             }
         }
+        d = next;
         row = next_row;
         unit = next_unit;
-        if (kAhead) d = next;
-        else if (unit < end) load(d, row);
     }
 #pragma unroll
     for (int k = 0; k < kSums; ++k) {
