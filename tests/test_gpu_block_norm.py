@@ -208,6 +208,21 @@ def test_rows_that_lie_apart_and_buffers_used_again(kind, cols):
     assert (wg[:, :1] == 5).all() and (wg[:, 1 + cols:] == 5).all()
 
 
+@pytest.mark.parametrize("stream", [BF16, torch.float32])
+@pytest.mark.parametrize("cols", [768, 8000, 8192, 12008, 16000])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_gradients_over_what_they_were_made_from(kind, cols, stream):
+    c = Case(300, cols, kind, gates=3, stream=stream)          # (several rows to a workgroup)
+    c.run().backward()
+    want = [c.grads[n] for n in ("dx", "df", "dgate", "dpre_weight")]
+    ws = torch.empty(fo.block_norm_backward_workspace(c.spec, c.rows, 3), dtype=torch.uint8, device="cuda")
+    for over in ("f", "dy"):
+        dh, f, dy, dgate, dpre = c.dh.clone(), c.f.clone(), c.dy.clone(), torch.empty_like(c.gate), torch.empty_like(want[3])
+        df = f if over == "f" else dy
+        fo.block_norm_backward(c.spec, c.h, c.stats, f=f, gate=c.gate, dy=dy, dh=dh, dx=dh, df=df, dgate=dgate, dpre_weight=dpre, workspace=ws)
+        assert all(torch.equal(x, y) for x, y in zip((dh, df, dgate, dpre), want)), over
+
+
 def test_gradients_that_are_not_wanted_change_nothing():
     c = Case(50, 900, "layer", gates=5)
     c.run().backward()
