@@ -153,7 +153,7 @@ struct RowSums {
         if constexpr (kWaves > 1) {
             f32x4* p = part + turn * kWaves;
             turn ^= 1;
-            if (threadIdx.x % 64 == 0) p[threadIdx.x / 64] = f32x4{a, b, 0.0f, 0.0f};
+            if (threadIdx.x % 64 == 0) p[threadIdx.x / 64 % kWaves] = f32x4{a, b, 0.0f, 0.0f};
             __syncthreads();
             a = b = 0.0f;
 #pragma unroll
@@ -323,16 +323,15 @@ struct RowData {
     float post_mean, post_rstd, pre_mean, pre_rstd;
 };
 
-template <bool STREAM_FP32, bool BRANCH_FP32, int LANES, int CHUNKS, bool NARROW, bool LAYER, bool BRANCH>
-__global__ __launch_bounds__(LANES * lines_of(LANES)) void norm_gradients(GradArgs a) {
-    constexpr int kLines = lines_of(LANES);
-    __shared__ f32x4 part_sums[2 * (LANES / 64)];
-    __shared__ float joined[kLines > 1 ? kLines : 1][kLines > 1 ? LANES * 8 * CHUNKS : 1];
+template <bool STREAM_FP32, bool BRANCH_FP32, int LANES, int CHUNKS, bool NARROW, int LINES, bool LAYER, bool BRANCH>
+__global__ __launch_bounds__(LANES * LINES) void norm_gradients(GradArgs a) {
+    __shared__ f32x4 part_sums[LINES][2 * (LANES / 64)];
+    __shared__ float joined[LINES > 1 ? LINES : 1][LINES > 1 ? LANES * 8 * CHUNKS : 1];
     asm volatile("" ::FO_ROWS(a.h), FO_ROWS(a.f), FO_ROWS(a.gate), FO_ROWS(a.dy), FO_ROWS(a.dh), FO_ROWS(a.dx), FO_ROWS(a.df), "s"(a.post_weight),
                  "s"(a.post_bias), "s"(a.pre_weight), "s"(a.stats), "s"(a.rows), "s"(a.rows_per_gate), "s"(a.unit_rows), "s"(a.part_units),
                  "s"(a.units_per_group), "s"(a.parts_per_group), "s"(a.cols), "s"(a.residual_scale));
-    const int line = kLines > 1 ? threadIdx.x / LANES : 0, lane = threadIdx.x % LANES;
-    RowSums<LANES> sums = {part_sums, 0};
+    const int line = LINES > 1 ? threadIdx.x / LANES : 0, lane = threadIdx.x % LANES;
+    RowSums<LANES> sums = {part_sums[line], 0};
     Place<NARROW> at[CHUNKS];
 #pragma unroll
     for (int j = 0; j < CHUNKS; ++j) {
@@ -395,7 +394,7 @@ __global__ __launch_bounds__(LANES * lines_of(LANES)) void norm_gradients(GradAr
         // the next row is on its way while this one goes through its sums
         uint32_t next_row = row + 1, next_unit = unit;
         if (next_row == (unit + 1) * a.unit_rows) {
-            next_unit = unit + kLines;
+            next_unit = unit + LINES;
             next_row = next_unit * a.unit_rows;
         }
         if (next_unit < end) load(next, next_row);
@@ -499,11 +498,20 @@ __global__ __launch_bounds__(LANES * lines_of(LANES)) void norm_gradients(GradAr
         row = next_row;
         unit = next_unit;
     }
+    if constexpr (LINES > 1 && LANES > 64) {
+        // a line that has no row left goes along with the barriers of those that have
+        const uint32_t count = end - min(begin, end), own = count - min(count, (uint32_t)line);
+        const uint32_t left = ((count + LINES - 1) / LINES - (own + LINES - 1) / LINES) * a.unit_rows;
+        for (uint32_t i = 0; i < left; ++i) {
+            if (a.dy.data) __syncthreads();
+            if (BRANCH && a.post_norm) __syncthreads();
+        }
+    }
 #pragma unroll
     for (int k = 0; k < kSums; ++k) {
         if (a.slot[k] < 0 || (!BRANCH && k >= kPostWeight) || (!LAYER && (k == kPreBias || k == kPostBias))) continue;
         float* out = a.part + ((int64_t)a.slot[k] * a.parts + blockIdx.x) * a.cols;
-        if constexpr (kLines > 1) {
+        if constexpr (LINES > 1) {
             __syncthreads();
 #pragma unroll
             for (int j = 0; j < CHUNKS; ++j)
@@ -516,7 +524,7 @@ __global__ __launch_bounds__(LANES * lines_of(LANES)) void norm_gradients(GradAr
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
 #pragma unroll
-                        for (int l = 1; l < kLines; ++l) acc[k][j][i] += joined[l][(j * 8 + i) * LANES + lane];
+                        for (int l = 1; l < LINES; ++l) acc[k][j][i] += joined[l][(j * 8 + i) * LANES + lane];
                     store8(out, true, 0, at[j], acc[k][j]);
                 }
             }
@@ -618,7 +626,7 @@ struct Shape {
     static constexpr bool kNarrow = NARROW;
 };
 // Eight values to a lane as far as 512 lanes reach.  The backward pass keeps up to five sums a value, for which 1024 lanes, of 128 registers each,
-// have no room: it takes 512 lanes with 16 or 32 values.
+// have no room: it takes 512 lanes with 16 or 32 values, as the forward pass does.
 template <typename F>
 void with_shape(int64_t cols, F launch) {
     if (cols < 8) launch(Shape<64, 1, true>{});
@@ -637,11 +645,16 @@ struct Parts {
     int64_t unit_rows, part_units, units_per_group, parts_per_group, parts;
     bool gate_done;
 };
+// Rows that a workgroup of the backward pass handles side by side.  What it sums over its rows, five values a column, is written and read again: with
+// 2000 rows of 768 in 1000 workgroups as many bytes as the rows themselves.  So eight where a wavefront has a row to itself, and four of two
+// wavefronts where there are few rows; their barriers hold up all four, which many rows do not pay for (us, one line / four, layer norms of 768
+// values: 2048 rows 18.2 / 16.2, 4096 23.3 / 22.9, 8192 37 / 41; of two lines of 256 lanes: 4096 rows of 2048 36 / 41).
+int lines_of_gradients(int64_t rows, int64_t cols) { return cols <= 512 ? 8 : cols <= 1024 && rows <= 4096 ? 4 : 1; }
 Parts cut(int64_t rows, int64_t gates, int64_t cols) {
-    const int64_t rows_per_gate = rows / gates;
+    const int64_t rows_per_gate = rows / gates, lines = lines_of_gradients(rows, cols);
     // As many parts as there are compute units times what one holds of them, from 1024 of 128 lanes to 256 of 512 (us, 256 / 512 / 1024 / 1536 parts: 16384
     // rows of 1024 values 116 / 74 / 48 / 47, 8192 of 4096 98 / 99 / 106 / 121, 4096 of 2048, layer norms, 42 / 33 / 41 / 47).
-    const int64_t least = cols <= 512 ? lines_of(64) : 2, most = cols <= 512 ? 512 : cols <= 1024 ? 1024 : cols <= 2048 ? 512 : 256;
+    const int64_t least = lines > 1 ? lines : 2, most = lines > 1 ? 256 : cols <= 1024 ? 1024 : cols <= 2048 ? 512 : 256;
     int64_t part_rows = up(rows, most);
     if (part_rows < least) part_rows = least;
     Parts p;
@@ -786,19 +799,28 @@ int flashoptim_block_norm_backward(const flashoptim_block_norm_spec* spec, const
         a.gate_done = c.gate_done;
         const bool sf = h->dtype == FLASHOPTIM_FP32, bf = branch_type == FLASHOPTIM_FP32;
         with_shape(cols, [&](auto shape) {
-            constexpr int L = decltype(shape)::kLanes, C = decltype(shape)::kChunks, T = L * lines_of(L);
-        constexpr bool N = decltype(shape)::kNarrow;
-            const dim3 grid((unsigned)c.parts), block(T);
-            auto launch = [&](auto layer_c, auto branch_c) {
+            constexpr int L = decltype(shape)::kLanes, C = decltype(shape)::kChunks;
+            constexpr bool N = decltype(shape)::kNarrow;
+            const dim3 grid((unsigned)c.parts);
+            auto launch = [&](auto lines_c, auto layer_c, auto branch_c) {
+                constexpr int K = decltype(lines_c)::value;
                 constexpr bool LN = decltype(layer_c)::value, BR = decltype(branch_c)::value;
-                if (bf) hipLaunchKernelGGL((norm_gradients<true, true, L, C, N, LN, BR>), grid, block, 0, (hipStream_t)stream, a);
-                else if (sf) hipLaunchKernelGGL((norm_gradients<true, false, L, C, N, LN, BR>), grid, block, 0, (hipStream_t)stream, a);
-                else hipLaunchKernelGGL((norm_gradients<false, false, L, C, N, LN, BR>), grid, block, 0, (hipStream_t)stream, a);
+                const dim3 block(L * K);
+                if (bf) hipLaunchKernelGGL((norm_gradients<true, true, L, C, N, K, LN, BR>), grid, block, 0, (hipStream_t)stream, a);
+                else if (sf) hipLaunchKernelGGL((norm_gradients<true, false, L, C, N, K, LN, BR>), grid, block, 0, (hipStream_t)stream, a);
+                else hipLaunchKernelGGL((norm_gradients<false, false, L, C, N, K, LN, BR>), grid, block, 0, (hipStream_t)stream, a);
             };
             using Yes = std::true_type;
             using No = std::false_type;
-            if (layer) { if (f) launch(Yes{}, Yes{}); else launch(Yes{}, No{}); }
-            else { if (f) launch(No{}, Yes{}); else launch(No{}, No{}); }
+            auto with_lines = [&](auto k) {
+                if (layer) { if (f) launch(k, Yes{}, Yes{}); else launch(k, Yes{}, No{}); }
+                else { if (f) launch(k, No{}, Yes{}); else launch(k, No{}, No{}); }
+            };
+            if constexpr (L == 64) with_lines(std::integral_constant<int, 8>{});
+            else if constexpr (L == 128) {
+                if (lines_of_gradients(rows, cols) == 4) with_lines(std::integral_constant<int, 4>{});
+                else with_lines(std::integral_constant<int, 1>{});
+            } else with_lines(std::integral_constant<int, 1>{});
         });
         FO_TRY(fo::hip_status(hipGetLastError()));
     }

@@ -160,6 +160,15 @@ def test_many_rows_and_every_way_to_share_a_gate(rows, gates, cols):
     c.backward().check_backward()
 
 
+@pytest.mark.parametrize("branch,pre", [(True, True), (False, True), (True, False)])
+@pytest.mark.parametrize("rows,gates", [(1, 1), (2, 1), (3, 3), (9, 3), (257, 1), (1030, 2), (1030, 103), (4095, 1), (4097, 1)])
+def test_rows_that_do_not_fill_a_workgroup(rows, gates, branch, pre):
+    for cols, kind in ((300, "layer"), (768, "layer"), (1024, "rms")):
+        c = Case(rows, cols, kind, branch=branch, gates=gates, pre=pre)
+        c.run().check_forward()
+        c.backward().check_backward()
+
+
 @pytest.mark.parametrize("kind", ["rms", "layer"])
 def test_rows_that_are_zero_or_constant(kind):
     c = Case(12, 777, kind)
