@@ -359,14 +359,14 @@ int flashoptim_mx4_dequantize(const flashoptim_mx4* q, const flashoptim_matrix* 
  * call's result is the same every time.  A product over zero terms is zero.
  * matmul: c [m, n] <- a [m, k] b [n, k]^T.
  * linear: y [m, n] <- Q(x) w^T with x [m, k] quantised to nearest along its rows and w [n, k]; if xt [k, m] is not NULL, Q(x^T) is
- *   left there for the backward pass.  Up to 16 rows without xt are one launch, made for single tokens: the weights stream through
- *   once.
+ *   left there for the backward pass.  Without xt a few rows are one launch, made for single tokens, through which the weights stream
+ *   once: up to 16 rows, fewer with long ones (16 of 6144 values, 6 of 16384, half as many where the rows of w take a second round of workgroups).
  * linear_backward: dx [m, k] <- Q(dy) wt^T and dw [n, k] <- Q(dy^T) xt^T, with dy [m, n] quantised along its rows and along
  *   its columns in one pass (stochastically with `rand`), wt [k, n] the transposed weights in 4 bits (quantize's out_t) and xt [k, m].
  *   dx or dw may be NULL, and with it wt or xt.  These are the gradients of the product of its quantised operands, the
  *   quantisation itself counted as the identity, each with its operands in 4 bits along its own sum.
  * workspace: DEVICE memory, 16-byte aligned, of at least the bytes that the *_workspace call returns for the same sizes (0: NULL will
- *   do; negative: a status), and the call's until its work on `stream` is done.  (With `train` or rand nothing changes in size.) */
+ *   do; negative: a status), and the call's until its work on `stream` is done. */
 int64_t flashoptim_mx4_matmul_workspace(int64_t m, int64_t n, int64_t k);
 int64_t flashoptim_mx4_linear_workspace(int64_t m, int64_t n, int64_t k);
 int64_t flashoptim_mx4_linear_backward_workspace(int64_t m, int64_t n, int64_t k);
