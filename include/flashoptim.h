@@ -388,7 +388,8 @@ int flashoptim_mx4_linear_backward(const flashoptim_matrix* dy, const uint8_t* r
  * each channel; g = rows: one for each value).  Sums and everything between loads and stores are FP32; y is formed from h before
  * h is rounded.
  * Left out: weights and biases (NULL: 1, 0; biases are for layer norms only), the gate (NULL: 1), the norm in front (y NULL), the branch (f NULL: h = x, not written;
- * gate must be NULL).  x and h have one type, f, gate and y one type, which is BF16, or FP32 if x is FP32.  1 <= cols <= 16384.
+ * gate must be NULL).  x and h have one type, f, gate and y one type, which is BF16, or FP32 if x is FP32.  1 <= cols <= 16384; rows < 2^31,
+ * and in the forward call less than 2^23 (2^26 for cols <= 512, 2^25 to 1024, 2^24 to 2048).
  * h may be x's own buffer, y f's.
  * stats: NULL, or [4, rows] FP32 for the backward pass: mean and 1/sqrt(...) of the norm behind, of the norm in front (0 where
  *   there is none). */

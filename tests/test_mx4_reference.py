@@ -131,6 +131,8 @@ def test_block_norm_refusals_before_anything_runs():
     assert call(spec(), m(8, 64, data=4097), None, None, None, x, None, None) == -2
     assert call(spec(), m(8, 64, stride=63), None, None, None, x, None, None) == -1
     assert call(spec(), m(8, 64, data=None), None, None, None, x, None, None) == -1
+    for cols, rows in ((64, 1 << 26), (1024, 1 << 25), (2048, 1 << 24), (16384, 1 << 23)):  # more lanes than a launch has
+        assert call(spec(cols=cols), m(rows, cols), None, None, None, m(rows, cols), None, None) == -3
     back = L.flashoptim_block_norm_backward
     grads = lambda **k: B._BlockNormGrads(**{n: C.pointer(v) if isinstance(v, B._Matrix) else v for n, v in k.items()})     # noqa: E731
     assert back(spec(), x, None, None, 4096, grads(dx=x), 4096, 1 << 30, None) == -1        # no gradient comes in
