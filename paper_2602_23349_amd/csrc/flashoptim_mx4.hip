@@ -12,9 +12,9 @@
 
 #include <type_traits>
 
-
 #include "flashoptim.h"
 #include "flashoptim_host.h"
+#include "flashoptim_mx4.h"
 
 namespace {
 
@@ -23,9 +23,11 @@ using i32x8 = int __attribute__((ext_vector_type(8)));
 using f32x4 = float __attribute__((ext_vector_type(4)));
 using bf16x4 = __bf16 __attribute__((ext_vector_type(4)));
 
-constexpr int kBlock = 32;                  // values that share a scale
-constexpr int kSegment = 256;               // a row of codes is filled up to a multiple of this many values
-constexpr int kSegmentBytes = kSegment / 2;
+using fo::kBlock;
+using fo::kScaleBytes;
+using fo::kScaleSteps;
+using fo::kSegment;
+using fo::kSegmentBytes;
 
 inline int64_t up(int64_t n, int64_t unit) { return (n + unit - 1) / unit; }
 
@@ -491,7 +493,6 @@ __global__ __launch_bounds__(64 * WAVES) void product_small(Mx4 b, Mx4 a, Result
 // The tile of 256 by 256 fills the LDS (160 KB), so that one workgroup is resident on a compute unit.
 using f32x16 = float __attribute__((ext_vector_type(16)));
 
-constexpr int kScaleTerms = 1024, kScaleBytes = kScaleTerms / kBlock, kScaleSteps = kScaleTerms / kSegment;
 template <int ROWS>
 struct Stage {
     uint8_t codes[ROWS * kSegmentBytes];
@@ -500,17 +501,11 @@ template <int ROWS>
 struct Scales {
     uint8_t bytes[ROWS * kScaleBytes];
 };
-// In LDS, a row's codes are eight pieces of 16 bytes; piece c of row r lies at c ^ swizzle(r), so that the 64 lanes of a read, 32 rows
-// of the same piece in each half, spread evenly over the banks; its scales are two.  A copy to LDS writes consecutive lanes to
-// consecutive places, so the lanes ask memory for their pieces in that order.
-__device__ __forceinline__ int swizzle(int row) { return row >> 1 & 7; }
-__device__ __forceinline__ int scale_swizzle(int row) { return row >> 3 & 1; }
-
 constexpr int64_t kMaxTiledTerms = (int64_t)1 << 23;      // 256 rows of codes stay below 2^31 bytes, which a lane's offset reaches
 
 #define FO_LDS(p) ((__attribute__((address_space(3))) void*)(p))
 
-// `bytes` bytes from p on as a buffer; addresses into it are a lane's 32-bit offset and a scalar one.
+// `bytes` bytes from p on as a buffer; an address into it is a lane's 32-bit offset.
 __device__ __forceinline__ i32x4 buffer_of(const uint8_t* p, uint32_t bytes) {
     const uint64_t at = (uint64_t)p;
     return i32x4{__builtin_amdgcn_readfirstlane((int)(uint32_t)at), __builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32)),
@@ -521,9 +516,9 @@ __device__ __forceinline__ i32x4 buffer_of(const uint8_t* p, uint32_t bytes) {
 // fetched.  It has no result in registers, so that written as assembly it is safe; written with the builtin, the compiler has every later read
 // of LDS wait for it, whichever stage it reads.  What waits for it is wait_copies.  (s_nop: m0 is to be set one cycle
 // ahead.  The compiler sets m0 right ahead of its own uses, and has none in these kernels.)
-__device__ __forceinline__ void copy_to_lds(i32x4 buffer, uint32_t lane_offset, uint32_t offset, void* to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"((uint32_t)(uintptr_t)FO_LDS(to)), "v"(lane_offset), "s"(buffer),
-                 "s"(offset) : "memory");
+__device__ __forceinline__ void copy_to_lds(i32x4 buffer, uint32_t lane_offset, void* to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"((uint32_t)(uintptr_t)FO_LDS(to)), "v"(lane_offset), "s"(buffer)
+                 : "memory");
 }
 // Waits until all but the last `VM` of this wavefront's copies have landed and its reads of LDS have come back.
 template <int VM>
@@ -556,35 +551,34 @@ struct Copier {
         code_bytes = (last + 1) * pitch;
         scale_bytes = (last + 1) * m.scale_pitch;
 #pragma unroll
-        for (int i = 0; i < kCodes; ++i) {
-            const int row = (wave * kCodes + i) * 8 + lane / 8;
-            code_at[i] = min((uint32_t)row, last) * pitch + (uint32_t)((lane % 8 ^ swizzle(row)) * 16);
-        }
+        for (int i = 0; i < kCodes; ++i) code_at[i] = fo::code_place(wave * kCodes + i, lane, last, pitch);
 #pragma unroll
-        for (int i = 0; i < kScales; ++i) {
-            const int row = (wave * kScales + i) % kAllScales * 32 + lane / 2;
-            scale_at[i] = min((uint32_t)row, last) * m.scale_pitch + (uint32_t)((lane % 2 ^ scale_swizzle(row)) * 16);
-        }
+        for (int i = 0; i < kScales; ++i) scale_at[i] = fo::scale_place((wave * kScales + i) % kAllScales, lane, last, m.scale_pitch);
     }
-    __device__ __forceinline__ i32x4 buffer(bool there) const { return buffer_of(codes, there ? code_bytes : 0); }
-    __device__ __forceinline__ void copy_codes(i32x4 buffer, Stage<ROWS>& to, uint32_t step, int i) const {
-        copy_to_lds(buffer, code_at[i], step * kSegmentBytes, to.codes + (wave * kCodes + i) * 1024);
+    // The codes of a step; `there`: there is such a step.
+    __device__ __forceinline__ i32x4 buffer(uint32_t step, bool there) const {
+        const fo::CopyBuffer b = fo::copy_buffer(code_bytes, step * kSegmentBytes, there);
+        return buffer_of(codes + b.begin, b.bytes);
+    }
+    __device__ __forceinline__ void copy_codes(i32x4 buffer, Stage<ROWS>& to, int i) const {
+        copy_to_lds(buffer, code_at[i], to.codes + (wave * kCodes + i) * 1024);
     }
     __device__ __forceinline__ void copy_scales(Scales<ROWS>& to, uint32_t group, bool there) const {
-        const i32x4 buffer = buffer_of(scales, there ? scale_bytes : 0);
+        const fo::CopyBuffer b = fo::copy_buffer(scale_bytes, group * kScaleBytes, there);
+        const i32x4 buffer = buffer_of(scales + b.begin, b.bytes);
 #pragma unroll
-        for (int i = 0; i < kScales; ++i) copy_to_lds(buffer, scale_at[i], group * kScaleBytes, to.bytes + (wave * kScales + i) % kAllScales * 1024);
+        for (int i = 0; i < kScales; ++i) copy_to_lds(buffer, scale_at[i], to.bytes + (wave * kScales + i) % kAllScales * 1024);
     }
 };
 
 template <int ROWS>
 __device__ __forceinline__ i32x4 piece(const Stage<ROWS>& s, int row, int c) {
-    return *(const i32x4*)(s.codes + row * kSegmentBytes + (c ^ swizzle(row)) * 16);
+    return *(const i32x4*)(s.codes + row * kSegmentBytes + (c ^ fo::code_swizzle(row)) * 16);
 }
 // The scales of half h of the row's blocks in the step-th segment of the 1024 terms: the lowest byte is the first one's.
 template <int ROWS>
 __device__ __forceinline__ int scales_of(const Scales<ROWS>& s, int row, int step, int h) {
-    return *(const int*)(s.bytes + row * kScaleBytes + ((step * 8 + h * 4) ^ scale_swizzle(row) * 16));
+    return *(const int*)(s.bytes + row * kScaleBytes + ((step * 8 + h * 4) ^ fo::scale_swizzle(row) * 16));
 }
 
 template <int TURN>
@@ -660,8 +654,8 @@ __global__ __launch_bounds__(64 * WP * WQ, RESIDENT) void product_tiles(Products
     const uint32_t steps = b.segments;
     f32x16 acc[TP][TQ] = {};
     auto copy = [&](i32x4 p_buffer, i32x4 q_buffer, uint32_t step, int i) {
-        if (i < p_copy.kCodes) p_copy.copy_codes(p_buffer, p_stage[step % STAGES], step, i);
-        else q_copy.copy_codes(q_buffer, q_stage[step % STAGES], step, i - p_copy.kCodes);
+        if (i < p_copy.kCodes) p_copy.copy_codes(p_buffer, p_stage[step % STAGES], i);
+        else q_copy.copy_codes(q_buffer, q_stage[step % STAGES], i - p_copy.kCodes);
     };
     constexpr int kCopies = p_copy.kCodes + q_copy.kCodes;
     constexpr int kEvery = TP * TQ * 2 / kCopies > 0 ? TP * TQ * 2 / kCopies : 1;      // products to a copy: all in the first half of a step
@@ -671,7 +665,7 @@ __global__ __launch_bounds__(64 * WP * WQ, RESIDENT) void product_tiles(Products
 #pragma unroll
     for (int j = 0; j < STAGES - 1; ++j)
 #pragma unroll
-        for (int i = 0; i < kCopies; ++i) copy(p_copy.buffer(j < steps), q_copy.buffer(j < steps), j, i);
+        for (int i = 0; i < kCopies; ++i) copy(p_copy.buffer(j, j < steps), q_copy.buffer(j, j < steps), j, i);
     for (uint32_t t = 0; t < steps; ++t) {
         // this wavefront's copies for step t have landed; behind the barrier all have, and nobody reads the stage of step t - 1 any more
         wait_copies<(STAGES - 2) * kCopies>();
@@ -681,7 +675,7 @@ __global__ __launch_bounds__(64 * WP * WQ, RESIDENT) void product_tiles(Products
             p_copy.copy_scales(p_scales[group % 2 ^ 1], group + 1, t + kScaleSteps < steps);
             q_copy.copy_scales(q_scales[group % 2 ^ 1], group + 1, t + kScaleSteps < steps);
         }
-        const i32x4 p_buffer = p_copy.buffer(next < steps), q_buffer = q_copy.buffer(next < steps);
+        const i32x4 p_buffer = p_copy.buffer(next, next < steps), q_buffer = q_copy.buffer(next, next < steps);
         auto behind = [&](int product) {
             if (product % kEvery != 0 || product / kEvery >= kCopies) return;
             __builtin_amdgcn_sched_barrier(0);

@@ -1,0 +1,62 @@
+"""The arithmetic of the 4-bit matrices' kernels that needs no GPU (csrc/flashoptim_mx4.h), compiled into a small program."""
+import os
+import shutil
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+pytestmark = pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
+
+
+def _run(tmp_path, body):
+    """Compiles `body` as main()'s statements behind the header and returns the lines that it prints."""
+    src, exe = tmp_path / "mx4.cpp", tmp_path / "mx4"
+    src.write_text('#include <cstdio>\n#include <initializer_list>\n#include "flashoptim_mx4.h"\nint main() {\n' + body + "\n}\n")
+    subprocess.run(["g++", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-O1", "-I",
+                    os.path.join(ROOT, "paper_2602_23349_amd", "csrc"), str(src), "-o", str(exe)], check=True)
+    return subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.splitlines()
+
+
+@pytest.mark.parametrize("edge,stages", [(64, 4), (128, 2), (256, 2)])
+def test_copies_of_a_tile_stay_within_the_matrix(tmp_path, edge, stages):
+    # every lane of every copy, those for steps behind the last one among them, of tiles of one to all rows and of sums that end
+    # within a group of scales: what is fetched (16 bytes at a place below the buffer's size) lies in the tile's rows, and of
+    # steps that there are it is the piece that the lane's place in LDS stands for
+    out = _run(tmp_path, f"""
+    const int edge = {edge}, stages = {stages};
+    long long fetched = 0, outside = 0, wrong = 0, absent = 0;
+    for (uint32_t rows : {{1, 2, 31, 33, edge - 1, edge}})
+        for (uint32_t segments = 1; segments <= 13; ++segments) {{
+            const uint32_t last = rows - 1, pitch = segments * fo::kSegmentBytes, scale_pitch = (segments + 1) / 2 * 16;
+            for (uint32_t step = 0; step < segments + stages - 1; ++step) {{
+                const fo::CopyBuffer b = fo::copy_buffer(rows * pitch, step * fo::kSegmentBytes, step < segments);
+                for (int copy = 0; copy < edge / 8; ++copy)
+                    for (int lane = 0; lane < 64; ++lane) {{
+                        const uint32_t place = fo::code_place(copy, lane, last, pitch);
+                        if (place >= b.bytes) {{ absent += step < segments; continue; }}
+                        ++fetched;
+                        outside += place + 16 > b.bytes || b.begin + b.bytes > (uint64_t)rows * pitch;
+                        const uint32_t row = copy * 8 + lane / 8, piece = (lane % 8) ^ fo::code_swizzle(row);
+                        wrong += b.begin + place != (row < last ? row : last) * pitch + step * fo::kSegmentBytes + piece * 16;
+                    }}
+            }}
+            const uint32_t groups = (segments + fo::kScaleSteps - 1) / fo::kScaleSteps;
+            for (uint32_t group = 0; group <= groups; ++group) {{
+                const fo::CopyBuffer b = fo::copy_buffer(rows * scale_pitch, group * fo::kScaleBytes, group < groups);
+                for (int copy = 0; copy < edge / 32; ++copy)
+                    for (int lane = 0; lane < 64; ++lane) {{
+                        const uint32_t place = fo::scale_place(copy, lane, last, scale_pitch);
+                        const uint32_t row = copy * 32 + lane / 2, piece = (lane % 2) ^ fo::scale_swizzle(row), own = row < last ? row : last;
+                        const bool used = group < groups && group * fo::kScaleBytes + piece * 16 < scale_pitch;
+                        if (place >= b.bytes) {{ absent += used; continue; }}
+                        ++fetched;
+                        outside += place + 16 > b.bytes || b.begin + b.bytes > (uint64_t)rows * scale_pitch;
+                        if (used) wrong += b.begin + place != own * scale_pitch + group * fo::kScaleBytes + piece * 16;
+                    }}
+            }}
+        }}
+    std::printf("%lld %lld %lld %lld\\n", fetched, outside, wrong, absent);
+    """)
+    fetched, outside, wrong, absent = (int(x) for x in out[0].split())
+    assert fetched > 100000 and outside == 0 and wrong == 0 and absent == 0
