@@ -514,12 +514,16 @@ __device__ __forceinline__ i32x4 buffer_of(const uint8_t* p, uint32_t bytes) {
 
 // Copies 16 bytes for each lane from the buffer to LDS, consecutive lanes to consecutive places from `to` on; from an empty buffer, nothing is
 // fetched.  It has no result in registers, so that written as assembly it is safe; written with the builtin, the compiler has every later read
-// of LDS wait for it, whichever stage it reads.  What waits for it is wait_copies.  (s_nop: m0 is to be set one cycle
-// ahead.  The compiler sets m0 right ahead of its own uses, and has none in these kernels.)
+// of LDS wait for it, whichever stage it reads.  What waits for it is wait_copies.  The compiler does not see into it, so what it would do is done here: m0
+// is declared as written (it warns that it keeps nothing in m0 across a statement, as is right: it sets m0 right ahead of its own uses); s_nop
+// makes the five cycles that a scalar register which a vector instruction wrote needs before a load reads it, and the one that m0 needs.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void copy_to_lds(i32x4 buffer, uint32_t lane_offset, void* to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"((uint32_t)(uintptr_t)FO_LDS(to)), "v"(lane_offset), "s"(buffer)
-                 : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"((uint32_t)(uintptr_t)FO_LDS(to)), "v"(lane_offset), "s"(buffer)
+                 : "memory", "m0");
 }
+#pragma clang diagnostic pop
 // Waits until all but the last `VM` of this wavefront's copies have landed and its reads of LDS have come back.
 template <int VM>
 __device__ __forceinline__ void wait_copies() {
