@@ -3,6 +3,7 @@
 // binding.py hands the library's function addresses to; arguments are positional, None is a matrix that is left out.
 // Every function returns the call's status.
 
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>
@@ -256,7 +257,16 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
-#define FO_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
+// What torch throws on the way becomes a Python error: a tensor without memory (inside torch.vmap, a wrapper of torch.func) has no address to
+// give, and one of a class of its own asks Python for its device.
+template <PyObject* (*CALL)(PyObject*, PyObject* const*, Py_ssize_t)>
+PyObject* guarded(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    return CALL(self, args, n);
+    END_HANDLE_TH_ERRORS
+}
+
+#define FO_METHOD(name) {#name, (PyCFunction)(void (*)(void))guarded<name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FO_METHOD(bind),   FO_METHOD(quantize),        FO_METHOD(dequantize), FO_METHOD(matmul),
                          FO_METHOD(linear), FO_METHOD(linear_backward), FO_METHOD(norm),       FO_METHOD(norm_backward),
                          {nullptr, nullptr, 0, nullptr}};
