@@ -177,7 +177,15 @@ struct RowSums {
 constexpr int lines_of(int lanes) { return lanes == 64 ? 4 : 1; }
 
 // (The hardware's exponential and reciprocal, within a few units of the last place, where the sums around it are off by dozens.)
-__device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -0x1.715476p+0f)); }
+__device__ __forceinline__ float sigmoid(float v, float* rest) {      // *rest: 1 - sigmoid(v)
+    const float e = __builtin_amdgcn_exp2f(v * -0x1.715476p+0f), s = __builtin_amdgcn_rcpf(1.0f + e);
+    *rest = e > 1.0f ? 1.0f - s : e * s;        // (the difference of a sigmoid near 1 from 1 would keep few of its bits, beyond 17 none)
+    return s;
+}
+__device__ __forceinline__ float sigmoid(float v) {
+    float rest;
+    return sigmoid(v, &rest);
+}
 
 struct NormArgs {
     Rows x, f, gate, h, y;
@@ -454,8 +462,9 @@ __global__ __launch_bounds__(LANES * LINES) void norm_gradients(GradArgs a) {
                     if (a.sigmoid) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
-                            act[i] = sigmoid(act[i]);
-                            u[i] *= act[i] * (1.0f - act[i]);
+                            float rest;
+                            act[i] = sigmoid(act[i], &rest);
+                            u[i] *= act[i] * rest;
                         }
                     }
                     acc[kGate][j] += u;

@@ -330,3 +330,22 @@ def test_another_stream_and_replays_of_a_captured_graph():
         torch.cuda.synchronize()
         calls()
         assert all(torch.equal(a, b) for a, b in zip(got, (c.h, c.y, c.stats, *c.grads.values())))
+
+
+def test_gradients_of_saturated_gates():
+    # Beside the same call with linear gates, which leaves c dH u, the sigmoid's slope is a factor s(g) s(-g) for each value: relative to
+    # it, the exponent g log2(e) (two roundings) makes an error of 2 |g| u, and exponential, reciprocals, sums and products, each within an
+    # ulp (2 u), less than 16 u.
+    rows, cols = 61, 300
+    c = Case(rows, cols, "rms", gates=rows, act="sigmoid", stream=FP32, dtype=FP32, params=FP32)
+    g = np.linspace(-60, 60, rows * cols).reshape(rows, cols).astype(np.float32)
+    c.gate.copy_(torch.from_numpy(g))
+    c.run().backward()
+    linear = fo.BlockNorm(cols, kind="rms", eps=c.eps, post_norm=True, gate_act="linear", residual_scale=c.a, branch_scale=c.c, **c.w)
+    without = torch.empty_like(c.gate)
+    ws = torch.empty(fo.block_norm_backward_workspace(linear, rows, rows), dtype=torch.uint8, device="cuda")
+    fo.block_norm_backward(linear, c.h, c.stats, f=c.f, gate=c.gate, dy=c.dy, dh=c.dh, dgate=without, workspace=ws)
+    g = g.astype(np.float64)
+    want = f64(without) / (1 + np.exp(-g)) / (1 + np.exp(g))
+    off = np.abs(f64(c.grads["dgate"]) - want)
+    assert (off <= (2 * np.abs(g) + 16) * U * np.abs(want)).all(), np.nanmax(off / np.abs(want)) / U
