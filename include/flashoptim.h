@@ -319,7 +319,7 @@ int flashoptim_checkpoint_unpack(int kind, const void* blob, int64_t blob_bytes,
  *   scales: [rows, 16 ceil(cols/512)] bytes, one to a block: the block's values are its codes' times 2^(byte - 127);
  *           byte 255 makes the whole block NaN.
  * What lies behind column cols of a row is zero in both arrays (every call here writes it so, and the products count
- * on it).  Both arrays 16-byte aligned and contiguous.
+ * on it).  Both arrays 16-byte aligned and contiguous.  rows (ceil(cols/256) + 1) <= 2^27.
  *
  * Quantisation, by block, with E the exponent field of the FP32 value max|v| of the block:
  *   to nearest:   byte = max(E - 2, 0); each v 2^(127 - byte) goes to the nearest of the eight magnitudes, ties to the
@@ -349,7 +349,7 @@ typedef struct flashoptim_mx4 {
 /* quantize: `out` <- x in 4 bits along its rows; `out_t` <- the transpose of x (cols by rows) in 4 bits along ITS rows, from
  *   the same pass over x.  Either may be NULL.  rho: NULL, or the [rows, cols] INT8 corrections (contiguous) of x, which is then
  *   a contiguous BF16 matrix of split weights: what is quantised is the reconstructed FP32 weight.  rand: NULL, or [rows, cols]
- *   random bytes (contiguous): stochastic rounding; out and out_t use the same byte of a value.
+ *   random bytes (contiguous): stochastic rounding; out and out_t use the same byte of a value.  With out_t, ceil(rows/256) ceil(cols/256) < 2^21.
  * dequantize: x <- the values that q stands for, in BF16 (exact) or FP32 (exact). */
 int flashoptim_mx4_quantize(const flashoptim_matrix* x, const int8_t* rho, const uint8_t* rand,
                             const flashoptim_mx4* out, const flashoptim_mx4* out_t, void* stream);

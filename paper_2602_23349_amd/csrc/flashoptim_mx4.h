@@ -11,6 +11,19 @@ constexpr int kBlock = 32;                  // values that share a scale
 constexpr int kSegment = 256;               // a row of codes is filled up to a multiple of this many values
 constexpr int kSegmentBytes = kSegment / 2;
 
+constexpr int64_t up(int64_t n, int64_t unit) { return (n + unit - 1) / unit; }
+
+// Quantisation along columns, or both ways: tiles of this many rows by 128 columns, over rows and columns filled up to whole segments.
+// Rows of a tile, in us with 32 / 64 / 128: BF16, 1024 x 2304 4.4 / 4.8 / 6.1, 8192 x 4096 25.2 / 24.2 / 26.2, 14336 x 4096 38.7 / 36.5 / 38.4,
+// stochastic 68 / 61 / 68; split weights, 1001 x 768 4.0 / 4.8 / 6.9, 14336 x 4096 45.2 / 45.4 / 56.4.
+constexpr int kTileCols = 128, kTileLanes = 256;
+constexpr int quantize_tile_rows(int64_t rows, int64_t cols) { return rows * cols < ((int64_t)1 << 25) ? 32 : 64; }
+constexpr int64_t quantize_tiles(int64_t rows, int64_t cols) {
+    return up(rows, kSegment) * (kSegment / quantize_tile_rows(rows, cols)) * up(cols, kSegment) * (kSegment / kTileCols);
+}
+// A launch has fewer than 2^32 lanes.
+constexpr bool quantize_fits(int64_t rows, int64_t cols) { return quantize_tiles(rows, cols) < ((int64_t)1 << 32) / kTileLanes; }
+
 // Tiles of the products come to LDS in copies of 16 bytes for each lane.  A step takes a segment of 256 terms, 128 bytes of codes of each row in eight
 // pieces; of the scales, 1024 terms at a time, 32 bytes of each row in two.  In LDS, piece c of row r lies at c ^ swizzle(r), so that the 64
 // lanes of a read, 32 rows of the same piece in each half, spread evenly over the banks.  A copy to LDS writes consecutive lanes to

@@ -28,8 +28,8 @@ using fo::kScaleBytes;
 using fo::kScaleSteps;
 using fo::kSegment;
 using fo::kSegmentBytes;
-
-inline int64_t up(int64_t n, int64_t unit) { return (n + unit - 1) / unit; }
+using fo::kTileCols;
+using fo::up;
 
 // A 4-bit matrix as a kernel takes it.
 struct Mx4 {
@@ -252,10 +252,8 @@ __global__ __launch_bounds__(256) void quantize_rows(Source s, Mx4 out, uint32_t
 // Bound: HBM.  An XCD goes through its tiles in bands of 1024 rows, down each column of a band: its L2 then puts the tiles' 16 or 32 bytes of a row of
 // out_t together, and a band's rows of out, 64 bytes from each tile, while they are there.  In us, down whole columns / in bands / and with x read
 // past the caches: 14336 x 4096 split weights from memory 63 / 57 / 54, BF16 55 / 48 / 45, along the rows 66 and 53.
-constexpr int kTileCols = 128;
-
 template <int SRC, bool RANDOM, int ROWS>
-__global__ __launch_bounds__(256) void quantize_both(Source s, Mx4 out, Mx4 out_t, bool rows_too, uint32_t row_tiles, uint32_t tiles) {
+__global__ __launch_bounds__(fo::kTileLanes) void quantize_both(Source s, Mx4 out, Mx4 out_t, bool rows_too, uint32_t row_tiles, uint32_t tiles) {
     using Cell = typename std::conditional<SRC == kBf16, uint16_t, float>::type;
     constexpr int kPasses = ROWS / 16;
     __shared__ Cell tile[ROWS][kTileCols];
@@ -923,15 +921,15 @@ int launch_quantize(const Source& s, const flashoptim_mx4* out, const flashoptim
         const uint32_t total = o.rows * o.segments;
         hipLaunchKernelGGL((quantize_rows<SRC, RANDOM>), dim3((total + 7) / 8), dim3(256), 0, stream, s, o, total);
     } else {
+        // (`out`, checked as a matrix in 4 bits, keeps this small; x by itself may be a row of out_t and more than a launch of tiles)
+        if (!fo::quantize_fits(s.rows, s.cols)) return FLASHOPTIM_ERR_NUMEL_RANGE;
         const Mx4 t = to_dev(*out_t), o = out ? to_dev(*out) : Mx4{};
         auto launch = [&](auto rows) {
             constexpr int R = decltype(rows)::value;
-            const uint32_t row_tiles = t.segments * (kSegment / R), tiles = row_tiles * (uint32_t)up(s.cols, kSegment) * (kSegment / kTileCols);
-            hipLaunchKernelGGL((quantize_both<SRC, RANDOM, R>), dim3(tiles), dim3(256), 0, stream, s, o, t, out != nullptr, row_tiles, tiles);
+            const uint32_t row_tiles = t.segments * (kSegment / R), tiles = (uint32_t)fo::quantize_tiles(s.rows, s.cols);
+            hipLaunchKernelGGL((quantize_both<SRC, RANDOM, R>), dim3(tiles), dim3(fo::kTileLanes), 0, stream, s, o, t, out != nullptr, row_tiles, tiles);
         };
-        // Rows of a tile, in us with 32 / 64 / 128: BF16, 1024 x 2304 4.4 / 4.8 / 6.1, 8192 x 4096 25.2 / 24.2 / 26.2, 14336 x 4096 38.7 / 36.5 / 38.4,
-        // stochastic 68 / 61 / 68; split weights, 1001 x 768 4.0 / 4.8 / 6.9, 14336 x 4096 45.2 / 45.4 / 56.4.
-        if ((int64_t)s.rows * s.cols < ((int64_t)1 << 25)) launch(std::integral_constant<int, 32>{});
+        if (fo::quantize_tile_rows(s.rows, s.cols) == 32) launch(std::integral_constant<int, 32>{});
         else launch(std::integral_constant<int, 64>{});
     }
     return fo::hip_status(hipGetLastError());

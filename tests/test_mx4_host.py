@@ -60,3 +60,34 @@ def test_copies_of_a_tile_stay_within_the_matrix(tmp_path, edge, stages):
     """)
     fetched, outside, wrong, absent = (int(x) for x in out[0].split())
     assert fetched > 100000 and outside == 0 and wrong == 0 and absent == 0
+
+
+def test_quantisation_beyond_one_launch_is_refused(tmp_path):
+    # out_t alone admits a matrix of up to 2^31 rows of a few columns, whose tiles would be more than 2^32 lanes
+    import paper_2602_23349_amd as fo
+    from paper_2602_23349_amd import binding as B
+    call = fo.load_library().flashoptim_mx4_quantize
+    for rows, cols in ((1 << 29, 1), (1 << 30, 1), (1 << 30, 8), ((1 << 31) - 1, 1), (1 << 29, 63)):
+        x, out_t = B._Matrix(4096, rows, cols, cols, 0), B._Mx4(4096, 4096, cols, rows)
+        assert call(x, None, None, None, out_t, None) == -3, (rows, cols)
+        assert call(x, None, 4096, None, out_t, None) == -3, (rows, cols)
+    # and whatever is accepted, by itself or with `out` (2^27 segments at most in either direction), fits
+    out = _run(tmp_path, """
+    long long accepted = 0, wrong = 0;
+    for (int r = 0; r <= 31; ++r)
+        for (int c = 0; c <= 31; ++c)
+            for (int d = -1; d <= 1; ++d) {
+                const int64_t rows = ((int64_t)1 << r) + d, cols = ((int64_t)1 << c) + d;
+                if (rows < 1 || cols < 1 || rows >= (int64_t)1 << 31 || cols >= (int64_t)1 << 31) continue;
+                const bool fits = fo::quantize_fits(rows, cols), lanes = fo::quantize_tiles(rows, cols) * 256 < (int64_t)1 << 32;
+                wrong += fits != lanes;
+                if (fo::quantize_tile_rows(rows, cols) == 64) wrong += fits != (fo::up(rows, 256) * fo::up(cols, 256) < 1 << 21);
+                else wrong += !fits;
+                const bool both = rows * (fo::up(cols, 256) + 1) <= 1 << 27 && cols * (fo::up(rows, 256) + 1) <= 1 << 27;
+                wrong += both && !fits;
+                accepted += fits;
+            }
+    std::printf("%lld %lld\\n", accepted, wrong);
+    """)
+    accepted, wrong = (int(x) for x in out[0].split())
+    assert accepted > 1000 and wrong == 0
