@@ -360,7 +360,8 @@ int flashoptim_mx4_dequantize(const flashoptim_mx4* q, const flashoptim_matrix* 
  * matmul: c [m, n] <- a [m, k] b [n, k]^T.
  * linear: y [m, n] <- Q(x) w^T with x [m, k] quantised to nearest along its rows and w [n, k]; if xt [k, m] is not NULL, Q(x^T) is
  *   left there for the backward pass.  Without xt a few rows are one launch, made for single tokens, through which the weights stream
- *   once: up to 16 rows, fewer with long ones (16 of 6144 values, 6 of 16384, half as many where the rows of w take a second round of workgroups).
+ *   once: up to 16 rows, fewer with long ones (16 of 6144 values, 6 of 16384, half as many where the rows of w take a second round of workgroups).  That
+ *   launch takes no workspace: NULL will do.
  * linear_backward: dx [m, k] <- Q(dy) wt^T and dw [n, k] <- Q(dy^T) xt^T, with dy [m, n] quantised along its rows and along
  *   its columns in one pass (stochastically with `rand`), wt [k, n] the transposed weights in 4 bits (quantize's out_t) and xt [k, m].
  *   dx or dw may be NULL, and with it wt or xt.  These are the gradients of the product of its quantised operands, the

@@ -553,7 +553,8 @@ def mx4_matmul(a, b, out, workspace=None, stream=None):
 
 
 def mx4_linear(x, w, out, xt=None, workspace=None, stream=None):
-    """out [m, n] <- Q(x) w^T with x [m, k] quantised on the way, w an Mx4Tensor [n, k]; xt: Mx4Tensor [k, m] for Q(x^T)."""
+    """out [m, n] <- Q(x) w^T with x [m, k] quantised on the way, w an Mx4Tensor [n, k]; xt: Mx4Tensor [k, m] for Q(x^T).  Without xt
+    a few rows, up to 16 where they are not long, are one launch that takes no workspace."""
     status = (_fast or _marshal()).linear(x, w.address, None if xt is None else xt.address, out, workspace, _handle(stream))
     if status:
         raise FlashOptimError(status, "flashoptim_mx4_linear")

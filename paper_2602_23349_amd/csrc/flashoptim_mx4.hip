@@ -1183,8 +1183,9 @@ int flashoptim_mx4_linear(const flashoptim_matrix* x, const flashoptim_mx4* w, c
     if (xt) FO_TRY(check_mx4(xt));
     if (w->cols != x->cols || y->rows != x->rows || y->cols != w->rows) return FLASHOPTIM_ERR_INVALID_ARG;
     if (xt && (xt->rows != x->cols || xt->cols != x->rows)) return FLASHOPTIM_ERR_INVALID_ARG;
-    FO_TRY(check_workspace(workspace, workspace_bytes, flashoptim_mx4_linear_workspace(x->rows, w->rows, x->cols)));
+    FO_TRY(check_sizes(x->rows, w->rows, x->cols));
     if (!xt && takes_few_rows(x->rows, y->cols, x->cols)) return linear_few_rows(*x, *w, *y, (hipStream_t)stream);
+    FO_TRY(check_workspace(workspace, workspace_bytes, flashoptim_mx4_linear_workspace(x->rows, w->rows, x->cols)));
     uint8_t* at = (uint8_t*)workspace;
     const flashoptim_mx4 q = carve(at, x->rows, x->cols);
     FO_TRY(quantize(*x, nullptr, nullptr, &q, xt, (hipStream_t)stream));

@@ -341,3 +341,15 @@ def test_refusals():
                  lambda: fo.Mx4Tensor(40, 64, buffers=(q.codes, q.scales[:, :8]))):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 48, 64), (1, 4096, 4096), (16, 300, 1000)])
+def test_a_few_rows_take_no_workspace(m, n, k):
+    x = torch.randn(m, k, device="cuda", generator=torch.Generator("cuda").manual_seed(m)).bfloat16()
+    w, wv = random_matrix(n, k, "w")
+    out = torch.full((m, n), float("nan"), dtype=torch.bfloat16, device="cuda")
+    fo.mx4_linear(x, w, out)
+    check_product(out, R.values(*R.quantize(x.double().cpu().numpy())), wv)
+    status = lambda **kw: pytest.raises(fo.FlashOptimError, fo.mx4_linear, x, w, out, **kw).value.status        # noqa: E731
+    assert status(xt=fo.Mx4Tensor(k, m)) == -1              # Q(x) of the training form goes through memory
+    assert status(xt=fo.Mx4Tensor(k, m), workspace=scratch(16)) == -8
