@@ -7,6 +7,13 @@
 
 #include "flashoptim.h"
 
+// Returns from the function with the status of `expr` if that is not FLASHOPTIM_OK.
+#define FO_TRY(expr)                          \
+    do {                                      \
+        const int rc_ = (int)(expr);          \
+        if (rc_ != FLASHOPTIM_OK) return rc_; \
+    } while (0)
+
 namespace fo {
 
 // FLASHOPTIM_OK, or FLASHOPTIM_ERR_HIP after noting `e` for flashoptim_last_hip_error.

@@ -7,6 +7,9 @@
 
 namespace fo {
 
+// n in whole units.
+constexpr int64_t up(int64_t n, int64_t unit) { return (n + unit - 1) / unit; }
+
 // A launch over a list maps workgroup b to (tensor, tile), or in a copy to (segment, piece), in two steps:
 // coarse[b >> shift] is the table entry that holds workgroup (b >> shift) << shift, coarse[(b >> shift) + 1] the next such (behind
 // the last one: the table's last entry), and entry_of searches between the two (usually they are the same).  Both tables

@@ -5,13 +5,13 @@
 
 #include <stdint.h>
 
+#include "flashoptim_launch.h"
+
 namespace fo {
 
 constexpr int kBlock = 32;                  // values that share a scale
 constexpr int kSegment = 256;               // a row of codes is filled up to a multiple of this many values
 constexpr int kSegmentBytes = kSegment / 2;
-
-constexpr int64_t up(int64_t n, int64_t unit) { return (n + unit - 1) / unit; }
 
 // Quantisation along columns, or both ways: tiles of this many rows by 128 columns, over rows and columns filled up to whole segments.
 // Rows of a tile, in us with 32 / 64 / 128: BF16, 1024 x 2304 4.4 / 4.8 / 6.1, 8192 x 4096 25.2 / 24.2 / 26.2, 14336 x 4096 38.7 / 36.5 / 38.4,

@@ -14,21 +14,24 @@
 
 #include "flashoptim.h"
 #include "flashoptim_host.h"
+#include "flashoptim_layers.h"
 #include "flashoptim_mx4.h"
 
 namespace {
 
-using i32x4 = int __attribute__((ext_vector_type(4)));
 using i32x8 = int __attribute__((ext_vector_type(8)));
-using f32x4 = float __attribute__((ext_vector_type(4)));
 using bf16x4 = __bf16 __attribute__((ext_vector_type(4)));
 
+using fo::f32x4;
+using fo::i32x4;
 using fo::kBlock;
 using fo::kScaleBytes;
 using fo::kScaleSteps;
 using fo::kSegment;
 using fo::kSegmentBytes;
 using fo::kTileCols;
+using fo::load_as;
+using fo::store_as;
 using fo::up;
 
 // A 4-bit matrix as a kernel takes it.
@@ -52,21 +55,11 @@ struct Source {
     uint32_t rows, cols;
 };
 
-template <typename T>
-__device__ __forceinline__ T load_as(const void* p) {       // any alignment: the hardware takes global accesses at any byte
-    T v;
-    __builtin_memcpy(&v, p, sizeof(T));
-    return v;
-}
-// The same of data that this kernel reads once: it leaves the caches to what is read again.
+// load_as of data that this kernel reads once: it leaves the caches to what is read again.
 template <typename T, int ALIGN>
 __device__ __forceinline__ T load_once(const void* p) {
     typedef T Unaligned __attribute__((aligned(ALIGN)));
     return __builtin_nontemporal_load((const Unaligned*)p);
-}
-template <typename T>
-__device__ __forceinline__ void store_as(void* p, T v) {
-    __builtin_memcpy(p, &v, sizeof(T));
 }
 
 __device__ __forceinline__ float bf16_value(uint32_t bits) { return __uint_as_float(bits << 16); }
@@ -1114,12 +1107,6 @@ int check_workspace(const void* workspace, int64_t bytes, int64_t need) {
     if (bytes < need) return FLASHOPTIM_ERR_WORKSPACE;
     return fo::aligned_to(workspace, 16) ? FLASHOPTIM_OK : FLASHOPTIM_ERR_MISALIGNED;
 }
-
-#define FO_TRY(expr)                          \
-    do {                                      \
-        const int rc_ = (int)(expr);          \
-        if (rc_ != FLASHOPTIM_OK) return rc_; \
-    } while (0)
 
 }  // namespace
 

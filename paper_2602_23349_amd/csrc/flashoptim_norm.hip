@@ -15,24 +15,19 @@
 
 #include "flashoptim.h"
 #include "flashoptim_host.h"
+#include "flashoptim_launch.h"
+#include "flashoptim_layers.h"
 
 namespace {
 
-using i32x4 = int __attribute__((ext_vector_type(4)));
-using f32x4 = float __attribute__((ext_vector_type(4)));
+using fo::f32x4;
+using fo::i32x4;
+using fo::load_as;
+using fo::store_as;
+using fo::up;
 using f32x8 = float __attribute__((ext_vector_type(8)));
 using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
 
-template <typename T>
-__device__ __forceinline__ T load_as(const void* p) {       // any alignment: the hardware takes global accesses at any byte
-    T v;
-    __builtin_memcpy(&v, p, sizeof(T));
-    return v;
-}
-template <typename T>
-__device__ __forceinline__ void store_as(void* p, T v) {
-    __builtin_memcpy(p, &v, sizeof(T));
-}
 
 // A matrix as a kernel takes it; data NULL: left out.
 struct Rows {
@@ -614,12 +609,6 @@ int check_rows(const flashoptim_matrix* m, int64_t rows, int64_t cols, int dtype
     return m->rows == rows && m->cols == cols && m->dtype == dtype ? FLASHOPTIM_OK : FLASHOPTIM_ERR_INVALID_ARG;
 }
 
-#define FO_TRY(expr)                          \
-    do {                                      \
-        const int rc_ = (int)(expr);          \
-        if (rc_ != FLASHOPTIM_OK) return rc_; \
-    } while (0)
-
 // The gate's rows, 0 without a gate.
 int check_gate(const flashoptim_matrix* gate, int64_t rows, int64_t cols, int dtype, int64_t* rows_per_gate) {
     *rows_per_gate = rows > 0 ? rows : 1;
@@ -648,8 +637,6 @@ void with_shape(int64_t cols, F launch) {
     else if (cols <= 8192) launch(Shape<512, 2>{});
     else launch(Shape<512, 4>{});
 }
-
-inline int64_t up(int64_t n, int64_t unit) { return (n + unit - 1) / unit; }
 
 // How the rows of a backward call are cut into parts.
 struct Parts {
