@@ -492,8 +492,6 @@ template <int ROWS>
 struct Scales {
     uint8_t bytes[ROWS * kScaleBytes];
 };
-constexpr int64_t kMaxTiledTerms = (int64_t)1 << 23;      // 256 rows of codes stay below 2^31 bytes, which a lane's offset reaches
-
 #define FO_LDS(p) ((__attribute__((address_space(3))) void*)(p))
 
 // `bytes` bytes from p on as a buffer; an address into it is a lane's 32-bit offset.
@@ -762,7 +760,7 @@ __device__ __forceinline__ i32x4 move_down(i32x4 w, int left) {
 template <int SRC, bool FP32, int WAVES, int TILES>
 __global__ __launch_bounds__(64 * WAVES) void linear_small(Few a) {
     extern __shared__ __align__(16) uint8_t lds[];
-    constexpr int kAhead = 2;      // segments of a wavefront's weights that are on their way at a time
+    constexpr int kAhead = fo::kFewAhead;
     const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64, q = lane / 16, x_row = lane % 16;
     const uint32_t segments = a.w.segments;
     const uint8_t *codes[TILES], *scales[TILES];
@@ -837,7 +835,7 @@ __global__ __launch_bounds__(64 * WAVES) void linear_small(Few a) {
     };
     if (a.x.cols >= 8) {
         if (total <= 64 * WAVES) quantize(std::integral_constant<int, 1>{});
-        else quantize(std::integral_constant<int, 4>{});
+        else quantize(std::integral_constant<int, fo::kFewBatch>{});
     } else {
         load(now, wave);
         for (uint32_t item = threadIdx.x; item < total; item += 64 * WAVES) {
@@ -945,25 +943,10 @@ int quantize(const flashoptim_matrix& x, const int8_t* rho, const uint8_t* rand,
 // Calls launch with the number of wavefronts that share out a sum over this many segments.
 template <typename F>
 void with_waves(int64_t segments, F launch) {
-    if (segments <= 4) launch(std::integral_constant<int, 4>{});
-    else if (segments <= 16) launch(std::integral_constant<int, 8>{});
+    const int waves = fo::sum_waves(segments);
+    if (waves == 4) launch(std::integral_constant<int, 4>{});
+    else if (waves == 8) launch(std::integral_constant<int, 8>{});
     else launch(std::integral_constant<int, 16>{});
-}
-
-// How a product of m by n sums over k terms is made: by the largest tiles of which there are enough.  In us, with tiles of 16 (the wavefronts of a
-// workgroup share out the sum) / 64 / 128 / 256:
-//   kTiny while they are at most 256 tiles: 33 x 64 x 7600 (m, n, k) 6.1 / 9.6 / 16 / 39, 200 x 200 x 14000 11.1 / 16.2 / 28 / 71, 40 x 500 x 300
-//     2.4 / 3.1 / 4.0 / 6.2; 90 x 950 x 950, 360 of them, 3.5 / 3.6, 600 x 600 x 600, 1444, 5.2 / 3.5;
-//   kTile256 from 192 tiles on, three quarters of the compute units: 3000 x 4096 x 4096 - / 53 / 39.5 / 36.1; with 128 of them, 2048 x 4096 x 4096,
-//     - / 37 / 26.6 / 32.7;
-//   kTile64 up to 512 tiles, which is two for each compute unit: 512 x 4096 x 4096 86 / 10.4 / 12.1, 2304 x 768 x 1024 - / 5.2 / 6.2, 768 x 768 x 8000 49 /
-//     10.8 / 19.8; kTile128 beyond: 1001 x 2304 x 768, 576 of them, - / 7.0 / 6.2, 1024 x 4096 x 4096 - / 19.5 / 15.7, 8192 x 768 x 768 - / 12.1 / 9.9.
-// Sums split over workgroups and joined by another launch: 768 x 768 x 8000 in two 13.5, in four 16.2.
-enum Shape { kTiny, kTile64, kTile128, kTile256 };
-Shape product_shape(int64_t m, int64_t n, int64_t k) {
-    if (k > kMaxTiledTerms || up(m, 16) * up(n, 16) <= 256) return kTiny;
-    if (up(m, 256) * up(n, 256) >= 192) return kTile256;
-    return m > 64 && n > 64 && up(m, 64) * up(n, 64) > 512 ? kTile128 : kTile64;
 }
 
 Result to_dev(const flashoptim_matrix& c) { return {c.data, c.stride, (uint32_t)c.rows, (uint32_t)c.cols}; }
@@ -975,7 +958,7 @@ struct Operands {
 
 // Every c = a b^T, all of one type and shape of tiles, in one launch.
 template <bool FP32, typename... T>
-int launch_tiles(Shape shape, hipStream_t stream, const T&... operands) {
+int launch_tiles(fo::Shape shape, hipStream_t stream, const T&... operands) {
     constexpr int kCount = sizeof...(operands);
     auto launch = [&](auto kernel, int edge, int threads) {
         auto product = [&](const Operands& o) {
@@ -984,8 +967,8 @@ int launch_tiles(Shape shape, hipStream_t stream, const T&... operands) {
         const Products<kCount> p = {{product(operands)...}};
         hipLaunchKernelGGL(kernel, dim3(p.of[0].tiles + (kCount > 1 ? p.of[kCount - 1].tiles : 0)), dim3(threads), 0, stream, p);
     };
-    if (shape == kTile256) launch(product_tiles<kCount, FP32, 256, 256, 4, 2, 2, 2>, 256, 512);
-    else if (shape == kTile128) launch(product_tiles<kCount, FP32, 128, 128, 2, 2, 2, 2>, 128, 256);
+    if (shape == fo::kTile256) launch(product_tiles<kCount, FP32, 256, 256, 4, 2, 2, 2>, 256, 512);
+    else if (shape == fo::kTile128) launch(product_tiles<kCount, FP32, 128, 128, 2, 2, 2, 2>, 128, 256);
     else launch(product_tiles<kCount, FP32, 64, 64, 2, 2, 4, 2>, 64, 256);
     return fo::hip_status(hipGetLastError());
 }
@@ -998,8 +981,8 @@ int product(const flashoptim_mx4& a, const flashoptim_mx4& b, const flashoptim_m
         hipLaunchKernelGGL(fill_zero, dim3((unsigned)up(c.cols, 256), (unsigned)(c.rows < 1024 ? c.rows : 1024)), dim3(256), 0, stream, r, fp32 ? 4 : 2);
         return fo::hip_status(hipGetLastError());
     }
-    const Shape shape = product_shape(c.rows, c.cols, a.cols);
-    if (shape != kTiny)
+    const fo::Shape shape = fo::product_shape(c.rows, c.cols, a.cols);
+    if (shape != fo::kTiny)
         return fp32 ? launch_tiles<true>(shape, stream, Operands{a, b, c}) : launch_tiles<false>(shape, stream, Operands{a, b, c});
     const uint32_t pt = (uint32_t)up(c.cols, 16), qt = (uint32_t)up(c.rows, 16);
     auto launch = [&](auto waves) {
@@ -1014,54 +997,26 @@ int product(const flashoptim_mx4& a, const flashoptim_mx4& b, const flashoptim_m
 // Two products that do not depend on each other, in one launch where they go by the same tiles.
 int two_products(const Operands& x, const Operands& y, hipStream_t stream) {
     auto empty = [](const Operands& o) { return o.c.rows == 0 || o.c.cols == 0 || o.a.cols == 0; };
-    const Shape shape = product_shape(x.c.rows, x.c.cols, x.a.cols);
-    if (empty(x) || empty(y) || x.c.dtype != y.c.dtype || shape == kTiny || shape != product_shape(y.c.rows, y.c.cols, y.a.cols)) {
+    const fo::Shape shape = fo::product_shape(x.c.rows, x.c.cols, x.a.cols);
+    if (empty(x) || empty(y) || x.c.dtype != y.c.dtype || shape == fo::kTiny || shape != fo::product_shape(y.c.rows, y.c.cols, y.a.cols)) {
         const int rc = product(x.a, x.b, x.c, stream);
         return rc != FLASHOPTIM_OK ? rc : product(y.a, y.b, y.c, stream);
     }
     return x.c.dtype == FLASHOPTIM_FP32 ? launch_tiles<true>(shape, stream, x, y) : launch_tiles<false>(shape, stream, x, y);
 }
 
-constexpr int64_t kFewRows = 16;
-
-// How linear_small goes about it: tiles of 16 columns to a workgroup, and wavefronts.  In us:
-//   two tiles where one each would be more than one workgroup for each compute unit: 6000 x 6000 (n, k), 375 tiles, 1 row 8.4 with one, 8.0 with two, 16
-//     rows 17.6, 12.5; 14336 x 4096 1 row 10.2, 9.2, 8 rows 14.1, 11.8; 8192 x 2048 1 row 4.4, 4.6, 16 rows 7.0, 6.2;
-//   16 wavefronts where there is no more than one workgroup for each compute unit, and many segments or rows: 4096 x 4096 with 8 / 16, 1 row 4.3 / 4.5, 16 rows
-//     8.0 / 6.9; 6000 x 6000 as above 8.4 / 8.0 and 14.4 / 12.5; 14336 x 4096 9.2 / 11.4;
-//   4 for up to four segments and few rows: 12000 x 500 with 4 / 8, 1 row 3.9 / 4.0, 16 rows 4.8 / 4.4.
-struct FewPlan {
-    int tiles, waves;
-    int64_t workgroups;
-};
-FewPlan plan_few(int64_t m, int64_t n, int64_t k) {
-    const int64_t tiles = up(n, 16), segments = up(k, kSegment);
-    FewPlan p = {tiles > 256 ? 2 : 1, 8, 0};
-    p.workgroups = up(tiles, p.tiles);
-    if (segments <= 4) p.waves = m >= 8 ? 8 : 4;
-    else if (p.workgroups <= 256 && (m >= 4 || segments > 16)) p.waves = 16;
-    return p;
-}
-// Whether x is quantised by every workgroup of linear_small, or once by a launch of its own: by the work on x that a compute unit then has.  One launch /
-// two, us: 4096 x 4096 with 1 row 4.4 / 6.5, 16 rows 6.9 / 7.8; 4096 x 14336 4 rows 11.4 / 12.2, 8 rows 14.3 / 13.5; 14336 x 4096 8 rows 11.8 / 11.3, 16 rows
-// 15.0 / 11.3; 6000 x 6000 16 rows 12.5 / 13.6.
-constexpr int64_t kFewValues = 98304;
-
 // What linear_small keeps of x in LDS: rows of codes begin 16 bytes apart in the banks.
 int64_t few_code_pitch(int64_t k) { return up(k, kSegment) * kSegmentBytes + 16; }
 int64_t few_scale_pitch(int64_t k) { return up(k, kSegment) * 8 + 8; }
 // Exact for items and units below 2^16 (there are at most 12288 units of eight).
 uint32_t few_units_magic(int64_t k) { return (uint32_t)(((uint64_t)1 << 32) / (uint64_t)(up(k, kSegment) * (kSegment / 8)) + 1); }
-bool takes_few_rows(int64_t m, int64_t n, int64_t k) {
-    return m >= 1 && m <= kFewRows && n >= 1 && k >= 1 && m * up(k, kSegment) * kSegment * up(plan_few(m, n, k).workgroups, 256) <= kFewValues;
-}
 
 int linear_few_rows(const flashoptim_matrix& x, const flashoptim_mx4& w, const flashoptim_matrix& y, hipStream_t stream) {
     const Few a = {{x.data, nullptr, nullptr, x.stride, (uint32_t)x.rows, (uint32_t)x.cols}, to_dev(w), {y.data, y.stride, (uint32_t)y.rows, (uint32_t)y.cols},
                    (uint32_t)few_code_pitch(x.cols), (uint32_t)few_scale_pitch(x.cols), few_units_magic(x.cols)};
     const bool fp32 = y.dtype == FLASHOPTIM_FP32, x_fp32 = x.dtype == FLASHOPTIM_FP32;
     const int64_t x_bytes = x.rows * (few_code_pitch(x.cols) + few_scale_pitch(x.cols));
-    const FewPlan p = plan_few(x.rows, y.cols, x.cols);
+    const fo::FewPlan p = fo::plan_few(x.rows, y.cols, x.cols);
     auto launch = [&](auto waves, auto tiles) {
         constexpr int W = decltype(waves)::value, T = decltype(tiles)::value;
         const int64_t part_bytes = W * T * 1024;
@@ -1171,7 +1126,7 @@ int flashoptim_mx4_linear(const flashoptim_matrix* x, const flashoptim_mx4* w, c
     if (w->cols != x->cols || y->rows != x->rows || y->cols != w->rows) return FLASHOPTIM_ERR_INVALID_ARG;
     if (xt && (xt->rows != x->cols || xt->cols != x->rows)) return FLASHOPTIM_ERR_INVALID_ARG;
     FO_TRY(check_sizes(x->rows, w->rows, x->cols));
-    if (!xt && takes_few_rows(x->rows, y->cols, x->cols)) return linear_few_rows(*x, *w, *y, (hipStream_t)stream);
+    if (!xt && fo::takes_few_rows(x->rows, y->cols, x->cols)) return linear_few_rows(*x, *w, *y, (hipStream_t)stream);
     FO_TRY(check_workspace(workspace, workspace_bytes, flashoptim_mx4_linear_workspace(x->rows, w->rows, x->cols)));
     uint8_t* at = (uint8_t*)workspace;
     const flashoptim_mx4 q = carve(at, x->rows, x->cols);

@@ -91,3 +91,37 @@ def test_quantisation_beyond_one_launch_is_refused(tmp_path):
     """)
     accepted, wrong = (int(x) for x in out[0].split())
     assert accepted > 1000 and wrong == 0
+
+
+def test_sizes_of_the_tests_reach_every_way_of_dispatch(tmp_path):
+    import mx4_sizes as S
+    rows = "".join(f"product({m}, {n}, {k});\n" for _, m, n, k in S.PRODUCTS)
+    rows += "".join(f"product({m}, {k}, {n}); product({n}, {k}, {m});\n" for _, m, n, k in S.GRADIENTS)
+    rows += "".join(f"few({m}, {n}, {k});\n" for _, m, n, k in S.FEW) + "".join(f"quantised({r}, {c});\n" for _, r, c in S.QUANTISED)
+    out = _run(tmp_path, """
+    auto product = [](int64_t m, int64_t n, int64_t k) {
+        const fo::Shape s = fo::product_shape(m, n, k);
+        if (s == fo::kTiny) std::printf("16, %d wavefronts\\n", fo::sum_waves(fo::up(k, fo::kSegment)));
+        else std::printf("%d\\n", s == fo::kTile64 ? 64 : s == fo::kTile128 ? 128 : 256);
+    };
+    auto few = [](int64_t m, int64_t n, int64_t k) {
+        const fo::FewPlan p = fo::plan_few(m, n, k);
+        const int64_t segments = fo::up(k, fo::kSegment), units = m * segments * (fo::kSegment / 8);
+        if (!fo::takes_few_rows(m, n, k)) std::printf("no ");
+        std::printf("%d x %d%s%s%s\\n", p.waves, p.tiles, segments > fo::kFewAhead * p.waves ? ", w" : "",
+                    units > 64 * p.waves * fo::kFewBatch ? ", x" : "", p.workgroups > 256 ? ", 2 each" : "");
+    };
+    auto quantised = [](int64_t r, int64_t c) { std::printf("%d%s\\n", fo::quantize_tile_rows(r, c), r > 1024 ? ", bands" : ""); };
+    """ + rows)
+    pairs = [out.pop(len(S.PRODUCTS)) for _ in range(2 * len(S.GRADIENTS))]
+    joined = [a if a == b else f"{a}, {b}" for a, b in zip(pairs[0::2], pairs[1::2])]
+    assert joined == [g[0] for g in S.GRADIENTS]
+    assert out == [s[0] for s in S.PRODUCTS + S.FEW + S.QUANTISED]
+    # all there are: a sum's wavefronts and the tiles, each tile alone and in joint launches; wavefronts by tiles of few rows, with
+    # further rounds where there can be any; both tiles of the quantisation
+    assert {s[0] for s in S.PRODUCTS} == {f"16, {w} wavefronts" for w in (4, 8, 16)} | {"64", "128", "256"}
+    assert {"64", "128", "256"} < set(joined)
+    ways = {s[0] for s in S.FEW}
+    assert {way.split(",")[0] for way in ways} == {f"{w} x {t}" for w in (4, 8, 16) for t in (1, 2)}
+    assert {"16 x 1, w, x", "16 x 2, w, x", "8 x 2, x, 2 each", "8 x 2, w, x, 2 each"} <= ways
+    assert {s[0] for s in S.QUANTISED} == {"32", "32, bands", "64", "64, bands"}
