@@ -349,3 +349,29 @@ def test_gradients_of_saturated_gates():
     want = f64(without) / (1 + np.exp(-g)) / (1 + np.exp(g))
     off = np.abs(f64(c.grads["dgate"]) - want)
     assert (off <= (2 * np.abs(g) + 16) * U * np.abs(want)).all(), np.nanmax(off / np.abs(want)) / U
+
+
+def test_only_the_given_stream_is_launched_on():
+    # Captured on one stream and called on another, which is not captured: what goes to the given stream is in the graph and nothing of it has
+    # run when the capture ends; the current stream, on which it would have run at once, has seen nothing.
+    c = Case(300, 2000, "layer", gates=3, act="sigmoid")
+    ws = torch.empty(fo.block_norm_backward_workspace(c.spec, 300, 3), dtype=torch.uint8, device="cuda")
+    c.run().backward(workspace=ws)
+    outs = (c.h, c.y, c.stats, *c.grads.values())
+    want = [t.clone() for t in outs]
+    for t in outs:
+        t.fill_(7)
+    torch.cuda.synchronize()
+    side, other, graph = torch.cuda.Stream(), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        graph.capture_begin(capture_error_mode="relaxed")
+    with torch.cuda.stream(other):
+        fo.block_norm(c.spec, c.x, f=c.f, gate=c.gate, h=c.h, y=c.y, stats=c.stats, stream=side)
+        fo.block_norm_backward(c.spec, c.h, c.stats, f=c.f, gate=c.gate, dy=c.dy, dh=c.dh, workspace=ws, stream=side, **c.grads)
+    with torch.cuda.stream(side):
+        graph.capture_end()
+    torch.cuda.synchronize()
+    assert all(bool((t == 7).all()) for t in outs)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, outs))

@@ -214,3 +214,43 @@ def test_quantisation_both_ways(way, rows, cols, source, random):
         width, blocks = pt.codes.shape[1], -(-(end - begin) // 32)
         assert torch.equal(qt.codes[:, begin // 2:begin // 2 + width], pt.codes)
         assert torch.equal(qt.scales[:, begin // 32:begin // 32 + blocks], pt.scales[:, :blocks])
+
+
+def test_only_the_given_stream_is_launched_on():
+    # Captured on one stream and called on another, which is not captured: what goes to the given stream is in the graph and nothing of it has
+    # run when the capture ends; the current stream, on which it would have run at once, has seen nothing.
+    cases = [(1, 300, 1000), (65, 200, 700), (300, 500, 640)]
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    for m, n, k in cases:
+        x, w, wt = inputs(m, k, BF16, "x"), random_matrix(n, k, "w"), random_matrix(k, n, "wt")
+        ws = scratch(max(fo.mx4_linear_workspace(m, n, k), fo.mx4_linear_backward_workspace(m, n, k)))
+        q, xt = fo.Mx4Tensor(m, k), fo.Mx4Tensor(k, m)
+        back, few, y, c = (torch.empty(m, s, device="cuda") for s in (k, n, n, n))
+        dx, dw = torch.empty(m, k, device="cuda"), torch.empty(n, k, device="cuda")
+        outs = (q.codes, q.scales, xt.codes, xt.scales, back, few, y, c, dx, dw)
+
+        def calls(stream=None):
+            fo.mx4_quantize(x, q, stream=stream)
+            fo.mx4_dequantize(q, back, stream=stream)
+            fo.mx4_linear(x, w, few, workspace=ws, stream=stream)
+            fo.mx4_linear(x, w, y, xt=xt, workspace=ws, stream=stream)
+            fo.mx4_matmul(q, w, c, stream=stream)
+            fo.mx4_linear_backward(y, wt, xt, dx, dw, workspace=ws, stream=stream)
+
+        calls()
+        want = [t.clone() for t in outs]
+        for t in outs:
+            t.fill_(0x55 if t.dtype == torch.uint8 else 7)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(side):
+            graph.capture_begin(capture_error_mode="relaxed")
+        with torch.cuda.stream(other):
+            calls(side)
+        with torch.cuda.stream(side):
+            graph.capture_end()
+        torch.cuda.synchronize()
+        assert all(bool((t == (0x55 if t.dtype == torch.uint8 else 7)).all()) for t in outs)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, outs))
