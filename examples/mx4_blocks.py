@@ -40,6 +40,7 @@ class Linear:
         self.n, self.k = n, k
         self.weight = Param(torch.randn(n, k, generator=g, device="cuda") * k ** -0.5, weight_decay=0.01)
         self.w, self.wt = fo.Mx4Tensor(n, k), fo.Mx4Tensor(k, n)
+        self.xt = None                    # x transposed, for the backward pass; the same memory in every step
         self.refresh()
 
     def refresh(self):
@@ -47,8 +48,9 @@ class Linear:
 
     def forward(self, x, workspace, keep):
         y = empty(x.shape[0], self.n)
-        self.xt = fo.Mx4Tensor(self.k, x.shape[0]) if keep else None
-        fo.mx4_linear(x, self.w, y, xt=self.xt, workspace=workspace)
+        if keep and (self.xt is None or self.xt.cols != x.shape[0]):
+            self.xt = fo.Mx4Tensor(self.k, x.shape[0])
+        fo.mx4_linear(x, self.w, y, xt=self.xt if keep else None, workspace=workspace)
         return y
 
     def backward(self, dy, workspace, rand):

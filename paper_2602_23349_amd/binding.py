@@ -495,8 +495,8 @@ def _handle(stream):
 
 class Mx4Tensor:
     """A matrix of rows by cols values in microscaled 4 bits: `codes` [rows, 128 ceil(cols/256)] and `scales`
-    [rows, 16 ceil(cols/512)], both uint8, laid out as flashoptim.h describes.  `buffers`: a (codes, scales) pair to use
-    instead of new ones."""
+    [rows, 16 ceil(cols/512)], both uint8, laid out as flashoptim.h describes.  A new one is a matrix of
+    zeros; `buffers`: a (codes, scales) pair to use instead of new memory, of which a call that writes the matrix writes every byte."""
 
     def __init__(self, rows, cols, device="cuda", buffers=None):
         self.rows, self.cols = int(rows), int(cols)
