@@ -32,7 +32,7 @@ constexpr int kScaleTerms = 1024, kScaleBytes = kScaleTerms / kBlock, kScaleStep
 constexpr int code_swizzle(int row) { return row >> 1 & 7; }
 constexpr int scale_swizzle(int row) { return row >> 3 & 1; }
 
-// Where a lane of wavefront `wave` finds what its i-th copy takes, from the tile's first row and the step's first byte on.  Rows begin `pitch` bytes
+// Where a lane finds what copy number `copy` of a tile takes, from the tile's first row and the step's first byte on.  Rows begin `pitch` bytes
 // apart; behind row `last`, the matrix's last one in the tile, it takes that row again.
 constexpr int code_row(int copy, int lane) { return copy * 8 + lane / 8; }
 constexpr uint32_t code_place(int copy, int lane, uint32_t last, uint32_t pitch) {

@@ -474,8 +474,10 @@ __global__ __launch_bounds__(64 * WAVES) void product_small(Mx4 b, Mx4 a, Result
 // BP / WP by BQ / WQ values in tiles of 32 by 32, whose instruction takes 64 terms: half h of its lanes takes blocks 4 h .. 4 h + 3 of the
 // segment in four turns, so that a lane's four scales are one word.
 //
-// What bounds it: the matrix cores and the package's power.  8192 x 8192 x 8192: 266 us, 4.1 PFLOP/s; with all codes zero, which
-// costs less power, 207 us, 5.3 PFLOP/s.  What it took, for 8192 x 8192 x 8192:
+// What bounds it: 8192 x 14336 x 4096 takes 430 thousand cycles, in 229 thousand of which the matrix cores are busy; between the products of two
+// segments lie the meeting of all wavefronts and their first reads of LDS behind it.  And the package's power, which holds the clock at 1.82 GHz: 236 us, 4.1
+// PFLOP/s; with all codes zero, in as many cycles at 2.39 GHz, 178 us, 5.4 PFLOP/s.  8192 x 8192 x 8192 246 us, 4.5 PFLOP/s, zeros 185, 5.9.
+// What it took, for 8192 x 8192 x 8192 as it was before the results left through LDS:
 //   * scales for 1024 terms at a time instead of 256 (a copy's rows pass the memory pipe one after the other, and 8 bytes of a row take it
 //     as long as 128): 305 -> 300 us, and with 128 by 128 tiles 357 -> 296;
 //   * the next segment's copies go out one by one between the products (together, all wavefronts of a workgroup queue up in front of the memory
@@ -696,7 +698,7 @@ __global__ __launch_bounds__(64 * WP * WQ, RESIDENT) void product_tiles(Products
     wait_copies<0>();
     meet();
     // Out through LDS, 32 rows of c at a time, so that a wavefront's stores are whole pieces of rows: a lane has four neighbouring columns of 32 rows, and
-    // stores of those, 16 bytes of each row, would take the memory pipe as long as the products (8192 x 14336 x 4096: 285 us, and 230 so).
+    // stores of those, 16 bytes of each row, would take the memory pipe as long as the products (8192 x 14336 x 4096: 285 us, and 231-237 so).
     constexpr int kValue = FP32 ? 4 : 2, kRow = BP / WP * kValue, kPitch = kRow + 16, kLanes = kRow / 16, kRows = 64 / kLanes;
     static_assert(kWaves * 32 * kPitch <= (int)sizeof(Lds), "a slab for each wavefront");
     uint8_t* const slab = (uint8_t*)&lds + wave * 32 * kPitch;

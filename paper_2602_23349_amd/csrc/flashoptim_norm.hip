@@ -5,8 +5,9 @@
 //   dx = a dH,  dgate = sum c dH u act',  du = c dH act,  df = the same through the norm behind
 //   dw' = sum dy hat(h),  db' = sum dy,  dw = sum du hat(f),  db = sum du       (over rows)
 // Bound: HBM.  A row is loaded once, kept in registers through all its sums, which are FP32, and stored once (of the widest rows in the backward pass
-// see norm_gradients).  RMS norms of 4096 BF16 values: 16384 rows forward with a branch as it is 92 us, 5.8 TB/s; 8192 rows backward with
-// both norms and a gate 91 us with the sums over rows, 4.4 TB/s.  One row forward 3.1 us.
+// see norm_gradients).  RMS norms of 4096 BF16 values: 16384 rows forward with a branch as it is 91 us, 5.9 TB/s; 8192 rows backward with
+// both norms and a gate 90 us with the sums over rows, 4.5 TB/s.  One row forward 3.2 us.  Forward, rows wider than 4096 with a branch, as it is / normalised: 4096
+// rows of 8192 BF16 values 62 / 74 us (4.3 / 3.6 TB/s), layer norms on an FP32 stream 84 / 102 (4.8 / 3.9); 2000 of 12000 56 / 67; 8192 of 16384 210 / 254.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
