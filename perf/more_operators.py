@@ -292,8 +292,8 @@ def _log_probabilities(logits, tokens, temperature):
 
 
 def _logit_gradient(x, lse, tokens, d, dtype):
-    """d ([j = token] - exp(x - lse)), in the memory of x until it is rounded."""
-    x.sub_(lse[:, None].float()).exp_().mul_(-d[:, None].float())
+    """d ([j = token] - exp(x - lse)).  (x may be the logits themselves.)"""
+    x = (x - lse[:, None].float()).exp_().mul_(-d[:, None].float())
     return x.scatter_add_(1, tokens.clamp(min=0)[:, None], d[:, None].float()).to(dtype)
 
 
