@@ -426,6 +426,102 @@ int flashoptim_block_norm_backward(const flashoptim_block_norm_spec* spec, const
                                    const flashoptim_matrix* gate, const float* stats, const flashoptim_block_norm_grads* grads,
                                    void* workspace, int64_t workspace_bytes, void* stream);
 
+/* ---- the losses on the logits, where a backward pass begins ----------------------------------------------
+ * logits [rows, vocab]: BF16 or FP32, one row for each token that a model has to account for, tokens [rows] INT64 (contiguous) the
+ * token itself.  With T the temperature:
+ *   lse_i = log sum_j exp(logits_ij / T),    logprob_i = logits_i,t / T - lse_i   with t = tokens_i
+ * A row with a negative token does not count: its logits are not read, its logprob, lse and gradients are 0.  A token of vocab or more
+ * makes its row's logprob and gradients NaN, and so the loss.  So does a row that holds a NaN or +infinity, or nothing but -infinity
+ * (whose lse is -infinity); a -infinity beside other values has the probability 0.  Sums over a row are FP32 by lane and FP64 where lanes
+ * join, what is computed once for a row is FP64; the order of all sums depends on the sizes alone.  Vectors are contiguous FP32.
+ *   1 <= vocab < 2^31 - 4096 unless rows = 0; rows < 2^31; T > 0 and finite.
+ * token_logprob: logprob, lse [rows], either may be NULL (not both, unless rows = 0).
+ * token_logprob_backward: dlogits_ij = dlogprob_i / T ([j = t] - exp(logits_ij / T - lse_i)), of the type of logits, from the lse that the forward
+ *   call left.  The logits of a row whose dlogprob is 0 are not read; its gradient is 0.  dlogits may be logits' own buffer.
+ * workspace: as in the products above, of the bytes that the *_workspace call returns for the same sizes and type. */
+int64_t flashoptim_token_logprob_workspace(int64_t rows, int64_t vocab, int dtype);
+int flashoptim_token_logprob(const flashoptim_matrix* logits, const int64_t* tokens, float temperature, float* logprob, float* lse,
+                             void* workspace, int64_t workspace_bytes, void* stream);
+int flashoptim_token_logprob_backward(const flashoptim_matrix* logits, const int64_t* tokens, float temperature, const float* lse,
+                                      const float* dlogprob, const flashoptim_matrix* dlogits, void* stream);
+
+/* policy_loss: the clipped policy loss with a KL term to a reference policy, and its gradient in the same pass over the logits.  By row,
+ * with A the advantage and w the weight:
+ *   r = exp(logprob - old_logprob)                 (old_logprob NULL: of the policy to itself, r = 1, through which the gradient goes all the same)
+ *   surrogate = -min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A)
+ *   kl = exp(d) - d - 1,  d = ref_logprob - logprob         (ref_logprob NULL: 0)
+ *   stats [4] = { sum w (surrogate + kl_weight kl),  sum w surrogate,  sum w kl,  sum w [blocked] }     the first is the loss
+ *   dlogits = grad_scale * the loss's gradient.  A row is blocked, its surrogate without gradient, where A > 0 and r > 1 + clip_high or
+ *   A < 0 and r < 1 - clip_low.
+ * A row whose weight is 0 does not count, as one with a negative token does not.  weights NULL: 1.  A mean is had by weights that sum to 1.
+ * logprob [rows] and dlogits may be NULL (not wanted); dlogits may be logits' own buffer.  clip_low, clip_high and kl_weight are not
+ * negative; clip_high may be infinite. */
+typedef struct flashoptim_policy_spec {
+    float temperature, clip_low, clip_high, kl_weight, grad_scale;
+} flashoptim_policy_spec;
+
+typedef struct flashoptim_policy_inputs {
+    const float *advantages, *old_logprob, *ref_logprob, *weights;       /* [rows]; all but the first may be NULL */
+} flashoptim_policy_inputs;
+
+int64_t flashoptim_policy_loss_workspace(int64_t rows, int64_t vocab, int dtype);
+int flashoptim_policy_loss(const flashoptim_policy_spec* spec, const flashoptim_matrix* logits, const int64_t* tokens,
+                           const flashoptim_policy_inputs* inputs, float* stats, float* logprob, const flashoptim_matrix* dlogits,
+                           void* workspace, int64_t workspace_bytes, void* stream);
+
+/* preference_loss: of pairs of sequences, one chosen and one rejected, from the log-probabilities of their tokens.
+ *   gain(s) = sum over the rows of s of weights (logprob - ref_logprob),   z = beta (gain(chosen) - gain(rejected))
+ *   loss = the mean over the pairs of, by kind:  SIGMOID  (1 - label_smoothing) log(1 + exp(-z)) + label_smoothing log(1 + exp(z))
+ *                                                HINGE    max(0, 1 - z)
+ *                                                SQUARED  (z / beta - 1 / (2 beta))^2
+ *   margins [pairs] = z (may be NULL);  dlogprob [rows] = grad_scale * the loss's gradient (may be NULL), 0 for rows of no sequence.
+ * offsets [2 pairs + 1] INT64, not descending, within [0, rows] (what lies outside is taken as the nearest bound): sequence i is the rows
+ * offsets[i] .. offsets[i + 1] - 1, possibly none.  order: sequences 2p and 2p + 1 are the chosen and the rejected one of pair p
+ * (FLASHOPTIM_PAIRS_BY_TURNS), or p and pairs + p (FLASHOPTIM_PAIRS_HALVES).  Rows whose weight is 0 do not count, whatever their
+ * logprob; weights, ref_logprob NULL: 1, 0.  No pairs: a loss of 0.  beta > 0, 0 <= label_smoothing <= 0.5, which is for SIGMOID only.
+ * Sums are FP64.  rows < 2^31, pairs < 2^30. */
+enum { FLASHOPTIM_PREFERENCE_SIGMOID = 0, FLASHOPTIM_PREFERENCE_HINGE = 1, FLASHOPTIM_PREFERENCE_SQUARED = 2 };
+enum { FLASHOPTIM_PAIRS_BY_TURNS = 0, FLASHOPTIM_PAIRS_HALVES = 1 };
+
+typedef struct flashoptim_preference_spec {
+    int32_t kind, order;
+    float beta, label_smoothing, grad_scale;
+} flashoptim_preference_spec;
+
+int flashoptim_preference_loss(const flashoptim_preference_spec* spec, const float* logprob, const float* ref_logprob,
+                               const float* weights, int64_t rows, const int64_t* offsets, int64_t pairs, float* loss, float* margins,
+                               float* dlogprob, void* stream);
+
+/* ---- the norm of all gradients and their clipping, between a backward pass and the step -----------------
+ * A list of gradients, each flattened, contiguous and 16-byte aligned; src of BF16 or FP32 (src_dtype, one for the whole list).  Its
+ * descriptors travel with the launches: nothing is cached, and a captured call keeps the list that it was captured with.
+ * grad_norm: *factor (DEVICE memory, 16-byte aligned) <- sum_squares, the sum of the squares of all elements in FP64 (no finite gradient
+ *   overflows it); norm, its root; scale = max_norm / norm where norm > max_norm, else 1, and NaN where sum_squares is not finite.  A list without
+ *   elements has the norm 0.  max_norm >= 0, possibly infinite.  dst is ignored.  The order of the sum depends on the sizes alone.
+ * clip_factor_from_sum: recomputes norm and scale of *factor from its sum_squares, to which other lists' or ranks' sums have been added meanwhile (shards
+ *   of one model on several ranks: an all-reduce of that value).
+ * clip_gradients: dst <- src * scale, rounded once, of type dst_dtype: that of src, or BF16 for FP32 src (gradients accumulated in FP32, into
+ *   the ones that the step reads).  dst may be src itself if the types are the same; where scale is 1 such a buffer is not touched.  With a
+ *   scale of NaN every element becomes NaN.  Other overlaps of buffers are errors of the caller.
+ * 0 <= numel < 2^40 each, fewer than 2^43 together; an empty tensor's pointers are ignored.  workspace as above, for the same list. */
+typedef struct flashoptim_clip_factor {
+    double sum_squares;
+    float  norm, scale;
+} flashoptim_clip_factor;
+
+typedef struct flashoptim_gradient {
+    const void* src;
+    void*       dst;
+    int64_t     numel;
+} flashoptim_gradient;
+
+int64_t flashoptim_grad_norm_workspace(const flashoptim_gradient* grads, int64_t n_grads, int src_dtype);
+int flashoptim_grad_norm(const flashoptim_gradient* grads, int64_t n_grads, int src_dtype, float max_norm,
+                         flashoptim_clip_factor* factor, void* workspace, int64_t workspace_bytes, void* stream);
+int flashoptim_clip_factor_from_sum(flashoptim_clip_factor* factor, float max_norm, void* stream);
+int flashoptim_clip_gradients(const flashoptim_gradient* grads, int64_t n_grads, int src_dtype, int dst_dtype,
+                              const flashoptim_clip_factor* factor, void* stream);
+
 /* ---- housekeeping --------------------------------------------------------------------
  * strerror: static string for a status.  last_hip_error: hipError_t value of the most recent
  * failed HIP call on this thread (0 if none).  release_cache: frees the cached device chunk

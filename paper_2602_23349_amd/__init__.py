@@ -13,6 +13,9 @@ from .binding import (  # noqa: F401
     Mx4Tensor, mx4_quantize, mx4_dequantize, mx4_matmul, mx4_linear, mx4_linear_backward,
     mx4_matmul_workspace, mx4_linear_workspace, mx4_linear_backward_workspace,
     BlockNorm, block_norm, block_norm_backward, block_norm_backward_workspace,
+    token_logprob, token_logprob_backward, token_logprob_workspace, PolicyLoss, policy_loss, policy_loss_workspace,
+    PreferenceLoss, preference_loss,
+    GradList, ClipFactor, grad_norm, grad_norm_workspace, clip_factor_from_sum, clip_gradients,
     checkpoint_size, checkpoint_pack, checkpoint_unpack,
     strerror, release_cache, version, selftest, faithful_rounding_stats, short_sqrt_state, ClockMonitor, EXPORTED_SYMBOLS, KIND,
 )

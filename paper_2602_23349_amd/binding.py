@@ -33,6 +33,9 @@ EXPORTED_SYMBOLS = [
     "flashoptim_mx4_quantize", "flashoptim_mx4_dequantize", "flashoptim_mx4_matmul_workspace", "flashoptim_mx4_linear_workspace",
     "flashoptim_mx4_linear_backward_workspace", "flashoptim_mx4_matmul", "flashoptim_mx4_linear", "flashoptim_mx4_linear_backward",
     "flashoptim_block_norm", "flashoptim_block_norm_backward_workspace", "flashoptim_block_norm_backward",
+    "flashoptim_token_logprob_workspace", "flashoptim_token_logprob", "flashoptim_token_logprob_backward",
+    "flashoptim_policy_loss_workspace", "flashoptim_policy_loss", "flashoptim_preference_loss",
+    "flashoptim_grad_norm_workspace", "flashoptim_grad_norm", "flashoptim_clip_factor_from_sum", "flashoptim_clip_gradients",
 ]
 
 
@@ -89,6 +92,22 @@ class _BlockNormGrads(C.Structure):
                [(n, C.c_void_p) for n in ("dpost_weight", "dpost_bias", "dpre_weight", "dpre_bias")]
 
 
+class _PolicySpec(C.Structure):
+    _fields_ = [(n, C.c_float) for n in ("temperature", "clip_low", "clip_high", "kl_weight", "grad_scale")]
+
+
+class _PolicyInputs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("advantages", "old_logprob", "ref_logprob", "weights")]
+
+
+class _PreferenceSpec(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("order", C.c_int32), ("beta", C.c_float), ("label_smoothing", C.c_float), ("grad_scale", C.c_float)]
+
+
+class _Gradient(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("numel", C.c_int64)]
+
+
 def library_path():
     return _LIB_PATH
 
@@ -143,6 +162,17 @@ def load_library():
     L.flashoptim_block_norm_backward_workspace.argtypes = [spec, i64, i64]
     for name in ("flashoptim_mx4_matmul_workspace", "flashoptim_mx4_linear_workspace", "flashoptim_mx4_linear_backward_workspace"):
         getattr(L, name).argtypes = [i64, i64, i64]
+    for name in ("flashoptim_token_logprob_workspace", "flashoptim_policy_loss_workspace"):
+        getattr(L, name).argtypes = [i64, i64, i32]
+    L.flashoptim_token_logprob.argtypes = [mat, vp, C.c_float, vp, vp, vp, i64, vp]
+    L.flashoptim_token_logprob_backward.argtypes = [mat, vp, C.c_float, vp, vp, mat, vp]
+    L.flashoptim_policy_loss.argtypes = [C.POINTER(_PolicySpec), mat, vp, C.POINTER(_PolicyInputs), vp, vp, mat, vp, i64, vp]
+    L.flashoptim_preference_loss.argtypes = [C.POINTER(_PreferenceSpec), vp, vp, vp, i64, vp, i64, vp, vp, vp, vp]
+    grads = C.POINTER(_Gradient)
+    L.flashoptim_grad_norm_workspace.argtypes = [grads, i64, i32]
+    L.flashoptim_grad_norm.argtypes = [grads, i64, i32, C.c_float, vp, vp, i64, vp]
+    L.flashoptim_clip_factor_from_sum.argtypes = [vp, C.c_float, vp]
+    L.flashoptim_clip_gradients.argtypes = [grads, i64, i32, i32, vp, vp]
     L.flashoptim_strerror.argtypes = [i32]
     L.flashoptim_strerror.restype = C.c_char_p
     for name in EXPORTED_SYMBOLS:
@@ -166,7 +196,8 @@ def _marshal():
         except ImportError as e:
             raise RuntimeError("_marshal.so is missing: build it with `python paper_2602_23349_amd/build.py`") from e
         lib = load_library()
-        names = [n for n in EXPORTED_SYMBOLS if n.startswith(("flashoptim_mx4_", "flashoptim_block_norm"))]
+        names = [n for n in EXPORTED_SYMBOLS if n.startswith(("flashoptim_mx4_", "flashoptim_block_norm", "flashoptim_token_logprob",
+                                                             "flashoptim_policy_loss", "flashoptim_preference_loss"))]
         fast.bind({n: C.cast(getattr(lib, n), C.c_void_p).value for n in names}, torch._C._cuda_getCurrentRawStream,
                   torch._C._cuda_getDevice)
         torch.cuda.init()
@@ -608,6 +639,143 @@ def block_norm_backward(spec, h, stats, f=None, gate=None, dy=None, dh=None, dx=
                                                  dpre_weight, dpre_bias, workspace, _handle(stream))
     if status:
         raise FlashOptimError(status, "flashoptim_block_norm_backward")
+
+
+def token_logprob_workspace(logits):
+    """Bytes of workspace of token_logprob for logits of this shape and type."""
+    return _size(load_library().flashoptim_token_logprob_workspace(*logits.shape, _DTYPE[logits.dtype]), "flashoptim_token_logprob_workspace")
+
+
+def token_logprob(logits, tokens, logprob=None, lse=None, temperature=1.0, workspace=None, stream=None):
+    """logprob [rows] <- the log-probability of each row's token (int64, negative: the row does not count), lse <- the log of the row's
+    sum of exponentials, for the backward pass; one of the two may be None."""
+    status = (_fast or _marshal()).logprob(logits, tokens, temperature, logprob, lse, workspace, _handle(stream))
+    if status:
+        raise FlashOptimError(status, "flashoptim_token_logprob")
+
+
+def token_logprob_backward(logits, tokens, lse, dlogprob, dlogits, temperature=1.0, stream=None):
+    """dlogits <- the gradient of the logits (which it may replace in their memory) from that of the log-probabilities."""
+    status = (_fast or _marshal()).logprob_backward(logits, tokens, temperature, lse, dlogprob, dlogits, _handle(stream))
+    if status:
+        raise FlashOptimError(status, "flashoptim_token_logprob_backward")
+
+
+class PolicyLoss:
+    """What a clipped policy loss is made of (flashoptim_policy_spec)."""
+
+    def __init__(self, clip_low=0.2, clip_high=0.2, kl_weight=0.0, temperature=1.0, grad_scale=1.0):
+        self.desc = _PolicySpec(temperature, clip_low, clip_high, kl_weight, grad_scale)
+        self.address = C.addressof(self.desc)
+
+
+def policy_loss_workspace(logits):
+    return _size(load_library().flashoptim_policy_loss_workspace(*logits.shape, _DTYPE[logits.dtype]), "flashoptim_policy_loss_workspace")
+
+
+def policy_loss(spec, logits, tokens, advantages, stats, old_logprob=None, ref_logprob=None, weights=None, logprob=None, dlogits=None,
+                workspace=None, stream=None):
+    """stats [4] <- the loss, its surrogate, KL and clipped parts; logprob [rows] and the gradient dlogits (which may replace the logits
+    in their memory) where they are not None."""
+    status = (_fast or _marshal()).policy(spec.address, logits, tokens, advantages, old_logprob, ref_logprob, weights, stats, logprob, dlogits,
+                                          workspace, _handle(stream))
+    if status:
+        raise FlashOptimError(status, "flashoptim_policy_loss")
+
+
+class PreferenceLoss:
+    """What a preference loss is made of (flashoptim_preference_spec).  order: "by_turns" or "halves"."""
+
+    def __init__(self, beta=0.1, kind="sigmoid", label_smoothing=0.0, order="by_turns", grad_scale=1.0):
+        self.desc = _PreferenceSpec({"sigmoid": 0, "hinge": 1, "squared": 2}.get(kind, -1), {"by_turns": 0, "halves": 1}.get(order, -1),
+                                    beta, label_smoothing, grad_scale)
+        self.address = C.addressof(self.desc)
+
+
+def preference_loss(spec, logprob, offsets, loss, ref_logprob=None, weights=None, margins=None, dlogprob=None, stream=None):
+    """loss [1] <- the mean over pairs of sequences, sequence i being the rows offsets[i] .. offsets[i + 1] - 1 of logprob; margins
+    [pairs] and the gradient dlogprob [rows] where they are not None."""
+    status = (_fast or _marshal()).preference(spec.address, logprob, offsets, loss, ref_logprob, weights, margins, dlogprob, _handle(stream))
+    if status:
+        raise FlashOptimError(status, "flashoptim_preference_loss")
+
+
+class GradList:
+    """A host array of flashoptim_gradient descriptors, built once and reused: `src` contiguous GPU tensors of one type, bfloat16 or
+    float32, `dst` where clip_gradients leaves them (None: in place), of that type or bfloat16."""
+
+    def __init__(self, src, dst=None):
+        self.src, self.dst = list(src), None if dst is None else list(dst)
+        if self.dst is not None and len(self.dst) != len(self.src):
+            raise ValueError("as many destinations as gradients")
+        self.n = len(self.src)
+        self.array = (_Gradient * max(self.n, 1))()
+        self.src_dtype = self._type(self.src, "gradients")
+        self.dst_dtype = self.src_dtype if self.dst is None else self._type(self.dst, "destinations")
+        for i, t in enumerate(self.src):
+            to = t if self.dst is None else self.dst[i]
+            if to.numel() != t.numel():
+                raise ValueError("a destination has the elements of its gradient")
+            d = self.array[i]
+            d.src, d.dst, d.numel = t.data_ptr(), to.data_ptr(), t.numel()
+
+    @staticmethod
+    def _type(tensors, what):
+        if any(t.dtype not in _DTYPE or t.dtype != tensors[0].dtype or not t.is_contiguous() or not t.is_cuda for t in tensors):
+            raise ValueError(f"{what}: contiguous tensors on the GPU, bfloat16 or float32, one type for all")
+        return _DTYPE[tensors[0].dtype] if tensors else 0
+
+    @classmethod
+    def of(cls, params):
+        """The gradients of a TensorList as its descriptors have them now, clipped in place."""
+        out = cls([])
+        out.n = params.n
+        out.array = (_Gradient * max(out.n, 1))()
+        for d, t in zip(out.array, params.array[:params.n]):
+            d.src, d.dst, d.numel = t.grad, t.grad, t.numel
+        out.src = params
+        return out
+
+
+class ClipFactor:
+    """The device record of a norm (flashoptim_clip_factor): `sum_squares` (float64), `norm` and `scale` (float32) are views of one
+    element each."""
+
+    def __init__(self, device="cuda"):
+        self.data = torch.zeros(2, dtype=torch.float64, device=device)
+        self.sum_squares = self.data[:1]
+        self.norm, self.scale = self.data.view(torch.float32)[2:3], self.data.view(torch.float32)[3:4]
+        self.address = self.data.data_ptr()
+
+
+def grad_norm_workspace(grads):
+    """Bytes of workspace of grad_norm for this list."""
+    return _size(load_library().flashoptim_grad_norm_workspace(grads.array, grads.n, grads.src_dtype), "flashoptim_grad_norm_workspace")
+
+
+def _memory(workspace):
+    if workspace is None:
+        return None, 0
+    if not workspace.is_contiguous() or not workspace.is_cuda:
+        raise ValueError("workspace: contiguous memory on the GPU")
+    return workspace.data_ptr(), workspace.nbytes
+
+
+def grad_norm(grads, max_norm, factor, workspace=None, stream=None):
+    """factor (ClipFactor) <- the norm of all gradients of a GradList, and max_norm / norm where that is less than 1."""
+    _check(load_library().flashoptim_grad_norm(grads.array, grads.n, grads.src_dtype, max_norm, factor.address, *_memory(workspace),
+                                               _stream_handle(stream)), "flashoptim_grad_norm")
+
+
+def clip_factor_from_sum(factor, max_norm, stream=None):
+    """norm and scale of `factor` from its sum_squares as it is now."""
+    _check(load_library().flashoptim_clip_factor_from_sum(factor.address, max_norm, _stream_handle(stream)), "flashoptim_clip_factor_from_sum")
+
+
+def clip_gradients(grads, factor, stream=None):
+    """The destinations of a GradList <- its gradients times the factor's scale."""
+    _check(load_library().flashoptim_clip_gradients(grads.array, grads.n, grads.src_dtype, grads.dst_dtype, factor.address,
+                                                    _stream_handle(stream)), "flashoptim_clip_gradients")
 
 
 def faithful_rounding_stats(stream=None):

@@ -14,9 +14,10 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libflashoptim.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")
 MARSHAL_SOURCES = [os.path.join(CSRC, "marshal.cpp"), os.path.join(ROOT, "include", "flashoptim.h")]
-SOURCES = [os.path.join(CSRC, n) for n in ("flashoptim_kernels.hip", "flashoptim_api.hip", "flashoptim_mx4.hip", "flashoptim_norm.hip")]
+SOURCES = [os.path.join(CSRC, n) for n in ("flashoptim_kernels.hip", "flashoptim_api.hip", "flashoptim_mx4.hip", "flashoptim_norm.hip",
+                                             "flashoptim_loss.hip", "flashoptim_clip.hip")]
 HEADERS = [os.path.join(CSRC, "flashoptim_device.h"), os.path.join(CSRC, "flashoptim_launch.h"), os.path.join(CSRC, "flashoptim_host.h"),
-           os.path.join(CSRC, "flashoptim_layers.h"), os.path.join(CSRC, "flashoptim_mx4.h"),
+           os.path.join(CSRC, "flashoptim_layers.h"), os.path.join(CSRC, "flashoptim_mx4.h"), os.path.join(CSRC, "flashoptim_clip.h"),
            os.path.join(ROOT, "include", "flashoptim.h")]
 
 # Exact arithmetic is part of the contract: no FMA contraction, IEEE division and square root,

@@ -1,0 +1,39 @@
+// Internal: how the calls over a list of gradients (flashoptim_clip.hip) are cut into tiles, workgroups and launches.  Plain C++ without
+// HIP, so that its limits can be tested without a GPU.
+#ifndef FLASHOPTIM_CLIP_H
+#define FLASHOPTIM_CLIP_H
+
+#include <stdint.h>
+
+#include "flashoptim_launch.h"
+
+namespace fo {
+
+// A tile is what a workgroup handles at a time: consecutive elements of one tensor.
+constexpr int kGradThreads = 256, kGradVec = 8;          // lanes, and elements that a lane has side by side
+constexpr int kGradTile = 8192;
+
+// A launch's tensors, as they travel in its arguments.  `first[i]` is tensor i's first tile, counted within the launch; `lack[i]` the elements that its last
+// tile is short of.
+template <int N, bool DST>
+struct GradTable {
+    const void* src[N];
+    void* dst[DST ? N : 1];
+    uint32_t first[N + 1];      // behind the launch's last tensor, and in what is left of the table: all its tiles
+    uint16_t lack[N];
+};
+// As many as the 4 KB of a launch's arguments hold, or few, for which the host has fewer bytes to copy.
+constexpr int kGradFew = 16, kGradMany = 280, kClipMany = 176;
+constexpr int64_t kGradArgBytes = 4096 - 64;             // beside the other arguments
+static_assert(sizeof(GradTable<kGradMany, false>) <= kGradArgBytes && sizeof(GradTable<kClipMany, true>) <= kGradArgBytes, "kernel arguments");
+
+constexpr int64_t grad_tiles(int64_t numel) { return up(numel, kGradTile); }
+// The most tiles of a launch: so many that their number fits 31 bits, and of a clipping launch, one workgroup each, that its lanes fit 32.
+constexpr int64_t kMostTiles = kMaxWorkItems / kGradThreads;
+
+// The workgroups of a launch that sums up: each takes every so many-th tile and leaves one sum.
+constexpr int64_t kNormGroups = 2048;
+constexpr int64_t norm_groups(int64_t tiles) { return tiles < kNormGroups ? tiles : kNormGroups; }
+
+}  // namespace fo
+#endif

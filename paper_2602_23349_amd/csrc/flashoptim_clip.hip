@@ -1,0 +1,316 @@
+// The global norm of a list of gradients and their clipping, for gfx950.
+//
+//   sum_squares = sum over all tensors of g^2,   norm = sqrt(sum_squares),   scale = norm > max_norm ? max_norm / norm : 1,   dst = round(src * scale)
+// Bound: HBM for all but small lists: the norm reads a gradient once, clipping reads it again and writes it.  Squares are summed in FP64: no finite
+// gradient overflows them and no order of the sum is visible in the FP32 norm, at one conversion and one multiply-add for each element, which
+// hide behind the loads.
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <cstring>
+
+#include "flashoptim.h"
+#include "flashoptim_clip.h"
+#include "flashoptim_host.h"
+#include "flashoptim_layers.h"
+
+namespace {
+
+using fo::GradTable;
+using fo::i32x4;
+using fo::kGradThreads;
+using fo::kGradTile;
+using fo::kGradVec;
+using fo::load_as;
+using fo::store_as;
+
+constexpr int kPasses = kGradTile / (kGradThreads * kGradVec);       // of a workgroup over its tile
+constexpr int kJoinThreads = 1024;
+
+// Where a tile lies: its tensor, its first element there and how many elements it has.
+struct Tile {
+    uint32_t tensor;
+    int64_t begin;
+    int left;
+};
+template <int N, bool DST>
+__device__ __forceinline__ Tile locate(const GradTable<N, DST>& t, uint32_t n, uint32_t tile) {
+    const uint32_t i = fo::entry_of(tile, 0u, n - 1, [&](uint32_t k) { return t.first[k]; });
+    const uint32_t last = t.first[i + 1] - 1;
+    return {i, (int64_t)(tile - t.first[i]) * kGradTile, tile == last ? kGradTile - (int)t.lack[i] : kGradTile};
+}
+
+// Eight neighbouring elements as FP32, `count` of which exist (the others 0).
+template <bool FP32>
+__device__ __forceinline__ void load8(float (&v)[8], const void* p, int64_t at, int count) {
+    if (count >= 8) {
+        if constexpr (FP32) {
+            const i32x4 a = load_as<i32x4>((const float*)p + at), b = load_as<i32x4>((const float*)p + at + 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { v[i] = __int_as_float(a[i]); v[4 + i] = __int_as_float(b[i]); }
+        } else {
+            const i32x4 a = load_as<i32x4>((const uint16_t*)p + at);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[2 * i] = __uint_as_float((uint32_t)a[i] << 16);
+                v[2 * i + 1] = __uint_as_float((uint32_t)a[i] & 0xffff0000u);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            v[i] = 0.0f;
+            if (i < count) v[i] = FP32 ? ((const float*)p)[at + i] : __uint_as_float((uint32_t)((const uint16_t*)p)[at + i] << 16);
+        }
+    }
+}
+template <bool FP32>
+__device__ __forceinline__ void store8(void* p, int64_t at, int count, const float (&v)[8]) {
+    if constexpr (FP32) {
+        float* f = (float*)p + at;
+        if (count >= 8) {
+            store_as(f, fo::f32x4{v[0], v[1], v[2], v[3]});
+            store_as(f + 4, fo::f32x4{v[4], v[5], v[6], v[7]});
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) if (i < count) f[i] = v[i];
+        }
+    } else {
+        using f32x8 = float __attribute__((ext_vector_type(8)));
+        using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
+        const bf16x8 w = __builtin_convertvector((f32x8){v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]}, bf16x8);
+        __bf16* f = (__bf16*)p + at;
+        if (count >= 8) store_as(f, w);
+        else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) if (i < count) f[i] = w[i];
+        }
+    }
+}
+
+// The sum over a workgroup, in lane 0, in a fixed order.
+template <int THREADS>
+__device__ __forceinline__ double group_sum(double s) {
+    __shared__ double part[THREADS / 64];
+    for (int off = 32; off > 0; off >>= 1) s += __shfl_down(s, off);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = 0.0;
+#pragma unroll
+    for (int k = 0; k < THREADS / 64; ++k) s += part[k];
+    return s;
+}
+
+__device__ __forceinline__ void set_factor(flashoptim_clip_factor* f, double sum, float max_norm) {
+    const double norm = sqrt(sum);
+    f->sum_squares = sum;
+    f->norm = (float)norm;
+    f->scale = !(sum < __builtin_inf()) ? __builtin_nanf("") : norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.0f;
+}
+
+template <bool FP32, int N>
+__global__ __launch_bounds__(kGradThreads) void norm_kernel(GradTable<N, false> t, uint32_t n, uint32_t tiles, double* part) {
+    double sum = 0.0;
+    for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const Tile at = locate(t, n, tile);
+        const void* src = t.src[at.tensor];
+        float v[kPasses][8];
+#pragma unroll
+        for (int p = 0; p < kPasses; ++p) {
+            const int in = (p * kGradThreads + (int)threadIdx.x) * kGradVec;
+            load8<FP32>(v[p], src, at.begin + in, at.left - in);
+        }
+#pragma unroll
+        for (int p = 0; p < kPasses; ++p) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const double d = (double)v[p][i];
+                sum = fma(d, d, sum);
+            }
+        }
+    }
+    sum = group_sum<kGradThreads>(sum);
+    if (threadIdx.x == 0) part[blockIdx.x] = sum;
+}
+
+__global__ __launch_bounds__(kJoinThreads) void norm_join_kernel(const double* part, uint32_t parts, float max_norm, flashoptim_clip_factor* factor) {
+    double sum = 0.0;
+    for (uint32_t i = threadIdx.x; i < parts; i += kJoinThreads) sum += part[i];
+    sum = group_sum<kJoinThreads>(sum);
+    if (threadIdx.x == 0) set_factor(factor, sum, max_norm);
+}
+
+__global__ void factor_kernel(flashoptim_clip_factor* factor, float max_norm) {
+    if (threadIdx.x == 0) set_factor(factor, factor->sum_squares, max_norm);
+}
+
+// DST: dst differs from src (otherwise the same buffers, left alone where the factor is 1).
+template <bool SRC32, bool DST32, bool DST, int N>
+__global__ __launch_bounds__(kGradThreads) void clip_kernel(GradTable<N, DST> t, uint32_t n, uint32_t tiles, const flashoptim_clip_factor* factor) {
+    const float scale = factor->scale;
+    if (!DST && scale == 1.0f) return;
+    for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const Tile at = locate(t, n, tile);
+        const void* src = t.src[at.tensor];
+        void* dst = DST ? t.dst[at.tensor] : const_cast<void*>(src);
+        if (DST && dst == src && scale == 1.0f) continue;
+        float v[kPasses][8];
+#pragma unroll
+        for (int p = 0; p < kPasses; ++p) {
+            const int in = (p * kGradThreads + (int)threadIdx.x) * kGradVec;
+            load8<SRC32>(v[p], src, at.begin + in, at.left - in);
+        }
+#pragma unroll
+        for (int p = 0; p < kPasses; ++p) {
+            const int in = (p * kGradThreads + (int)threadIdx.x) * kGradVec;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[p][i] *= scale;
+            store8<DST32>(dst, at.begin + in, at.left - in, v[p]);
+        }
+    }
+}
+
+bool known(int dtype) { return dtype == FLASHOPTIM_BF16 || dtype == FLASHOPTIM_FP32; }
+
+int check_list(const flashoptim_gradient* g, int64_t n, int src_dtype) {
+    if (n < 0 || (n > 0 && !g) || !known(src_dtype)) return FLASHOPTIM_ERR_INVALID_ARG;
+    int64_t all = 0;
+    for (int64_t i = 0; i < n; ++i) {
+        if (g[i].numel < 0 || g[i].numel >= fo::kMaxElems) return FLASHOPTIM_ERR_NUMEL_RANGE;
+        all += g[i].numel;
+        if (all >= ((int64_t)1 << 43)) return FLASHOPTIM_ERR_NUMEL_RANGE;
+    }
+    return FLASHOPTIM_OK;
+}
+int check_factor(const flashoptim_clip_factor* f) {
+    if (!f) return FLASHOPTIM_ERR_INVALID_ARG;
+    return fo::aligned_to(f, 16) ? FLASHOPTIM_OK : FLASHOPTIM_ERR_MISALIGNED;
+}
+
+// The next launch's tensors: those of the list from *at on that fit, the empty ones left out.
+struct Cut {
+    uint32_t n = 0, tiles = 0;
+};
+template <int N, bool DST>
+Cut fill(GradTable<N, DST>& t, const flashoptim_gradient* g, int64_t n, int64_t* at) {
+    Cut c;
+    for (; *at < n && c.n < (uint32_t)N; ++*at) {
+        const flashoptim_gradient& x = g[*at];
+        if (x.numel == 0) continue;
+        const int64_t tiles = fo::grad_tiles(x.numel);
+        if ((int64_t)c.tiles + tiles > 0x7fffffff) break;
+        t.src[c.n] = x.src;
+        if (DST) t.dst[c.n] = x.dst;
+        t.first[c.n] = c.tiles;
+        t.lack[c.n] = (uint16_t)(tiles * kGradTile - x.numel);
+        c.tiles += (uint32_t)tiles;
+        ++c.n;
+    }
+    t.first[c.n] = c.tiles;
+    return c;
+}
+
+// launch(table, its cut) for each of a call's launches, with tables of up to MANY tensors.
+template <int MANY, bool DST, typename F>
+int for_each_cut(const flashoptim_gradient* g, int64_t n, F launch) {
+    int64_t live = 0;
+    for (int64_t i = 0; i < n; ++i) live += g[i].numel > 0;
+    for (int64_t at = 0; at < n;) {
+        int rc = FLASHOPTIM_OK;
+        if (live <= fo::kGradFew) {
+            GradTable<fo::kGradFew, DST> t;
+            const Cut c = fill(t, g, n, &at);
+            if (c.n) rc = launch(t, c);
+        } else {
+            GradTable<MANY, DST> t;
+            const Cut c = fill(t, g, n, &at);
+            if (c.n) rc = launch(t, c);
+        }
+        FO_TRY(rc);
+    }
+    return FLASHOPTIM_OK;
+}
+
+template <bool SRC32, bool DST32, bool DST>
+int clip_launches(const flashoptim_gradient* g, int64_t n, const flashoptim_clip_factor* factor, void* stream) {
+    return for_each_cut<DST ? fo::kClipMany : fo::kGradMany, DST>(g, n, [&](auto& t, const Cut& c) {
+        const unsigned blocks = (unsigned)(c.tiles < fo::kMostTiles ? c.tiles : fo::kMostTiles);
+        constexpr int N = sizeof(t.lack) / sizeof(t.lack[0]);
+        hipLaunchKernelGGL((clip_kernel<SRC32, DST32, DST, N>), dim3(blocks), dim3(kGradThreads), 0, (hipStream_t)stream, t, c.n, c.tiles, factor);
+        return fo::hip_status(hipGetLastError());
+    });
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t flashoptim_grad_norm_workspace(const flashoptim_gradient* grads, int64_t n_grads, int src_dtype) {
+    FO_TRY(check_list(grads, n_grads, src_dtype));
+    int64_t parts = 0;
+    (void)for_each_cut<fo::kGradMany, false>(grads, n_grads, [&](auto&, const Cut& c) {
+        parts += fo::norm_groups(c.tiles);
+        return FLASHOPTIM_OK;
+    });
+    return parts * (int64_t)sizeof(double);
+}
+
+int flashoptim_grad_norm(const flashoptim_gradient* grads, int64_t n_grads, int src_dtype, float max_norm,
+                         flashoptim_clip_factor* factor, void* workspace, int64_t workspace_bytes, void* stream) {
+    FO_TRY(check_list(grads, n_grads, src_dtype));
+    if (!(max_norm >= 0.0f)) return FLASHOPTIM_ERR_INVALID_ARG;
+    FO_TRY(check_factor(factor));
+    for (int64_t i = 0; i < n_grads; ++i) {
+        if (grads[i].numel == 0) continue;
+        if (!grads[i].src) return FLASHOPTIM_ERR_INVALID_ARG;
+        if (!fo::aligned_to(grads[i].src, 16)) return FLASHOPTIM_ERR_MISALIGNED;
+    }
+    const int64_t need = flashoptim_grad_norm_workspace(grads, n_grads, src_dtype);
+    if (need < 0) return (int)need;
+    if (need > 0 && !workspace) return FLASHOPTIM_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return FLASHOPTIM_ERR_WORKSPACE;
+    if (!fo::aligned_to(workspace, 16)) return FLASHOPTIM_ERR_MISALIGNED;
+    double* part = (double*)workspace;
+    uint32_t parts = 0;
+    FO_TRY((for_each_cut<fo::kGradMany, false>(grads, n_grads, [&](auto& t, const Cut& c) {
+        const unsigned blocks = (unsigned)fo::norm_groups(c.tiles);
+        constexpr int N = sizeof(t.lack) / sizeof(t.lack[0]);
+        if (src_dtype == FLASHOPTIM_FP32)
+            hipLaunchKernelGGL((norm_kernel<true, N>), dim3(blocks), dim3(kGradThreads), 0, (hipStream_t)stream, t, c.n, c.tiles, part + parts);
+        else
+            hipLaunchKernelGGL((norm_kernel<false, N>), dim3(blocks), dim3(kGradThreads), 0, (hipStream_t)stream, t, c.n, c.tiles, part + parts);
+        parts += blocks;
+        return fo::hip_status(hipGetLastError());
+    })));
+    hipLaunchKernelGGL(norm_join_kernel, dim3(1), dim3(kJoinThreads), 0, (hipStream_t)stream, part, parts, max_norm, factor);
+    return fo::hip_status(hipGetLastError());
+}
+
+int flashoptim_clip_factor_from_sum(flashoptim_clip_factor* factor, float max_norm, void* stream) {
+    FO_TRY(check_factor(factor));
+    if (!(max_norm >= 0.0f)) return FLASHOPTIM_ERR_INVALID_ARG;
+    hipLaunchKernelGGL(factor_kernel, dim3(1), dim3(64), 0, (hipStream_t)stream, factor, max_norm);
+    return fo::hip_status(hipGetLastError());
+}
+
+int flashoptim_clip_gradients(const flashoptim_gradient* grads, int64_t n_grads, int src_dtype, int dst_dtype,
+                              const flashoptim_clip_factor* factor, void* stream) {
+    FO_TRY(check_list(grads, n_grads, src_dtype));
+    if (!known(dst_dtype) || (src_dtype == FLASHOPTIM_BF16 && dst_dtype == FLASHOPTIM_FP32)) return FLASHOPTIM_ERR_INVALID_ARG;
+    FO_TRY(check_factor(factor));
+    bool in_place = true;
+    for (int64_t i = 0; i < n_grads; ++i) {
+        const flashoptim_gradient& g = grads[i];
+        if (g.numel == 0) continue;
+        if (!g.src || !g.dst || (g.src == g.dst && src_dtype != dst_dtype)) return FLASHOPTIM_ERR_INVALID_ARG;
+        if (!fo::aligned_to(g.src, 16) || !fo::aligned_to(g.dst, 16)) return FLASHOPTIM_ERR_MISALIGNED;
+        in_place = in_place && g.src == g.dst;
+    }
+    const bool s = src_dtype == FLASHOPTIM_FP32, d = dst_dtype == FLASHOPTIM_FP32;
+    if (in_place) return s ? clip_launches<true, true, false>(grads, n_grads, factor, stream) : clip_launches<false, false, false>(grads, n_grads, factor, stream);
+    if (s) return d ? clip_launches<true, true, true>(grads, n_grads, factor, stream) : clip_launches<true, false, true>(grads, n_grads, factor, stream);
+    return clip_launches<false, false, true>(grads, n_grads, factor, stream);
+}
+
+}  // extern "C"

@@ -25,6 +25,10 @@ decltype(&flashoptim_mx4_linear) call_linear;
 decltype(&flashoptim_mx4_linear_backward) call_linear_backward;
 decltype(&flashoptim_block_norm) call_norm;
 decltype(&flashoptim_block_norm_backward) call_norm_backward;
+decltype(&flashoptim_token_logprob) call_logprob;
+decltype(&flashoptim_token_logprob_backward) call_logprob_backward;
+decltype(&flashoptim_policy_loss) call_policy;
+decltype(&flashoptim_preference_loss) call_preference;
 PyObject *current_stream, *current_device;      // torch._C._cuda_getCurrentRawStream, _cuda_getDevice
 
 // The arguments of one call, taken in order.  After the first failure a Python error is set and nothing more is taken.
@@ -81,6 +85,13 @@ struct Args {
             return nullptr;
         }
         return t->data_ptr();
+    }
+    float number() {
+        PyObject* o = next();
+        if (failed) return 0.0f;
+        const double v = PyFloat_AsDouble(o);
+        failed = v == -1.0 && PyErr_Occurred() != nullptr;
+        return (float)v;
     }
     void workspace(void** p, int64_t* bytes) {
         const at::Tensor* t = tensor("workspace");
@@ -233,6 +244,91 @@ PyObject* norm_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     return status(a, a.failed ? 0 : call_norm_backward(spec, h, f, gate, (const float*)stats, &g, ws, bytes, stream));
 }
 
+// Whether bind() has been given the call's address.
+template <typename F>
+void bound(Args& a, F* call) {
+    if (!call) a.fail(PyExc_RuntimeError, "%s", "an entry point is missing");
+}
+
+PyObject* logprob(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Args a(args, n, 7);
+    flashoptim_matrix mx;
+    void* ws;
+    int64_t bytes;
+    const flashoptim_matrix* x = a.matrix("logits", &mx);
+    const int64_t rows = x ? x->rows : 0;
+    const void* tokens = a.plain("tokens", at::kLong, -1, 0, rows);
+    const float temperature = a.number();
+    void* logprob = a.plain("logprob", at::kFloat, -1, 0, rows);
+    void* lse = a.plain("lse", at::kFloat, -1, 0, rows);
+    a.workspace(&ws, &bytes);
+    void* stream = a.stream();
+    bound(a, call_logprob);
+    return status(a, a.failed ? 0 : call_logprob(x, (const int64_t*)tokens, temperature, (float*)logprob, (float*)lse, ws, bytes, stream));
+}
+
+PyObject* logprob_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Args a(args, n, 7);
+    flashoptim_matrix mx, md;
+    const flashoptim_matrix* x = a.matrix("logits", &mx);
+    const int64_t rows = x ? x->rows : 0;
+    const void* tokens = a.plain("tokens", at::kLong, -1, 0, rows);
+    const float temperature = a.number();
+    const void* lse = a.plain("lse", at::kFloat, -1, 0, rows);
+    const void* d = a.plain("dlogprob", at::kFloat, -1, 0, rows);
+    const flashoptim_matrix* dx = a.matrix("dlogits", &md);
+    void* stream = a.stream();
+    bound(a, call_logprob_backward);
+    return status(a, a.failed ? 0 : call_logprob_backward(x, (const int64_t*)tokens, temperature, (const float*)lse, (const float*)d, dx, stream));
+}
+
+PyObject* policy(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Args a(args, n, 12);
+    flashoptim_matrix mx, md;
+    flashoptim_policy_inputs in;
+    void* ws;
+    int64_t bytes;
+    const auto* spec = a.address<flashoptim_policy_spec>();
+    const flashoptim_matrix* x = a.matrix("logits", &mx);
+    const int64_t rows = x ? x->rows : 0;
+    const void* tokens = a.plain("tokens", at::kLong, -1, 0, rows);
+    in.advantages = (const float*)a.plain("advantages", at::kFloat, -1, 0, rows);
+    in.old_logprob = (const float*)a.plain("old_logprob", at::kFloat, -1, 0, rows);
+    in.ref_logprob = (const float*)a.plain("ref_logprob", at::kFloat, -1, 0, rows);
+    in.weights = (const float*)a.plain("weights", at::kFloat, -1, 0, rows);
+    void* stats = a.plain("stats", at::kFloat, -1, 0, 4);
+    void* logprob = a.plain("logprob", at::kFloat, -1, 0, rows);
+    const flashoptim_matrix* dx = a.matrix("dlogits", &md);
+    a.workspace(&ws, &bytes);
+    void* stream = a.stream();
+    bound(a, call_policy);
+    return status(a, a.failed ? 0 : call_policy(spec, x, (const int64_t*)tokens, &in, (float*)stats, (float*)logprob, dx, ws, bytes, stream));
+}
+
+PyObject* preference(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Args a(args, n, 9);
+    const auto* spec = a.address<flashoptim_preference_spec>();
+    const at::Tensor* first = a.tensor("logprob");
+    const int64_t rows = first ? first->numel() : 0;
+    --a.i;
+    const void* logprob = a.plain("logprob", at::kFloat, -1, 0, rows);
+    const at::Tensor* cuts = a.tensor("offsets");
+    const int64_t bounds = cuts ? cuts->numel() : 1;
+    --a.i;
+    const void* offsets = a.plain("offsets", at::kLong, -1, 0, bounds);
+    if (bounds % 2 == 0) a.fail(PyExc_ValueError, "%s", "offsets: the bounds of an even number of sequences, one more than that");
+    const int64_t pairs = bounds / 2;
+    void* loss = a.plain("loss", at::kFloat, -1, 0, 1);
+    const void* ref = a.plain("ref_logprob", at::kFloat, -1, 0, rows);
+    const void* weights = a.plain("weights", at::kFloat, -1, 0, rows);
+    void* margins = a.plain("margins", at::kFloat, -1, 0, pairs);
+    void* d = a.plain("dlogprob", at::kFloat, -1, 0, rows);
+    void* stream = a.stream();
+    bound(a, call_preference);
+    return status(a, a.failed ? 0 : call_preference(spec, (const float*)logprob, (const float*)ref, (const float*)weights, rows,
+                                                    (const int64_t*)offsets, pairs, (float*)loss, (float*)margins, (float*)d, stream));
+}
+
 // bind(addresses by name, current_stream, current_device)
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (n != 3 || !PyDict_Check(args[0])) {
@@ -246,6 +342,10 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
     take(args[0], "flashoptim_mx4_linear_backward", call_linear_backward);
     take(args[0], "flashoptim_block_norm", call_norm);
     take(args[0], "flashoptim_block_norm_backward", call_norm_backward);
+    take(args[0], "flashoptim_token_logprob", call_logprob);
+    take(args[0], "flashoptim_token_logprob_backward", call_logprob_backward);
+    take(args[0], "flashoptim_policy_loss", call_policy);
+    take(args[0], "flashoptim_preference_loss", call_preference);
     if (!call_quantize || !call_dequantize || !call_matmul || !call_linear || !call_linear_backward || !call_norm || !call_norm_backward) {
         PyErr_SetString(PyExc_RuntimeError, "bind: an entry point is missing");
         return nullptr;
@@ -269,6 +369,7 @@ PyObject* guarded(PyObject* self, PyObject* const* args, Py_ssize_t n) {
 #define FO_METHOD(name) {#name, (PyCFunction)(void (*)(void))guarded<name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FO_METHOD(bind),   FO_METHOD(quantize),        FO_METHOD(dequantize), FO_METHOD(matmul),
                          FO_METHOD(linear), FO_METHOD(linear_backward), FO_METHOD(norm),       FO_METHOD(norm_backward),
+                         FO_METHOD(logprob), FO_METHOD(logprob_backward), FO_METHOD(policy), FO_METHOD(preference),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
