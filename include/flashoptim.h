@@ -434,7 +434,7 @@ int flashoptim_block_norm_backward(const flashoptim_block_norm_spec* spec, const
  * makes its row's logprob and gradients NaN, and so the loss.  So does a row that holds a NaN or +infinity, or nothing but -infinity
  * (whose lse is -infinity); a -infinity beside other values has the probability 0.  Sums over a row are FP32 by lane and FP64 where lanes
  * join, what is computed once for a row is FP64; the order of all sums depends on the sizes alone.  Vectors are contiguous FP32.
- *   1 <= vocab < 2^31 - 4096 unless rows = 0; rows < 2^31; T > 0 and finite.
+ *   1 <= vocab < 2^30 unless rows = 0; rows < 2^22, and fewer than 2^24 parts of 16384 BF16 or 8192 FP32 values; T > 0 and finite.
  * token_logprob: logprob, lse [rows], either may be NULL (not both, unless rows = 0).
  * token_logprob_backward: dlogits_ij = dlogprob_i / T ([j = t] - exp(logits_ij / T - lse_i)), of the type of logits, from the lse that the forward
  *   call left.  The logits of a row whose dlogprob is 0 are not read; its gradient is 0.  dlogits may be logits' own buffer.
