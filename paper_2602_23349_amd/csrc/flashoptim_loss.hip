@@ -21,10 +21,11 @@ namespace {
 using fo::f32x4;
 using fo::i32x4;
 using fo::load_as;
-using fo::store_as;
 using fo::up;
 using f32x8 = float __attribute__((ext_vector_type(8)));
 using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
+
+typedef i32x4 anywhere __attribute__((aligned(2)));      // (the hardware takes global accesses at any byte)
 
 constexpr double kLog2e = 1.4426950408889634;
 constexpr int kPairThreads = 1024;
@@ -43,6 +44,8 @@ template <bool FP32>
 __device__ __forceinline__ float value_at(const char* row, int32_t j) {
     return FP32 ? ((const float*)row)[j] : __uint_as_float((uint32_t)((const uint16_t*)row)[j] << 16);
 }
+// A token that is there as its place, one that is not as none that any lane holds.
+__device__ __forceinline__ int32_t token_in(int64_t token, int32_t vocab) { return token < vocab ? (int32_t)token : 0x7fffffff; }
 // The logit of a token; one that is not there has none.
 template <bool FP32>
 __device__ __forceinline__ float logit_of(const char* row, int64_t token, int32_t vocab) {
@@ -83,91 +86,103 @@ __device__ __forceinline__ Sum join(const Sum& a, const Sum& b, float c) {
     return {a.sum * (double)exp2_of((a.most - base) * c) + b.sum * (double)exp2_of((b.most - base) * c), most};
 }
 
-// What LANES lanes hold of a row in registers: the values from `begin` up to `end`, at most LANES * NV * 8 of them, lane l's i-th eight from begin +
-// 8 (i LANES + l) on.  Every lane loads eight values that exist, so that no load is a case distinction: the last eight of a ragged row begin within
-// their neighbours', and those behind the end are the last eight again.  What is not the lane's own becomes -infinity, which adds nothing.
-// (NARROW: rows of fewer than eight values, which lane 0 takes one by one.)
+// A word of sixteen bytes: eight BF16 values or four FP32 ones.
+template <bool FP32>
+constexpr int kValues = FP32 ? 4 : 8;
+
+// What LANES lanes hold of a row in registers, at most LANES * NV words: lane l's i-th word are the values from at(i) on, which is a 16-byte border of
+// memory (words across such borders: log-probabilities of 8192 x 50257 BF16 logits 169 us, so 141).  Every lane loads words that exist, so that no
+// load is a case distinction: the row's first values where its own word begins ahead of the row, the last ones where it reaches behind it, and the last
+// ones again where there is none.  What is not the lane's own becomes -infinity, which adds nothing.  (NARROW: rows of less than a word, which lane 0
+// takes value by value.)  Logits and gradients go past the caches: each is touched once, and there are more of them than the caches hold (with and without:
+// the same log-probabilities 125 and 141 us, the gradient of 4096 x 128256 360 and 388).
 template <bool FP32, int LANES, int NV, bool NARROW = false>
 struct Held {
-    static constexpr int kWords = FP32 ? 2 : 1;
-    i32x4 raw[NV][kWords];
-    int32_t begin, end;
+    static constexpr int kN = kValues<FP32>, kSize = FP32 ? 4 : 2;
+    i32x4 raw[NV];
+    int32_t begin, vocab;    // begin: 0 or less for a row's first part
     int lane;
 
     // Between two passes over what is held.  The values are unpacked again in each: kept from one to the next, they would take twice the registers.
     __device__ __forceinline__ void forget_values() {
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int k = 0; k < kWords; ++k) asm volatile("" : "+v"(raw[i][k]));
+        for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(raw[i]));
+        asm volatile("" : "+v"(lane));       // (nor are the places that follow from it kept)
+    }
+    // The part of the row that begins `first` values (whole words) behind the last border at or ahead of the row's beginning.
+    __device__ __forceinline__ void place(const char* row, int32_t first, int32_t vocab_, int lane_) {
+        const int32_t ahead = NARROW ? 0 : (int32_t)((uintptr_t)row & 15) / kSize;
+        begin = first - ahead; vocab = vocab_; lane = lane_;
     }
     // (32 bits beside the row's address, which is a wavefront's: vocab < 2^30)
-    static __device__ __forceinline__ uint32_t bytes(int32_t j) { return (uint32_t)j * (FP32 ? 4u : 2u); }
-    __device__ __forceinline__ int32_t at(int i) const { return begin + 8 * (i * LANES + lane); }
-    __device__ __forceinline__ void load(const char* row, int32_t begin_, int32_t end_, int lane_) {
-        begin = begin_; end = end_; lane = lane_;
+    static __device__ __forceinline__ uint32_t bytes(int32_t j) { return (uint32_t)j * (uint32_t)kSize; }
+    __device__ __forceinline__ int32_t at(int i) const { return begin + kN * (i * LANES + lane); }
+    // The first value that is loaded.
+    __device__ __forceinline__ int32_t from(int i) const { return NARROW ? 0 : min(max(at(i), 0), vocab - kN); }
+    // Whether the i-th words of all lanes are their own and whole.  (The same for all lanes.)
+    __device__ __forceinline__ bool inside(int i) const { return !NARROW && (i > 0 || begin >= 0) && begin + kN * (i + 1) * LANES <= vocab; }
+    __device__ __forceinline__ bool any(int i) const { return at(i) < vocab; }
+    __device__ __forceinline__ bool whole(int i) const { return !NARROW && at(i) >= 0 && at(i) + kN <= vocab; }
+    template <bool PAST = true>
+    __device__ __forceinline__ void load(const char* row) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if constexpr (NARROW) {
-                raw[i][0] = raw[i][kWords - 1] = i32x4{};
+                raw[i] = i32x4{};
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    if (i > 0 || k >= end) continue;
-                    if constexpr (FP32) raw[i][k / 4][k % 4] = ((const int*)row)[k];
-                    else raw[i][0][k / 2] |= (int)((uint32_t)((const uint16_t*)row)[k] << (16 * (k % 2)));
+                for (int k = 0; k < kN; ++k) {
+                    if (i > 0 || k >= vocab) continue;
+                    if constexpr (FP32) raw[i][k] = ((const int*)row)[k];
+                    else raw[i][k / 2] |= (int)((uint32_t)((const uint16_t*)row)[k] << (16 * (k % 2)));
                 }
             } else {
-                const uint32_t from = bytes(min(at(i), end - 8));
-#pragma unroll
-                for (int k = 0; k < kWords; ++k) raw[i][k] = load_as<i32x4>(row + from + 16 * k);
+                const char* p = row + bytes(from(i));
+                raw[i] = PAST ? __builtin_nontemporal_load((const anywhere*)p) : load_as<i32x4>(p);
             }
         }
     }
-    // Of the i-th eight, those that are the lane's own: [first, last).
+    // Of the i-th word as loaded, the values that are the lane's own: [first, last).
     __device__ __forceinline__ void own(int i, int* first, int* last) const {
-        const int32_t j = at(i);
-        if (NARROW) { *first = 0; *last = j == 0 ? end : 0; }
-        else { *first = min(max(j - (end - 8), 0), 8); *last = 8; }
+        if (NARROW) { *first = 0; *last = at(i) == 0 ? vocab : 0; }
+        else { *first = min(max(at(i) - from(i), 0), kN); *last = min(at(i) + kN - from(i), kN); }
     }
     // Puts -infinity where a value is not the lane's own.  (Before the first use.)
     __device__ __forceinline__ void settle(int i) {
-        if (begin + 8 * (i + 1) * LANES <= end || at(i) + 8 <= end) return;
+        if (inside(i) || whole(i)) return;
         int first, last;
         own(i, &first, &last);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < kN; ++k) {
             const bool keep = k >= first && k < last;
-            if constexpr (FP32) raw[i][k / 4][k % 4] = keep ? raw[i][k / 4][k % 4] : (int)0xff800000;
+            if constexpr (FP32) raw[i][k] = keep ? raw[i][k] : (int)0xff800000;
             else {
                 const uint32_t shift = 16 * (k % 2);
-                const uint32_t w = (uint32_t)raw[i][0][k / 2];
-                raw[i][0][k / 2] = keep ? (int)w : (int)((w & ~(0xffffu << shift)) | 0xff80u << shift);
+                const uint32_t w = (uint32_t)raw[i][k / 2];
+                raw[i][k / 2] = keep ? (int)w : (int)((w & ~(0xffffu << shift)) | 0xff80u << shift);
             }
         }
     }
-    __device__ __forceinline__ void values(int i, float (&v)[8]) const {
-        if constexpr (FP32) {
+    __device__ __forceinline__ void values(int i, float (&v)[kN]) const {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = __int_as_float(raw[i][k / 4][k % 4]);
-        } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                v[2 * k] = __uint_as_float((uint32_t)raw[i][0][k] << 16);
-                v[2 * k + 1] = __uint_as_float((uint32_t)raw[i][0][k] & 0xffff0000u);
+        for (int k = 0; k < 4; ++k) {
+            if constexpr (FP32) v[k] = __int_as_float(raw[i][k]);
+            else {
+                v[2 * k] = __uint_as_float((uint32_t)raw[i][k] << 16);
+                v[2 * k + 1] = __uint_as_float((uint32_t)raw[i][k] & 0xffff0000u);
             }
         }
     }
-    // The sum of the wavefront's part, in every lane.  A lane adds up in FP32, apart from eights that hold a value near the wavefront's largest, which go into
-    // an FP64 sum: beside a token that is all but certain the others would be lost in its rounding, and with them its log-probability.
+    // The sum of the wavefront's part, in every lane.  A lane adds up in FP32, apart from words of some weight beside the wavefront's largest value, which go
+    // into an FP64 sum: beside a token that is all but certain the others would be lost in its rounding, and with them its log-probability.
     __device__ __forceinline__ Sum wave_part(float c) {
         float most = minus_inf();
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             settle(i);
-            float v[8];
+            float v[kN];
             values(i, v);
 #pragma unroll
-            for (int k = 0; k < 8; k += 2) most = fmaxf(fmaxf(most, v[k]), v[k + 1]);
+            for (int k = 0; k < kN; k += 2) most = fmaxf(fmaxf(most, v[k]), v[k + 1]);
         }
         forget_values();
         most = wave_max(most);
@@ -176,66 +191,62 @@ struct Held {
         double near = 0.0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            float v[8];
+            float v[kN], word = 0.0f;
             values(i, v);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = exp2_of((v[k] - base) * c);
-            const float largest = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
-            if (__builtin_amdgcn_ballot_w64(largest >= 0.5f)) {
+            for (int k = 0; k < kN; ++k) v[k] = exp2_of((v[k] - base) * c);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) near += (double)v[k];
+            for (int k = 0; k < kN; k += 4) word += (v[k] + v[k + 1]) + (v[k + 2] + v[k + 3]);
+            if (__builtin_amdgcn_ballot_w64(word >= 0.5f)) {
+#pragma unroll
+                for (int k = 0; k < kN; ++k) near += (double)v[k];
             } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) sum += v[k];
+                sum += word;
             }
         }
         return {wave_sum(near + (double)sum), most};
     }
     // Stores -d p, or d (1 - p) for the token, of all that is held: p = 2^((x - base) c - shift).
-    __device__ __forceinline__ void store_gradient(char* row, int64_t token, float d, float base, float c, float shift) {
+    __device__ __forceinline__ void store_gradient(char* row, int32_t token, float d, float base, float c, float shift) {
         forget_values();
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int32_t j = at(i);
-            if (j >= end) continue;
-            float v[8];
+            const bool in = inside(i);
+            if (!in && !any(i)) continue;
+            float v[kN];
             values(i, v);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = -d * exp2_of(fmaf(v[k] - base, c, -shift));
-            const int32_t from = NARROW ? 0 : min(j, end - 8);
-            if (token >= from && token < from + 8) {
+            for (int k = 0; k < kN; ++k) v[k] = -d * exp2_of(fmaf(v[k] - base, c, -shift));
+            const int32_t j = in ? at(i) : from(i);
+            if ((uint32_t)(token - j) < (uint32_t)kN) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = token == from + k ? v[k] + d : v[k];
+                for (int k = 0; k < kN; ++k) v[k] = token == j + k ? v[k] + d : v[k];
             }
-            store(row, i, v);
+            store(row, i, in, v);
         }
     }
     __device__ __forceinline__ void store_zeros(char* row) const {
-        const float v[8] = {};
+        const float v[kN] = {};
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-            if (at(i) < end) store(row, i, v);
+            if (inside(i) || any(i)) store(row, i, inside(i), v);
     }
-    __device__ __forceinline__ void store(char* row, int i, const float (&v)[8]) const {
-        const int32_t j = at(i);
-        if (j + 8 <= end) {
-            char* p = row + bytes(j);
-            if constexpr (FP32) {
-                store_as(p, f32x4{v[0], v[1], v[2], v[3]});
-                store_as(p + 16, f32x4{v[4], v[5], v[6], v[7]});
-            } else {
-                store_as(p, __builtin_convertvector((f32x8){v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]}, bf16x8));
-            }
+    __device__ __forceinline__ void store(char* row, int i, bool in, const float (&v)[kN]) const {
+        const int32_t j = in ? at(i) : from(i);
+        if (in || whole(i)) {
+            i32x4 w;
+            if constexpr (FP32) w = __builtin_bit_cast(i32x4, (f32x4){v[0], v[1], v[2], v[3]});
+            else w = __builtin_bit_cast(i32x4, __builtin_convertvector((f32x8){v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]}, bf16x8));
+            __builtin_nontemporal_store(w, (anywhere*)(row + bytes(j)));
             return;
         }
         int first, last;
         own(i, &first, &last);
-        const int32_t from = NARROW ? 0 : end - 8;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < kN; ++k) {
             if (k < first || k >= last) continue;
-            if constexpr (FP32) ((float*)row)[from + k] = v[k];
-            else ((__bf16*)row)[from + k] = (__bf16)v[k];
+            if constexpr (FP32) ((float*)row)[j + k] = v[k];
+            else ((__bf16*)row)[j + k] = (__bf16)v[k];
         }
     }
 };
@@ -322,18 +333,18 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void policy_rows_kernel(
     const int64_t token = a.tokens[row];
     const float w = a.policy.in.weights ? a.policy.in.weights[row] : 1.0f;
     char* dx = a.dx ? a.dx + (int64_t)row * a.dx_stride * (FP32 ? 4 : 2) : nullptr;
+    const char* x = row_of<FP32>(a.x, row);
     Held<FP32, LANES, NV, NARROW> h;
+    h.place(x, 0, a.x.vocab, lane);
     if (token < 0 || w == 0.0f) {
         if (lane == 0) {
             if (a.logprob) a.logprob[row] = 0.0f;
             put_terms(a.policy, a.rows, row, {});
         }
-        h.begin = 0; h.end = a.x.vocab; h.lane = lane;
         if (dx) h.store_zeros(dx);
         return;
     }
-    const char* x = row_of<FP32>(a.x, row);
-    h.load(x, 0, a.x.vocab, lane);
+    h.load(x);
     const float logit = logit_of<FP32>(x, token, a.x.vocab);
     const Sum s = join_waves<LANES / 64>(h.wave_part(a.c), a.c);
     const RowLog l = row_log(s, logit, a.inv_t);
@@ -345,13 +356,13 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void policy_rows_kernel(
     if (!dx) return;
     const float d = p.slope * a.scale;
     if (d == 0.0f) h.store_zeros(dx);
-    else h.store_gradient(dx, token, d, base_of(s.most), a.c, (float)(l.log_sum * kLog2e));
+    else h.store_gradient(dx, token_in(token, a.x.vocab), d, base_of(s.most), a.c, (float)(l.log_sum * kLog2e));
 }
 
 // Log-probabilities only, one workgroup of WAVES wavefronts to a row, through which the wavefronts go in turn.
 template <bool FP32, int WAVES, bool NARROW>
 __global__ __launch_bounds__(WAVES * 64) void logprob_rows_kernel(RowsArgs a) {
-    constexpr int NV = NARROW ? 1 : FP32 ? 4 : 8;
+    constexpr int NV = NARROW ? 1 : 8, kPart = 64 * NV * kValues<FP32>;
     const uint32_t row = blockIdx.x;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int64_t token = a.tokens[row];
@@ -365,9 +376,10 @@ __global__ __launch_bounds__(WAVES * 64) void logprob_rows_kernel(RowsArgs a) {
     const char* x = row_of<FP32>(a.x, row);
     const float logit = logit_of<FP32>(x, token, a.x.vocab);
     Sum s = {0.0, minus_inf()};
-    for (int32_t begin = wave * 64 * NV * 8; begin < a.x.vocab; begin += WAVES * 64 * NV * 8) {
+    for (int32_t first = wave * kPart; first < a.x.vocab + kValues<FP32>; first += WAVES * kPart) {
         Held<FP32, 64, NV, NARROW> h;
-        h.load(x, begin, a.x.vocab, lane);
+        h.place(x, first, a.x.vocab, lane);
+        h.load(x);
         s = join(s, h.wave_part(a.c), a.c);
     }
     s = join_waves<WAVES>(s, a.c);
@@ -379,30 +391,27 @@ __global__ __launch_bounds__(WAVES * 64) void logprob_rows_kernel(RowsArgs a) {
 
 // ---- few rows, or rows that do not fit: each cut into parts, a workgroup to each, which leaves its sum; whoever needs a row's joins them.
 constexpr int kPartThreads = 256;
-template <bool FP32>
-constexpr int part_vecs() { return FP32 ? 4 : 8; }
 struct PartsArgs {
     RowsArgs r;
     Sum* sums;               // [rows, parts]
     float* logits;           // [rows]: of the tokens
     uint32_t parts;
-    int32_t part;            // values
 };
 __device__ __forceinline__ bool counts(const PartsArgs& a, uint32_t row, int64_t token, float* w) {
     *w = a.r.policy.in.weights ? a.r.policy.in.weights[row] : 1.0f;
     return token >= 0 && *w != 0.0f;
 }
 
-template <bool FP32>
+template <bool FP32, int NV>
 __global__ __launch_bounds__(kPartThreads) void parts_kernel(PartsArgs a) {
     const uint32_t row = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
     const int64_t token = a.r.tokens[row];
     float w;
     if (!counts(a, row, token, &w)) return;
     const char* x = row_of<FP32>(a.r.x, row);
-    const int32_t begin = (int32_t)part * a.part, end = min(a.r.x.vocab, begin + a.part);
-    Held<FP32, kPartThreads, part_vecs<FP32>()> h;
-    h.load(x, begin, end, (int)threadIdx.x);
+    Held<FP32, kPartThreads, NV> h;
+    h.place(x, (int32_t)part * (kPartThreads * NV * kValues<FP32>), a.r.x.vocab, (int)threadIdx.x);
+    h.template load<false>(x);       // (the gradient reads it again)
     if (part == 0 && threadIdx.x == 0) a.logits[row] = logit_of<FP32>(x, token, a.r.x.vocab);
     const Sum s = join_waves<kPartThreads / 64>(h.wave_part(a.r.c), a.r.c);
     if (threadIdx.x == 0) a.sums[(int64_t)row * a.parts + part] = s;
@@ -429,17 +438,17 @@ __global__ __launch_bounds__(kJoinRows * 64) void logprob_join_kernel(PartsArgs 
 }
 
 // The gradient of a part.  Every workgroup joins its row's sums and computes the row's slope for itself; the first of a row leaves what is kept of it.
-template <bool FP32>
+template <bool FP32, int NV>
 __global__ __launch_bounds__(kPartThreads) void policy_parts_kernel(PartsArgs a) {
     const uint32_t row = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
     const int64_t token = a.r.tokens[row];
     float w;
     const bool there = counts(a, row, token, &w);
     char* dx = a.r.dx ? a.r.dx + (int64_t)row * a.r.dx_stride * (FP32 ? 4 : 2) : nullptr;
-    const int32_t begin = (int32_t)part * a.part, end = min(a.r.x.vocab, begin + a.part);
-    Held<FP32, kPartThreads, part_vecs<FP32>()> h;
-    h.begin = begin; h.end = end; h.lane = (int)threadIdx.x;
-    if (there && dx) h.load(row_of<FP32>(a.r.x, row), begin, end, (int)threadIdx.x);
+    const char* x = row_of<FP32>(a.r.x, row);
+    Held<FP32, kPartThreads, NV> h;
+    h.place(x, (int32_t)part * (kPartThreads * NV * kValues<FP32>), a.r.x.vocab, (int)threadIdx.x);
+    if (there && dx) h.load(x);
     Sum s = {1.0, 0.0f};
     RowLog l = {0.0, 0.0, 0.0};
     PolicyRow p = {};
@@ -455,7 +464,7 @@ __global__ __launch_bounds__(kPartThreads) void policy_parts_kernel(PartsArgs a)
     if (!dx) return;
     const float d = p.slope * a.r.scale;
     if (d == 0.0f) h.store_zeros(dx);
-    else h.store_gradient(dx, token, d, base_of(s.most), a.r.c, (float)(l.log_sum * kLog2e));
+    else h.store_gradient(dx, token_in(token, a.r.x.vocab), d, base_of(s.most), a.r.c, (float)(l.log_sum * kLog2e));
 }
 
 // ---- the gradient of the logits from the lse of an earlier call
@@ -467,25 +476,24 @@ struct GradArgs {
     const float *lse, *slope;
     float scale, c;          // of the slopes
     uint32_t parts;
-    int32_t part;
 };
-template <bool FP32, bool NARROW>
+template <bool FP32, int NV, bool NARROW>
 __global__ __launch_bounds__(kPartThreads) void gradient_kernel(GradArgs a) {
     const uint32_t row = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
     char* dx = a.dx + (int64_t)row * a.stride * (FP32 ? 4 : 2);
-    const int32_t begin = (int32_t)part * a.part, end = min(a.x.vocab, begin + a.part);
+    const char* x = row_of<FP32>(a.x, row);
     const int64_t token = a.tokens[row];
     float d = token < 0 ? 0.0f : a.slope[row] * a.scale;
-    Held<FP32, kPartThreads, NARROW ? 1 : part_vecs<FP32>(), NARROW> h;
+    Held<FP32, kPartThreads, NV, NARROW> h;
+    h.place(x, (int32_t)part * (kPartThreads * NV * kValues<FP32>), a.x.vocab, (int)threadIdx.x);
     if (d == 0.0f) {
-        h.begin = begin; h.end = end; h.lane = (int)threadIdx.x;
         h.store_zeros(dx);
         return;
     }
     if (token >= a.x.vocab) d = __builtin_nanf("");
     const float shift = a.lse[row] * (float)kLog2e;
-    h.load(row_of<FP32>(a.x, row), begin, end, (int)threadIdx.x);
-    h.store_gradient(dx, token, d, 0.0f, a.c, shift);
+    h.load(x);
+    h.store_gradient(dx, token_in(token, a.x.vocab), d, 0.0f, a.c, shift);
 }
 
 // The sum over a workgroup, in every lane, in a fixed order.
@@ -523,57 +531,86 @@ struct PairArgs {
 
 __device__ __forceinline__ double softplus(double z) { return fmax(z, 0.0) + log1p(exp(-fabs(z))); }
 
-// One workgroup for all pairs, so that the loss needs no second launch: there are a few bytes for each row of logits.
-__global__ __launch_bounds__(kPairThreads) void preference_kernel(PairArgs a) {
+// What of a pair's margin the loss and its slope by the margin are.
+struct PairLoss {
+    double loss, slope;
+};
+__device__ __forceinline__ PairLoss pair_loss(const flashoptim_preference_spec& spec, double gain) {
+    const double beta = spec.beta, z = beta * gain, e = spec.label_smoothing;
+    if (spec.kind == FLASHOPTIM_PREFERENCE_SIGMOID)      // (z may be infinite)
+        return {(1.0 - e) * softplus(-z) + (e > 0.0 ? e * softplus(z) : 0.0), e / (1.0 + exp(-z)) - (1.0 - e) / (1.0 + exp(z))};
+    if (spec.kind == FLASHOPTIM_PREFERENCE_HINGE)        // (z may be NaN)
+        return {z < 1.0 ? 1.0 - z : z >= 1.0 ? 0.0 : z, z < 1.0 ? -1.0 : z >= 1.0 ? 0.0 : z};
+    const double r = gain - 0.5 / beta;
+    return {r * r, 2.0 * r / beta};
+}
+
+// One workgroup for all pairs, so that the loss needs no second launch: there are a few bytes for each row of logits.  Its wavefronts are shared out over
+// `groups` pairs at a time: from one wavefront each, with nothing to wait for between them, to all sixteen for a single pair.
+__global__ __launch_bounds__(kPairThreads) void preference_kernel(PairArgs a, int groups) {
+    constexpr int kWaves = kPairThreads / 64, kAhead = 4;
+    __shared__ double gains[kWaves], losses[kWaves];
     const auto bound = [&](int64_t i) { return min(max(a.offsets[i], (int64_t)0), a.rows); };
     const bool by_turns = a.spec.order == FLASHOPTIM_PAIRS_BY_TURNS;
-    const double beta = a.spec.beta, e = a.spec.label_smoothing;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = kWaves / groups, group = wave / waves;
+    const int lane = (wave % waves) * 64 + ((int)threadIdx.x & 63), lanes = waves * 64;
     double total = 0.0;
-    for (int64_t p = 0; p < a.pairs; ++p) {
-        const int64_t of[2] = {by_turns ? 2 * p : p, by_turns ? 2 * p + 1 : a.pairs + p};
+    for (int64_t first = 0; first < a.pairs; first += groups) {
+        const int64_t p = first + group;
+        const bool there = p < a.pairs;
+        int64_t begin[2] = {}, end[2] = {};
         double gain = 0.0;
-        for (int k = 0; k < 2; ++k) {
-            const int64_t end = bound(of[k] + 1);
+        for (int k = 0; k < 2 && there; ++k) {
+            const int64_t of = by_turns ? 2 * p + k : p + k * a.pairs;
+            begin[k] = bound(of);
+            end[k] = bound(of + 1);
             double s = 0.0;
-            for (int64_t i = bound(of[k]) + threadIdx.x; i < end; i += kPairThreads) {
-                const float w = a.weights ? a.weights[i] : 1.0f;
-                if (w != 0.0f) s += (double)w * ((double)a.logprob[i] - (a.ref ? (double)a.ref[i] : 0.0));
+            for (int64_t i = begin[k] + lane; i < end[k]; i += kAhead * lanes) {
+                float w[kAhead], v[kAhead], r[kAhead];
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) {      // (behind the end: the last row, which counts no second time)
+                    const int64_t at = min(i + (int64_t)u * lanes, end[k] - 1);
+                    w[u] = a.weights ? a.weights[at] : 1.0f;
+                    v[u] = a.logprob[at];
+                    r[u] = a.ref ? a.ref[at] : 0.0f;
+                }
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u)
+                    if (w[u] != 0.0f && i + (int64_t)u * lanes < end[k]) s += (double)w[u] * ((double)v[u] - (double)r[u]);
             }
-            s = group_sum<kPairThreads>(s);
             gain += k ? -s : s;
         }
-        const double z = beta * gain;
-        double loss, d;
-        if (a.spec.kind == FLASHOPTIM_PREFERENCE_SIGMOID) {
-            loss = (1.0 - e) * softplus(-z) + (e > 0.0 ? e * softplus(z) : 0.0);      // (z may be infinite)
-            d = e / (1.0 + exp(-z)) - (1.0 - e) / (1.0 + exp(z));
-        } else if (a.spec.kind == FLASHOPTIM_PREFERENCE_HINGE) {
-            loss = z < 1.0 ? 1.0 - z : z >= 1.0 ? 0.0 : z;                          // (z may be NaN)
-            d = z < 1.0 ? -1.0 : z >= 1.0 ? 0.0 : z;
-        } else {
-            const double r = gain - 0.5 / beta;
-            loss = r * r;
-            d = 2.0 * r / beta;
+        gain = wave_sum(gain);
+        if (waves > 1) {
+            __syncthreads();
+            if ((threadIdx.x & 63) == 0) gains[wave] = gain;
+            __syncthreads();
+            gain = 0.0;
+            for (int k = 0; k < waves; ++k) gain += gains[group * waves + k];
         }
-        total += loss;
-        if (threadIdx.x == 0 && a.margins) a.margins[p] = (float)z;
-        if (a.dlogprob) {
-            d *= beta * (double)a.spec.grad_scale / (double)a.pairs;
-            for (int k = 0; k < 2; ++k) {
-                const int64_t end = bound(of[k] + 1);
-                for (int64_t i = bound(of[k]) + threadIdx.x; i < end; i += kPairThreads) {
-                    const float w = a.weights ? a.weights[i] : 1.0f;
-                    a.dlogprob[i] = w == 0.0f ? 0.0f : (float)((k ? -d : d) * w);
-                }
+        if (!there) continue;
+        const PairLoss l = pair_loss(a.spec, gain);
+        total += l.loss;
+        if (lane == 0 && a.margins) a.margins[p] = (float)((double)a.spec.beta * gain);
+        if (!a.dlogprob) continue;
+        const double d = l.slope * ((double)a.spec.beta * (double)a.spec.grad_scale / (double)a.pairs);
+        for (int k = 0; k < 2; ++k)
+            for (int64_t i = begin[k] + lane; i < end[k]; i += lanes) {
+                const float w = a.weights ? a.weights[i] : 1.0f;
+                a.dlogprob[i] = w == 0.0f ? 0.0f : (float)((k ? -d : d) * (double)w);
             }
-        }
     }
     if (a.dlogprob) {
         const int64_t first = a.pairs ? bound(0) : a.rows, last = a.pairs ? bound(2 * a.pairs) : a.rows;
         for (int64_t i = threadIdx.x; i < first; i += kPairThreads) a.dlogprob[i] = 0.0f;
         for (int64_t i = last + threadIdx.x; i < a.rows; i += kPairThreads) a.dlogprob[i] = 0.0f;
     }
-    if (threadIdx.x == 0) *a.loss = a.pairs ? (float)(total / (double)a.pairs) : 0.0f;
+    if (lane == 0) losses[group] = total;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    total = 0.0;
+    for (int k = 0; k < groups; ++k) total += losses[k];
+    *a.loss = a.pairs ? (float)(total / (double)a.pairs) : 0.0f;
 }
 
 // --------------------------------------------------------------------------------------------------- host --
@@ -602,17 +639,36 @@ int check_gradient(const flashoptim_matrix* d, const flashoptim_matrix* logits) 
 }
 Logits to_dev(const flashoptim_matrix* m) { return {(const char*)m->data, m->rows > 1 ? m->stride : 0, (int32_t)m->cols}; }
 
-// How a row is cut: into parts of as many values as a workgroup holds, or of fewer where there are few rows, so that all compute units have one.
-constexpr int64_t kHeldPart[2] = {kPartThreads * 8 * part_vecs<false>(), kPartThreads * 8 * part_vecs<true>()};     // by dtype
-constexpr int64_t kLeastPart = 2048;
+// The words of 16 bytes that a row takes up: one more where it does not begin on such a border.
+int64_t words(int64_t vocab, int dtype, bool aligned) { return up(vocab * fo::elem_bytes(dtype), 16) + (aligned ? 0 : 1); }
+// Rows of less than a word.
+bool narrow(int64_t vocab, int dtype) { return vocab * fo::elem_bytes(dtype) < 16; }
+bool rows_aligned(const flashoptim_matrix* m) {
+    const int64_t size = fo::elem_bytes(m->dtype);
+    return fo::aligned_to(m->data, 16) && (m->rows <= 1 || m->stride * size % 16 == 0);
+}
+
+// How a row is cut: into parts of kPartThreads lanes that hold `vecs` words each, as many as registers allow, or fewer where there are few rows, so that all
+// compute units have one.
 struct Parts {
-    int32_t part;
+    int vecs;
     uint32_t parts;
 };
-Parts cut_rows(int64_t rows, int64_t vocab, int dtype) {
-    int64_t part = kHeldPart[dtype];
-    while (part > kLeastPart && rows * up(vocab, part) < 512) part /= 2;
-    return {(int32_t)part, (uint32_t)up(vocab, part)};
+Parts cut_rows(int64_t rows, int64_t vocab, int dtype, bool aligned) {
+    int vecs = 8;
+    const auto parts = [&] { return up(words(vocab, dtype, aligned), kPartThreads * vecs); };
+    while (vecs > 1 && rows * parts() < 512) vecs /= 2;
+    return {vecs, (uint32_t)parts()};
+}
+template <int N>
+using Int = std::integral_constant<int, N>;
+// Calls launch(fp32, vecs) with the two as types.
+template <typename F>
+void with_vecs(int dtype, int vecs, F launch) {
+    const auto with = [&](auto fp32) {
+        if (vecs == 8) launch(fp32, Int<8>{}); else if (vecs == 4) launch(fp32, Int<4>{}); else if (vecs == 2) launch(fp32, Int<2>{}); else launch(fp32, Int<1>{});
+    };
+    if (dtype == FLASHOPTIM_FP32) with(std::true_type{}); else with(std::false_type{});
 }
 bool known(int dtype) { return dtype == FLASHOPTIM_BF16 || dtype == FLASHOPTIM_FP32; }
 
@@ -625,57 +681,59 @@ void with_types(bool fp32, bool narrow, F launch) {
     else { if (narrow) launch(No{}, Yes{}); else launch(No{}, No{}); }
 }
 
-// Calls launch(shape) with the shape of the workgroups that hold rows of this many values, false if there is none.
+// Calls launch(shape) with the shape of the workgroups that hold rows of n words.
 template <int LANES, int NV, bool NARROW = false>
 struct Shape {
     static constexpr int kLanes = LANES, kVecs = NV;
     static constexpr bool kNarrow = NARROW;
 };
-template <bool FP32, typename F>
-bool with_held(int64_t vocab, F launch) {
-    constexpr int K = FP32 ? 2 : 1;        // (eight FP32 values are twice the registers)
-    if (vocab < 8) launch(Shape<64, 1, true>{});
-    else if (vocab <= 64 * 8 * 4 / K) launch(Shape<64, 4 / K>{});
-    else if (vocab <= 64 * 8 * 8 / K) launch(Shape<64, 8 / K>{});
-    else if (vocab <= 256 * 8 * 8 / K) launch(Shape<256, 8 / K>{});
-    else if (vocab <= 512 * 8 * 8 / K) launch(Shape<512, 8 / K>{});
-    else if (vocab <= 512 * 8 * 16 / K) launch(Shape<512, 16 / K>{});
-    else if (vocab <= 1024 * 8 * 16 / K) launch(Shape<1024, 16 / K>{});
-    else return false;
-    return true;
+template <typename F>
+void with_held(int64_t n, F launch) {
+    if (n <= 64 * 4) launch(Shape<64, 4>{});
+    else if (n <= 64 * 8) launch(Shape<64, 8>{});
+    else if (n <= 256 * 8) launch(Shape<256, 8>{});
+    else if (n <= 512 * 8) launch(Shape<512, 8>{});
+    else if (n <= 512 * 16) launch(Shape<512, 16>{});
+    else launch(Shape<1024, 16>{});
 }
-// Whether a call holds whole rows: those of a wavefront always, longer ones where there are as many as fill half the chip.
-bool holds_rows(int64_t rows, int64_t vocab, int dtype) {
-    const int64_t k = dtype == FLASHOPTIM_FP32 ? 2 : 1;
-    return vocab <= 4096 / k || (vocab <= 131072 / k && rows >= 128);
+// Whether a call holds whole rows: those of a wavefront always, longer ones, up to the largest shape's, where there are as many as fill half the chip.
+bool holds_rows(int64_t rows, int64_t vocab, int dtype, bool aligned) {
+    const int64_t n = words(vocab, dtype, aligned);
+    return n <= 64 * 8 || (n <= 1024 * 16 && rows >= 128);
 }
+constexpr int kStreamWaves = 8;
 bool streams_rows(int64_t rows, int64_t vocab) { return vocab <= 4096 || rows >= 512; }
 
-int launch_parts(const PartsArgs& p, int dtype, void* stream) {
-    const dim3 grid(p.r.rows * p.parts), block(kPartThreads);
-    if (dtype == FLASHOPTIM_FP32) hipLaunchKernelGGL(parts_kernel<true>, grid, block, 0, (hipStream_t)stream, p);
-    else hipLaunchKernelGGL(parts_kernel<false>, grid, block, 0, (hipStream_t)stream, p);
-    return fo::hip_status(hipGetLastError());
-}
 // A call's parts in its workspace.
 PartsArgs to_parts(const RowsArgs& a, const Parts& c, void* workspace) {
-    PartsArgs p = {a, (Sum*)workspace, nullptr, c.parts, c.part};
+    PartsArgs p = {a, (Sum*)workspace, nullptr, c.parts};
     p.logits = (float*)(p.sums + (int64_t)a.rows * c.parts);
     return p;
 }
-int64_t parts_bytes(int64_t rows, const Parts& c) { return up(rows * (int64_t)c.parts * (int64_t)sizeof(Sum) + rows * 4, 16) * 16; }
-
-template <bool FP32>
-int launch_held(const RowsArgs& a, void* stream) {
-    with_held<FP32>(a.x.vocab, [&](auto shape) {
-        constexpr int L = decltype(shape)::kLanes, NV = decltype(shape)::kVecs, LINES = L < 256 ? 256 / L : 1;
-        hipLaunchKernelGGL((policy_rows_kernel<FP32, L, NV, decltype(shape)::kNarrow>), dim3((unsigned)up(a.rows, LINES)), dim3(L * LINES), 0, (hipStream_t)stream, a);
+int64_t parts_bytes(int64_t rows, int64_t vocab, int dtype) {      // (of rows anywhere, which take up the most)
+    return up(rows * (int64_t)cut_rows(rows, vocab, dtype, false).parts * (int64_t)sizeof(Sum) + rows * 4, 16) * 16;
+}
+int launch_parts(const PartsArgs& p, int dtype, int vecs, void* stream) {
+    with_vecs(dtype, vecs, [&](auto f, auto nv) {
+        hipLaunchKernelGGL((parts_kernel<decltype(f)::value, decltype(nv)::value>), dim3(p.r.rows * p.parts), dim3(kPartThreads), 0, (hipStream_t)stream, p);
     });
     return fo::hip_status(hipGetLastError());
 }
 
+template <bool FP32>
+int launch_held(const RowsArgs& a, bool aligned, void* stream) {
+    const auto launch = [&](auto shape) {
+        constexpr int L = decltype(shape)::kLanes, NV = decltype(shape)::kVecs, LINES = L < 256 ? 256 / L : 1;
+        hipLaunchKernelGGL((policy_rows_kernel<FP32, L, NV, decltype(shape)::kNarrow>), dim3((unsigned)up(a.rows, LINES)), dim3(L * LINES), 0, (hipStream_t)stream, a);
+    };
+    constexpr int kType = FP32 ? FLASHOPTIM_FP32 : FLASHOPTIM_BF16;
+    if (narrow(a.x.vocab, kType)) launch(Shape<64, 1, true>{});
+    else with_held(words(a.x.vocab, kType, aligned), launch);
+    return fo::hip_status(hipGetLastError());
+}
+
 int check_launch(const flashoptim_matrix* logits) {
-    const int64_t blocks = logits->rows * (int64_t)cut_rows(logits->rows, logits->cols, logits->dtype).parts;
+    const int64_t blocks = logits->rows * (int64_t)cut_rows(logits->rows, logits->cols, logits->dtype, false).parts;
     return blocks > fo::kMaxWorkItems / kPartThreads || logits->rows > fo::kMaxWorkItems / 1024 ? FLASHOPTIM_ERR_NUMEL_RANGE : FLASHOPTIM_OK;
 }
 int check_workspace(int64_t need, const void* workspace, int64_t bytes) {
@@ -702,7 +760,7 @@ extern "C" {
 int64_t flashoptim_token_logprob_workspace(int64_t rows, int64_t vocab, int dtype) {
     if (!known(dtype)) return FLASHOPTIM_ERR_INVALID_ARG;
     FO_TRY(check_sizes(rows, vocab));
-    return rows == 0 || streams_rows(rows, vocab) ? 0 : parts_bytes(rows, cut_rows(rows, vocab, dtype));
+    return rows == 0 || streams_rows(rows, vocab) ? 0 : parts_bytes(rows, vocab, dtype);
 }
 
 int flashoptim_token_logprob(const flashoptim_matrix* logits, const int64_t* tokens, float temperature, float* logprob, float* lse,
@@ -719,13 +777,15 @@ int flashoptim_token_logprob(const flashoptim_matrix* logits, const int64_t* tok
     a.lse = lse;
     const bool fp32 = logits->dtype == FLASHOPTIM_FP32;
     if (streams_rows(rows, logits->cols)) {
-        with_types(fp32, logits->cols < 8, [&](auto f, auto narrow) {
-            hipLaunchKernelGGL((logprob_rows_kernel<decltype(f)::value, 4, decltype(narrow)::value>), dim3(a.rows), dim3(256), 0, (hipStream_t)stream, a);
+        with_types(fp32, narrow(logits->cols, logits->dtype), [&](auto f, auto n) {
+            hipLaunchKernelGGL((logprob_rows_kernel<decltype(f)::value, kStreamWaves, decltype(n)::value>), dim3(a.rows), dim3(kStreamWaves * 64), 0,
+                               (hipStream_t)stream, a);
         });
         return fo::hip_status(hipGetLastError());
     }
-    const PartsArgs p = to_parts(a, cut_rows(rows, logits->cols, logits->dtype), workspace);
-    FO_TRY(launch_parts(p, logits->dtype, stream));
+    const Parts c = cut_rows(rows, logits->cols, logits->dtype, rows_aligned(logits));
+    const PartsArgs p = to_parts(a, c, workspace);
+    FO_TRY(launch_parts(p, logits->dtype, c.vecs, stream));
     hipLaunchKernelGGL(logprob_join_kernel, dim3((unsigned)up(rows, kJoinRows)), dim3(kJoinRows * 64), 0, (hipStream_t)stream, p);
     return fo::hip_status(hipGetLastError());
 }
@@ -739,13 +799,18 @@ int flashoptim_token_logprob_backward(const flashoptim_matrix* logits, const int
     if (!lse || !dlogprob) return FLASHOPTIM_ERR_INVALID_ARG;
     if (!fo::aligned_to(lse, 4) || !fo::aligned_to(dlogprob, 4)) return FLASHOPTIM_ERR_MISALIGNED;
     FO_TRY(check_launch(logits));
-    const Parts c = cut_rows(logits->rows, logits->cols, logits->dtype);
+    const Parts c = cut_rows(logits->rows, logits->cols, logits->dtype, rows_aligned(logits));
     const GradArgs g = {to_dev(logits), (char*)dlogits->data, dlogits->rows > 1 ? dlogits->stride : 0, tokens, lse, dlogprob, 1.0f / temperature,
-                        (float)(kLog2e / (double)temperature), c.parts, c.part};
+                        (float)(kLog2e / (double)temperature), c.parts};
     const dim3 grid((unsigned)(logits->rows * (int64_t)c.parts)), block(kPartThreads);
-    with_types(logits->dtype == FLASHOPTIM_FP32, logits->cols < 8, [&](auto f, auto narrow) {
-        hipLaunchKernelGGL((gradient_kernel<decltype(f)::value, decltype(narrow)::value>), grid, block, 0, (hipStream_t)stream, g);
-    });
+    if (narrow(logits->cols, logits->dtype)) {
+        if (logits->dtype == FLASHOPTIM_FP32) hipLaunchKernelGGL((gradient_kernel<true, 1, true>), grid, block, 0, (hipStream_t)stream, g);
+        else hipLaunchKernelGGL((gradient_kernel<false, 1, true>), grid, block, 0, (hipStream_t)stream, g);
+    } else {
+        with_vecs(logits->dtype, c.vecs, [&](auto f, auto nv) {
+            hipLaunchKernelGGL((gradient_kernel<decltype(f)::value, decltype(nv)::value, false>), grid, block, 0, (hipStream_t)stream, g);
+        });
+    }
     return fo::hip_status(hipGetLastError());
 }
 
@@ -753,7 +818,7 @@ int64_t flashoptim_policy_loss_workspace(int64_t rows, int64_t vocab, int dtype)
     if (!known(dtype)) return FLASHOPTIM_ERR_INVALID_ARG;
     FO_TRY(check_sizes(rows, vocab));
     const int64_t terms = up(rows * 24, 16) * 16;
-    return terms + (rows == 0 || holds_rows(rows, vocab, dtype) ? 0 : parts_bytes(rows, cut_rows(rows, vocab, dtype)));
+    return terms + (rows == 0 || holds_rows(rows, vocab, dtype, false) ? 0 : parts_bytes(rows, vocab, dtype));
 }
 
 int flashoptim_policy_loss(const flashoptim_policy_spec* spec, const flashoptim_matrix* logits, const int64_t* tokens,
@@ -778,15 +843,16 @@ int flashoptim_policy_loss(const flashoptim_policy_spec* spec, const flashoptim_
         a.dx = (char*)dlogits->data;
         a.dx_stride = rows > 1 ? dlogits->stride : 0;
     }
-    const bool fp32 = logits->dtype == FLASHOPTIM_FP32;
-    if (rows > 0 && holds_rows(rows, logits->cols, logits->dtype)) {
-        FO_TRY(fp32 ? launch_held<true>(a, stream) : launch_held<false>(a, stream));
+    const bool aligned = rows_aligned(logits);
+    if (rows > 0 && holds_rows(rows, logits->cols, logits->dtype, aligned)) {
+        FO_TRY(logits->dtype == FLASHOPTIM_FP32 ? launch_held<true>(a, aligned, stream) : launch_held<false>(a, aligned, stream));
     } else if (rows > 0) {
-        const PartsArgs p = to_parts(a, cut_rows(rows, logits->cols, logits->dtype), (char*)workspace + up(rows * 24, 16) * 16);
-        FO_TRY(launch_parts(p, logits->dtype, stream));
-        const dim3 grid(p.r.rows * p.parts), block(kPartThreads);
-        if (fp32) hipLaunchKernelGGL(policy_parts_kernel<true>, grid, block, 0, (hipStream_t)stream, p);
-        else hipLaunchKernelGGL(policy_parts_kernel<false>, grid, block, 0, (hipStream_t)stream, p);
+        const Parts c = cut_rows(rows, logits->cols, logits->dtype, aligned);
+        const PartsArgs p = to_parts(a, c, (char*)workspace + up(rows * 24, 16) * 16);
+        FO_TRY(launch_parts(p, logits->dtype, c.vecs, stream));
+        with_vecs(logits->dtype, c.vecs, [&](auto f, auto nv) {
+            hipLaunchKernelGGL((policy_parts_kernel<decltype(f)::value, decltype(nv)::value>), dim3(p.r.rows * p.parts), dim3(kPartThreads), 0, (hipStream_t)stream, p);
+        });
         FO_TRY(fo::hip_status(hipGetLastError()));
     }
     hipLaunchKernelGGL(policy_stats_kernel, dim3(1), dim3(kPairThreads), 0, (hipStream_t)stream, a.policy.terms, a.rows, spec->kl_weight, stats);
@@ -807,7 +873,9 @@ int flashoptim_preference_loss(const flashoptim_preference_spec* spec, const flo
         if (!fo::aligned_to(p, 4)) return FLASHOPTIM_ERR_MISALIGNED;
     if (!fo::aligned_to(offsets, 8)) return FLASHOPTIM_ERR_MISALIGNED;
     const PairArgs a = {logprob, ref_logprob, weights, offsets, loss, margins, dlogprob, rows, pairs, *spec};
-    hipLaunchKernelGGL(preference_kernel, dim3(1), dim3(kPairThreads), 0, (hipStream_t)stream, a);
+    int groups = 1;
+    while (groups < 16 && groups < pairs) groups *= 2;
+    hipLaunchKernelGGL(preference_kernel, dim3(1), dim3(kPairThreads), 0, (hipStream_t)stream, a, groups);
     return fo::hip_status(hipGetLastError());
 }
 
