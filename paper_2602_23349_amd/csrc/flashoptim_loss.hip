@@ -46,6 +46,11 @@ __device__ __forceinline__ float value_at(const char* row, int32_t j) {
 }
 // A token that is there as its place, one that is not as none that any lane holds.
 __device__ __forceinline__ int32_t token_in(int64_t token, int32_t vocab) { return token < vocab ? (int32_t)token : 0x7fffffff; }
+template <bool FP32>
+__device__ __forceinline__ void put(char* row, int32_t j, float v) {
+    if constexpr (FP32) ((float*)row)[j] = v;
+    else ((__bf16*)row)[j] = (__bf16)v;
+}
 // The logit of a token; one that is not there has none.
 template <bool FP32>
 __device__ __forceinline__ float logit_of(const char* row, int64_t token, int32_t vocab) {
@@ -90,164 +95,151 @@ __device__ __forceinline__ Sum join(const Sum& a, const Sum& b, float c) {
 template <bool FP32>
 constexpr int kValues = FP32 ? 4 : 8;
 
-// What LANES lanes hold of a row in registers, at most LANES * NV words: lane l's i-th word are the values from at(i) on, which is a 16-byte border of
-// memory (words across such borders: log-probabilities of 8192 x 50257 BF16 logits 169 us, so 141).  Every lane loads words that exist, so that no
-// load is a case distinction: the row's first values where its own word begins ahead of the row, the last ones where it reaches behind it, and the last
-// ones again where there is none.  What is not the lane's own becomes -infinity, which adds nothing.  (NARROW: rows of less than a word, which lane 0
-// takes value by value.)  Logits and gradients go past the caches: each is touched once, and there are more of them than the caches hold (with and without:
-// the same log-probabilities 125 and 141 us, the gradient of 4096 x 128256 360 and 388).
-template <bool FP32, int LANES, int NV, bool NARROW = false>
+// What LANES lanes hold of a row in registers.  A row is its words between 16-byte borders of memory and, ahead of the first and behind the last of these, up to
+// kN - 1 values each, its edges.  (Words across such borders: log-probabilities of 8192 x 50257 BF16 logits 169 us, so 141.)  Lane l's i-th word is the row's
+// first + i LANES + l-th; where there is none the row's last one is loaded, so that no load is a case distinction, and left out of the sum.  The edges belong to the part with the row's first word, a value to a lane.  Logits and gradients go past the caches: each is touched once, and
+// there are more of them than the caches hold (with and without: the same log-probabilities 125 and 141 us, the gradient of 4096 x 128256 360 and 388).
+// SKIP: words that none of a wavefront's lanes has are passed over, of the loads the upper half together (8192 rows of 8192 in 256 lanes of 8 words 68 -> 53 us;
+// parts that are all full are not faster by it).
+template <bool FP32, int LANES, int NV, bool SKIP = false>
 struct Held {
     static constexpr int kN = kValues<FP32>, kSize = FP32 ? 4 : 2;
     i32x4 raw[NV];
-    int32_t begin, vocab;    // begin: 0 or less for a row's first part
-    int lane;
+    float edge;                          // -infinity: none
+    int32_t first, words, head, vocab;   // words: the row's; head: values ahead of the first
+    int lane, wave;                      // wave: the wavefront's first lane
 
-    // Between two passes over what is held.  The values are unpacked again in each: kept from one to the next, they would take twice the registers.
-    __device__ __forceinline__ void forget_values() {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(raw[i]));
-        asm volatile("" : "+v"(lane));       // (nor are the places that follow from it kept)
+    // The part of the row that begins with its `first_`-th word.
+    __device__ __forceinline__ void place(const char* row, int32_t first_, int32_t vocab_, int lane_) {
+        first = first_; vocab = vocab_; lane = lane_;
+        head = min((int32_t)(-(uintptr_t)row & 15) / kSize, vocab);
+        words = (vocab - head) / kN;
+        wave = LANES == 64 ? 0 : __builtin_amdgcn_readfirstlane(lane_);
+        asm volatile("" : "+v"(lane));       // (places are worked out where they are needed: kept through a loop, they take a register each)
     }
-    // The part of the row that begins `first` values (whole words) behind the last border at or ahead of the row's beginning.
-    __device__ __forceinline__ void place(const char* row, int32_t first, int32_t vocab_, int lane_) {
-        const int32_t ahead = NARROW ? 0 : (int32_t)((uintptr_t)row & 15) / kSize;
-        begin = first - ahead; vocab = vocab_; lane = lane_;
+    // Whether the row has no word at all.  (SKIP: the rows of a workgroup are always longer.)
+    __device__ __forceinline__ bool none() const { return (LANES == 64 || !SKIP) && words <= 0; }
+    __device__ __forceinline__ int32_t word(int i) const { return first + i * LANES + lane; }
+    // Whether the i-th words of the wavefront are there at all, and whether all are.
+    __device__ __forceinline__ bool some(int i) const { return !SKIP || first + i * LANES + wave < words; }
+    __device__ __forceinline__ bool all(int i) const { return first + i * LANES + wave + 64 <= words; }
+    // Where a word is, in bytes.  (32 bits beside the row's address, which is a wavefront's: vocab < 2^30.)
+    __device__ __forceinline__ uint32_t place_of(int32_t word) const { return (uint32_t)head * kSize + (uint32_t)word * 16u; }
+    // The lane's value of the edges, if it has one: the head's are the first kN lanes', the others' behind the words the next kN.
+    __device__ __forceinline__ bool edge_at(int32_t* j) const {
+        *j = lane < kN ? lane : head + words * kN + lane - kN;
+        return first == 0 && (lane < kN ? lane < head : lane < 2 * kN && *j < vocab);
     }
-    // (32 bits beside the row's address, which is a wavefront's: vocab < 2^30)
-    static __device__ __forceinline__ uint32_t bytes(int32_t j) { return (uint32_t)j * (uint32_t)kSize; }
-    __device__ __forceinline__ int32_t at(int i) const { return begin + kN * (i * LANES + lane); }
-    // The first value that is loaded.
-    __device__ __forceinline__ int32_t from(int i) const { return NARROW ? 0 : min(max(at(i), 0), vocab - kN); }
-    // Whether the i-th words of all lanes are their own and whole.  (The same for all lanes.)
-    __device__ __forceinline__ bool inside(int i) const { return !NARROW && (i > 0 || begin >= 0) && begin + kN * (i + 1) * LANES <= vocab; }
-    __device__ __forceinline__ bool any(int i) const { return at(i) < vocab; }
-    __device__ __forceinline__ bool whole(int i) const { return !NARROW && at(i) >= 0 && at(i) + kN <= vocab; }
+    template <bool PAST>
+    __device__ __forceinline__ void load_word(int i, const char* row, i32x4& to) const {
+        const i32x4* p = (const i32x4*)(row + place_of(min(word(i), words - 1)));
+        to = PAST ? __builtin_nontemporal_load(p) : *p;
+    }
     template <bool PAST = true>
     __device__ __forceinline__ void load(const char* row) {
+        load_edge(row);
+        if (none()) return;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            if constexpr (NARROW) {
-                raw[i] = i32x4{};
-#pragma unroll
-                for (int k = 0; k < kN; ++k) {
-                    if (i > 0 || k >= vocab) continue;
-                    if constexpr (FP32) raw[i][k] = ((const int*)row)[k];
-                    else raw[i][k / 2] |= (int)((uint32_t)((const uint16_t*)row)[k] << (16 * (k % 2)));
-                }
-            } else {
-                const char* p = row + bytes(from(i));
-                raw[i] = PAST ? __builtin_nontemporal_load((const anywhere*)p) : load_as<i32x4>(p);
-            }
+            if (i >= NV / 2 && !some(NV / 2)) continue;
+            load_word<PAST>(i, row, raw[i]);
         }
     }
-    // Of the i-th word as loaded, the values that are the lane's own: [first, last).
-    __device__ __forceinline__ void own(int i, int* first, int* last) const {
-        if (NARROW) { *first = 0; *last = at(i) == 0 ? vocab : 0; }
-        else { *first = min(max(at(i) - from(i), 0), kN); *last = min(at(i) + kN - from(i), kN); }
+    __device__ __forceinline__ void load_edge(const char* row) {
+        int32_t j;
+        edge = minus_inf();
+        if (edge_at(&j)) edge = value_at<FP32>(row, j);
     }
-    // Puts -infinity where a value is not the lane's own.  (Before the first use.)
-    __device__ __forceinline__ void settle(int i) {
-        if (inside(i) || whole(i)) return;
-        int first, last;
-        own(i, &first, &last);
-#pragma unroll
-        for (int k = 0; k < kN; ++k) {
-            const bool keep = k >= first && k < last;
-            if constexpr (FP32) raw[i][k] = keep ? raw[i][k] : (int)0xff800000;
-            else {
-                const uint32_t shift = 16 * (k % 2);
-                const uint32_t w = (uint32_t)raw[i][k / 2];
-                raw[i][k / 2] = keep ? (int)w : (int)((w & ~(0xffffu << shift)) | 0xff80u << shift);
-            }
+    // How a pass over what is held unpacks it.  Each has numbers of its own, unknown to the compiler, so that it unpacks again: values kept from one pass to
+    // the next would take twice the registers.
+    struct Pass {
+        uint32_t low, high;
+        __device__ __forceinline__ Pass() : low(16), high(0xffff0000u) {
+            if constexpr (!FP32) asm volatile("" : "+s"(low), "+s"(high));
         }
-    }
-    __device__ __forceinline__ void values(int i, float (&v)[kN]) const {
+    };
+    __device__ __forceinline__ void values(const Pass& pass, int i, float (&v)[kN]) const {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             if constexpr (FP32) v[k] = __int_as_float(raw[i][k]);
             else {
-                v[2 * k] = __uint_as_float((uint32_t)raw[i][k] << 16);
-                v[2 * k + 1] = __uint_as_float((uint32_t)raw[i][k] & 0xffff0000u);
+                v[2 * k] = __uint_as_float((uint32_t)raw[i][k] << pass.low);
+                v[2 * k + 1] = __uint_as_float((uint32_t)raw[i][k] & pass.high);
             }
         }
     }
     // The sum of the wavefront's part, in every lane.  A lane adds up in FP32, apart from words of some weight beside the wavefront's largest value, which go
     // into an FP64 sum: beside a token that is all but certain the others would be lost in its rounding, and with them its log-probability.
     __device__ __forceinline__ Sum wave_part(float c) {
-        float most = minus_inf();
+        float most = edge;
+        const Pass first_pass;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            settle(i);
+            if (none() || !some(i)) continue;      // (a word that is there twice is as good as one that is not)
             float v[kN];
-            values(i, v);
+            values(first_pass, i, v);
 #pragma unroll
             for (int k = 0; k < kN; k += 2) most = fmaxf(fmaxf(most, v[k]), v[k + 1]);
         }
-        forget_values();
         most = wave_max(most);
         const float base = base_of(most);
         float sum = 0.0f;
-        double near = 0.0;
+        const Pass second_pass;
+        double near = (double)exp2_of((edge - base) * c);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            float v[kN], word = 0.0f;
-            values(i, v);
+            if (none() || !some(i)) continue;
+            float v[kN], eight = 0.0f;
+            values(second_pass, i, v);
 #pragma unroll
             for (int k = 0; k < kN; ++k) v[k] = exp2_of((v[k] - base) * c);
+            if (!all(i)) {
+                const bool there = word(i) < words;
 #pragma unroll
-            for (int k = 0; k < kN; k += 4) word += (v[k] + v[k + 1]) + (v[k + 2] + v[k + 3]);
-            if (__builtin_amdgcn_ballot_w64(word >= 0.5f)) {
+                for (int k = 0; k < kN; ++k) v[k] = there ? v[k] : 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < kN; k += 4) eight += (v[k] + v[k + 1]) + (v[k + 2] + v[k + 3]);
+            if (__builtin_amdgcn_ballot_w64(eight >= 0.5f)) {
 #pragma unroll
                 for (int k = 0; k < kN; ++k) near += (double)v[k];
             } else {
-                sum += word;
+                sum += eight;
             }
         }
         return {wave_sum(near + (double)sum), most};
     }
     // Stores -d p, or d (1 - p) for the token, of all that is held: p = 2^((x - base) c - shift).
     __device__ __forceinline__ void store_gradient(char* row, int32_t token, float d, float base, float c, float shift) {
-        forget_values();
+        const Pass pass;
+        asm volatile("" : "+v"(lane));
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const bool in = inside(i);
-            if (!in && !any(i)) continue;
-            float v[kN];
-            values(i, v);
+            if (all(i) || word(i) < words) {
+                float v[kN];
+                values(pass, i, v);
 #pragma unroll
-            for (int k = 0; k < kN; ++k) v[k] = -d * exp2_of(fmaf(v[k] - base, c, -shift));
-            const int32_t j = in ? at(i) : from(i);
-            if ((uint32_t)(token - j) < (uint32_t)kN) {
+                for (int k = 0; k < kN; ++k) v[k] = -d * exp2_of(fmaf(v[k] - base, c, -shift));
+                const int32_t j = head + word(i) * kN;
+                if ((uint32_t)(token - j) < (uint32_t)kN) {
 #pragma unroll
-                for (int k = 0; k < kN; ++k) v[k] = token == j + k ? v[k] + d : v[k];
+                    for (int k = 0; k < kN; ++k) v[k] = token == j + k ? v[k] + d : v[k];
+                }
+                i32x4 w;
+                if constexpr (FP32) w = __builtin_bit_cast(i32x4, (f32x4){v[0], v[1], v[2], v[3]});
+                else w = __builtin_bit_cast(i32x4, __builtin_convertvector((f32x8){v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]}, bf16x8));
+                __builtin_nontemporal_store(w, (anywhere*)(row + place_of(word(i))));
             }
-            store(row, i, in, v);
         }
+        int32_t j;
+        if (edge_at(&j)) put<FP32>(row, j, (token == j ? d : 0.0f) - d * exp2_of(fmaf(edge - base, c, -shift)));
     }
     __device__ __forceinline__ void store_zeros(char* row) const {
-        const float v[kN] = {};
-#pragma unroll
+#pragma unroll 1
         for (int i = 0; i < NV; ++i)
-            if (inside(i) || any(i)) store(row, i, inside(i), v);
-    }
-    __device__ __forceinline__ void store(char* row, int i, bool in, const float (&v)[kN]) const {
-        const int32_t j = in ? at(i) : from(i);
-        if (in || whole(i)) {
-            i32x4 w;
-            if constexpr (FP32) w = __builtin_bit_cast(i32x4, (f32x4){v[0], v[1], v[2], v[3]});
-            else w = __builtin_bit_cast(i32x4, __builtin_convertvector((f32x8){v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]}, bf16x8));
-            __builtin_nontemporal_store(w, (anywhere*)(row + bytes(j)));
-            return;
-        }
-        int first, last;
-        own(i, &first, &last);
-#pragma unroll
-        for (int k = 0; k < kN; ++k) {
-            if (k < first || k >= last) continue;
-            if constexpr (FP32) ((float*)row)[j + k] = v[k];
-            else ((__bf16*)row)[j + k] = (__bf16)v[k];
-        }
+            if (word(i) < words) __builtin_nontemporal_store(i32x4{}, (anywhere*)(row + place_of(word(i))));
+        int32_t j;
+        if (edge_at(&j)) put<FP32>(row, j, 0.0f);
     }
 };
 
@@ -268,13 +260,52 @@ __device__ __forceinline__ Sum join_waves(const Sum& s, float c) {
     return all;
 }
 
+// What is computed once for a row, in FP64.  By series in loops over one table: unrolled, as the library's functions are, their coefficients take fifty
+// registers that a row is held in.
+constexpr int kTerms = 26;
+struct Inverses {
+    double of[kTerms];
+    constexpr Inverses() : of() {
+        for (int n = 1; n < kTerms; ++n) of[n] = 1.0 / n;
+    }
+};
+static __constant__ const Inverses inverses;
+constexpr double kLn2 = 0.69314718055994530942, kLn2Low = 2.3190468138462996e-17;      // (the sum is ln 2 to more than FP64)
+
+// exp(x) - 1 and exp(x): with x = k ln 2 + r, |r| <= ln 2 / 2, e^r - 1 = r (1 + r/2 (1 + r/3 (...))), whose 15th term is below 2^-60 of it.
+__device__ __forceinline__ double expm1_row(double x, bool less_one = true) {
+    if (x > 720.0) return (double)__builtin_inff();
+    if (x < -760.0) return less_one ? -1.0 : 0.0;
+    const double k = rint(x * kLog2e), r = fma(-k, kLn2, x) - k * kLn2Low;
+    double s = 1.0;
+#pragma unroll 1
+    for (int n = 15; n > 1; --n) s = fma(r * inverses.of[n], s, 1.0);
+    s *= r;
+    if (k == 0.0) return less_one ? s : 1.0 + s;
+    return ldexp(1.0 + s, (int)k) - (less_one ? 1.0 : 0.0);
+}
+__device__ __forceinline__ double exp_row(double x) { return expm1_row(x, false); }
+// log(x) of x >= 0: with x = 2^k m, 1/sqrt 2 <= m < sqrt 2 and z = (m - 1) / (m + 1), k ln 2 + 2 (z + z^3/3 + z^5/5 + ...), whose 13th term is below 2^-60 of it.
+__device__ __forceinline__ double log_row(double x) {
+    if (!(x > 0.0) || !(x < (double)__builtin_inff())) return x == 0.0 ? -(double)__builtin_inff() : x;
+    int k = ilogb(x);
+    double m = ldexp(x, -k);
+    if (m > 1.4142135623730951) { m *= 0.5; ++k; }
+    const double z = (m - 1.0) / (m + 1.0), zz = z * z;
+    double s = 0.0;
+#pragma unroll 1
+    for (int n = 25; n > 1; n -= 2) s = fma(s, zz, inverses.of[n]);
+    s = fma(s * zz, z, z);
+    return fma((double)k, kLn2, 2.0 * s + k * kLn2Low);
+}
+
 // log sum exp(x / T) and the token's log-probability; log_sum is what lse is beyond the largest value.
 struct RowLog {
     double lse, logprob, log_sum;
 };
 __device__ __forceinline__ RowLog row_log(const Sum& s, float x, double inv_t) {
     // (a sum beyond FP32 is that of a row with +infinity)
-    const double log_sum = s.most < __builtin_inff() ? log(s.sum) : (double)__builtin_nanf("");
+    const double log_sum = s.most < __builtin_inff() ? log_row(s.sum) : (double)__builtin_nanf("");
     return {(double)s.most * inv_t + log_sum, ((double)x - (double)s.most) * inv_t - log_sum, log_sum};
 }
 
@@ -290,13 +321,13 @@ struct PolicyArgs {
 };
 __device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& a, uint32_t row, double logprob, float w) {
     const double adv = a.in.advantages[row];
-    const double ratio = a.in.old_logprob ? exp(logprob - (double)a.in.old_logprob[row]) : logprob - logprob + 1.0;
+    const double ratio = a.in.old_logprob ? exp_row(logprob - (double)a.in.old_logprob[row]) : logprob - logprob + 1.0;
     const double low = 1.0 - (double)a.spec.clip_low, high = 1.0 + (double)a.spec.clip_high;
     const bool blocked = (adv > 0.0 && ratio > high) || (adv < 0.0 && ratio < low);
     const double surrogate = blocked ? -adv * (adv > 0.0 ? high : low) : -adv * ratio;
     double slope = blocked ? 0.0 : -adv * ratio, kl = 0.0;
     if (a.in.ref_logprob) {
-        const double d = (double)a.in.ref_logprob[row] - logprob, e = expm1(d);
+        const double d = (double)a.in.ref_logprob[row] - logprob, e = expm1_row(d);
         kl = e - d;
         slope -= (double)a.spec.kl_weight * e;
     }
@@ -323,7 +354,7 @@ struct RowsArgs {
 };
 
 // One row to LANES lanes, which hold it: the policy loss and its gradient in one pass over the logits.
-template <bool FP32, int LANES, int NV, bool NARROW>
+template <bool FP32, int LANES, int NV>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void policy_rows_kernel(RowsArgs a) {
     constexpr int LINES = LANES < 256 ? 256 / LANES : 1;
     static_assert(LANES == 64 || LINES == 1, "a row is a wavefront's or a workgroup's");
@@ -334,7 +365,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void policy_rows_kernel(
     const float w = a.policy.in.weights ? a.policy.in.weights[row] : 1.0f;
     char* dx = a.dx ? a.dx + (int64_t)row * a.dx_stride * (FP32 ? 4 : 2) : nullptr;
     const char* x = row_of<FP32>(a.x, row);
-    Held<FP32, LANES, NV, NARROW> h;
+    Held<FP32, LANES, NV, true> h;
     h.place(x, 0, a.x.vocab, lane);
     if (token < 0 || w == 0.0f) {
         if (lane == 0) {
@@ -353,16 +384,16 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void policy_rows_kernel(
         if (a.logprob) a.logprob[row] = (float)l.logprob;
         put_terms(a.policy, a.rows, row, p);
     }
-    if (!dx) return;
     const float d = p.slope * a.scale;
+    if (!dx) return;
     if (d == 0.0f) h.store_zeros(dx);
     else h.store_gradient(dx, token_in(token, a.x.vocab), d, base_of(s.most), a.c, (float)(l.log_sum * kLog2e));
 }
 
 // Log-probabilities only, one workgroup of WAVES wavefronts to a row, through which the wavefronts go in turn.
-template <bool FP32, int WAVES, bool NARROW>
+template <bool FP32, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void logprob_rows_kernel(RowsArgs a) {
-    constexpr int NV = NARROW ? 1 : 8, kPart = 64 * NV * kValues<FP32>;
+    constexpr int NV = 8, kPart = 64 * NV;
     const uint32_t row = blockIdx.x;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int64_t token = a.tokens[row];
@@ -376,9 +407,9 @@ __global__ __launch_bounds__(WAVES * 64) void logprob_rows_kernel(RowsArgs a) {
     const char* x = row_of<FP32>(a.x, row);
     const float logit = logit_of<FP32>(x, token, a.x.vocab);
     Sum s = {0.0, minus_inf()};
-    for (int32_t first = wave * kPart; first < a.x.vocab + kValues<FP32>; first += WAVES * kPart) {
-        Held<FP32, 64, NV, NARROW> h;
-        h.place(x, first, a.x.vocab, lane);
+    Held<FP32, 64, NV> h;
+    h.place(x, wave * kPart, a.x.vocab, lane);
+    for (; h.first == 0 || h.first < h.words; h.first += WAVES * kPart) {
         h.load(x);
         s = join(s, h.wave_part(a.c), a.c);
     }
@@ -410,7 +441,7 @@ __global__ __launch_bounds__(kPartThreads) void parts_kernel(PartsArgs a) {
     if (!counts(a, row, token, &w)) return;
     const char* x = row_of<FP32>(a.r.x, row);
     Held<FP32, kPartThreads, NV> h;
-    h.place(x, (int32_t)part * (kPartThreads * NV * kValues<FP32>), a.r.x.vocab, (int)threadIdx.x);
+    h.place(x, (int32_t)part * (kPartThreads * NV), a.r.x.vocab, (int)threadIdx.x);
     h.template load<false>(x);       // (the gradient reads it again)
     if (part == 0 && threadIdx.x == 0) a.logits[row] = logit_of<FP32>(x, token, a.r.x.vocab);
     const Sum s = join_waves<kPartThreads / 64>(h.wave_part(a.r.c), a.r.c);
@@ -447,7 +478,7 @@ __global__ __launch_bounds__(kPartThreads) void policy_parts_kernel(PartsArgs a)
     char* dx = a.r.dx ? a.r.dx + (int64_t)row * a.r.dx_stride * (FP32 ? 4 : 2) : nullptr;
     const char* x = row_of<FP32>(a.r.x, row);
     Held<FP32, kPartThreads, NV> h;
-    h.place(x, (int32_t)part * (kPartThreads * NV * kValues<FP32>), a.r.x.vocab, (int)threadIdx.x);
+    h.place(x, (int32_t)part * (kPartThreads * NV), a.r.x.vocab, (int)threadIdx.x);
     if (there && dx) h.load(x);
     Sum s = {1.0, 0.0f};
     RowLog l = {0.0, 0.0, 0.0};
@@ -477,15 +508,15 @@ struct GradArgs {
     float scale, c;          // of the slopes
     uint32_t parts;
 };
-template <bool FP32, int NV, bool NARROW>
+template <bool FP32, int NV>
 __global__ __launch_bounds__(kPartThreads) void gradient_kernel(GradArgs a) {
     const uint32_t row = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
     char* dx = a.dx + (int64_t)row * a.stride * (FP32 ? 4 : 2);
     const char* x = row_of<FP32>(a.x, row);
     const int64_t token = a.tokens[row];
     float d = token < 0 ? 0.0f : a.slope[row] * a.scale;
-    Held<FP32, kPartThreads, NV, NARROW> h;
-    h.place(x, (int32_t)part * (kPartThreads * NV * kValues<FP32>), a.x.vocab, (int)threadIdx.x);
+    Held<FP32, kPartThreads, NV> h;
+    h.place(x, (int32_t)part * (kPartThreads * NV), a.x.vocab, (int)threadIdx.x);
     if (d == 0.0f) {
         h.store_zeros(dx);
         return;
@@ -639,14 +670,8 @@ int check_gradient(const flashoptim_matrix* d, const flashoptim_matrix* logits) 
 }
 Logits to_dev(const flashoptim_matrix* m) { return {(const char*)m->data, m->rows > 1 ? m->stride : 0, (int32_t)m->cols}; }
 
-// The words of 16 bytes that a row takes up: one more where it does not begin on such a border.
-int64_t words(int64_t vocab, int dtype, bool aligned) { return up(vocab * fo::elem_bytes(dtype), 16) + (aligned ? 0 : 1); }
-// Rows of less than a word.
-bool narrow(int64_t vocab, int dtype) { return vocab * fo::elem_bytes(dtype) < 16; }
-bool rows_aligned(const flashoptim_matrix* m) {
-    const int64_t size = fo::elem_bytes(m->dtype);
-    return fo::aligned_to(m->data, 16) && (m->rows <= 1 || m->stride * size % 16 == 0);
-}
+// The most words that a row has between 16-byte borders.
+int64_t words(int64_t vocab, int dtype) { return vocab * fo::elem_bytes(dtype) / 16; }
 
 // How a row is cut: into parts of kPartThreads lanes that hold `vecs` words each, as many as registers allow, or fewer where there are few rows, so that all
 // compute units have one.
@@ -654,9 +679,10 @@ struct Parts {
     int vecs;
     uint32_t parts;
 };
-Parts cut_rows(int64_t rows, int64_t vocab, int dtype, bool aligned) {
-    int vecs = 8;
-    const auto parts = [&] { return up(words(vocab, dtype, aligned), kPartThreads * vecs); };
+Parts cut_rows(int64_t rows, int64_t vocab, int dtype) {
+    int vecs = 2;
+    const int64_t n = words(vocab, dtype);
+    const auto parts = [&] { return n > 0 ? up(n, kPartThreads * vecs) : 1; };
     while (vecs > 1 && rows * parts() < 512) vecs /= 2;
     return {vecs, (uint32_t)parts()};
 }
@@ -666,26 +692,16 @@ using Int = std::integral_constant<int, N>;
 template <typename F>
 void with_vecs(int dtype, int vecs, F launch) {
     const auto with = [&](auto fp32) {
-        if (vecs == 8) launch(fp32, Int<8>{}); else if (vecs == 4) launch(fp32, Int<4>{}); else if (vecs == 2) launch(fp32, Int<2>{}); else launch(fp32, Int<1>{});
+        if (vecs == 2) launch(fp32, Int<2>{}); else launch(fp32, Int<1>{});
     };
     if (dtype == FLASHOPTIM_FP32) with(std::true_type{}); else with(std::false_type{});
 }
 bool known(int dtype) { return dtype == FLASHOPTIM_BF16 || dtype == FLASHOPTIM_FP32; }
 
-// Calls launch(fp32, narrow) with the two as types.
-template <typename F>
-void with_types(bool fp32, bool narrow, F launch) {
-    using Yes = std::true_type;
-    using No = std::false_type;
-    if (fp32) { if (narrow) launch(Yes{}, Yes{}); else launch(Yes{}, No{}); }
-    else { if (narrow) launch(No{}, Yes{}); else launch(No{}, No{}); }
-}
-
 // Calls launch(shape) with the shape of the workgroups that hold rows of n words.
-template <int LANES, int NV, bool NARROW = false>
+template <int LANES, int NV>
 struct Shape {
     static constexpr int kLanes = LANES, kVecs = NV;
-    static constexpr bool kNarrow = NARROW;
 };
 template <typename F>
 void with_held(int64_t n, F launch) {
@@ -697,8 +713,8 @@ void with_held(int64_t n, F launch) {
     else launch(Shape<1024, 16>{});
 }
 // Whether a call holds whole rows: those of a wavefront always, longer ones, up to the largest shape's, where there are as many as fill half the chip.
-bool holds_rows(int64_t rows, int64_t vocab, int dtype, bool aligned) {
-    const int64_t n = words(vocab, dtype, aligned);
+bool holds_rows(int64_t rows, int64_t vocab, int dtype) {
+    const int64_t n = words(vocab, dtype);
     return n <= 64 * 8 || (n <= 1024 * 16 && rows >= 128);
 }
 constexpr int kStreamWaves = 8;
@@ -710,8 +726,8 @@ PartsArgs to_parts(const RowsArgs& a, const Parts& c, void* workspace) {
     p.logits = (float*)(p.sums + (int64_t)a.rows * c.parts);
     return p;
 }
-int64_t parts_bytes(int64_t rows, int64_t vocab, int dtype) {      // (of rows anywhere, which take up the most)
-    return up(rows * (int64_t)cut_rows(rows, vocab, dtype, false).parts * (int64_t)sizeof(Sum) + rows * 4, 16) * 16;
+int64_t parts_bytes(int64_t rows, int64_t vocab, int dtype) {
+    return up(rows * (int64_t)cut_rows(rows, vocab, dtype).parts * (int64_t)sizeof(Sum) + rows * 4, 16) * 16;
 }
 int launch_parts(const PartsArgs& p, int dtype, int vecs, void* stream) {
     with_vecs(dtype, vecs, [&](auto f, auto nv) {
@@ -721,19 +737,16 @@ int launch_parts(const PartsArgs& p, int dtype, int vecs, void* stream) {
 }
 
 template <bool FP32>
-int launch_held(const RowsArgs& a, bool aligned, void* stream) {
-    const auto launch = [&](auto shape) {
+int launch_held(const RowsArgs& a, void* stream) {
+    with_held(words(a.x.vocab, FP32 ? FLASHOPTIM_FP32 : FLASHOPTIM_BF16), [&](auto shape) {
         constexpr int L = decltype(shape)::kLanes, NV = decltype(shape)::kVecs, LINES = L < 256 ? 256 / L : 1;
-        hipLaunchKernelGGL((policy_rows_kernel<FP32, L, NV, decltype(shape)::kNarrow>), dim3((unsigned)up(a.rows, LINES)), dim3(L * LINES), 0, (hipStream_t)stream, a);
-    };
-    constexpr int kType = FP32 ? FLASHOPTIM_FP32 : FLASHOPTIM_BF16;
-    if (narrow(a.x.vocab, kType)) launch(Shape<64, 1, true>{});
-    else with_held(words(a.x.vocab, kType, aligned), launch);
+        hipLaunchKernelGGL((policy_rows_kernel<FP32, L, NV>), dim3((unsigned)up(a.rows, LINES)), dim3(L * LINES), 0, (hipStream_t)stream, a);
+    });
     return fo::hip_status(hipGetLastError());
 }
 
 int check_launch(const flashoptim_matrix* logits) {
-    const int64_t blocks = logits->rows * (int64_t)cut_rows(logits->rows, logits->cols, logits->dtype, false).parts;
+    const int64_t blocks = logits->rows * (int64_t)cut_rows(logits->rows, logits->cols, logits->dtype).parts;
     return blocks > fo::kMaxWorkItems / kPartThreads || logits->rows > fo::kMaxWorkItems / 1024 ? FLASHOPTIM_ERR_NUMEL_RANGE : FLASHOPTIM_OK;
 }
 int check_workspace(int64_t need, const void* workspace, int64_t bytes) {
@@ -775,15 +788,13 @@ int flashoptim_token_logprob(const flashoptim_matrix* logits, const int64_t* tok
     RowsArgs a = rows_args(logits, tokens, temperature);
     a.logprob = logprob;
     a.lse = lse;
-    const bool fp32 = logits->dtype == FLASHOPTIM_FP32;
     if (streams_rows(rows, logits->cols)) {
-        with_types(fp32, narrow(logits->cols, logits->dtype), [&](auto f, auto n) {
-            hipLaunchKernelGGL((logprob_rows_kernel<decltype(f)::value, kStreamWaves, decltype(n)::value>), dim3(a.rows), dim3(kStreamWaves * 64), 0,
-                               (hipStream_t)stream, a);
-        });
+        const dim3 grid(a.rows), block(kStreamWaves * 64);
+        if (logits->dtype == FLASHOPTIM_FP32) hipLaunchKernelGGL((logprob_rows_kernel<true, kStreamWaves>), grid, block, 0, (hipStream_t)stream, a);
+        else hipLaunchKernelGGL((logprob_rows_kernel<false, kStreamWaves>), grid, block, 0, (hipStream_t)stream, a);
         return fo::hip_status(hipGetLastError());
     }
-    const Parts c = cut_rows(rows, logits->cols, logits->dtype, rows_aligned(logits));
+    const Parts c = cut_rows(rows, logits->cols, logits->dtype);
     const PartsArgs p = to_parts(a, c, workspace);
     FO_TRY(launch_parts(p, logits->dtype, c.vecs, stream));
     hipLaunchKernelGGL(logprob_join_kernel, dim3((unsigned)up(rows, kJoinRows)), dim3(kJoinRows * 64), 0, (hipStream_t)stream, p);
@@ -799,18 +810,13 @@ int flashoptim_token_logprob_backward(const flashoptim_matrix* logits, const int
     if (!lse || !dlogprob) return FLASHOPTIM_ERR_INVALID_ARG;
     if (!fo::aligned_to(lse, 4) || !fo::aligned_to(dlogprob, 4)) return FLASHOPTIM_ERR_MISALIGNED;
     FO_TRY(check_launch(logits));
-    const Parts c = cut_rows(logits->rows, logits->cols, logits->dtype, rows_aligned(logits));
+    const Parts c = cut_rows(logits->rows, logits->cols, logits->dtype);
     const GradArgs g = {to_dev(logits), (char*)dlogits->data, dlogits->rows > 1 ? dlogits->stride : 0, tokens, lse, dlogprob, 1.0f / temperature,
                         (float)(kLog2e / (double)temperature), c.parts};
     const dim3 grid((unsigned)(logits->rows * (int64_t)c.parts)), block(kPartThreads);
-    if (narrow(logits->cols, logits->dtype)) {
-        if (logits->dtype == FLASHOPTIM_FP32) hipLaunchKernelGGL((gradient_kernel<true, 1, true>), grid, block, 0, (hipStream_t)stream, g);
-        else hipLaunchKernelGGL((gradient_kernel<false, 1, true>), grid, block, 0, (hipStream_t)stream, g);
-    } else {
-        with_vecs(logits->dtype, c.vecs, [&](auto f, auto nv) {
-            hipLaunchKernelGGL((gradient_kernel<decltype(f)::value, decltype(nv)::value, false>), grid, block, 0, (hipStream_t)stream, g);
-        });
-    }
+    with_vecs(logits->dtype, c.vecs, [&](auto f, auto nv) {
+        hipLaunchKernelGGL((gradient_kernel<decltype(f)::value, decltype(nv)::value>), grid, block, 0, (hipStream_t)stream, g);
+    });
     return fo::hip_status(hipGetLastError());
 }
 
@@ -818,7 +824,7 @@ int64_t flashoptim_policy_loss_workspace(int64_t rows, int64_t vocab, int dtype)
     if (!known(dtype)) return FLASHOPTIM_ERR_INVALID_ARG;
     FO_TRY(check_sizes(rows, vocab));
     const int64_t terms = up(rows * 24, 16) * 16;
-    return terms + (rows == 0 || holds_rows(rows, vocab, dtype, false) ? 0 : parts_bytes(rows, vocab, dtype));
+    return terms + (rows == 0 || holds_rows(rows, vocab, dtype) ? 0 : parts_bytes(rows, vocab, dtype));
 }
 
 int flashoptim_policy_loss(const flashoptim_policy_spec* spec, const flashoptim_matrix* logits, const int64_t* tokens,
@@ -843,11 +849,10 @@ int flashoptim_policy_loss(const flashoptim_policy_spec* spec, const flashoptim_
         a.dx = (char*)dlogits->data;
         a.dx_stride = rows > 1 ? dlogits->stride : 0;
     }
-    const bool aligned = rows_aligned(logits);
-    if (rows > 0 && holds_rows(rows, logits->cols, logits->dtype, aligned)) {
-        FO_TRY(logits->dtype == FLASHOPTIM_FP32 ? launch_held<true>(a, aligned, stream) : launch_held<false>(a, aligned, stream));
+    if (rows > 0 && holds_rows(rows, logits->cols, logits->dtype)) {
+        FO_TRY(logits->dtype == FLASHOPTIM_FP32 ? launch_held<true>(a, stream) : launch_held<false>(a, stream));
     } else if (rows > 0) {
-        const Parts c = cut_rows(rows, logits->cols, logits->dtype, aligned);
+        const Parts c = cut_rows(rows, logits->cols, logits->dtype);
         const PartsArgs p = to_parts(a, c, (char*)workspace + up(rows * 24, 16) * 16);
         FO_TRY(launch_parts(p, logits->dtype, c.vecs, stream));
         with_vecs(logits->dtype, c.vecs, [&](auto f, auto nv) {
