@@ -435,13 +435,14 @@ int flashoptim_block_norm_backward(const flashoptim_block_norm_spec* spec, const
  * (whose lse is -infinity); a -infinity beside other values has the probability 0.  Sums over a row are FP32 by lane and FP64 where lanes
  * join, what is computed once for a row is FP64; the order of all sums depends on the sizes alone.  Vectors are contiguous FP32.
  *   1 <= vocab < 2^30 unless rows = 0; rows < 2^22, and fewer than 2^24 parts of 16384 BF16 or 8192 FP32 values; T > 0 and finite.
- * token_logprob: logprob, lse [rows], either may be NULL (not both, unless rows = 0).
+ * token_logprob: logprob, lse [rows] and logprob64 [rows], the same as logprob in FP64, for the difference of long sums that a preference
+ *   loss is made of.  Each may be NULL (not all, unless rows = 0).
  * token_logprob_backward: dlogits_ij = dlogprob_i / T ([j = t] - exp(logits_ij / T - lse_i)), of the type of logits, from the lse that the forward
  *   call left.  The logits of a row whose dlogprob is 0 are not read; its gradient is 0.  dlogits may be logits' own buffer.
  * workspace: as in the products above, of the bytes that the *_workspace call returns for the same sizes and type. */
 int64_t flashoptim_token_logprob_workspace(int64_t rows, int64_t vocab, int dtype);
-int flashoptim_token_logprob(const flashoptim_matrix* logits, const int64_t* tokens, float temperature, float* logprob, float* lse,
-                             void* workspace, int64_t workspace_bytes, void* stream);
+int flashoptim_token_logprob(const flashoptim_matrix* logits, const int64_t* tokens, float temperature, float* logprob, double* logprob64,
+                             float* lse, void* workspace, int64_t workspace_bytes, void* stream);
 int flashoptim_token_logprob_backward(const flashoptim_matrix* logits, const int64_t* tokens, float temperature, const float* lse,
                                       const float* dlogprob, const flashoptim_matrix* dlogits, void* stream);
 
@@ -469,7 +470,8 @@ int flashoptim_policy_loss(const flashoptim_policy_spec* spec, const flashoptim_
                            const flashoptim_policy_inputs* inputs, float* stats, float* logprob, const flashoptim_matrix* dlogits,
                            void* workspace, int64_t workspace_bytes, void* stream);
 
-/* preference_loss: of pairs of sequences, one chosen and one rejected, from the log-probabilities of their tokens.
+/* preference_loss: of pairs of sequences, one chosen and one rejected, from the log-probabilities of their tokens, in FP32 or in FP64 (the
+ * other is NULL).
  *   gain(s) = sum over the rows of s of weights (logprob - ref_logprob),   z = beta (gain(chosen) - gain(rejected))
  *   loss = the mean over the pairs of, by kind:  SIGMOID  (1 - label_smoothing) log(1 + exp(-z)) + label_smoothing log(1 + exp(z))
  *                                                HINGE    max(0, 1 - z)
@@ -488,9 +490,9 @@ typedef struct flashoptim_preference_spec {
     float beta, label_smoothing, grad_scale;
 } flashoptim_preference_spec;
 
-int flashoptim_preference_loss(const flashoptim_preference_spec* spec, const float* logprob, const float* ref_logprob,
-                               const float* weights, int64_t rows, const int64_t* offsets, int64_t pairs, float* loss, float* margins,
-                               float* dlogprob, void* stream);
+int flashoptim_preference_loss(const flashoptim_preference_spec* spec, const float* logprob, const double* logprob64,
+                               const float* ref_logprob, const float* weights, int64_t rows, const int64_t* offsets, int64_t pairs,
+                               float* loss, float* margins, float* dlogprob, void* stream);
 
 /* ---- the norm of all gradients and their clipping, between a backward pass and the step -----------------
  * A list of gradients, each flattened, contiguous and 16-byte aligned; src of BF16 or FP32 (src_dtype, one for the whole list).  Its

@@ -164,10 +164,10 @@ def load_library():
         getattr(L, name).argtypes = [i64, i64, i64]
     for name in ("flashoptim_token_logprob_workspace", "flashoptim_policy_loss_workspace"):
         getattr(L, name).argtypes = [i64, i64, i32]
-    L.flashoptim_token_logprob.argtypes = [mat, vp, C.c_float, vp, vp, vp, i64, vp]
+    L.flashoptim_token_logprob.argtypes = [mat, vp, C.c_float, vp, vp, vp, vp, i64, vp]
     L.flashoptim_token_logprob_backward.argtypes = [mat, vp, C.c_float, vp, vp, mat, vp]
     L.flashoptim_policy_loss.argtypes = [C.POINTER(_PolicySpec), mat, vp, C.POINTER(_PolicyInputs), vp, vp, mat, vp, i64, vp]
-    L.flashoptim_preference_loss.argtypes = [C.POINTER(_PreferenceSpec), vp, vp, vp, i64, vp, i64, vp, vp, vp, vp]
+    L.flashoptim_preference_loss.argtypes = [C.POINTER(_PreferenceSpec), vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, vp]
     grads = C.POINTER(_Gradient)
     L.flashoptim_grad_norm_workspace.argtypes = [grads, i64, i32]
     L.flashoptim_grad_norm.argtypes = [grads, i64, i32, C.c_float, vp, vp, i64, vp]
@@ -646,10 +646,10 @@ def token_logprob_workspace(logits):
     return _size(load_library().flashoptim_token_logprob_workspace(*logits.shape, _DTYPE[logits.dtype]), "flashoptim_token_logprob_workspace")
 
 
-def token_logprob(logits, tokens, logprob=None, lse=None, temperature=1.0, workspace=None, stream=None):
-    """logprob [rows] <- the log-probability of each row's token (int64, negative: the row does not count), lse <- the log of the row's
-    sum of exponentials, for the backward pass; one of the two may be None."""
-    status = (_fast or _marshal()).logprob(logits, tokens, temperature, logprob, lse, workspace, _handle(stream))
+def token_logprob(logits, tokens, logprob=None, lse=None, temperature=1.0, logprob64=None, workspace=None, stream=None):
+    """logprob [rows] <- the log-probability of each row's token (int64, negative: the row does not count), logprob64 the same in float64,
+    lse <- the log of the row's sum of exponentials, for the backward pass; what is None is left out."""
+    status = (_fast or _marshal()).logprob(logits, tokens, temperature, logprob, logprob64, lse, workspace, _handle(stream))
     if status:
         raise FlashOptimError(status, "flashoptim_token_logprob")
 
@@ -693,8 +693,8 @@ class PreferenceLoss:
 
 
 def preference_loss(spec, logprob, offsets, loss, ref_logprob=None, weights=None, margins=None, dlogprob=None, stream=None):
-    """loss [1] <- the mean over pairs of sequences, sequence i being the rows offsets[i] .. offsets[i + 1] - 1 of logprob; margins
-    [pairs] and the gradient dlogprob [rows] where they are not None."""
+    """loss [1] <- the mean over pairs of sequences, sequence i being the rows offsets[i] .. offsets[i + 1] - 1 of logprob (float32, or
+    float64 as token_logprob leaves it in logprob64); margins [pairs] and the gradient dlogprob [rows] where they are not None."""
     status = (_fast or _marshal()).preference(spec.address, logprob, offsets, loss, ref_logprob, weights, margins, dlogprob, _handle(stream))
     if status:
         raise FlashOptimError(status, "flashoptim_preference_loss")

@@ -81,14 +81,21 @@ __device__ __forceinline__ double wave_sum(double v) {
     return v;
 }
 
+// log2(e) / T as the FP32 value below it and what that is short of it.  (The first alone is off by up to 2^-23, which goes into the log-probabilities of a
+// sequence with the same sign for every token.)  Both are positive, so that -infinity times the factor is -infinity.
+struct Factor {
+    float high, low;
+};
+__device__ __forceinline__ float times(float x, Factor c) { return fmaf(x, c.high, x * c.low); }
+
 // A part of a row: its largest value and the sum of 2^((x - most) c), FP64.
 struct Sum {
     double sum;
     float most;
 };
-__device__ __forceinline__ Sum join(const Sum& a, const Sum& b, float c) {
+__device__ __forceinline__ Sum join(const Sum& a, const Sum& b, Factor c) {
     const float most = fmaxf(a.most, b.most), base = base_of(most);
-    return {a.sum * (double)exp2_of((a.most - base) * c) + b.sum * (double)exp2_of((b.most - base) * c), most};
+    return {a.sum * (double)exp2_of(times(a.most - base, c)) + b.sum * (double)exp2_of(times(b.most - base, c)), most};
 }
 
 // A word of sixteen bytes: eight BF16 values or four FP32 ones.
@@ -170,7 +177,7 @@ struct Held {
     }
     // The sum of the wavefront's part, in every lane.  A lane adds up in FP32, apart from words of some weight beside the wavefront's largest value, which go
     // into an FP64 sum: beside a token that is all but certain the others would be lost in its rounding, and with them its log-probability.
-    __device__ __forceinline__ Sum wave_part(float c) {
+    __device__ __forceinline__ Sum wave_part(Factor c) {
         float most = edge;
         const Pass first_pass;
 #pragma unroll
@@ -185,14 +192,14 @@ struct Held {
         const float base = base_of(most);
         float sum = 0.0f;
         const Pass second_pass;
-        double near = (double)exp2_of((edge - base) * c);
+        double near = (double)exp2_of(times(edge - base, c));
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (none() || !some(i)) continue;
             float v[kN], eight = 0.0f;
             values(second_pass, i, v);
 #pragma unroll
-            for (int k = 0; k < kN; ++k) v[k] = exp2_of((v[k] - base) * c);
+            for (int k = 0; k < kN; ++k) v[k] = exp2_of(times(v[k] - base, c));
             if (!all(i)) {
                 const bool there = word(i) < words;
 #pragma unroll
@@ -245,7 +252,7 @@ struct Held {
 
 // The sum over a workgroup's wavefronts, in every lane.
 template <int WAVES>
-__device__ __forceinline__ Sum join_waves(const Sum& s, float c) {
+__device__ __forceinline__ Sum join_waves(const Sum& s, Factor c) {
     if constexpr (WAVES == 1) return s;
     __shared__ Sum parts[WAVES];
     if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = s;
@@ -256,7 +263,7 @@ __device__ __forceinline__ Sum join_waves(const Sum& s, float c) {
     const float base = base_of(all.most);
     all.sum = 0.0;
 #pragma unroll
-    for (int k = 0; k < WAVES; ++k) all.sum += parts[k].sum * (double)exp2_of((parts[k].most - base) * c);
+    for (int k = 0; k < WAVES; ++k) all.sum += parts[k].sum * (double)exp2_of(times(parts[k].most - base, c));
     return all;
 }
 
@@ -344,8 +351,9 @@ struct RowsArgs {
     Logits x;
     const int64_t* tokens;
     float *logprob, *lse;
+    double* wide;            // logprob in FP64
     double inv_t;
-    float c;
+    Factor c;
     uint32_t rows;
     char* dx;                // the gradient (policy loss; NULL: not wanted)
     int64_t dx_stride;
@@ -387,7 +395,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void policy_rows_kernel(
     const float d = p.slope * a.scale;
     if (!dx) return;
     if (d == 0.0f) h.store_zeros(dx);
-    else h.store_gradient(dx, token_in(token, a.x.vocab), d, base_of(s.most), a.c, (float)(l.log_sum * kLog2e));
+    else h.store_gradient(dx, token_in(token, a.x.vocab), d, base_of(s.most), a.c.high, (float)(l.log_sum * kLog2e));
 }
 
 // Log-probabilities only, one workgroup of WAVES wavefronts to a row, through which the wavefronts go in turn.
@@ -401,6 +409,7 @@ __global__ __launch_bounds__(WAVES * 64) void logprob_rows_kernel(RowsArgs a) {
         if (threadIdx.x == 0) {
             if (a.logprob) a.logprob[row] = 0.0f;
             if (a.lse) a.lse[row] = 0.0f;
+            if (a.wide) a.wide[row] = 0.0;
         }
         return;
     }
@@ -418,6 +427,7 @@ __global__ __launch_bounds__(WAVES * 64) void logprob_rows_kernel(RowsArgs a) {
     const RowLog l = row_log(s, logit, a.inv_t);
     if (a.logprob) a.logprob[row] = (float)l.logprob;
     if (a.lse) a.lse[row] = (float)l.lse;
+    if (a.wide) a.wide[row] = l.logprob;
 }
 
 // ---- few rows, or rows that do not fit: each cut into parts, a workgroup to each, which leaves its sum; whoever needs a row's joins them.
@@ -454,7 +464,7 @@ __device__ __forceinline__ Sum join_parts(const PartsArgs& a, uint32_t row) {
     Sum s = {0.0, minus_inf()};
     for (uint32_t i = threadIdx.x & 63; i < a.parts; i += 64) s = join(s, parts[i], a.r.c);
     const float most = wave_max(s.most);
-    return {wave_sum(s.sum * (double)exp2_of((s.most - base_of(most)) * a.r.c)), most};
+    return {wave_sum(s.sum * (double)exp2_of(times(s.most - base_of(most), a.r.c))), most};
 }
 
 constexpr int kJoinRows = 4;
@@ -466,6 +476,7 @@ __global__ __launch_bounds__(kJoinRows * 64) void logprob_join_kernel(PartsArgs 
     if (threadIdx.x & 63) return;
     if (a.r.logprob) a.r.logprob[row] = (float)l.logprob;
     if (a.r.lse) a.r.lse[row] = (float)l.lse;
+    if (a.r.wide) a.r.wide[row] = l.logprob;
 }
 
 // The gradient of a part.  Every workgroup joins its row's sums and computes the row's slope for itself; the first of a row leaves what is kept of it.
@@ -495,7 +506,7 @@ __global__ __launch_bounds__(kPartThreads) void policy_parts_kernel(PartsArgs a)
     if (!dx) return;
     const float d = p.slope * a.r.scale;
     if (d == 0.0f) h.store_zeros(dx);
-    else h.store_gradient(dx, token_in(token, a.r.x.vocab), d, base_of(s.most), a.r.c, (float)(l.log_sum * kLog2e));
+    else h.store_gradient(dx, token_in(token, a.r.x.vocab), d, base_of(s.most), a.r.c.high, (float)(l.log_sum * kLog2e));
 }
 
 // ---- the gradient of the logits from the lse of an earlier call
@@ -553,7 +564,9 @@ __global__ __launch_bounds__(kPairThreads) void policy_stats_kernel(const double
 }
 
 struct PairArgs {
-    const float *logprob, *ref, *weights;
+    const float* logprob;
+    const double* wide;      // logprob in FP64, instead
+    const float *ref, *weights;
     const int64_t* offsets;
     float *loss, *margins, *dlogprob;
     int64_t rows, pairs;
@@ -597,17 +610,18 @@ __global__ __launch_bounds__(kPairThreads) void preference_kernel(PairArgs a, in
             end[k] = bound(of + 1);
             double s = 0.0;
             for (int64_t i = begin[k] + lane; i < end[k]; i += kAhead * lanes) {
-                float w[kAhead], v[kAhead], r[kAhead];
+                float w[kAhead], r[kAhead];
+                double v[kAhead];
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u) {      // (behind the end: the last row, which counts no second time)
                     const int64_t at = min(i + (int64_t)u * lanes, end[k] - 1);
                     w[u] = a.weights ? a.weights[at] : 1.0f;
-                    v[u] = a.logprob[at];
+                    v[u] = a.wide ? a.wide[at] : (double)a.logprob[at];
                     r[u] = a.ref ? a.ref[at] : 0.0f;
                 }
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u)
-                    if (w[u] != 0.0f && i + (int64_t)u * lanes < end[k]) s += (double)w[u] * ((double)v[u] - (double)r[u]);
+                    if (w[u] != 0.0f && i + (int64_t)u * lanes < end[k]) s += (double)w[u] * (v[u] - (double)r[u]);
             }
             gain += k ? -s : s;
         }
@@ -755,12 +769,19 @@ int check_workspace(int64_t need, const void* workspace, int64_t bytes) {
     if (bytes < need) return FLASHOPTIM_ERR_WORKSPACE;
     return fo::aligned_to(workspace, 16) ? FLASHOPTIM_OK : FLASHOPTIM_ERR_MISALIGNED;
 }
+Factor factor_of(float temperature) {
+    const double c = kLog2e / (double)temperature;
+    float high = (float)c;
+    if ((double)high > c) high = std::nextafter(high, 0.0f);
+    const float low = (float)(c - (double)high);
+    return {high, low > 1e-30f ? low : 1e-30f};
+}
 RowsArgs rows_args(const flashoptim_matrix* logits, const int64_t* tokens, float temperature) {
     RowsArgs a = {};
     a.x = to_dev(logits);
     a.tokens = tokens;
     a.inv_t = 1.0 / (double)temperature;
-    a.c = (float)(kLog2e / (double)temperature);
+    a.c = factor_of(temperature);
     a.scale = 1.0f / temperature;
     a.rows = (uint32_t)logits->rows;
     return a;
@@ -776,17 +797,18 @@ int64_t flashoptim_token_logprob_workspace(int64_t rows, int64_t vocab, int dtyp
     return rows == 0 || streams_rows(rows, vocab) ? 0 : parts_bytes(rows, vocab, dtype);
 }
 
-int flashoptim_token_logprob(const flashoptim_matrix* logits, const int64_t* tokens, float temperature, float* logprob, float* lse,
-                             void* workspace, int64_t workspace_bytes, void* stream) {
+int flashoptim_token_logprob(const flashoptim_matrix* logits, const int64_t* tokens, float temperature, float* logprob, double* logprob64,
+                             float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
     FO_TRY(check_logits(logits, tokens, temperature));
     const int64_t rows = logits->rows;
     if (rows == 0) return FLASHOPTIM_OK;
-    if (!logprob && !lse) return FLASHOPTIM_ERR_INVALID_ARG;
-    if (!fo::aligned_to(logprob, 4) || !fo::aligned_to(lse, 4)) return FLASHOPTIM_ERR_MISALIGNED;
+    if (!logprob && !logprob64 && !lse) return FLASHOPTIM_ERR_INVALID_ARG;
+    if (!fo::aligned_to(logprob, 4) || !fo::aligned_to(logprob64, 8) || !fo::aligned_to(lse, 4)) return FLASHOPTIM_ERR_MISALIGNED;
     FO_TRY(check_launch(logits));
     FO_TRY(check_workspace(flashoptim_token_logprob_workspace(rows, logits->cols, logits->dtype), workspace, workspace_bytes));
     RowsArgs a = rows_args(logits, tokens, temperature);
     a.logprob = logprob;
+    a.wide = logprob64;
     a.lse = lse;
     if (streams_rows(rows, logits->cols)) {
         const dim3 grid(a.rows), block(kStreamWaves * 64);
@@ -864,20 +886,20 @@ int flashoptim_policy_loss(const flashoptim_policy_spec* spec, const flashoptim_
     return fo::hip_status(hipGetLastError());
 }
 
-int flashoptim_preference_loss(const flashoptim_preference_spec* spec, const float* logprob, const float* ref_logprob,
-                               const float* weights, int64_t rows, const int64_t* offsets, int64_t pairs, float* loss, float* margins,
-                               float* dlogprob, void* stream) {
-    if (!spec || !loss || rows < 0 || pairs < 0 || spec->kind < 0 || spec->kind > 2 || spec->order < 0 || spec->order > 1)
+int flashoptim_preference_loss(const flashoptim_preference_spec* spec, const float* logprob, const double* logprob64,
+                               const float* ref_logprob, const float* weights, int64_t rows, const int64_t* offsets, int64_t pairs,
+                               float* loss, float* margins, float* dlogprob, void* stream) {
+    if (!spec || !loss || rows < 0 || pairs < 0 || spec->kind < 0 || spec->kind > 2 || spec->order < 0 || spec->order > 1 || (logprob && logprob64))
         return FLASHOPTIM_ERR_INVALID_ARG;
     if (!(spec->beta > 0.0f) || !std::isfinite(spec->beta) || !(spec->label_smoothing >= 0.0f && spec->label_smoothing <= 0.5f) ||
         (spec->label_smoothing != 0.0f && spec->kind != FLASHOPTIM_PREFERENCE_SIGMOID))
         return FLASHOPTIM_ERR_INVALID_ARG;
     if (rows >= ((int64_t)1 << 31) || pairs >= ((int64_t)1 << 30)) return FLASHOPTIM_ERR_NUMEL_RANGE;
-    if ((rows > 0 && !logprob) || (pairs > 0 && !offsets)) return FLASHOPTIM_ERR_INVALID_ARG;
+    if ((rows > 0 && !logprob && !logprob64) || (pairs > 0 && !offsets)) return FLASHOPTIM_ERR_INVALID_ARG;
     for (const float* p : {logprob, ref_logprob, weights, (const float*)loss, (const float*)margins, (const float*)dlogprob})
         if (!fo::aligned_to(p, 4)) return FLASHOPTIM_ERR_MISALIGNED;
-    if (!fo::aligned_to(offsets, 8)) return FLASHOPTIM_ERR_MISALIGNED;
-    const PairArgs a = {logprob, ref_logprob, weights, offsets, loss, margins, dlogprob, rows, pairs, *spec};
+    if (!fo::aligned_to(offsets, 8) || !fo::aligned_to(logprob64, 8)) return FLASHOPTIM_ERR_MISALIGNED;
+    const PairArgs a = {logprob, logprob64, ref_logprob, weights, offsets, loss, margins, dlogprob, rows, pairs, *spec};
     int groups = 1;
     while (groups < 16 && groups < pairs) groups *= 2;
     hipLaunchKernelGGL(preference_kernel, dim3(1), dim3(kPairThreads), 0, (hipStream_t)stream, a, groups);

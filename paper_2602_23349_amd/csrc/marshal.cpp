@@ -251,7 +251,7 @@ void bound(Args& a, F* call) {
 }
 
 PyObject* logprob(PyObject*, PyObject* const* args, Py_ssize_t n) {
-    Args a(args, n, 7);
+    Args a(args, n, 8);
     flashoptim_matrix mx;
     void* ws;
     int64_t bytes;
@@ -260,11 +260,12 @@ PyObject* logprob(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const void* tokens = a.plain("tokens", at::kLong, -1, 0, rows);
     const float temperature = a.number();
     void* logprob = a.plain("logprob", at::kFloat, -1, 0, rows);
+    void* wide = a.plain("logprob64", at::kDouble, -1, 0, rows);
     void* lse = a.plain("lse", at::kFloat, -1, 0, rows);
     a.workspace(&ws, &bytes);
     void* stream = a.stream();
     bound(a, call_logprob);
-    return status(a, a.failed ? 0 : call_logprob(x, (const int64_t*)tokens, temperature, (float*)logprob, (float*)lse, ws, bytes, stream));
+    return status(a, a.failed ? 0 : call_logprob(x, (const int64_t*)tokens, temperature, (float*)logprob, (double*)wide, (float*)lse, ws, bytes, stream));
 }
 
 PyObject* logprob_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -310,11 +311,12 @@ PyObject* preference(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const auto* spec = a.address<flashoptim_preference_spec>();
     const at::Tensor* first = a.tensor("logprob");
     const int64_t rows = first ? first->numel() : 0;
-    --a.i;
-    const void* logprob = a.plain("logprob", at::kFloat, -1, 0, rows);
+    const bool wide = first && first->scalar_type() == at::kDouble;
+    if (!a.failed) --a.i;
+    const void* logprob = a.plain("logprob", wide ? at::kDouble : at::kFloat, -1, 0, rows);
     const at::Tensor* cuts = a.tensor("offsets");
     const int64_t bounds = cuts ? cuts->numel() : 1;
-    --a.i;
+    if (!a.failed) --a.i;
     const void* offsets = a.plain("offsets", at::kLong, -1, 0, bounds);
     if (bounds % 2 == 0) a.fail(PyExc_ValueError, "%s", "offsets: the bounds of an even number of sequences, one more than that");
     const int64_t pairs = bounds / 2;
@@ -325,7 +327,7 @@ PyObject* preference(PyObject*, PyObject* const* args, Py_ssize_t n) {
     void* d = a.plain("dlogprob", at::kFloat, -1, 0, rows);
     void* stream = a.stream();
     bound(a, call_preference);
-    return status(a, a.failed ? 0 : call_preference(spec, (const float*)logprob, (const float*)ref, (const float*)weights, rows,
+    return status(a, a.failed ? 0 : call_preference(spec, wide ? nullptr : (const float*)logprob, wide ? (const double*)logprob : nullptr, (const float*)ref, (const float*)weights, rows,
                                                     (const int64_t*)offsets, pairs, (float*)loss, (float*)margins, (float*)d, stream));
 }
 

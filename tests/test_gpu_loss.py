@@ -78,6 +78,10 @@ def forward(c, stream=None, workspace=None):
 def check_logprob(c):
     logprob, lse = forward(c)
     ref = R.Rows(c.logits, c.tokens, c.temperature)
+    wide = torch.full((c.rows,), 7.0, dtype=torch.float64, device="cuda")
+    fo.token_logprob(c.logits, c.tokens, logprob64=wide, temperature=c.temperature, workspace=memory(fo.token_logprob_workspace(c.logits)))
+    assert torch.equal(wide.float().nan_to_num(nan=-1.0), logprob.nan_to_num(nan=-1.0))
+    R.close(wide, ref.logprob, torch.where(ref.counted, ref.err, 0.0) + 1e-14 * ref.logprob.abs(), "logprob64")
     R.close(logprob, ref.logprob, torch.where(ref.counted, ref.err, 0.0) + R.U * ref.logprob.abs(), "logprob")
     R.close(lse, ref.lse, torch.where(ref.counted, ref.err, 0.0) + R.U * ref.lse.abs(), "lse")
     return ref, lse
@@ -301,6 +305,9 @@ def test_preference_loss(kind, smoothing, lengths):
             R.close(out, torch.tensor([loss]), torch.tensor([R.U * abs(loss) + 1e-9 * (1 + abs(loss))]), "loss")
             R.close(m, margins, R.U * margins.abs() + 1e-10, "margins")
             R.close(d, grad, R.U * grad.abs() + 1e-9 * (1 + grad.abs()), "dlogprob")
+            again = [t.clone() for t in (out, m, d)]
+            fo.preference_loss(spec, lp.double().cuda(), cut.cuda(), out, ref_logprob=cuda(ref), weights=cuda(w), margins=m, dlogprob=d)
+            assert all(torch.equal(a, b) for a, b in zip(again, (out, m, d)))
 
 
 def test_preference_loss_of_values_that_do_not_count():
@@ -354,7 +361,7 @@ def test_preference_step_matches_autograd():
     z = 0.2 * torch.stack([gap[0:20].sum() - gap[20:45].sum(), gap[45:45].sum() - gap[45:90].sum()])
     loss = torch.nn.functional.softplus(-z).mean()
     loss.backward()
-    assert abs(float(out["loss"]) - float(loss)) <= 1e-5 * float(loss)
+    assert abs(float(out["loss"]) - loss.item()) <= 1e-5 * loss.item()
     # log-probabilities are off by a few u of 10 each, the gradient's scale by that of 70 of them
     assert float((out["dx"].double().cpu() - x.grad).abs().max()) <= 1e-5 * float(x.grad.abs().max())
 

@@ -20,8 +20,8 @@ def matrix(rows=4, cols=100, stride=None, dtype=0, data=P):
     return B._Matrix(data, rows, cols, cols if stride is None else stride, dtype)
 
 
-def logprob(x=None, tokens=P, temperature=1.0, out=P, lse=P, ws=P, size=1 << 30):
-    return fo.load_library().flashoptim_token_logprob(matrix() if x is None else x, tokens, temperature, out, lse, ws, size, None)
+def logprob(x=None, tokens=P, temperature=1.0, out=P, wide=P, lse=P, ws=P, size=1 << 30):
+    return fo.load_library().flashoptim_token_logprob(matrix() if x is None else x, tokens, temperature, out, wide, lse, ws, size, None)
 
 
 def backward(x=None, tokens=P, temperature=1.0, lse=P, d=P, dx=None):
@@ -34,8 +34,8 @@ def policy(x=None, spec=(1.0, 0.2, 0.2, 0.0, 1.0), inputs=(P, P, P, P), tokens=P
                                                     stats, lp, matrix(data=2 * P) if dx is None else dx, ws, size, None)
 
 
-def preference(spec=(0, 0, 0.1, 0.0, 1.0), lp=P, ref=P, w=P, rows=10, offsets=P, pairs=2, loss=P, m=P, d=P):
-    return fo.load_library().flashoptim_preference_loss(B._PreferenceSpec(*spec), lp, ref, w, rows, offsets, pairs, loss, m, d, None)
+def preference(spec=(0, 0, 0.1, 0.0, 1.0), lp=P, wide=None, ref=P, w=P, rows=10, offsets=P, pairs=2, loss=P, m=P, d=P):
+    return fo.load_library().flashoptim_preference_loss(B._PreferenceSpec(*spec), lp, wide, ref, w, rows, offsets, pairs, loss, m, d, None)
 
 
 BAD_LOGITS = [(dict(x=matrix(rows=-1)), -1), (dict(x=matrix(cols=0)), -1), (dict(x=matrix(dtype=2)), -1), (dict(x=matrix(stride=99)), -1),
@@ -56,7 +56,7 @@ def test_log_probabilities_refuse():
         assert backward(**kw) == status, kw
     for t in NUMBERS:
         assert logprob(temperature=t) == -1 and backward(temperature=t) == -1
-    assert logprob(out=None, lse=None) == -1 and logprob(out=P + 2) == -2 and logprob(lse=P + 1) == -2
+    assert logprob(out=None, wide=None, lse=None) == -1 and logprob(wide=P + 4) == -2 and logprob(out=P + 2) == -2 and logprob(lse=P + 1) == -2
     assert backward(lse=None) == -1 and backward(d=None) == -1 and backward(lse=P + 2) == -2
     for dx in (matrix(rows=3), matrix(cols=99), matrix(dtype=1), matrix(stride=101)):       # (the last: over the logits, rows elsewhere)
         assert backward(dx=dx) == -1
@@ -92,6 +92,7 @@ def test_preference_loss_refuses():
             assert preference(spec=spec) == -1, spec
     assert preference(spec=(1, 0, 0.1, 0.1, 1.0)) == -1
     assert preference(rows=-1) == -1 and preference(pairs=-1) == -1 and preference(rows=1 << 31) == -3 and preference(pairs=1 << 30) == -3
+    assert preference(wide=P) == -1 and preference(lp=None, wide=P + 4) == -2
     assert preference(lp=None) == -1 and preference(offsets=None) == -1 and preference(loss=None) == -1
     assert preference(offsets=P + 4) == -2 and preference(m=P + 2) == -2 and preference(d=P + 1) == -2 and preference(w=P + 3) == -2
 
