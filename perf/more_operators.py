@@ -247,6 +247,7 @@ def prepare(case, seed):
         else:
             size = fo.token_logprob_workspace(s["logits"])
         if c["op"] == "preference":
+            s["logprob64"] = torch.empty(rows, dtype=FP64, device="cuda")
             s["spec"] = fo.PreferenceLoss(beta=BETA, kind=c["kind"], label_smoothing=c["smoothing"])
         s["workspace"] = torch.empty(size, dtype=torch.uint8, device="cuda")
     return s
@@ -274,10 +275,10 @@ def _own_run(s):
                        workspace=s["workspace"])
         return {"stats": s["stats"], "logprob": s["logprob"], "dlogits": s["dlogits"]}
     fo.token_logprob(s["logits"], s["tokens"], s["logprob"], s["lse"], temperature=c.get("temperature", 1.0),
-                     workspace=s["workspace"])
+                     logprob64=s.get("logprob64"), workspace=s["workspace"])
     if c["op"] == "logprob":
         return {"logprob": s["logprob"], "lse": s["lse"]}
-    fo.preference_loss(s["spec"], s["logprob"], s["offsets"], s["loss"], ref_logprob=s["ref"], weights=s["weights"],
+    fo.preference_loss(s["spec"], s["logprob64"], s["offsets"], s["loss"], ref_logprob=s["ref"], weights=s["weights"],
                        margins=s["margins"], dlogprob=s["dlogprob"])
     fo.token_logprob_backward(s["logits"], s["tokens"], s["lse"], s["dlogprob"], s["dlogits"])
     return {"loss": s["loss"], "margins": s["margins"], "logprob": s["logprob"], "dlogits": s["dlogits"]}
