@@ -267,52 +267,13 @@ __device__ __forceinline__ Sum join_waves(const Sum& s, Factor c) {
     return all;
 }
 
-// What is computed once for a row, in FP64.  By series in loops over one table: unrolled, as the library's functions are, their coefficients take fifty
-// registers that a row is held in.
-constexpr int kTerms = 26;
-struct Inverses {
-    double of[kTerms];
-    constexpr Inverses() : of() {
-        for (int n = 1; n < kTerms; ++n) of[n] = 1.0 / n;
-    }
-};
-static __constant__ const Inverses inverses;
-constexpr double kLn2 = 0.69314718055994530942, kLn2Low = 2.3190468138462996e-17;      // (the sum is ln 2 to more than FP64)
-
-// exp(x) - 1 and exp(x): with x = k ln 2 + r, |r| <= ln 2 / 2, e^r - 1 = r (1 + r/2 (1 + r/3 (...))), whose 15th term is below 2^-60 of it.
-__device__ __forceinline__ double expm1_row(double x, bool less_one = true) {
-    if (x > 720.0) return (double)__builtin_inff();
-    if (x < -760.0) return less_one ? -1.0 : 0.0;
-    const double k = rint(x * kLog2e), r = fma(-k, kLn2, x) - k * kLn2Low;
-    double s = 1.0;
-#pragma unroll 1
-    for (int n = 15; n > 1; --n) s = fma(r * inverses.of[n], s, 1.0);
-    s *= r;
-    if (k == 0.0) return less_one ? s : 1.0 + s;
-    return ldexp(1.0 + s, (int)k) - (less_one ? 1.0 : 0.0);
-}
-__device__ __forceinline__ double exp_row(double x) { return expm1_row(x, false); }
-// log(x) of x >= 0: with x = 2^k m, 1/sqrt 2 <= m < sqrt 2 and z = (m - 1) / (m + 1), k ln 2 + 2 (z + z^3/3 + z^5/5 + ...), whose 13th term is below 2^-60 of it.
-__device__ __forceinline__ double log_row(double x) {
-    if (!(x > 0.0) || !(x < (double)__builtin_inff())) return x == 0.0 ? -(double)__builtin_inff() : x;
-    int k = ilogb(x);
-    double m = ldexp(x, -k);
-    if (m > 1.4142135623730951) { m *= 0.5; ++k; }
-    const double z = (m - 1.0) / (m + 1.0), zz = z * z;
-    double s = 0.0;
-#pragma unroll 1
-    for (int n = 25; n > 1; n -= 2) s = fma(s, zz, inverses.of[n]);
-    s = fma(s * zz, z, z);
-    return fma((double)k, kLn2, 2.0 * s + k * kLn2Low);
-}
-
 // log sum exp(x / T) and the token's log-probability; log_sum is what lse is beyond the largest value.
 struct RowLog {
     double lse, logprob, log_sum;
 };
 __device__ __forceinline__ RowLog row_log(const Sum& s, float x, double inv_t) {
     // (a sum beyond FP32 is that of a row with +infinity)
-    const double log_sum = s.most < __builtin_inff() ? log_row(s.sum) : (double)__builtin_nanf("");
+    const double log_sum = s.most < __builtin_inff() ? log(s.sum) : (double)__builtin_nanf("");
     return {(double)s.most * inv_t + log_sum, ((double)x - (double)s.most) * inv_t - log_sum, log_sum};
 }
 
@@ -328,13 +289,13 @@ struct PolicyArgs {
 };
 __device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& a, uint32_t row, double logprob, float w) {
     const double adv = a.in.advantages[row];
-    const double ratio = a.in.old_logprob ? exp_row(logprob - (double)a.in.old_logprob[row]) : logprob - logprob + 1.0;
+    const double ratio = a.in.old_logprob ? exp(logprob - (double)a.in.old_logprob[row]) : logprob - logprob + 1.0;
     const double low = 1.0 - (double)a.spec.clip_low, high = 1.0 + (double)a.spec.clip_high;
     const bool blocked = (adv > 0.0 && ratio > high) || (adv < 0.0 && ratio < low);
     const double surrogate = blocked ? -adv * (adv > 0.0 ? high : low) : -adv * ratio;
     double slope = blocked ? 0.0 : -adv * ratio, kl = 0.0;
     if (a.in.ref_logprob) {
-        const double d = (double)a.in.ref_logprob[row] - logprob, e = expm1_row(d);
+        const double d = (double)a.in.ref_logprob[row] - logprob, e = expm1(d);
         kl = e - d;
         slope -= (double)a.spec.kl_weight * e;
     }
@@ -538,29 +499,27 @@ __global__ __launch_bounds__(kPartThreads) void gradient_kernel(GradArgs a) {
     h.store_gradient(dx, token_in(token, a.x.vocab), d, 0.0f, a.c, shift);
 }
 
-// The sum over a workgroup, in every lane, in a fixed order.
-template <int THREADS>
-__device__ __forceinline__ double group_sum(double s) {
-    __shared__ double part[THREADS / 64];
-    s = wave_sum(s);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
-    __syncthreads();
-    s = 0.0;
-#pragma unroll
-    for (int k = 0; k < THREADS / 64; ++k) s += part[k];
-    return s;
-}
-
+// Three sums over a workgroup's rows, and from them the statistics.
 __global__ __launch_bounds__(kPairThreads) void policy_stats_kernel(const double* terms, uint32_t rows, float kl_weight, float* stats) {
+    __shared__ double part[3][kPairThreads / 64];
     double s[3] = {};
     for (uint32_t i = threadIdx.x; i < rows; i += kPairThreads)
+#pragma unroll
         for (int k = 0; k < 3; ++k) s[k] += terms[(int64_t)k * rows + i];
-    for (int k = 0; k < 3; ++k) s[k] = group_sum<kPairThreads>(s[k]);
-    if (threadIdx.x == 0) {
-        stats[0] = (float)(s[0] + (double)kl_weight * s[1]);
-        for (int k = 0; k < 3; ++k) stats[1 + k] = (float)s[k];
+    for (int off = 32; off > 0; off >>= 1)
+#pragma unroll
+        for (int k = 0; k < 3; ++k) s[k] += __shfl_xor(s[k], off);
+    if ((threadIdx.x & 63) < 3) part[threadIdx.x & 63][threadIdx.x >> 6] = (threadIdx.x & 63) == 0 ? s[0] : (threadIdx.x & 63) == 1 ? s[1] : s[2];
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        s[k] = 0.0;
+#pragma unroll
+        for (int j = 0; j < kPairThreads / 64; ++j) s[k] += part[k][j];
+        stats[1 + k] = (float)s[k];
     }
+    stats[0] = (float)(s[0] + (double)kl_weight * s[1]);
 }
 
 struct PairArgs {
@@ -573,16 +532,18 @@ struct PairArgs {
     flashoptim_preference_spec spec;
 };
 
-__device__ __forceinline__ double softplus(double z) { return fmax(z, 0.0) + log1p(exp(-fabs(z))); }
-
 // What of a pair's margin the loss and its slope by the margin are.
 struct PairLoss {
     double loss, slope;
 };
 __device__ __forceinline__ PairLoss pair_loss(const flashoptim_preference_spec& spec, double gain) {
     const double beta = spec.beta, z = beta * gain, e = spec.label_smoothing;
-    if (spec.kind == FLASHOPTIM_PREFERENCE_SIGMOID)      // (z may be infinite)
-        return {(1.0 - e) * softplus(-z) + (e > 0.0 ? e * softplus(z) : 0.0), e / (1.0 + exp(-z)) - (1.0 - e) / (1.0 + exp(z))};
+    if (spec.kind == FLASHOPTIM_PREFERENCE_SIGMOID) {      // (z may be infinite)
+        const double t = exp(-fabs(z)), l = log1p(t), near = 1.0 / (1.0 + t), far = t * near;       // sigmoid(|z|), sigmoid(-|z|)
+        const double up = z >= 0.0 ? near : far, down = z >= 0.0 ? far : near;
+        const double plus = fmax(-z, 0.0) + l, minus = fmax(z, 0.0) + l;                             // -log sigmoid(z), -log sigmoid(-z)
+        return {(1.0 - e) * plus + (e > 0.0 ? e * minus : 0.0), e * up - (1.0 - e) * down};
+    }
     if (spec.kind == FLASHOPTIM_PREFERENCE_HINGE)        // (z may be NaN)
         return {z < 1.0 ? 1.0 - z : z >= 1.0 ? 0.0 : z, z < 1.0 ? -1.0 : z >= 1.0 ? 0.0 : z};
     const double r = gain - 0.5 / beta;
@@ -592,7 +553,7 @@ __device__ __forceinline__ PairLoss pair_loss(const flashoptim_preference_spec& 
 // One workgroup for all pairs, so that the loss needs no second launch: there are a few bytes for each row of logits.  Its wavefronts are shared out over
 // `groups` pairs at a time: from one wavefront each, with nothing to wait for between them, to all sixteen for a single pair.
 __global__ __launch_bounds__(kPairThreads) void preference_kernel(PairArgs a, int groups) {
-    constexpr int kWaves = kPairThreads / 64, kAhead = 4;
+    constexpr int kWaves = kPairThreads / 64, kAhead = 2;
     __shared__ double gains[kWaves], losses[kWaves];
     const auto bound = [&](int64_t i) { return min(max(a.offsets[i], (int64_t)0), a.rows); };
     const bool by_turns = a.spec.order == FLASHOPTIM_PAIRS_BY_TURNS;
@@ -604,26 +565,34 @@ __global__ __launch_bounds__(kPairThreads) void preference_kernel(PairArgs a, in
         const bool there = p < a.pairs;
         int64_t begin[2] = {}, end[2] = {};
         double gain = 0.0;
-        for (int k = 0; k < 2 && there; ++k) {
-            const int64_t of = by_turns ? 2 * p + k : p + k * a.pairs;
-            begin[k] = bound(of);
-            end[k] = bound(of + 1);
-            double s = 0.0;
-            for (int64_t i = begin[k] + lane; i < end[k]; i += kAhead * lanes) {
-                float w[kAhead], r[kAhead];
-                double v[kAhead];
+        if (there)
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u) {      // (behind the end: the last row, which counts no second time)
-                    const int64_t at = min(i + (int64_t)u * lanes, end[k] - 1);
-                    w[u] = a.weights ? a.weights[at] : 1.0f;
-                    v[u] = a.wide ? a.wide[at] : (double)a.logprob[at];
-                    r[u] = a.ref ? a.ref[at] : 0.0f;
+            for (int k = 0; k < 2; ++k) {
+                const int64_t of = by_turns ? 2 * p + k : p + k * a.pairs;
+                begin[k] = bound(of);
+                end[k] = bound(of + 1);
+            }
+        const int64_t longest = max(end[0] - begin[0], end[1] - begin[1]);
+        for (int64_t i = lane; i < longest; i += kAhead * lanes) {      // (of both sequences, so that all loads are on their way together)
+            float w[2][kAhead], r[2][kAhead];
+            double v[2][kAhead];
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) {
+                    const int64_t at = begin[k] + i + (int64_t)u * lanes;
+                    const bool in = at < end[k];
+                    w[k][u] = !in ? 0.0f : a.weights ? a.weights[at] : 1.0f;
+                    v[k][u] = !in ? 0.0 : a.wide ? a.wide[at] : (double)a.logprob[at];
+                    r[k][u] = in && a.ref ? a.ref[at] : 0.0f;
                 }
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u)
-                    if (w[u] != 0.0f && i + (int64_t)u * lanes < end[k]) s += (double)w[u] * (v[u] - (double)r[u]);
-            }
-            gain += k ? -s : s;
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) {
+                    const double d = w[k][u] != 0.0f ? (double)w[k][u] * (v[k][u] - (double)r[k][u]) : 0.0;
+                    gain += k ? -d : d;
+                }
         }
         gain = wave_sum(gain);
         if (waves > 1) {
