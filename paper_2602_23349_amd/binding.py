@@ -728,6 +728,8 @@ class GradList:
     @classmethod
     def of(cls, params):
         """The gradients of a TensorList as its descriptors have them now, clipped in place."""
+        if any(getattr(b, "grad", None) is not None and not b.grad.is_cuda for b in params.buffers):
+            raise ValueError("gradients: tensors on the GPU")
         out = cls([])
         out.n = params.n
         out.array = (_Gradient * max(out.n, 1))()
@@ -743,6 +745,8 @@ class ClipFactor:
 
     def __init__(self, device="cuda"):
         self.data = torch.zeros(2, dtype=torch.float64, device=device)
+        if not self.data.is_cuda:
+            raise ValueError("a factor lies on the GPU")
         self.sum_squares = self.data[:1]
         self.norm, self.scale = self.data.view(torch.float32)[2:3], self.data.view(torch.float32)[3:4]
         self.address = self.data.data_ptr()

@@ -503,9 +503,18 @@ __global__ __launch_bounds__(kPartThreads) void gradient_kernel(GradArgs a) {
 __global__ __launch_bounds__(kPairThreads) void policy_stats_kernel(const double* terms, uint32_t rows, float kl_weight, float* stats) {
     __shared__ double part[3][kPairThreads / 64];
     double s[3] = {};
-    for (uint32_t i = threadIdx.x; i < rows; i += kPairThreads)
+    constexpr uint32_t kAhead = 4;                                 // (loads that are on their way together)
+    for (uint32_t i = threadIdx.x; i < rows; i += kAhead * kPairThreads) {
+        double v[kAhead][3];
 #pragma unroll
-        for (int k = 0; k < 3; ++k) s[k] += terms[(int64_t)k * rows + i];
+        for (uint32_t u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int k = 0; k < 3; ++k) v[u][k] = i + u * kPairThreads < rows ? terms[(int64_t)k * rows + i + u * kPairThreads] : 0.0;
+#pragma unroll
+        for (uint32_t u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int k = 0; k < 3; ++k) s[k] += v[u][k];
+    }
     for (int off = 32; off > 0; off >>= 1)
 #pragma unroll
         for (int k = 0; k < 3; ++k) s[k] += __shfl_xor(s[k], off);
