@@ -250,13 +250,16 @@ struct Held {
     }
 };
 
-// The sum over a workgroup's wavefronts, in every lane.
-template <int WAVES>
-__device__ __forceinline__ Sum join_waves(const Sum& s, Factor c) {
+// The sum over a workgroup's wavefronts, in every lane.  ALONG: loads on their way are not waited for, and of several calls in a row every other one takes the
+// other slot (a wavefront that is one call ahead waits there).
+template <int WAVES, bool ALONG = false>
+__device__ __forceinline__ Sum join_waves(const Sum& s, Factor c, int slot = 0) {
     if constexpr (WAVES == 1) return s;
-    __shared__ Sum parts[WAVES];
+    __shared__ Sum slots[ALONG ? 2 : 1][WAVES];
+    Sum* parts = slots[slot];
     if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = s;
-    __syncthreads();
+    if constexpr (ALONG) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    else __syncthreads();
     Sum all = parts[0];
 #pragma unroll
     for (int k = 1; k < WAVES; ++k) all.most = fmaxf(all.most, parts[k].most);
@@ -267,13 +270,64 @@ __device__ __forceinline__ Sum join_waves(const Sum& s, Factor c) {
     return all;
 }
 
+// What is computed once for a row, in FP64, from the functions' series.  A coefficient is put into scalar registers where it is used: the compiler keeps those of
+// the library's functions in vector registers all the time, in which a row is held.
+template <int64_t BITS>
+__device__ __forceinline__ double constant() {
+    int low, high;
+    asm volatile("s_mov_b32 %0, %1" : "=s"(low) : "i"((int)BITS));
+    asm volatile("s_mov_b32 %0, %1" : "=s"(high) : "i"((int)(BITS >> 32)));
+    return __hiloint2double(high, low);
+}
+#define FO_CONSTANT(value) constant<__builtin_bit_cast(int64_t, (double)(value))>()
+constexpr double kLn2 = 0.69314718055994530942, kLn2Low = 2.3190468138462996e-17;      // (the sum is ln 2 to more than FP64)
+constexpr double factorial(int n) { return n > 1 ? n * factorial(n - 1) : 1.0; }
+// 1 / N! + r / (N + 1)! + ... up to r^(LAST - N) / LAST!, and 1 / N + r / (N + 2) + ... up to the power of 1 / LAST.
+template <int N, int LAST>
+__device__ __forceinline__ double exp_series(double r) {
+    if constexpr (N == LAST) return FO_CONSTANT(1.0 / factorial(N));
+    else return fma(r, exp_series<N + 1, LAST>(r), FO_CONSTANT(1.0 / factorial(N)));
+}
+template <int N, int LAST>
+__device__ __forceinline__ double log_series(double r) {
+    if constexpr (N == LAST) return FO_CONSTANT(1.0 / N);
+    else return fma(r, log_series<N + 2, LAST>(r), FO_CONSTANT(1.0 / N));
+}
+// e^x - 1 and e^x.  With x = k ln 2 + r, |r| <= ln 2 / 2, the first term left out of e^r - 1, r^14 / 14!, is 2^-56 of it.
+__device__ __forceinline__ double expm1_of(double x, double less = 1.0) {
+    x = x > 800.0 ? 800.0 : x < -800.0 ? -800.0 : x;       // (NaN stays; beyond these the power of two gives infinity and 0)
+    const double k = rint(x * FO_CONSTANT(kLog2e)), r = fma(-k, FO_CONSTANT(kLn2Low), fma(-k, FO_CONSTANT(kLn2), x));
+    const double s = r * exp_series<1, 13>(r);
+    return k == 0.0 ? s + (1.0 - less) : ldexp(1.0 + s, (int)k) - less;
+}
+__device__ __forceinline__ double exp_of(double x) { return expm1_of(x, 0.0); }
+// log x for x >= 0: with x = 2^e m, sqrt(1/2) <= m < sqrt 2, and t = (m - 1) / (m + 1) it is e ln 2 + 2 t (1 + t^2 / 3 + t^4 / 5 + ...), whose first term left
+// out, t^22 / 23, is 2^-60.
+__device__ __forceinline__ double log_of(double x) {
+    if (x == 0.0) return (double)minus_inf();
+    double m = __builtin_amdgcn_frexp_mant(x);
+    int e = __builtin_amdgcn_frexp_exp(x);
+    if (m < FO_CONSTANT(0.70710678118654752440)) {
+        m += m;
+        --e;
+    }
+    const double n = m - 1.0, d = m + 1.0;
+    double q = __builtin_amdgcn_rcp(d);
+    q = fma(q, fma(-d, q, 1.0), q);
+    q = fma(q, fma(-d, q, 1.0), q);
+    double t = n * q;
+    t = fma(q, fma(-d, t, n), t);
+    const double s = 2.0 * t * log_series<1, 21>(t * t);
+    return fma((double)e, FO_CONSTANT(kLn2), fma((double)e, FO_CONSTANT(kLn2Low), s));
+}
+
 // log sum exp(x / T) and the token's log-probability; log_sum is what lse is beyond the largest value.
 struct RowLog {
     double lse, logprob, log_sum;
 };
 __device__ __forceinline__ RowLog row_log(const Sum& s, float x, double inv_t) {
     // (a sum beyond FP32 is that of a row with +infinity)
-    const double log_sum = s.most < __builtin_inff() ? log(s.sum) : (double)__builtin_nanf("");
+    const double log_sum = s.most < __builtin_inff() ? log_of(s.sum) : (double)__builtin_nanf("");
     return {(double)s.most * inv_t + log_sum, ((double)x - (double)s.most) * inv_t - log_sum, log_sum};
 }
 
@@ -287,19 +341,26 @@ struct PolicyArgs {
     flashoptim_policy_inputs in;
     double* terms;                      // [3, rows]
 };
-__device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& a, uint32_t row, double logprob, float w) {
-    const double adv = a.in.advantages[row];
-    const double ratio = a.in.old_logprob ? exp(logprob - (double)a.in.old_logprob[row]) : logprob - logprob + 1.0;
+struct PolicyIn {
+    float w, advantage, old, ref;
+};
+__device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& a, const PolicyIn& in, double logprob) {
+    const double adv = in.advantage, w = in.w;
+    const double ratio = a.in.old_logprob ? exp_of(logprob - (double)in.old) : logprob - logprob + 1.0;
     const double low = 1.0 - (double)a.spec.clip_low, high = 1.0 + (double)a.spec.clip_high;
     const bool blocked = (adv > 0.0 && ratio > high) || (adv < 0.0 && ratio < low);
     const double surrogate = blocked ? -adv * (adv > 0.0 ? high : low) : -adv * ratio;
     double slope = blocked ? 0.0 : -adv * ratio, kl = 0.0;
     if (a.in.ref_logprob) {
-        const double d = (double)a.in.ref_logprob[row] - logprob, e = expm1(d);
+        const double d = (double)in.ref - logprob, e = expm1_of(d);
         kl = e - d;
         slope -= (double)a.spec.kl_weight * e;
     }
-    return {(float)(slope * (double)w * (double)a.spec.grad_scale), surrogate * w, kl * w, blocked ? (double)w : 0.0};
+    return {(float)(slope * w * (double)a.spec.grad_scale), surrogate * w, kl * w, blocked ? w : 0.0};
+}
+__device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& a, uint32_t row, double logprob, float w) {
+    const PolicyIn in = {w, a.in.advantages[row], a.in.old_logprob ? a.in.old_logprob[row] : 0.0f, a.in.ref_logprob ? a.in.ref_logprob[row] : 0.0f};
+    return policy_row(a, in, logprob);
 }
 __device__ __forceinline__ void put_terms(const PolicyArgs& a, uint32_t rows, uint32_t row, const PolicyRow& r) {
     a.terms[row] = r.surrogate;
@@ -357,6 +418,96 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void policy_rows_kernel(
     if (!dx) return;
     if (d == 0.0f) h.store_zeros(dx);
     else h.store_gradient(dx, token_in(token, a.x.vocab), d, base_of(s.most), a.c.high, (float)(l.log_sum * kLog2e));
+}
+
+// Rows of which a compute unit holds one at a time.  Workgroups stay and take every so many-th row: of the next one the first kAhead words of each lane, as many as
+// LDS holds, are on their way there while this one is worked on and stored, so that the memory is not idle between two rows.  (4096 rows of 128256 BF16 values
+// 440-453 us without, 391-402 with; half as many words ahead 393-403.  Smaller shapes, of which a unit holds two or more rows, are no faster by it, or slower.)
+// A wavefront fetches and reads its own words, so that nothing but the sums is shared.  Vector loads arrive in order: what is needed while the words are on their
+// way comes as scalars or ahead of them, and nothing but the row's own loads is waited for.
+template <bool FP32>
+__global__ __launch_bounds__(1024) void policy_long_rows_kernel(RowsArgs a) {
+    constexpr int NV = 16, LANES = 1024, kAhead = 9;
+    using Row = Held<FP32, LANES, NV, true>;
+    __shared__ i32x4 ahead[kAhead][LANES];
+    struct In {                          // what goes into a row's loss, as scalars
+        int64_t token;
+        PolicyIn p;
+        bool there;
+    };
+    const auto scalar = [](auto p, uint32_t row) {
+        using T = std::remove_cv_t<std::remove_pointer_t<decltype(p)>>;
+        return ((const __attribute__((address_space(4))) T*)(uintptr_t)p)[row];
+    };
+    const auto inputs = [&](uint32_t row) {
+        In in = {-1, {}, false};
+        if (row >= a.rows) return in;
+        in.token = scalar(a.tokens, row);
+        in.p.w = a.policy.in.weights ? scalar(a.policy.in.weights, row) : 1.0f;
+        in.p.advantage = scalar(a.policy.in.advantages, row);
+        in.p.old = a.policy.in.old_logprob ? scalar(a.policy.in.old_logprob, row) : 0.0f;
+        in.p.ref = a.policy.in.ref_logprob ? scalar(a.policy.in.ref_logprob, row) : 0.0f;
+        in.there = in.token >= 0 && in.p.w != 0.0f;
+        return in;
+    };
+    using Raw = std::conditional_t<FP32, uint32_t, uint16_t>;
+    const auto fetch = [&](uint32_t row) {
+        const char* x = row_of<FP32>(a.x, row);
+        Row next;
+        next.place(x, 0, a.x.vocab, (int)threadIdx.x);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(x + next.place_of(min(next.word(i), next.words - 1))),
+                                             (__attribute__((address_space(3))) void*)&ahead[i][next.wave], 16, 0, 2);
+    };
+    In in = inputs(blockIdx.x);
+    if (in.there) fetch(blockIdx.x);
+    int slot = 0;
+    for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const In next = inputs(row + gridDim.x);
+        char* dx = a.dx ? a.dx + (int64_t)row * a.dx_stride * (FP32 ? 4 : 2) : nullptr;
+        const char* x = row_of<FP32>(a.x, row);
+        Row h;
+        h.place(x, 0, a.x.vocab, (int)threadIdx.x);
+        float d = 0.0f, shift = 0.0f;
+        double logprob = 0.0;
+        PolicyRow p = {};
+        Sum s = {1.0, 0.0f};
+        if (in.there) {
+#pragma unroll
+            for (int i = kAhead; i < NV; ++i) h.template load_word<true>(i, x, h.raw[i]);
+            int32_t j;
+            const bool has_edge = h.edge_at(&j);
+            uint32_t edge = ((const Raw*)x)[has_edge ? j : 0], value = ((const Raw*)x)[in.token < a.x.vocab ? (int32_t)in.token : 0];
+            __builtin_amdgcn_s_waitcnt(0x0f70);                     // vmcnt(0): this row is there
+            asm volatile("" : "+v"(value), "+v"(edge)::"memory");
+            h.edge = has_edge ? __uint_as_float(FP32 ? edge : edge << 16) : minus_inf();
+            const float logit = in.token < a.x.vocab ? __uint_as_float(FP32 ? value : value << 16) : __builtin_nanf("");
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) h.raw[i] = ahead[i][threadIdx.x];
+            __builtin_amdgcn_s_waitcnt(0xc07f);                     // lgkmcnt(0): and read, before the next one takes its place
+            asm volatile("" ::: "memory");
+            if (next.there) fetch(row + gridDim.x);
+            s = join_waves<LANES / 64, true>(h.wave_part(a.c), a.c, slot);
+            slot ^= 1;
+            const RowLog l = row_log(s, logit, a.inv_t);
+            logprob = l.logprob;
+            p = policy_row(a.policy, in.p, l.logprob);
+            d = p.slope * a.scale;
+            shift = (float)(l.log_sum * kLog2e);
+        } else if (next.there) {
+            fetch(row + gridDim.x);
+        }
+        if (threadIdx.x == 0) {
+            if (a.logprob) a.logprob[row] = (float)logprob;
+            put_terms(a.policy, a.rows, row, p);
+        }
+        if (dx) {
+            if (d == 0.0f) h.store_zeros(dx);
+            else h.store_gradient(dx, token_in(in.token, a.x.vocab), d, base_of(s.most), a.c.high, shift);
+        }
+        in = next;
+    }
 }
 
 // Log-probabilities only, one workgroup of WAVES wavefronts to a row, through which the wavefronts go in turn.
@@ -709,6 +860,7 @@ bool holds_rows(int64_t rows, int64_t vocab, int dtype) {
     const int64_t n = words(vocab, dtype);
     return n <= 64 * 8 || (n <= 1024 * 16 && rows >= 128);
 }
+constexpr unsigned kUnits = 256;      // compute units
 constexpr int kStreamWaves = 8;
 bool streams_rows(int64_t rows, int64_t vocab) { return vocab <= 4096 || rows >= 512; }
 
@@ -730,7 +882,12 @@ int launch_parts(const PartsArgs& p, int dtype, int vecs, void* stream) {
 
 template <bool FP32>
 int launch_held(const RowsArgs& a, void* stream) {
-    with_held(words(a.x.vocab, FP32 ? FLASHOPTIM_FP32 : FLASHOPTIM_BF16), [&](auto shape) {
+    const int64_t n = words(a.x.vocab, FP32 ? FLASHOPTIM_FP32 : FLASHOPTIM_BF16);
+    if (n > 512 * 16 && a.rows >= 2 * kUnits) {
+        hipLaunchKernelGGL((policy_long_rows_kernel<FP32>), dim3(kUnits), dim3(1024), 0, (hipStream_t)stream, a);
+        return fo::hip_status(hipGetLastError());
+    }
+    with_held(n, [&](auto shape) {
         constexpr int L = decltype(shape)::kLanes, NV = decltype(shape)::kVecs, LINES = L < 256 ? 256 / L : 1;
         hipLaunchKernelGGL((policy_rows_kernel<FP32, L, NV>), dim3((unsigned)up(a.rows, LINES)), dim3(L * LINES), 0, (hipStream_t)stream, a);
     });
