@@ -855,14 +855,21 @@ void with_held(int64_t n, F launch) {
     else if (n <= 512 * 16) launch(Shape<512, 16>{});
     else launch(Shape<1024, 16>{});
 }
-// Whether a call holds whole rows: those of a wavefront always, longer ones, up to the largest shape's, where there are as many as fill half the chip.
+// Whether the policy loss holds whole rows, up to the largest shape's: short ones always (two launches against three, one row of 5000 BF16 values 7.5 us against 11.1,
+// 64 of 10000 8.6 against 11.2, of 32000 11.9 against 11.6), longer ones where there are as many as fill half the chip (128256 BF16 values, 100 rows 23.8 us against
+// 20.3 in parts, 128 rows 23.9 against 23.7).
+constexpr unsigned kUnits = 256;      // compute units
 bool holds_rows(int64_t rows, int64_t vocab, int dtype) {
     const int64_t n = words(vocab, dtype);
-    return n <= 64 * 8 || (n <= 1024 * 16 && rows >= 128);
+    return n <= 256 * 8 || (n <= 1024 * 16 && rows >= kUnits / 2);
 }
-constexpr unsigned kUnits = 256;      // compute units
-constexpr int kStreamWaves = 8;
-bool streams_rows(int64_t rows, int64_t vocab) { return vocab <= 4096 || rows >= 512; }
+// Whether log-probabilities take a row to a workgroup: short ones (one launch against two, 32000 BF16 values, one row 5.2 us against 7.2, 16 rows 5.9 against 6.3;
+// 50257 values, one row 7.1 against 6.7, 64 rows 8.3 against 7.3), and as many as there are compute units (256 rows of 128256 15.3 us against 19.1, 128 rows
+// 13.8 against 12.3).
+bool streams_rows(int64_t rows, int64_t vocab, int dtype) { return words(vocab, dtype) <= 4096 || rows >= kUnits; }
+// And by how many wavefronts: few rows by all that a workgroup may have (256 rows of 10000 BF16 values 6.1 -> 5.1 us, of 128256 17.6 -> 15.3), many, or rows of 512
+// words, by eight, so that a unit has several rows.
+int stream_waves(int64_t rows, int64_t vocab, int dtype) { return rows < 2 * kUnits && words(vocab, dtype) > 512 ? 16 : 8; }
 
 // A call's parts in its workspace.
 PartsArgs to_parts(const RowsArgs& a, const Parts& c, void* workspace) {
@@ -929,7 +936,7 @@ extern "C" {
 int64_t flashoptim_token_logprob_workspace(int64_t rows, int64_t vocab, int dtype) {
     if (!known(dtype)) return FLASHOPTIM_ERR_INVALID_ARG;
     FO_TRY(check_sizes(rows, vocab));
-    return rows == 0 || streams_rows(rows, vocab) ? 0 : parts_bytes(rows, vocab, dtype);
+    return rows == 0 || streams_rows(rows, vocab, dtype) ? 0 : parts_bytes(rows, vocab, dtype);
 }
 
 int flashoptim_token_logprob(const flashoptim_matrix* logits, const int64_t* tokens, float temperature, float* logprob, double* logprob64,
@@ -945,10 +952,15 @@ int flashoptim_token_logprob(const flashoptim_matrix* logits, const int64_t* tok
     a.logprob = logprob;
     a.wide = logprob64;
     a.lse = lse;
-    if (streams_rows(rows, logits->cols)) {
-        const dim3 grid(a.rows), block(kStreamWaves * 64);
-        if (logits->dtype == FLASHOPTIM_FP32) hipLaunchKernelGGL((logprob_rows_kernel<true, kStreamWaves>), grid, block, 0, (hipStream_t)stream, a);
-        else hipLaunchKernelGGL((logprob_rows_kernel<false, kStreamWaves>), grid, block, 0, (hipStream_t)stream, a);
+    if (streams_rows(rows, logits->cols, logits->dtype)) {
+        const auto launch = [&](auto fp32, auto waves) {
+            constexpr int W = decltype(waves)::value;
+            hipLaunchKernelGGL((logprob_rows_kernel<decltype(fp32)::value, W>), dim3(a.rows), dim3(W * 64), 0, (hipStream_t)stream, a);
+        };
+        const auto with = [&](auto fp32) {
+            if (stream_waves(rows, logits->cols, logits->dtype) == 16) launch(fp32, Int<16>{}); else launch(fp32, Int<8>{});
+        };
+        if (logits->dtype == FLASHOPTIM_FP32) with(std::true_type{}); else with(std::false_type{});
         return fo::hip_status(hipGetLastError());
     }
     const Parts c = cut_rows(rows, logits->cols, logits->dtype);
