@@ -524,6 +524,19 @@ int flashoptim_clip_factor_from_sum(flashoptim_clip_factor* factor, float max_no
 int flashoptim_clip_gradients(const flashoptim_gradient* grads, int64_t n_grads, int src_dtype, int dst_dtype,
                               const flashoptim_clip_factor* factor, void* stream);
 
+/* The steps above with the clipping in them: the gradients count times factor->scale (read on the device when the step runs), a product in FP32 that
+ * is not rounded to BF16, and are left as they are; nothing of theirs is read or written a second time.  With a scale of 1 the results are
+ * those of the step without; with a scale of NaN, that of gradients which are not finite, weights and states stay as they are (also the weight
+ * decay is left out), only the rates of a list's table change.  A list's tables are the same with and without. */
+int flashoptim_adamw_step_clipped(const flashoptim_tensor* tensors, int64_t n_tensors, const flashoptim_adamw_hp* hp,
+                                  const flashoptim_clip_factor* factor, void* stream);
+int flashoptim_adamw_step_exact_clipped(const flashoptim_tensor* tensors, int64_t n_tensors, const flashoptim_adamw_hp* hp,
+                                        const flashoptim_clip_factor* factor, void* stream);
+int flashoptim_sgd_step_clipped(const flashoptim_tensor* tensors, int64_t n_tensors, const flashoptim_sgd_hp* hp,
+                                const flashoptim_clip_factor* factor, void* stream);
+int flashoptim_lion_step_clipped(const flashoptim_tensor* tensors, int64_t n_tensors, const flashoptim_lion_hp* hp,
+                                 const flashoptim_clip_factor* factor, void* stream);
+
 /* ---- housekeeping --------------------------------------------------------------------
  * strerror: static string for a status.  last_hip_error: hipError_t value of the most recent
  * failed HIP call on this thread (0 if none).  release_cache: frees the cached device chunk

@@ -36,6 +36,7 @@ EXPORTED_SYMBOLS = [
     "flashoptim_token_logprob_workspace", "flashoptim_token_logprob", "flashoptim_token_logprob_backward",
     "flashoptim_policy_loss_workspace", "flashoptim_policy_loss", "flashoptim_preference_loss",
     "flashoptim_grad_norm_workspace", "flashoptim_grad_norm", "flashoptim_clip_factor_from_sum", "flashoptim_clip_gradients",
+    "flashoptim_adamw_step_clipped", "flashoptim_adamw_step_exact_clipped", "flashoptim_sgd_step_clipped", "flashoptim_lion_step_clipped",
 ]
 
 
@@ -173,6 +174,8 @@ def load_library():
     L.flashoptim_grad_norm.argtypes = [grads, i64, i32, C.c_float, vp, vp, i64, vp]
     L.flashoptim_clip_factor_from_sum.argtypes = [vp, C.c_float, vp]
     L.flashoptim_clip_gradients.argtypes = [grads, i64, i32, i32, vp, vp]
+    for name, hp in (("adamw_step", _AdamWHp), ("adamw_step_exact", _AdamWHp), ("sgd_step", _SgdHp), ("lion_step", _LionHp)):
+        getattr(L, f"flashoptim_{name}_clipped").argtypes = [C.POINTER(_Tensor), i64, C.POINTER(hp), vp, vp]
     L.flashoptim_strerror.argtypes = [i32]
     L.flashoptim_strerror.restype = C.c_char_p
     for name in EXPORTED_SYMBOLS:
@@ -365,15 +368,25 @@ def _as_list(tensors):
     return tensors if isinstance(tensors, TensorList) else TensorList(tensors)
 
 
-def adamw_step(tensors, beta1, beta2, eps, step, stream=None):
+def _clipped(name, tl, hp, clip, stream):
+    call = f"flashoptim_{name}_clipped"
+    _check(getattr(load_library(), call)(tl.array, tl.n, hp, clip.address, _stream_handle(stream)), call)
+
+
+def adamw_step(tensors, beta1, beta2, eps, step, stream=None, clip=None):
+    """`clip` (ClipFactor, here and in the steps below): the gradients count times its scale; NaN there leaves everything as it is."""
     tl = _as_list(tensors)
     hp = _AdamWHp(beta1, beta2, eps, int(step))
+    if clip is not None:
+        return _clipped("adamw_step", tl, hp, clip, stream)
     _check(load_library().flashoptim_adamw_step(tl.array, tl.n, hp, _stream_handle(stream)), "flashoptim_adamw_step")
 
 
-def adamw_step_exact(tensors, beta1, beta2, eps, step, stream=None):
+def adamw_step_exact(tensors, beta1, beta2, eps, step, stream=None, clip=None):
     tl = _as_list(tensors)
     hp = _AdamWHp(beta1, beta2, eps, int(step))
+    if clip is not None:
+        return _clipped("adamw_step_exact", tl, hp, clip, stream)
     _check(load_library().flashoptim_adamw_step_exact(tl.array, tl.n, hp, _stream_handle(stream)),
            "flashoptim_adamw_step_exact")
 
@@ -393,15 +406,19 @@ def shard_range(numel, world, rank):
     return int(begin.value), int(length.value)
 
 
-def sgd_step(tensors, momentum, stream=None):
+def sgd_step(tensors, momentum, stream=None, clip=None):
     tl = _as_list(tensors)
     hp = _SgdHp(momentum)
+    if clip is not None:
+        return _clipped("sgd_step", tl, hp, clip, stream)
     _check(load_library().flashoptim_sgd_step(tl.array, tl.n, hp, _stream_handle(stream)), "flashoptim_sgd_step")
 
 
-def lion_step(tensors, beta1, beta2, stream=None):
+def lion_step(tensors, beta1, beta2, stream=None, clip=None):
     tl = _as_list(tensors)
     hp = _LionHp(beta1, beta2)
+    if clip is not None:
+        return _clipped("lion_step", tl, hp, clip, stream)
     _check(load_library().flashoptim_lion_step(tl.array, tl.n, hp, _stream_handle(stream)), "flashoptim_lion_step")
 
 

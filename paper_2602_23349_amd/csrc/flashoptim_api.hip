@@ -348,21 +348,21 @@ enum LiveOp { kOpStep = 0, kOpCompress = 1, kOpDecompress = 2, kOpProbe = 3, kOp
 constexpr int32_t kOpPack = 5, kOpUnpack = 6;
 
 hipError_t launch_segment(LiveOp op, int kind, bool direct, bool split, bool quant, fo::StepShape shape, const StepArgs& a,
-                          int64_t blocks, hipStream_t stream) {
+                          int64_t blocks, const float* scale, hipStream_t stream) {
     if (op == kOpStep || op == kOpStepExact)
-        return fo::launch_step(kind, direct, split, quant, shape, op == kOpStepExact, a, blocks, stream);
+        return fo::launch_step(kind, direct, split, quant, shape, op == kOpStepExact, a, blocks, scale, stream);
     if (op == kOpProbe) return fo::launch_probe(kind, direct, shape, a, blocks, stream);
     return fo::launch_convert(kind == FLASHOPTIM_ADAMW, op == kOpCompress, direct, a, blocks, stream);
 }
 
 // The workgroups 0 .. blocks-1 of one logical launch (each handles `tile_elems` elements), issued as
-// back-to-back launches on the same stream, each covering at most kSegmentElems elements.
+// back-to-back launches on the same stream, each covering at most kSegmentElems elements.  scale: a clipped step's word.
 hipError_t launch_op(LiveOp op, int kind, bool direct, bool split, bool quant, fo::StepShape shape, StepArgs a, int64_t blocks,
-                     int64_t tile_elems, hipStream_t stream) {
+                     int64_t tile_elems, hipStream_t stream, const float* scale = nullptr) {
     const auto launch_part = [&](int64_t first, int64_t n, bool through) {
         a.block_offset = (uint32_t)first;
         a.through = through;
-        return launch_segment(op, kind, direct, split, quant, shape, a, n, stream);
+        return launch_segment(op, kind, direct, split, quant, shape, a, n, scale, stream);
     };
     if (op != kOpCompress && op != kOpDecompress) return fo::for_each_step_segment(kind, split, quant, blocks, tile_elems, launch_part);
     return fo::for_each_segment(blocks, tile_elems, [&](int64_t first, int64_t n) { return launch_part(first, n, a.through); });
@@ -370,7 +370,7 @@ hipError_t launch_op(LiveOp op, int kind, bool direct, bool split, bool quant, f
 
 // Launches one operation over the live tensors (already validated and converted).
 int launch_live(int kind, bool split, bool quant, std::vector<TensorDev>& live, const StepConsts& c,
-                hipStream_t stream, LiveOp op = kOpStep, const float* sqrt_min_word = nullptr) {
+                hipStream_t stream, LiveOp op = kOpStep, const float* sqrt_min_word = nullptr, const float* scale = nullptr) {
     if (live.empty()) return FLASHOPTIM_OK;
     StepArgs a;
     std::memset(&a, 0, sizeof(a));
@@ -397,7 +397,7 @@ int launch_live(int kind, bool split, bool quant, std::vector<TensorDev>& live, 
     if (live.size() == 1) {
         // gradient-release call: no table, no allocation, no lock
         a.single = live[0];
-        FO_HIP(launch_op(op, kind, true, split, quant, shape, a, total_chunks, ce, stream));
+        FO_HIP(launch_op(op, kind, true, split, quant, shape, a, total_chunks, ce, stream, scale));
         return FLASHOPTIM_OK;
     }
 
@@ -438,7 +438,7 @@ int launch_live(int kind, bool split, bool quant, std::vector<TensorDev>& live, 
     a.tensors = static_cast<TensorDev*>(plan->d_table);
     a.coarse = static_cast<const uint32_t*>(plan->d_index);
     a.coarse_shift = shift;
-    const hipError_t e = launch_op(op, kind, false, split, quant, shape, a, plan->n_chunks, ce, stream);
+    const hipError_t e = launch_op(op, kind, false, split, quant, shape, a, plan->n_chunks, ce, stream, scale);
     if (e != hipSuccess) plan->table_known = false;        // the launches that were accepted may have written a rate
     FO_HIP(e);
     return FLASHOPTIM_OK;
@@ -526,7 +526,7 @@ void set_ranges(StepConsts& c) {
 }
 
 int run_step(int kind, const flashoptim_tensor* tensors, int64_t n_tensors, const StepConsts& c, void* stream_,
-             LiveOp op = kOpStep) {
+             LiveOp op = kOpStep, const flashoptim_clip_factor* factor = nullptr) {
     const bool has_v = (kind == FLASHOPTIM_ADAMW);
     int rc = validate_tensors(tensors, n_tensors, has_v);
     if (rc != FLASHOPTIM_OK) return rc;
@@ -546,7 +546,14 @@ int run_step(int kind, const flashoptim_tensor* tensors, int64_t n_tensors, cons
         if (rc != FLASHOPTIM_OK) return rc;
         set_ranges(cc);
     }
-    return launch_live(kind, true, true, live, cc, static_cast<hipStream_t>(stream_), op, word);
+    return launch_live(kind, true, true, live, cc, static_cast<hipStream_t>(stream_), op, word, factor ? &factor->scale : nullptr);
+}
+
+int run_clipped(int kind, const flashoptim_tensor* tensors, int64_t n_tensors, const StepConsts& c, const flashoptim_clip_factor* factor,
+                void* stream, LiveOp op = kOpStep) {
+    if (!factor) return FLASHOPTIM_ERR_INVALID_ARG;
+    if (!aligned16(factor)) return FLASHOPTIM_ERR_MISALIGNED;
+    return run_step(kind, tensors, n_tensors, c, stream, op, factor);
 }
 
 // Conversion between the FP32 state and the compressed layout: every buffer of both layouts is needed.
@@ -986,6 +993,34 @@ int flashoptim_lion_step(const flashoptim_tensor* tensors, int64_t n_tensors, co
     StepConsts c;
     if (!lion_consts(hp, c)) return FLASHOPTIM_ERR_INVALID_ARG;
     return run_step(FLASHOPTIM_LION, tensors, n_tensors, c, stream);
+}
+
+int flashoptim_adamw_step_clipped(const flashoptim_tensor* tensors, int64_t n_tensors, const flashoptim_adamw_hp* hp,
+                                  const flashoptim_clip_factor* factor, void* stream) {
+    StepConsts c;
+    if (!adamw_consts(hp, c)) return FLASHOPTIM_ERR_INVALID_ARG;
+    return run_clipped(FLASHOPTIM_ADAMW, tensors, n_tensors, c, factor, stream);
+}
+
+int flashoptim_adamw_step_exact_clipped(const flashoptim_tensor* tensors, int64_t n_tensors, const flashoptim_adamw_hp* hp,
+                                        const flashoptim_clip_factor* factor, void* stream) {
+    StepConsts c;
+    if (!adamw_consts(hp, c)) return FLASHOPTIM_ERR_INVALID_ARG;
+    return run_clipped(FLASHOPTIM_ADAMW, tensors, n_tensors, c, factor, stream, kOpStepExact);
+}
+
+int flashoptim_sgd_step_clipped(const flashoptim_tensor* tensors, int64_t n_tensors, const flashoptim_sgd_hp* hp,
+                                const flashoptim_clip_factor* factor, void* stream) {
+    StepConsts c;
+    if (!sgd_consts(hp, c)) return FLASHOPTIM_ERR_INVALID_ARG;
+    return run_clipped(FLASHOPTIM_SGD, tensors, n_tensors, c, factor, stream);
+}
+
+int flashoptim_lion_step_clipped(const flashoptim_tensor* tensors, int64_t n_tensors, const flashoptim_lion_hp* hp,
+                                 const flashoptim_clip_factor* factor, void* stream) {
+    StepConsts c;
+    if (!lion_consts(hp, c)) return FLASHOPTIM_ERR_INVALID_ARG;
+    return run_clipped(FLASHOPTIM_LION, tensors, n_tensors, c, factor, stream);
 }
 
 int flashoptim_adamw_step_ex(const flashoptim_tensor_ex* tensors, int64_t n_tensors, const flashoptim_adamw_hp* hp,

@@ -254,7 +254,7 @@ struct CheckedCopyArgs : CopyArgs {
 };
 
 hipError_t launch_step(int kind, bool direct, bool split, bool quant, StepShape shape, bool exact, const StepArgs& a,
-                       int64_t n_blocks, hipStream_t s);
+                       int64_t n_blocks, const float* scale, hipStream_t s);
 // Lanes per workgroup and elements per tile of the layout conversions.  Compressing stages nothing: calls whose stores go
 // through take single wavefronts (GPT-2 344.8 -> 322.6 us, 300 M elements 816 -> 777, 25 M 70.0 -> 69.8);
 // smaller ones 256 lanes (5 M 15.0 us, as single wavefronts 15.5).  Decompressing takes 256 (GPT-2 340.0 us, 128 lanes 343.9, single

@@ -731,9 +731,10 @@ __device__ __forceinline__ void master_weights(const LaneIO<VEC>& x, const StepT
 // the scales included, is exact in both modes.
 // M_HAT (AdamW only): the momentum's bias correction is not 1; otherwise (from step 165 on with beta1 = 0.9) m_hat = m_t.
 // cnt: the elements of the lane that exist (VEC where FULL).
-template <int KIND, int VEC, bool SPLIT, bool QUANT, bool EXACT, bool M_HAT, bool FULL>
+// CLIP: the gradients count times `scale`, a product that is rounded to FP32 only.
+template <int KIND, int VEC, bool SPLIT, bool QUANT, bool EXACT, bool M_HAT, bool FULL, bool CLIP = false>
 __device__ __forceinline__ void update_lane(const LaneIO<VEC>& x, LaneIO<VEC>& y, const StepTables& tab,
-                                            const StepConsts& c, float lr, float wd, int cnt) {
+                                            const StepConsts& c, float lr, float wd, int cnt, float scale = 1.0f) {
     constexpr bool HAS_V = (KIND == 0);
     const float s_m = QUANT ? (float)__builtin_bit_cast(_Float16, (uint16_t)x.ms) : 0.0f;
     const float s_v = (QUANT && HAS_V) ? (float)__builtin_bit_cast(_Float16, (uint16_t)x.vs) : 0.0f;
@@ -750,7 +751,7 @@ __device__ __forceinline__ void update_lane(const LaneIO<VEC>& x, LaneIO<VEC>& y
     master_weights<VEC, SPLIT>(x, tab, th);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
-        const float g = bf16_of(x.g, i);
+        const float g = CLIP ? bf16_of(x.g, i) * scale : bf16_of(x.g, i);
         float m;
         if (QUANT) m = tab.m[(x.mq[i >> 2] >> (8 * (i & 3))) & 0xffu] * s_m;       // Q_m^-1
         else m = x.m32[i];
@@ -984,6 +985,14 @@ template <int KIND, bool DIRECT, bool M_HAT, bool THROUGH>
 struct VariantArgs : TensorArgs<DIRECT, KIND == 0>, KindConsts<KIND> {
     explicit VariantArgs(const StepArgs& a) : TensorArgs<DIRECT, KIND == 0>(a.single), KindConsts<KIND>(a) {}
 };
+// A clipped step's: the word that holds the factor of the gradients.  NaN: the step leaves weights and states as they are.  (Without and with it, us: AdamW on
+// GPT-2's list 244.3 and 245.3, on a Llama layer 427 and 430, Lion 189.0 and 188.6, 334 and 336; gradients clipped in place ahead of the step instead 334 and
+// 575, 280 and 477.)
+template <int KIND, bool DIRECT, bool M_HAT, bool THROUGH>
+struct ClippedArgs : VariantArgs<KIND, DIRECT, M_HAT, THROUGH> {
+    const float* scale;
+    ClippedArgs(const StepArgs& a, const float* s) : VariantArgs<KIND, DIRECT, M_HAT, THROUGH>(a), scale(s) {}
+};
 // The first arguments.  Of one tensor, the arrays that the variant has, the element count (low half, high half) and the first
 // workgroup's tile; of a list, p0 the table, p1 the coarse table, u0 its shift, u1 and u3 what makes the rate (StepArgs).
 struct HotArgs {
@@ -1011,9 +1020,10 @@ __device__ __forceinline__ int64_t wave_start(int64_t tile, int64_t numel) {
 // tensor but possibly its last); the code then has no per-lane case distinction at all.
 // (Variants in which a workgroup loads two or four such tiles up front and then updates them in
 // turn - fewer look-ups, more bytes in flight per workgroup - ran at the same rate.)
-template <int KIND, int VEC, int THREADS, bool SPLIT, bool QUANT, bool EXACT, bool M_HAT, bool THROUGH, bool FULL>
+template <int KIND, int VEC, int THREADS, bool SPLIT, bool QUANT, bool EXACT, bool M_HAT, bool THROUGH, bool FULL, bool CLIP>
 __device__ __forceinline__ void step_tile(const TensorDev& T, const KindConsts<KIND>& consts, StepTables& tab,
-                                          const TableEntries& entries, int64_t tile0, uint32_t lane_el, int rem, int tid) {
+                                          const TableEntries& entries, int64_t tile0, uint32_t lane_el, int rem, int tid,
+                                          const float* scale_word) {
     constexpr bool HAS_V = (KIND == 0);
     const bool leader = (tid & (kGroup / VEC - 1)) == 0;
     // the number of them that fall to this lane
@@ -1027,9 +1037,12 @@ __device__ __forceinline__ void step_tile(const TensorDev& T, const KindConsts<K
         __syncthreads();
     }
     const StepConsts c = consts.get();       // (behind the streaming loads)
+    float scale = 1.0f;
+    if constexpr (CLIP) scale = *(const __attribute__((address_space(4))) float*)scale_word;
     // All lanes of a group run the update together (a lane with cnt == 0 may share its group
     // with lanes that hold elements); lanes past the end compute on zeros and store nothing.
-    update_lane<KIND, VEC, SPLIT, QUANT, EXACT, M_HAT, FULL>(x, y, tab, c, T.lr, T.wd, cnt);
+    update_lane<KIND, VEC, SPLIT, QUANT, EXACT, M_HAT, FULL, CLIP>(x, y, tab, c, T.lr, T.wd, cnt, scale);
+    if (CLIP && scale != scale) return;
     if (FULL || cnt == VEC) store_full<VEC, HAS_V, SPLIT, QUANT, THROUGH>(y, T, tile0, lane_el, leader);
     else store_tail<VEC, HAS_V, SPLIT, QUANT>(y, T, tile0 + lane_el, cnt, leader);
 }
@@ -1038,8 +1051,9 @@ __device__ __forceinline__ void step_tile(const TensorDev& T, const KindConsts<K
 // over many tiles were measured 10 % slower: an iteration's loads then wait behind the previous
 // iteration's stores).  Order of issue: decode-table loads, the (tensor, tile) look-up, the
 // streaming loads; then the tables go to LDS.
-template <int KIND, int VEC, int THREADS, bool DIRECT, bool SPLIT, bool QUANT, bool EXACT, bool M_HAT, bool THROUGH>
-__device__ __forceinline__ void step_workgroup(const HotArgs& h, const VariantArgs<KIND, DIRECT, M_HAT, THROUGH>& a) {
+template <int KIND, int VEC, int THREADS, bool DIRECT, bool SPLIT, bool QUANT, bool EXACT, bool M_HAT, bool THROUGH, bool CLIP>
+__device__ __forceinline__ void step_workgroup(const HotArgs& h, const VariantArgs<KIND, DIRECT, M_HAT, THROUGH>& a,
+                                               const float* scale_word) {
     constexpr int kTile = THREADS * VEC;       // elements per workgroup
     __shared__ StepTables tab;
     const int tid = (int)threadIdx.x;
@@ -1076,11 +1090,12 @@ __device__ __forceinline__ void step_workgroup(const HotArgs& h, const VariantAr
     const float table_lr = T.lr;
     if (!DIRECT) T.lr = u2f((f2u(table_lr) & h.u1) | h.u3);    // (integers: stays on the scalar unit)
     if (rem >= kTile) {
-        step_tile<KIND, VEC, THREADS, SPLIT, QUANT, EXACT, M_HAT, THROUGH, true>(T, a, tab, entries, tile0, lane_el, kTile, tid);
+        step_tile<KIND, VEC, THREADS, SPLIT, QUANT, EXACT, M_HAT, THROUGH, true, CLIP>(T, a, tab, entries, tile0, lane_el, kTile, tid,
+                                                                                       scale_word);
     } else {
         // (less than a tile, so within an int; negative for a wavefront behind the tensor's end)
-        step_tile<KIND, VEC, THREADS, SPLIT, QUANT, EXACT, M_HAT, THROUGH, false>(T, a, tab, entries, tile0, lane_el,
-                                                                                  (int)(T.numel - tile0), tid);
+        step_tile<KIND, VEC, THREADS, SPLIT, QUANT, EXACT, M_HAT, THROUGH, false, CLIP>(T, a, tab, entries, tile0, lane_el,
+                                                                                        (int)(T.numel - tile0), tid, scale_word);
     }
     // (only with a mask of 0: no workgroup of this launch uses what the others read of the entry's rate)
     if (!DIRECT && chunk == 0 && f2u(T.lr) != f2u(table_lr) && tid == 0) entry->lr = T.lr;
@@ -1092,7 +1107,14 @@ __device__ __forceinline__ void step_workgroup(const HotArgs& h, const VariantAr
                                                            const void* p4, uint32_t u0, uint32_t u1, uint32_t block_offset, \
                                                            uint32_t u3, VariantArgs<KIND, DIRECT, M_HAT, THROUGH> a) {      \
         const HotArgs h = {p0, p1, p2, p3, p4, u0, u1, block_offset, u3};                                                   \
-        step_workgroup<KIND, VEC, THREADS, DIRECT, SPLIT, QUANT, EXACT, M_HAT, THROUGH>(h, a);                              \
+        step_workgroup<KIND, VEC, THREADS, DIRECT, SPLIT, QUANT, EXACT, M_HAT, THROUGH, false>(h, a, nullptr);              \
+    }                                                                                                                       \
+    template <int KIND, int VEC, int THREADS, bool DIRECT, bool SPLIT, bool QUANT, bool EXACT>                              \
+    __global__ __launch_bounds__(THREADS) void step_kernel(const void* p0, const void* p1, const void* p2, const void* p3,  \
+                                                           const void* p4, uint32_t u0, uint32_t u1, uint32_t block_offset, \
+                                                           uint32_t u3, ClippedArgs<KIND, DIRECT, M_HAT, THROUGH> a) {      \
+        const HotArgs h = {p0, p1, p2, p3, p4, u0, u1, block_offset, u3};                                                   \
+        step_workgroup<KIND, VEC, THREADS, DIRECT, SPLIT, QUANT, EXACT, M_HAT, THROUGH, true>(h, a, a.scale);               \
     }
 FO_STEP_KERNEL(true, true)
 FO_STEP_KERNEL(true, false)
@@ -1101,63 +1123,70 @@ FO_STEP_KERNEL(false, false)
 #undef FO_STEP_KERNEL
 
 template <int KIND, bool SPLIT, bool QUANT, bool EXACT, StepShape SHAPE, bool M_HAT, bool THROUGH, bool DIRECT>
-static hipError_t launch_direct(const StepArgs& a, unsigned n_blocks, unsigned lds, hipStream_t s) {
+static hipError_t launch_direct(const StepArgs& a, unsigned n_blocks, unsigned lds, const float* scale, hipStream_t s) {
     constexpr int VEC = step_vec(SPLIT, QUANT, SHAPE), THREADS = step_threads(SPLIT, QUANT, SHAPE);
-    typedef VariantArgs<KIND, DIRECT, M_HAT, THROUGH> args_t;
-    void (*kernel)(const void*, const void*, const void*, const void*, const void*, uint32_t, uint32_t, uint32_t, uint32_t, args_t) =
-        step_kernel<KIND, VEC, THREADS, DIRECT, SPLIT, QUANT, EXACT>;
     const HotArgs h = hot_args<DIRECT, SPLIT, QUANT>(a);
-    return launch(kernel, n_blocks, THREADS, lds, s, h.p0, h.p1, h.p2, h.p3, h.p4, h.u0, h.u1, h.block_offset, h.u3, args_t(a));
+    const auto with = [&](const auto& args) {
+        typedef std::remove_cv_t<std::remove_reference_t<decltype(args)>> args_t;
+        void (*kernel)(const void*, const void*, const void*, const void*, const void*, uint32_t, uint32_t, uint32_t, uint32_t, args_t) =
+            step_kernel<KIND, VEC, THREADS, DIRECT, SPLIT, QUANT, EXACT>;
+        return launch(kernel, n_blocks, THREADS, lds, s, h.p0, h.p1, h.p2, h.p3, h.p4, h.u0, h.u1, h.block_offset, h.u3, args);
+    };
+    if constexpr (SPLIT && QUANT) {
+        if (scale) return with(ClippedArgs<KIND, DIRECT, M_HAT, THROUGH>(a, scale));
+    }
+    return with(VariantArgs<KIND, DIRECT, M_HAT, THROUGH>(a));
 }
 template <int KIND, bool SPLIT, bool QUANT, bool EXACT, StepShape SHAPE, bool M_HAT, bool THROUGH>
-static hipError_t launch_through(bool direct, const StepArgs& a, int64_t n_blocks, hipStream_t s) {
+static hipError_t launch_through(bool direct, const StepArgs& a, int64_t n_blocks, const float* scale, hipStream_t s) {
     const int resident = step_resident(KIND, SPLIT, QUANT, SHAPE, direct, n_blocks * chunk_elems(SPLIT, QUANT, SHAPE), THROUGH);
     const unsigned lds = lds_to_hold(resident, SPLIT || QUANT ? sizeof(StepTables) : 0);
-    return direct ? launch_direct<KIND, SPLIT, QUANT, EXACT, SHAPE, M_HAT, THROUGH, true>(a, (unsigned)n_blocks, lds, s)
-                  : launch_direct<KIND, SPLIT, QUANT, EXACT, SHAPE, M_HAT, THROUGH, false>(a, (unsigned)n_blocks, lds, s);
+    return direct ? launch_direct<KIND, SPLIT, QUANT, EXACT, SHAPE, M_HAT, THROUGH, true>(a, (unsigned)n_blocks, lds, scale, s)
+                  : launch_direct<KIND, SPLIT, QUANT, EXACT, SHAPE, M_HAT, THROUGH, false>(a, (unsigned)n_blocks, lds, scale, s);
 }
 template <int KIND, bool SPLIT, bool QUANT, bool EXACT, StepShape SHAPE, bool M_HAT>
-static hipError_t launch_m_hat(bool direct, const StepArgs& a, int64_t n_blocks, hipStream_t s) {
+static hipError_t launch_m_hat(bool direct, const StepArgs& a, int64_t n_blocks, const float* scale, hipStream_t s) {
     if constexpr (SHAPE != StepShape::kSmall) {
-        if (a.through) return launch_through<KIND, SPLIT, QUANT, EXACT, SHAPE, M_HAT, true>(direct, a, n_blocks, s);
+        if (a.through) return launch_through<KIND, SPLIT, QUANT, EXACT, SHAPE, M_HAT, true>(direct, a, n_blocks, scale, s);
     }
-    return launch_through<KIND, SPLIT, QUANT, EXACT, SHAPE, M_HAT, false>(direct, a, n_blocks, s);
+    return launch_through<KIND, SPLIT, QUANT, EXACT, SHAPE, M_HAT, false>(direct, a, n_blocks, scale, s);
 }
 template <int KIND, bool SPLIT, bool QUANT, bool EXACT, StepShape SHAPE>
-static hipError_t launch_variant(bool direct, const StepArgs& a, int64_t n_blocks, hipStream_t s) {
+static hipError_t launch_variant(bool direct, const StepArgs& a, int64_t n_blocks, const float* scale, hipStream_t s) {
     if constexpr (KIND == 0) {
-        if (a.c.rbc1 != 1.0f) return launch_m_hat<KIND, SPLIT, QUANT, EXACT, SHAPE, true>(direct, a, n_blocks, s);
+        if (a.c.rbc1 != 1.0f) return launch_m_hat<KIND, SPLIT, QUANT, EXACT, SHAPE, true>(direct, a, n_blocks, scale, s);
     }
-    return launch_m_hat<KIND, SPLIT, QUANT, EXACT, SHAPE, false>(direct, a, n_blocks, s);
+    return launch_m_hat<KIND, SPLIT, QUANT, EXACT, SHAPE, false>(direct, a, n_blocks, scale, s);
 }
 
 template <int KIND, bool EXACT>
-static hipError_t launch_packed(bool direct, StepShape shape, const StepArgs& a, int64_t n_blocks, hipStream_t s) {
-    if (shape == StepShape::kSmall) return launch_variant<KIND, true, true, EXACT, StepShape::kSmall>(direct, a, n_blocks, s);
+static hipError_t launch_packed(bool direct, StepShape shape, const StepArgs& a, int64_t n_blocks, const float* scale, hipStream_t s) {
+    if (shape == StepShape::kSmall) return launch_variant<KIND, true, true, EXACT, StepShape::kSmall>(direct, a, n_blocks, scale, s);
     if constexpr (KIND != 0) {
-        if (shape == StepShape::kWide) return launch_variant<KIND, true, true, EXACT, StepShape::kWide>(direct, a, n_blocks, s);
+        if (shape == StepShape::kWide) return launch_variant<KIND, true, true, EXACT, StepShape::kWide>(direct, a, n_blocks, scale, s);
     }
-    return launch_variant<KIND, true, true, EXACT, StepShape::kUsual>(direct, a, n_blocks, s);
+    return launch_variant<KIND, true, true, EXACT, StepShape::kUsual>(direct, a, n_blocks, scale, s);
 }
 
 template <int KIND>
 static hipError_t launch_kind(bool direct, bool split, bool quant, StepShape shape, const StepArgs& a, int64_t n_blocks,
-                              hipStream_t s) {
-    if (split && quant) return launch_packed<KIND, true>(direct, shape, a, n_blocks, s);
-    if (split) return launch_variant<KIND, true, false, true, StepShape::kUsual>(direct, a, n_blocks, s);
-    if (quant) return launch_variant<KIND, false, true, true, StepShape::kUsual>(direct, a, n_blocks, s);
-    return launch_variant<KIND, false, false, true, StepShape::kUsual>(direct, a, n_blocks, s);
+                              const float* scale, hipStream_t s) {
+    if (split && quant) return launch_packed<KIND, true>(direct, shape, a, n_blocks, scale, s);
+    if (split) return launch_variant<KIND, true, false, true, StepShape::kUsual>(direct, a, n_blocks, scale, s);
+    if (quant) return launch_variant<KIND, false, true, true, StepShape::kUsual>(direct, a, n_blocks, scale, s);
+    return launch_variant<KIND, false, false, true, StepShape::kUsual>(direct, a, n_blocks, scale, s);
 }
 
 // exact = false selects the faithful division; it exists for AdamW in the compressed
-// layout only (SGD and Lion have neither operation; the ablation variants are always exact).
+// layout only (SGD and Lion have neither operation; the ablation variants are always exact).  scale: nullptr, or a clipped step's word,
+// in the compressed layout only.
 hipError_t launch_step(int kind, bool direct, bool split, bool quant, StepShape shape, bool exact, const StepArgs& a,
-                       int64_t n_blocks, hipStream_t s) {
+                       int64_t n_blocks, const float* scale, hipStream_t s) {
     if (kind == 0 && !a.sqrt_min_word) return hipErrorInvalidValue;     // the AdamW kernels dereference it
-    if (kind == 0 && split && quant && !exact) return launch_packed<0, false>(direct, shape, a, n_blocks, s);
-    if (kind == 0) return launch_kind<0>(direct, split, quant, shape, a, n_blocks, s);
-    if (kind == 1) return launch_kind<1>(direct, split, quant, shape, a, n_blocks, s);
-    return launch_kind<2>(direct, split, quant, shape, a, n_blocks, s);
+    if (kind == 0 && split && quant && !exact) return launch_packed<0, false>(direct, shape, a, n_blocks, scale, s);
+    if (kind == 0) return launch_kind<0>(direct, split, quant, shape, a, n_blocks, scale, s);
+    if (kind == 1) return launch_kind<1>(direct, split, quant, shape, a, n_blocks, scale, s);
+    return launch_kind<2>(direct, split, quant, shape, a, n_blocks, scale, s);
 }
 
 // ------------------------------------------------------------- stream probe --
