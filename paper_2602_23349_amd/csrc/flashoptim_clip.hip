@@ -66,7 +66,7 @@ __device__ __forceinline__ float value_at(const void* p, int64_t at) {
 template <int THREADS>
 __device__ __forceinline__ double group_sum(double s) {
     __shared__ double part[THREADS / 64];
-    for (int off = 32; off > 0; off >>= 1) s += __shfl_down(s, off);
+    s = fo::sum_of_wave(s);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
     __syncthreads();
     s = 0.0;

@@ -21,6 +21,7 @@ namespace {
 using fo::f32x4;
 using fo::i32x4;
 using fo::load_as;
+using fo::sum_of_wave;
 using fo::up;
 using f32x8 = float __attribute__((ext_vector_type(8)));
 using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
@@ -75,10 +76,6 @@ __device__ __forceinline__ float wave_max(float v) {
     v = max_with<0x142, 0xa>(v);         // row_bcast 15, into the second and the fourth row
     v = max_with<0x143, 0xc>(v);         // row_bcast 31, into the upper half
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
-}
-__device__ __forceinline__ double wave_sum(double v) {
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
-    return v;
 }
 
 // log2(e) / T as the FP32 value below it and what that is short of it.  (The first alone is off by up to 2^-23, which goes into the log-probabilities of a
@@ -214,7 +211,7 @@ struct Held {
                 sum += eight;
             }
         }
-        return {wave_sum(near + (double)sum), most};
+        return {sum_of_wave(near + (double)sum), most};
     }
     // Stores -d p, or d (1 - p) for the token, of all that is held: p = 2^((x - base) c - shift).
     __device__ __forceinline__ void store_gradient(char* row, int32_t token, float d, float base, float c, float shift) {
@@ -576,7 +573,7 @@ __device__ __forceinline__ Sum join_parts(const PartsArgs& a, uint32_t row) {
     Sum s = {0.0, minus_inf()};
     for (uint32_t i = threadIdx.x & 63; i < a.parts; i += 64) s = join(s, parts[i], a.r.c);
     const float most = wave_max(s.most);
-    return {wave_sum(s.sum * (double)exp2_of(times(s.most - base_of(most), a.r.c))), most};
+    return {sum_of_wave(s.sum * (double)exp2_of(times(s.most - base_of(most), a.r.c))), most};
 }
 
 constexpr int kJoinRows = 4;
@@ -666,9 +663,8 @@ __global__ __launch_bounds__(kPairThreads) void policy_stats_kernel(const double
 #pragma unroll
             for (int k = 0; k < 3; ++k) s[k] += v[u][k];
     }
-    for (int off = 32; off > 0; off >>= 1)
 #pragma unroll
-        for (int k = 0; k < 3; ++k) s[k] += __shfl_xor(s[k], off);
+    for (int k = 0; k < 3; ++k) s[k] = sum_of_wave(s[k]);
     if ((threadIdx.x & 63) < 3) part[threadIdx.x & 63][threadIdx.x >> 6] = (threadIdx.x & 63) == 0 ? s[0] : (threadIdx.x & 63) == 1 ? s[1] : s[2];
     __syncthreads();
     if (threadIdx.x != 0) return;
@@ -754,7 +750,7 @@ __global__ __launch_bounds__(kPairThreads) void preference_kernel(PairArgs a, in
                     gain += k ? -d : d;
                 }
         }
-        gain = wave_sum(gain);
+        gain = sum_of_wave(gain);
         if (waves > 1) {
             __syncthreads();
             if ((threadIdx.x & 63) == 0) gains[wave] = gain;
