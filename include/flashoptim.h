@@ -434,7 +434,7 @@ int flashoptim_block_norm_backward(const flashoptim_block_norm_spec* spec, const
  * makes its row's logprob and gradients NaN, and so the loss.  So does a row that holds a NaN or +infinity, or nothing but -infinity
  * (whose lse is -infinity); a -infinity beside other values has the probability 0.  Sums over a row are FP32 by lane and FP64 where lanes
  * join, what is computed once for a row is FP64; the order of all sums depends on the sizes alone.  Vectors are contiguous FP32.
- *   1 <= vocab < 2^30 unless rows = 0; rows < 2^22, and fewer than 2^24 parts of 16384 BF16 or 8192 FP32 values; T > 0 and finite.
+ *   1 <= vocab < 2^30 unless rows = 0; rows < 2^22, and fewer than 2^24 parts of 4096 BF16 or 2048 FP32 values; T > 0 and finite.
  * token_logprob: logprob, lse [rows] and logprob64 [rows], the same as logprob in FP64, for the difference of long sums that a preference
  *   loss is made of.  Each may be NULL (not all, unless rows = 0).
  * token_logprob_backward: dlogits_ij = dlogprob_i / T ([j = t] - exp(logits_ij / T - lse_i)), of the type of logits, from the lse that the forward

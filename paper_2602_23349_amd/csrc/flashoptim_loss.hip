@@ -540,7 +540,7 @@ __global__ __launch_bounds__(WAVES * 64) void logprob_rows_kernel(RowsArgs a) {
 }
 
 // ---- few rows, or rows that do not fit: each cut into parts, a workgroup to each, which leaves its sum; whoever needs a row's joins them.
-constexpr int kPartThreads = 256;
+constexpr int kPartThreads = 256, kPartWords = 2;      // lanes, and words of a lane
 struct PartsArgs {
     RowsArgs r;
     Sum* sums;               // [rows, parts]
@@ -552,15 +552,15 @@ __device__ __forceinline__ bool counts(const PartsArgs& a, uint32_t row, int64_t
     return token >= 0 && *w != 0.0f;
 }
 
-template <bool FP32, int NV>
+template <bool FP32>
 __global__ __launch_bounds__(kPartThreads) void parts_kernel(PartsArgs a) {
     const uint32_t row = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
     const int64_t token = a.r.tokens[row];
     float w;
     if (!counts(a, row, token, &w)) return;
     const char* x = row_of<FP32>(a.r.x, row);
-    Held<FP32, kPartThreads, NV> h;
-    h.place(x, (int32_t)part * (kPartThreads * NV), a.r.x.vocab, (int)threadIdx.x);
+    Held<FP32, kPartThreads, kPartWords> h;
+    h.place(x, (int32_t)part * (kPartThreads * kPartWords), a.r.x.vocab, (int)threadIdx.x);
     h.template load<false>(x);       // (the gradient reads it again)
     if (part == 0 && threadIdx.x == 0) a.logits[row] = logit_of<FP32>(x, token, a.r.x.vocab);
     const Sum s = join_waves<kPartThreads / 64>(h.wave_part(a.r.c), a.r.c);
@@ -589,7 +589,7 @@ __global__ __launch_bounds__(kJoinRows * 64) void logprob_join_kernel(PartsArgs 
 }
 
 // The gradient of a part.  Every workgroup joins its row's sums and computes the row's slope for itself; the first of a row leaves what is kept of it.
-template <bool FP32, int NV>
+template <bool FP32>
 __global__ __launch_bounds__(kPartThreads) void policy_parts_kernel(PartsArgs a) {
     const uint32_t row = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
     const int64_t token = a.r.tokens[row];
@@ -597,8 +597,8 @@ __global__ __launch_bounds__(kPartThreads) void policy_parts_kernel(PartsArgs a)
     const bool there = counts(a, row, token, &w);
     char* dx = a.r.dx ? a.r.dx + (int64_t)row * a.r.dx_stride * (FP32 ? 4 : 2) : nullptr;
     const char* x = row_of<FP32>(a.r.x, row);
-    Held<FP32, kPartThreads, NV> h;
-    h.place(x, (int32_t)part * (kPartThreads * NV), a.r.x.vocab, (int)threadIdx.x);
+    Held<FP32, kPartThreads, kPartWords> h;
+    h.place(x, (int32_t)part * (kPartThreads * kPartWords), a.r.x.vocab, (int)threadIdx.x);
     if (there && dx) h.load(x);
     Sum s = {1.0, 0.0f};
     RowLog l = {0.0, 0.0, 0.0};
@@ -812,29 +812,20 @@ Logits to_dev(const flashoptim_matrix* m) { return {(const char*)m->data, m->row
 // The most words that a row has between 16-byte borders.
 int64_t words(int64_t vocab, int dtype) { return vocab * fo::elem_bytes(dtype) / 16; }
 
-// How a row is cut: into parts of kPartThreads lanes that hold `vecs` words each, as many as registers allow, or fewer where there are few rows, so that all
-// compute units have one.
-struct Parts {
-    int vecs;
-    uint32_t parts;
-};
-Parts cut_rows(int64_t rows, int64_t vocab, int dtype) {
-    int vecs = 2;
+// The parts of a row, of kPartThreads lanes that hold `vecs` words each.
+int64_t parts_of(int64_t vocab, int dtype, int vecs = kPartWords) {
     const int64_t n = words(vocab, dtype);
-    const auto parts = [&] { return n > 0 ? up(n, kPartThreads * vecs) : 1; };
-    while (vecs > 1 && rows * parts() < 512) vecs /= 2;
-    return {vecs, (uint32_t)parts()};
+    return n > 0 ? up(n, kPartThreads * vecs) : 1;
+}
+// The words of a lane in the gradient's parts: two, or one where parts of that size have clearly fewer lanes without a word (8192 rows of 50257 BF16 values, 13 parts or
+// 25, 279 us and 265; 16384 rows of 8192, 2 or 4, 82 and 88; 2048 rows of 128256, 32 or 63, 167 and 172) and there are not too many.  Parts that have to be joined are
+// never faster with one (100 rows of 128256, policy loss, 18.6 us and 24.0).
+int gradient_vecs(int64_t rows, int64_t vocab, int dtype) {
+    const int64_t one = parts_of(vocab, dtype, 1);
+    return one * 103 < 200 * parts_of(vocab, dtype) && rows * one <= fo::kMaxWorkItems / kPartThreads ? 1 : 2;
 }
 template <int N>
 using Int = std::integral_constant<int, N>;
-// Calls launch(fp32, vecs) with the two as types.
-template <typename F>
-void with_vecs(int dtype, int vecs, F launch) {
-    const auto with = [&](auto fp32) {
-        if (vecs == 2) launch(fp32, Int<2>{}); else launch(fp32, Int<1>{});
-    };
-    if (dtype == FLASHOPTIM_FP32) with(std::true_type{}); else with(std::false_type{});
-}
 bool known(int dtype) { return dtype == FLASHOPTIM_BF16 || dtype == FLASHOPTIM_FP32; }
 
 // Calls launch(shape) with the shape of the workgroups that hold rows of n words.
@@ -868,18 +859,18 @@ bool streams_rows(int64_t rows, int64_t vocab, int dtype) { return words(vocab, 
 int stream_waves(int64_t rows, int64_t vocab, int dtype) { return rows < 2 * kUnits && words(vocab, dtype) > 512 ? 16 : 8; }
 
 // A call's parts in its workspace.
-PartsArgs to_parts(const RowsArgs& a, const Parts& c, void* workspace) {
-    PartsArgs p = {a, (Sum*)workspace, nullptr, c.parts};
-    p.logits = (float*)(p.sums + (int64_t)a.rows * c.parts);
+PartsArgs to_parts(const RowsArgs& a, int dtype, void* workspace) {
+    PartsArgs p = {a, (Sum*)workspace, nullptr, (uint32_t)parts_of(a.x.vocab, dtype)};
+    p.logits = (float*)(p.sums + (int64_t)a.rows * p.parts);
     return p;
 }
 int64_t parts_bytes(int64_t rows, int64_t vocab, int dtype) {
-    return up(rows * (int64_t)cut_rows(rows, vocab, dtype).parts * (int64_t)sizeof(Sum) + rows * 4, 16) * 16;
+    return up(rows * parts_of(vocab, dtype) * (int64_t)sizeof(Sum) + rows * 4, 16) * 16;
 }
-int launch_parts(const PartsArgs& p, int dtype, int vecs, void* stream) {
-    with_vecs(dtype, vecs, [&](auto f, auto nv) {
-        hipLaunchKernelGGL((parts_kernel<decltype(f)::value, decltype(nv)::value>), dim3(p.r.rows * p.parts), dim3(kPartThreads), 0, (hipStream_t)stream, p);
-    });
+int launch_parts(const PartsArgs& p, int dtype, void* stream) {
+    const dim3 grid(p.r.rows * p.parts), block(kPartThreads);
+    if (dtype == FLASHOPTIM_FP32) hipLaunchKernelGGL((parts_kernel<true>), grid, block, 0, (hipStream_t)stream, p);
+    else hipLaunchKernelGGL((parts_kernel<false>), grid, block, 0, (hipStream_t)stream, p);
     return fo::hip_status(hipGetLastError());
 }
 
@@ -898,7 +889,7 @@ int launch_held(const RowsArgs& a, void* stream) {
 }
 
 int check_launch(const flashoptim_matrix* logits) {
-    const int64_t blocks = logits->rows * (int64_t)cut_rows(logits->rows, logits->cols, logits->dtype).parts;
+    const int64_t blocks = logits->rows * parts_of(logits->cols, logits->dtype);
     return blocks > fo::kMaxWorkItems / kPartThreads || logits->rows > fo::kMaxWorkItems / 1024 ? FLASHOPTIM_ERR_NUMEL_RANGE : FLASHOPTIM_OK;
 }
 int check_workspace(int64_t need, const void* workspace, int64_t bytes) {
@@ -959,9 +950,8 @@ int flashoptim_token_logprob(const flashoptim_matrix* logits, const int64_t* tok
         if (logits->dtype == FLASHOPTIM_FP32) with(std::true_type{}); else with(std::false_type{});
         return fo::hip_status(hipGetLastError());
     }
-    const Parts c = cut_rows(rows, logits->cols, logits->dtype);
-    const PartsArgs p = to_parts(a, c, workspace);
-    FO_TRY(launch_parts(p, logits->dtype, c.vecs, stream));
+    const PartsArgs p = to_parts(a, logits->dtype, workspace);
+    FO_TRY(launch_parts(p, logits->dtype, stream));
     hipLaunchKernelGGL(logprob_join_kernel, dim3((unsigned)up(rows, kJoinRows)), dim3(kJoinRows * 64), 0, (hipStream_t)stream, p);
     return fo::hip_status(hipGetLastError());
 }
@@ -975,13 +965,17 @@ int flashoptim_token_logprob_backward(const flashoptim_matrix* logits, const int
     if (!lse || !dlogprob) return FLASHOPTIM_ERR_INVALID_ARG;
     if (!fo::aligned_to(lse, 4) || !fo::aligned_to(dlogprob, 4)) return FLASHOPTIM_ERR_MISALIGNED;
     FO_TRY(check_launch(logits));
-    const Parts c = cut_rows(logits->rows, logits->cols, logits->dtype);
+    const int vecs = gradient_vecs(logits->rows, logits->cols, logits->dtype);
     const GradArgs g = {to_dev(logits), (char*)dlogits->data, dlogits->rows > 1 ? dlogits->stride : 0, tokens, lse, dlogprob, 1.0f / temperature,
-                        (float)(kLog2e / (double)temperature), c.parts};
-    const dim3 grid((unsigned)(logits->rows * (int64_t)c.parts)), block(kPartThreads);
-    with_vecs(logits->dtype, c.vecs, [&](auto f, auto nv) {
-        hipLaunchKernelGGL((gradient_kernel<decltype(f)::value, decltype(nv)::value>), grid, block, 0, (hipStream_t)stream, g);
-    });
+                        (float)(kLog2e / (double)temperature), (uint32_t)parts_of(logits->cols, logits->dtype, vecs)};
+    const dim3 grid((unsigned)(logits->rows * (int64_t)g.parts)), block(kPartThreads);
+    const auto launch = [&](auto fp32, auto nv) {
+        hipLaunchKernelGGL((gradient_kernel<decltype(fp32)::value, decltype(nv)::value>), grid, block, 0, (hipStream_t)stream, g);
+    };
+    const auto with = [&](auto fp32) {
+        if (vecs == 2) launch(fp32, Int<2>{}); else launch(fp32, Int<1>{});
+    };
+    if (logits->dtype == FLASHOPTIM_FP32) with(std::true_type{}); else with(std::false_type{});
     return fo::hip_status(hipGetLastError());
 }
 
@@ -1017,12 +1011,11 @@ int flashoptim_policy_loss(const flashoptim_policy_spec* spec, const flashoptim_
     if (rows > 0 && holds_rows(rows, logits->cols, logits->dtype)) {
         FO_TRY(logits->dtype == FLASHOPTIM_FP32 ? launch_held<true>(a, stream) : launch_held<false>(a, stream));
     } else if (rows > 0) {
-        const Parts c = cut_rows(rows, logits->cols, logits->dtype);
-        const PartsArgs p = to_parts(a, c, (char*)workspace + up(rows * 24, 16) * 16);
-        FO_TRY(launch_parts(p, logits->dtype, c.vecs, stream));
-        with_vecs(logits->dtype, c.vecs, [&](auto f, auto nv) {
-            hipLaunchKernelGGL((policy_parts_kernel<decltype(f)::value, decltype(nv)::value>), dim3(p.r.rows * p.parts), dim3(kPartThreads), 0, (hipStream_t)stream, p);
-        });
+        const PartsArgs p = to_parts(a, logits->dtype, (char*)workspace + up(rows * 24, 16) * 16);
+        FO_TRY(launch_parts(p, logits->dtype, stream));
+        const dim3 grid(p.r.rows * p.parts), block(kPartThreads);
+        if (logits->dtype == FLASHOPTIM_FP32) hipLaunchKernelGGL((policy_parts_kernel<true>), grid, block, 0, (hipStream_t)stream, p);
+        else hipLaunchKernelGGL((policy_parts_kernel<false>), grid, block, 0, (hipStream_t)stream, p);
         FO_TRY(fo::hip_status(hipGetLastError()));
     }
     hipLaunchKernelGGL(policy_stats_kernel, dim3(1), dim3(kPairThreads), 0, (hipStream_t)stream, a.policy.terms, a.rows, spec->kl_weight, stats);
