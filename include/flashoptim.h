@@ -438,8 +438,11 @@ int flashoptim_block_norm_backward(const flashoptim_block_norm_spec* spec, const
  * token_logprob: logprob, lse [rows] and logprob64 [rows], the same as logprob in FP64, for the difference of long sums that a preference
  *   loss is made of.  Each may be NULL (not all, unless rows = 0).
  * token_logprob_backward: dlogits_ij = dlogprob_i / T ([j = t] - exp(logits_ij / T - lse_i)), of the type of logits, from the lse that the forward
- *   call left.  The logits of a row whose dlogprob is 0 are not read; its gradient is 0.  dlogits may be logits' own buffer.
- * workspace: as in the products above, of the bytes that the *_workspace call returns for the same sizes and type. */
+ *   call left.  That lse is rounded to FP32 goes into the exponent, so that the probabilities are off by |lse| 2^-24 of themselves; where |lse| is
+ *   2^17 or more (logits of the type's lowest value and no others) the gradient is NaN.  (policy_loss, which does not go by lse, has one.)
+ *   The logits of a row whose dlogprob is 0 are not read; its gradient is 0.  dlogits may be logits' own buffer.
+ * workspace: as in the products above, of the bytes that the *_workspace call returns for the same sizes and type.
+ * Here and below, buffers that are written overlap no others of the call unless it says so. */
 int64_t flashoptim_token_logprob_workspace(int64_t rows, int64_t vocab, int dtype);
 int flashoptim_token_logprob(const flashoptim_matrix* logits, const int64_t* tokens, float temperature, float* logprob, double* logprob64,
                              float* lse, void* workspace, int64_t workspace_bytes, void* stream);
@@ -456,7 +459,7 @@ int flashoptim_token_logprob_backward(const flashoptim_matrix* logits, const int
  *   A < 0 and r < 1 - clip_low.
  * A row whose weight is 0 does not count, as one with a negative token does not.  weights NULL: 1.  A mean is had by weights that sum to 1.
  * logprob [rows] and dlogits may be NULL (not wanted); dlogits may be logits' own buffer.  clip_low, clip_high and kl_weight are not
- * negative; clip_high may be infinite. */
+ * negative; clip_high may be infinite.  logprob is none of the inputs (to keep it as the next call's old_logprob, give it a buffer of its own). */
 typedef struct flashoptim_policy_spec {
     float temperature, clip_low, clip_high, kl_weight, grad_scale;
 } flashoptim_policy_spec;
@@ -476,7 +479,8 @@ int flashoptim_policy_loss(const flashoptim_policy_spec* spec, const flashoptim_
  *   loss = the mean over the pairs of, by kind:  SIGMOID  (1 - label_smoothing) log(1 + exp(-z)) + label_smoothing log(1 + exp(z))
  *                                                HINGE    max(0, 1 - z)
  *                                                SQUARED  (z / beta - 1 / (2 beta))^2
- *   margins [pairs] = z (may be NULL);  dlogprob [rows] = grad_scale * the loss's gradient (may be NULL), 0 for rows of no sequence.
+ *   margins [pairs] = z (may be NULL);  dlogprob [rows] = grad_scale * the loss's gradient (may be NULL), 0 for rows of no sequence; it may be
+ *   logprob's own buffer.
  * offsets [2 pairs + 1] INT64, not descending, within [0, rows] (what lies outside is taken as the nearest bound): sequence i is the rows
  * offsets[i] .. offsets[i + 1] - 1, possibly none.  order: sequences 2p and 2p + 1 are the chosen and the rejected one of pair p
  * (FLASHOPTIM_PAIRS_BY_TURNS), or p and pairs + p (FLASHOPTIM_PAIRS_HALVES).  Rows whose weight is 0 do not count, whatever their

@@ -343,14 +343,15 @@ struct PolicyIn {
 };
 __device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& a, const PolicyIn& in, double logprob) {
     const double adv = in.advantage, w = in.w;
-    const double ratio = a.in.old_logprob ? exp_of(logprob - (double)in.old) : logprob - logprob + 1.0;
+    // (of the policy to itself 1 whatever its logprob, also for a token of probability 0; NaN stays)
+    const double ratio = a.in.old_logprob ? exp_of(logprob - (double)in.old) : logprob == logprob ? 1.0 : logprob;
     const double low = 1.0 - (double)a.spec.clip_low, high = 1.0 + (double)a.spec.clip_high;
     const bool blocked = (adv > 0.0 && ratio > high) || (adv < 0.0 && ratio < low);
     const double surrogate = blocked ? -adv * (adv > 0.0 ? high : low) : -adv * ratio;
     double slope = blocked ? 0.0 : -adv * ratio, kl = 0.0;
     if (a.in.ref_logprob) {
         const double d = (double)in.ref - logprob, e = expm1_of(d);
-        kl = e - d;
+        kl = d < __builtin_inf() ? e - d : d;
         slope -= (double)a.spec.kl_weight * e;
     }
     return {(float)(slope * w * (double)a.spec.grad_scale), surrogate * w, kl * w, blocked ? w : 0.0};
@@ -628,6 +629,7 @@ struct GradArgs {
     float scale, c;          // of the slopes
     uint32_t parts;
 };
+constexpr float kMostLse = 131072.0f;
 template <bool FP32, int NV>
 __global__ __launch_bounds__(kPartThreads) void gradient_kernel(GradArgs a) {
     const uint32_t row = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
@@ -641,7 +643,8 @@ __global__ __launch_bounds__(kPartThreads) void gradient_kernel(GradArgs a) {
         h.store_zeros(dx);
         return;
     }
-    if (token >= a.x.vocab) d = __builtin_nanf("");
+    // (from kMostLse on what FP32 has lost of lse would be more than 1 % of the probabilities, at the type's lowest value all of them)
+    if (token >= a.x.vocab || !(fabsf(a.lse[row]) < kMostLse)) d = __builtin_nanf("");
     const float shift = a.lse[row] * (float)kLog2e;
     h.load(x);
     h.store_gradient(dx, token_in(token, a.x.vocab), d, 0.0f, a.c, shift);
@@ -1001,6 +1004,9 @@ int flashoptim_policy_loss(const flashoptim_policy_spec* spec, const flashoptim_
     for (const float* p : {inputs->advantages, inputs->old_logprob, inputs->ref_logprob, inputs->weights, (const float*)stats, (const float*)logprob})
         if (!fo::aligned_to(p, 4)) return FLASHOPTIM_ERR_MISALIGNED;
     FO_TRY(check_workspace(flashoptim_policy_loss_workspace(rows, logits->cols, logits->dtype), workspace, workspace_bytes));
+    // (a row's inputs are read by many lanes while one writes its logprob)
+    for (const float* p : {inputs->advantages, inputs->old_logprob, inputs->ref_logprob, inputs->weights})
+        if (rows > 0 && p && p == logprob) return FLASHOPTIM_ERR_INVALID_ARG;
     RowsArgs a = rows_args(logits, tokens, spec->temperature);
     a.logprob = logprob;
     a.policy = {*spec, *inputs, (double*)workspace};

@@ -248,6 +248,52 @@ def test_rows_without_a_result(vocab):
     assert bool(torch.isnan(stats[0])) and bool(torch.isnan(d[:5]).all()) and bool(torch.isfinite(d[5]).all())
 
 
+@pytest.mark.parametrize("vocab", [9, 1000, 40003])
+def test_a_token_of_probability_zero(vocab):
+    c = Case(4, vocab, BF16, masked=0, seed=17)
+    c.logits[1, c.tokens[1]] = float("-inf")
+    a, stats, lp, d = torch.full((4,), 2.0, device="cuda"), torch.empty(4, device="cuda"), torch.empty(4, device="cuda"), torch.empty_like(c.logits)
+    call = lambda **kw: fo.policy_loss(fo.PolicyLoss(kl_weight=0.1), c.logits, c.tokens, a, stats, logprob=lp, dlogits=d,       # noqa: E731
+                                       workspace=memory(fo.policy_loss_workspace(c.logits)), **kw)
+    # the ratio of the policy to itself is 1 all the same
+    call()
+    ref = R.Rows(c.logits, c.tokens)
+    want, err = ref.gradient(torch.full((4,), -2.0, dtype=torch.float64), torch.zeros(4, dtype=torch.float64), False)
+    R.close(d, want, err, "dlogits")
+    assert stats.tolist() == [-8.0, -8.0, 0.0, 0.0] and float(lp[1]) == float("-inf")
+    # that to another policy is 0, and to a reference that gives it a chance the KL term is infinite
+    call(old_logprob=torch.full((4,), -3.0, device="cuda"))
+    assert bool((d[1] == 0).all()) and bool(torch.isfinite(stats).all())
+    call(ref_logprob=torch.full((4,), -3.0, device="cuda"))
+    assert float(stats[0]) == float("inf") and float(stats[2]) == float("inf") and float(stats[1]) == -8.0
+
+
+@pytest.mark.parametrize("vocab", [9, 1000, 40003])
+def test_the_gradient_from_an_lse_without_digits(vocab):
+    # nothing but the type's lowest value: in FP32 lse does not differ from it by the vocabulary's size any more
+    for low, dtype in ((torch.finfo(BF16).min, BF16), (torch.finfo(FP32).min, FP32), (-131072.0, FP32), (131072.0, BF16)):
+        c = Case(3, vocab, dtype, masked=0, seed=18)
+        c.logits[1] = low
+        d, slopes = torch.empty_like(c.logits), torch.ones(3, device="cuda")
+        lse = forward(c)[1]
+        fo.token_logprob_backward(c.logits, c.tokens, lse, slopes, d)
+        gone = bool(lse[1].abs() >= 131072)
+        assert bool(torch.isfinite(d[::2]).all()) and bool(torch.isnan(d[1]).all()) == gone and (gone or low == -131072.0)
+        slopes[1] = 0
+        fo.token_logprob_backward(c.logits, c.tokens, lse, slopes, d)
+        assert bool((d[1] == 0).all())
+
+
+def test_preference_gradient_over_the_log_probabilities():
+    for lengths in ([700, 300], [5, 9] * 20, [0, 4, 3000, 1]):
+        lp, ref, w, cut = preference_case(lengths, 4, behind=3, ahead=2)
+        lp, ref, w, cut = lp.cuda(), ref.cuda(), w.cuda(), cut.cuda()
+        out, d = [torch.empty(1, device="cuda") for _ in range(2)], torch.empty_like(lp)
+        fo.preference_loss(fo.PreferenceLoss(), lp, cut, out[0], ref_logprob=ref, weights=w, dlogprob=d)
+        fo.preference_loss(fo.PreferenceLoss(), lp, cut, out[1], ref_logprob=ref, weights=w, dlogprob=lp)
+        assert torch.equal(lp, d) and torch.equal(out[0], out[1])
+
+
 @pytest.mark.parametrize("vocab", [11, 3001])
 def test_gradients_against_differences(vocab):
     # the directional derivative of the loss, from two FP64 evaluations of its definition
