@@ -727,6 +727,7 @@ class GradList:
             raise ValueError("as many destinations as gradients")
         self.n = len(self.src)
         self.array = (_Gradient * max(self.n, 1))()
+        self.device = self.src[0].get_device() if self.src else None
         self.src_dtype = self._type(self.src, "gradients")
         self.dst_dtype = self.src_dtype if self.dst is None else self._type(self.dst, "destinations")
         for i, t in enumerate(self.src):
@@ -736,10 +737,10 @@ class GradList:
             d = self.array[i]
             d.src, d.dst, d.numel = t.data_ptr(), to.data_ptr(), t.numel()
 
-    @staticmethod
-    def _type(tensors, what):
-        if any(t.dtype not in _DTYPE or t.dtype != tensors[0].dtype or not t.is_contiguous() or not t.is_cuda for t in tensors):
-            raise ValueError(f"{what}: contiguous tensors on the GPU, bfloat16 or float32, one type for all")
+    def _type(self, tensors, what):
+        if any(t.dtype not in _DTYPE or t.dtype != tensors[0].dtype or not t.is_contiguous() or not t.is_cuda or t.get_device() != self.device
+               for t in tensors):
+            raise ValueError(f"{what}: contiguous tensors on one GPU, bfloat16 or float32, one type for all")
         return _DTYPE[tensors[0].dtype] if tensors else 0
 
     @classmethod
@@ -782,10 +783,18 @@ def _memory(workspace):
     return workspace.data_ptr(), workspace.nbytes
 
 
+def _on_its_device(grads, factor, stream):
+    """The handle of a stream for a call on a GradList; the current one has to be of the device that everything lies on."""
+    device = factor.data.get_device()
+    if grads.device not in (None, device) or (stream is None and _raw_current_device() != device):
+        raise ValueError("the gradients, the factor and the current device are not the same device")
+    return _stream_handle(stream)
+
+
 def grad_norm(grads, max_norm, factor, workspace=None, stream=None):
     """factor (ClipFactor) <- the norm of all gradients of a GradList, and max_norm / norm where that is less than 1."""
     _check(load_library().flashoptim_grad_norm(grads.array, grads.n, grads.src_dtype, max_norm, factor.address, *_memory(workspace),
-                                               _stream_handle(stream)), "flashoptim_grad_norm")
+                                               _on_its_device(grads, factor, stream)), "flashoptim_grad_norm")
 
 
 def clip_factor_from_sum(factor, max_norm, stream=None):
@@ -796,7 +805,7 @@ def clip_factor_from_sum(factor, max_norm, stream=None):
 def clip_gradients(grads, factor, stream=None):
     """The destinations of a GradList <- its gradients times the factor's scale."""
     _check(load_library().flashoptim_clip_gradients(grads.array, grads.n, grads.src_dtype, grads.dst_dtype, factor.address,
-                                                    _stream_handle(stream)), "flashoptim_clip_gradients")
+                                                    _on_its_device(grads, factor, stream)), "flashoptim_clip_gradients")
 
 
 def faithful_rounding_stats(stream=None):

@@ -36,8 +36,10 @@ struct Args {
     PyObject* const* at;
     Py_ssize_t n, i = 0;
     bool failed = false;
+    const bool one_device;               // all tensors lie on one device, that of the current stream where no other is given
+    int64_t device = -1;
 
-    Args(PyObject* const* args, Py_ssize_t count, Py_ssize_t expected) : at(args), n(count) {
+    Args(PyObject* const* args, Py_ssize_t count, Py_ssize_t expected, bool one_device_ = false) : at(args), n(count), one_device(one_device_) {
         if (n != expected) fail(PyExc_TypeError, "%s", "wrong number of arguments");
     }
     template <typename... T>
@@ -56,6 +58,10 @@ struct Args {
         }
         const at::Tensor* t = &THPVariable_Unpack(o);
         if (!t->is_cuda()) fail(PyExc_ValueError, "%s: not on the GPU", name);
+        if (one_device && !failed) {
+            if (device >= 0 && device != t->get_device()) fail(PyExc_ValueError, "%s: on another device than the others", name);
+            device = t->get_device();
+        }
         return failed ? nullptr : t;
     }
     // A two-dimensional tensor with neighbouring columns, whose rows may lie apart.
@@ -123,9 +129,10 @@ struct Args {
             failed = PyErr_Occurred() != nullptr;
             return v;
         }
-        PyObject* device = PyObject_CallNoArgs(current_device);
-        PyObject* handle = device ? PyObject_CallOneArg(current_stream, device) : nullptr;
-        Py_XDECREF(device);
+        PyObject* current = PyObject_CallNoArgs(current_device);
+        if (current && one_device && device >= 0 && PyLong_AsLongLong(current) != device) fail(PyExc_ValueError, "%s", "the tensors lie on another device than the current one");
+        PyObject* handle = current && !failed ? PyObject_CallOneArg(current_stream, current) : nullptr;
+        Py_XDECREF(current);
         if (!handle) {
             failed = true;
             return nullptr;
@@ -251,7 +258,7 @@ void bound(Args& a, F* call) {
 }
 
 PyObject* logprob(PyObject*, PyObject* const* args, Py_ssize_t n) {
-    Args a(args, n, 8);
+    Args a(args, n, 8, true);
     flashoptim_matrix mx;
     void* ws;
     int64_t bytes;
@@ -269,7 +276,7 @@ PyObject* logprob(PyObject*, PyObject* const* args, Py_ssize_t n) {
 }
 
 PyObject* logprob_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
-    Args a(args, n, 7);
+    Args a(args, n, 7, true);
     flashoptim_matrix mx, md;
     const flashoptim_matrix* x = a.matrix("logits", &mx);
     const int64_t rows = x ? x->rows : 0;
@@ -284,7 +291,7 @@ PyObject* logprob_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
 }
 
 PyObject* policy(PyObject*, PyObject* const* args, Py_ssize_t n) {
-    Args a(args, n, 12);
+    Args a(args, n, 12, true);
     flashoptim_matrix mx, md;
     flashoptim_policy_inputs in;
     void* ws;
@@ -307,7 +314,7 @@ PyObject* policy(PyObject*, PyObject* const* args, Py_ssize_t n) {
 }
 
 PyObject* preference(PyObject*, PyObject* const* args, Py_ssize_t n) {
-    Args a(args, n, 9);
+    Args a(args, n, 9, true);
     const auto* spec = a.address<flashoptim_preference_spec>();
     const at::Tensor* first = a.tensor("logprob");
     const int64_t rows = first ? first->numel() : 0;

@@ -137,6 +137,41 @@ def test_the_binding_refuses():
         assert getattr(spec.desc, name) == -1
 
 
+def test_log_probabilities_over_the_inputs_of_the_policy_loss_are_refused():
+    # one lane writes a row's logprob while others still read its inputs
+    for i in range(4):
+        assert policy(inputs=[P if k == i else 3 * P for k in range(4)], stats=4 * P) == -1
+
+
+class Tensor:
+    """What a list of gradients looks at, on a GPU that exists in name only."""
+    dtype, is_cuda = torch.bfloat16, True
+
+    def __init__(self, device):
+        self.get_device, self.is_contiguous, self.numel, self.data_ptr = lambda: device, lambda: True, lambda: 8, lambda: P
+
+
+class Factor:
+    address = P
+
+    def __init__(self, device):
+        self.data = Tensor(device)
+
+
+def test_lists_over_several_devices_are_refused(monkeypatch):
+    monkeypatch.setattr(B, "_raw_current_device", lambda: 0)
+    here, there = Tensor(0), Tensor(1)
+    for args in (([here, there],), ([here], [there])):
+        with pytest.raises(ValueError):
+            fo.GradList(*args)
+    for tensor, factor in ((here, 1), (there, 0), (there, 1)):
+        grads = fo.GradList([tensor])
+        with pytest.raises(ValueError):
+            fo.grad_norm(grads, 1.0, Factor(factor))
+        with pytest.raises(ValueError):
+            fo.clip_gradients(grads, Factor(factor))
+
+
 def test_struct_layouts():
     assert C.sizeof(B._Gradient) == 24 and C.sizeof(B._PolicySpec) == 20 and C.sizeof(B._PolicyInputs) == 32 and C.sizeof(B._PreferenceSpec) == 20
 
