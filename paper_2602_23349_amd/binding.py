@@ -200,7 +200,8 @@ def _marshal():
             raise RuntimeError("_marshal.so is missing: build it with `python paper_2602_23349_amd/build.py`") from e
         lib = load_library()
         names = [n for n in EXPORTED_SYMBOLS if n.startswith(("flashoptim_mx4_", "flashoptim_block_norm", "flashoptim_token_logprob",
-                                                             "flashoptim_policy_loss", "flashoptim_preference_loss"))]
+                                                             "flashoptim_policy_loss", "flashoptim_preference_loss", "flashoptim_grad_norm",
+                                                             "flashoptim_clip_gradients"))]
         fast.bind({n: C.cast(getattr(lib, n), C.c_void_p).value for n in names}, torch._C._cuda_getCurrentRawStream,
                   torch._C._cuda_getDevice)
         torch.cuda.init()
@@ -736,6 +737,10 @@ class GradList:
                 raise ValueError("a destination has the elements of its gradient")
             d = self.array[i]
             d.src, d.dst, d.numel = t.data_ptr(), to.data_ptr(), t.numel()
+        self._pack()
+
+    def _pack(self):
+        self.args = C.addressof(self.array), self.n, self.src_dtype, self.dst_dtype
 
     def _type(self, tensors, what):
         if any(t.dtype not in _DTYPE or t.dtype != tensors[0].dtype or not t.is_contiguous() or not t.is_cuda or t.get_device() != self.device
@@ -754,6 +759,7 @@ class GradList:
         for d, t in zip(out.array, params.array[:params.n]):
             d.src, d.dst, d.numel = t.grad, t.grad, t.numel
         out.src = params
+        out._pack()
         return out
 
 
@@ -767,7 +773,7 @@ class ClipFactor:
             raise ValueError("a factor lies on the GPU")
         self.sum_squares = self.data[:1]
         self.norm, self.scale = self.data.view(torch.float32)[2:3], self.data.view(torch.float32)[3:4]
-        self.address = self.data.data_ptr()
+        self.address, self.device = self.data.data_ptr(), self.data.get_device()
 
 
 def grad_norm_workspace(grads):
@@ -775,26 +781,17 @@ def grad_norm_workspace(grads):
     return _size(load_library().flashoptim_grad_norm_workspace(grads.array, grads.n, grads.src_dtype), "flashoptim_grad_norm_workspace")
 
 
-def _memory(workspace):
-    if workspace is None:
-        return None, 0
-    if not workspace.is_contiguous() or not workspace.is_cuda:
-        raise ValueError("workspace: contiguous memory on the GPU")
-    return workspace.data_ptr(), workspace.nbytes
-
-
-def _on_its_device(grads, factor, stream):
-    """The handle of a stream for a call on a GradList; the current one has to be of the device that everything lies on."""
-    device = factor.data.get_device()
-    if grads.device not in (None, device) or (stream is None and _raw_current_device() != device):
-        raise ValueError("the gradients, the factor and the current device are not the same device")
-    return _stream_handle(stream)
+def _same_device(grads, factor):
+    if grads.device not in (None, factor.device):
+        raise ValueError("the gradients and the factor lie on different devices")
 
 
 def grad_norm(grads, max_norm, factor, workspace=None, stream=None):
     """factor (ClipFactor) <- the norm of all gradients of a GradList, and max_norm / norm where that is less than 1."""
-    _check(load_library().flashoptim_grad_norm(grads.array, grads.n, grads.src_dtype, max_norm, factor.address, *_memory(workspace),
-                                               _on_its_device(grads, factor, stream)), "flashoptim_grad_norm")
+    _same_device(grads, factor)
+    status = (_fast or _marshal()).grad_norm(*grads.args, factor.device, max_norm, factor.address, workspace, _handle(stream))
+    if status:
+        raise FlashOptimError(status, "flashoptim_grad_norm")
 
 
 def clip_factor_from_sum(factor, max_norm, stream=None):
@@ -804,8 +801,10 @@ def clip_factor_from_sum(factor, max_norm, stream=None):
 
 def clip_gradients(grads, factor, stream=None):
     """The destinations of a GradList <- its gradients times the factor's scale."""
-    _check(load_library().flashoptim_clip_gradients(grads.array, grads.n, grads.src_dtype, grads.dst_dtype, factor.address,
-                                                    _on_its_device(grads, factor, stream)), "flashoptim_clip_gradients")
+    _same_device(grads, factor)
+    status = (_fast or _marshal()).clip(*grads.args, factor.device, factor.address, _handle(stream))
+    if status:
+        raise FlashOptimError(status, "flashoptim_clip_gradients")
 
 
 def faithful_rounding_stats(stream=None):

@@ -23,7 +23,8 @@ struct GradTable {
     uint16_t lack[N];
 };
 // As many as the 4 KB of a launch's arguments hold, or few, for which the host has fewer bytes to copy.
-constexpr int kGradFew = 16, kGradSome = 64, kGradMany = 280, kClipMany = 176;
+// (kGradSome and one more are a wavefront's lanes.)
+constexpr int kGradFew = 16, kGradSome = 63, kGradMany = 280, kClipMany = 176;
 constexpr int64_t kGradArgBytes = 4096 - 64;             // beside the other arguments
 static_assert(sizeof(GradTable<kGradMany, false>) <= kGradArgBytes && sizeof(GradTable<kClipMany, true>) <= kGradArgBytes, "kernel arguments");
 
@@ -34,9 +35,10 @@ constexpr int64_t kMostTiles = kMaxWorkItems / kGradThreads;
 // The workgroups of a launch that sums up: each takes every so many-th tile and leaves one sum.
 constexpr int64_t kNormGroups = 2048;
 constexpr int64_t norm_groups(int64_t tiles) { return tiles < kNormGroups ? tiles : kNormGroups; }
-// Lists of up to so many tiles are summed up by one workgroup, whose four groups of wavefronts take a tile each (one launch against two, 128 Ki gradients
-// 5.9 us against 7.3, 256 Ki 9.3 against 7.3).
-constexpr int64_t kSmallTiles = 16;
+// Lists of up to so many tiles are summed up by one workgroup, whose four groups of wavefronts take a tile each: one launch against two.  The sums of
+// squares, which are FP64, bind it, 0.25 us a tile.  (Called one after the other: 8 tiles 4.6 us against 7.1, 12 tiles 5.6 against 7.1, 16 tiles 6.5 against 7.1; in a
+// graph, without the host's time for a launch, 4.1, 5.3 and 6.4 against 4.2.)
+constexpr int64_t kSmallTiles = 12;
 // What the sum leaves in the 256 MB memory-side cache.
 constexpr int64_t kKeptBytes = (int64_t)160 << 20;
 

@@ -29,6 +29,8 @@ decltype(&flashoptim_token_logprob) call_logprob;
 decltype(&flashoptim_token_logprob_backward) call_logprob_backward;
 decltype(&flashoptim_policy_loss) call_policy;
 decltype(&flashoptim_preference_loss) call_preference;
+decltype(&flashoptim_grad_norm) call_grad_norm;
+decltype(&flashoptim_clip_gradients) call_clip;
 PyObject *current_stream, *current_device;      // torch._C._cuda_getCurrentRawStream, _cuda_getDevice
 
 // The arguments of one call, taken in order.  After the first failure a Python error is set and nothing more is taken.
@@ -98,6 +100,13 @@ struct Args {
         const double v = PyFloat_AsDouble(o);
         failed = v == -1.0 && PyErr_Occurred() != nullptr;
         return (float)v;
+    }
+    int64_t integer() {
+        PyObject* o = next();
+        if (failed) return 0;
+        const long long v = PyLong_AsLongLong(o);
+        failed = v == -1 && PyErr_Occurred() != nullptr;
+        return (int64_t)v;
     }
     void workspace(void** p, int64_t* bytes) {
         const at::Tensor* t = tensor("workspace");
@@ -338,6 +347,42 @@ PyObject* preference(PyObject*, PyObject* const* args, Py_ssize_t n) {
                                                     (const int64_t*)offsets, pairs, (float*)loss, (float*)margins, (float*)d, stream));
 }
 
+// A list of gradients: its address, length, the types of what is read and of what is written, and the device that it and its factor lie on.
+struct Gradients {
+    const flashoptim_gradient* list;
+    int64_t n;
+    int src, dst;
+    explicit Gradients(Args& a) {
+        list = a.address<flashoptim_gradient>();
+        n = a.integer();
+        src = (int)a.integer();
+        dst = (int)a.integer();
+        a.device = a.integer();
+    }
+};
+
+PyObject* grad_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Args a(args, n, 9, true);
+    void* ws;
+    int64_t bytes;
+    const Gradients g(a);
+    const float max_norm = a.number();
+    auto* factor = const_cast<flashoptim_clip_factor*>(a.address<flashoptim_clip_factor>());
+    a.workspace(&ws, &bytes);
+    void* stream = a.stream();
+    bound(a, call_grad_norm);
+    return status(a, a.failed ? 0 : call_grad_norm(g.list, g.n, g.src, max_norm, factor, ws, bytes, stream));
+}
+
+PyObject* clip(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Args a(args, n, 7, true);
+    const Gradients g(a);
+    const auto* factor = a.address<flashoptim_clip_factor>();
+    void* stream = a.stream();
+    bound(a, call_clip);
+    return status(a, a.failed ? 0 : call_clip(g.list, g.n, g.src, g.dst, factor, stream));
+}
+
 // bind(addresses by name, current_stream, current_device)
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (n != 3 || !PyDict_Check(args[0])) {
@@ -355,6 +400,8 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
     take(args[0], "flashoptim_token_logprob_backward", call_logprob_backward);
     take(args[0], "flashoptim_policy_loss", call_policy);
     take(args[0], "flashoptim_preference_loss", call_preference);
+    take(args[0], "flashoptim_grad_norm", call_grad_norm);
+    take(args[0], "flashoptim_clip_gradients", call_clip);
     if (!call_quantize || !call_dequantize || !call_matmul || !call_linear || !call_linear_backward || !call_norm || !call_norm_backward) {
         PyErr_SetString(PyExc_RuntimeError, "bind: an entry point is missing");
         return nullptr;
@@ -379,6 +426,7 @@ PyObject* guarded(PyObject* self, PyObject* const* args, Py_ssize_t n) {
 PyMethodDef methods[] = {FO_METHOD(bind),   FO_METHOD(quantize),        FO_METHOD(dequantize), FO_METHOD(matmul),
                          FO_METHOD(linear), FO_METHOD(linear_backward), FO_METHOD(norm),       FO_METHOD(norm_backward),
                          FO_METHOD(logprob), FO_METHOD(logprob_backward), FO_METHOD(policy), FO_METHOD(preference),
+                         FO_METHOD(grad_norm), FO_METHOD(clip),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -101,6 +101,27 @@ def test_norm_and_clipping(sizes, dtype):
         assert all(torch.equal(a, b) for a, b in zip(views, want))
 
 
+@pytest.mark.parametrize("count", [2, 15, 16, 17, 62, 63, 64, 65, 176, 177, 280, 281])
+def test_numbers_of_tensors(count):
+    # tensors of one tile and of several, whole and not, where a launch's table has one more or less
+    sizes = [(TILE, 1, 2 * TILE + 9, 0, 4095, 3 * TILE)[i % 6] for i in range(count)]
+    for dtype in (BF16, FP32):
+        _, views = make(sizes, dtype)
+        _, out = make(sizes, BF16, seed=1)
+        factor = norm_of(fo.GradList(views, out), 0.5)
+        check_norm(factor, views, 0.5)
+        fo.clip_gradients(fo.GradList(views, out), factor)
+        assert all(torch.equal(o, times(v, factor.scale, BF16)) for v, o in zip(views, out))
+
+
+@pytest.mark.parametrize("tiles", [1, 3, 4, 5, 11, 12, 13, 16, 17])
+def test_numbers_of_tiles(tiles):
+    for dtype in (BF16, FP32):
+        for sizes in ([tiles * TILE], [(tiles - 1) * TILE + 1], [TILE - 5] * tiles):
+            _, views = make(sizes, dtype)
+            check_norm(norm_of(fo.GradList(views), 1.0), views, 1.0)
+
+
 def test_some_in_place_and_some_not():
     for max_norm in (0.5, 1e9):
         _, views = make([100, 9000, 31], BF16)
