@@ -381,14 +381,16 @@ struct RowsArgs {
     PolicyArgs policy;
 };
 
-// One row to LANES lanes, which hold it: the policy loss and its gradient in one pass over the logits.
+// The statistics from the sums of the three terms.
+__device__ __forceinline__ void put_stats(const double (&s)[3], float kl_weight, float* stats) {
+#pragma unroll
+    for (int k = 0; k < 3; ++k) stats[1 + k] = (float)s[k];
+    stats[0] = (float)(s[0] + (double)kl_weight * s[1]);
+}
+
+// One row to LANES lanes, which hold it: the policy loss and its gradient in one pass over the logits.  What the row's terms are, in lane 0.
 template <bool FP32, int LANES, int NV>
-__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void policy_rows_kernel(RowsArgs a) {
-    constexpr int LINES = LANES < 256 ? 256 / LANES : 1;
-    static_assert(LANES == 64 || LINES == 1, "a row is a wavefront's or a workgroup's");
-    const uint32_t row = LINES == 1 ? blockIdx.x : blockIdx.x * LINES + (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int lane = (int)threadIdx.x & (LANES - 1);
-    if (row >= a.rows) return;
+__device__ __forceinline__ PolicyRow policy_of_row(const RowsArgs& a, uint32_t row, int lane) {
     const int64_t token = a.tokens[row];
     const float w = a.policy.in.weights ? a.policy.in.weights[row] : 1.0f;
     char* dx = a.dx ? a.dx + (int64_t)row * a.dx_stride * (FP32 ? 4 : 2) : nullptr;
@@ -396,26 +398,56 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void policy_rows_kernel(
     Held<FP32, LANES, NV, true> h;
     h.place(x, 0, a.x.vocab, lane);
     if (token < 0 || w == 0.0f) {
-        if (lane == 0) {
-            if (a.logprob) a.logprob[row] = 0.0f;
-            put_terms(a.policy, a.rows, row, {});
-        }
+        if (lane == 0 && a.logprob) a.logprob[row] = 0.0f;
         if (dx) h.store_zeros(dx);
-        return;
+        return {};
     }
     h.load(x);
     const float logit = logit_of<FP32>(x, token, a.x.vocab);
     const Sum s = join_waves<LANES / 64>(h.wave_part(a.c), a.c);
     const RowLog l = row_log(s, logit, a.inv_t);
     const PolicyRow p = policy_row(a.policy, row, l.logprob, w);
-    if (lane == 0) {
-        if (a.logprob) a.logprob[row] = (float)l.logprob;
-        put_terms(a.policy, a.rows, row, p);
-    }
+    if (lane == 0 && a.logprob) a.logprob[row] = (float)l.logprob;
     const float d = p.slope * a.scale;
-    if (!dx) return;
+    if (!dx) return p;
     if (d == 0.0f) h.store_zeros(dx);
     else h.store_gradient(dx, token_in(token, a.x.vocab), d, base_of(s.most), a.c.high, (float)(l.log_sum * kLog2e));
+    return p;
+}
+template <bool FP32, int LANES, int NV>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void policy_rows_kernel(RowsArgs a) {
+    constexpr int LINES = LANES < 256 ? 256 / LANES : 1;
+    static_assert(LANES == 64 || LINES == 1, "a row is a wavefront's or a workgroup's");
+    const uint32_t row = LINES == 1 ? blockIdx.x : blockIdx.x * LINES + (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int lane = (int)threadIdx.x & (LANES - 1);
+    if (row >= a.rows) return;
+    const PolicyRow p = policy_of_row<FP32, LANES, NV>(a, row, lane);
+    if (lane == 0) put_terms(a.policy, a.rows, row, p);
+}
+
+// A few short rows, a wavefront each, by one workgroup that adds up their terms itself: no second launch (12 rows of 1001 FP32 values
+// 6.3 us against 7.8; 16 rows 7.0 and 17, by two launches, 7.8; rows of 8 words a lane are no faster so, 16 of 2000 values 8.9 us, 17 by two launches 8.7).
+constexpr uint32_t kFewRows = 16;
+constexpr int kFewVecs = 4;
+template <bool FP32>
+__global__ __launch_bounds__(kFewRows * 64) void policy_few_rows_kernel(RowsArgs a, float* stats) {
+    __shared__ double terms[kFewRows][3];
+    const uint32_t row = (uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    if (row < a.rows) {
+        const PolicyRow p = policy_of_row<FP32, 64, kFewVecs>(a, row, (int)threadIdx.x & 63);
+        if ((threadIdx.x & 63) == 0) {
+            terms[row][0] = p.surrogate;
+            terms[row][1] = p.kl;
+            terms[row][2] = p.blocked;
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    double s[3] = {};
+    for (uint32_t i = 0; i < a.rows; ++i)
+#pragma unroll
+        for (int k = 0; k < 3; ++k) s[k] += terms[i][k];
+    put_stats(s, a.policy.spec.kl_weight, stats);
 }
 
 // Rows of which a compute unit holds one at a time.  Workgroups stay and take every so many-th row: of the next one the first kAhead words of each lane, as many as
@@ -676,9 +708,8 @@ __global__ __launch_bounds__(kPairThreads) void policy_stats_kernel(const double
         s[k] = 0.0;
 #pragma unroll
         for (int j = 0; j < kPairThreads / 64; ++j) s[k] += part[k][j];
-        stats[1 + k] = (float)s[k];
     }
-    stats[0] = (float)(s[0] + (double)kl_weight * s[1]);
+    put_stats(s, kl_weight, stats);
 }
 
 struct PairArgs {
@@ -891,6 +922,14 @@ int launch_held(const RowsArgs& a, void* stream) {
     return fo::hip_status(hipGetLastError());
 }
 
+// Whether one workgroup takes all rows, a wavefront each.
+bool few_rows(int64_t rows, int64_t vocab, int dtype) { return rows <= kFewRows && words(vocab, dtype) <= 64 * kFewVecs; }
+template <bool FP32>
+int launch_few(const RowsArgs& a, float* stats, void* stream) {
+    hipLaunchKernelGGL((policy_few_rows_kernel<FP32>), dim3(1), dim3(a.rows * 64), 0, (hipStream_t)stream, a, stats);
+    return fo::hip_status(hipGetLastError());
+}
+
 int check_launch(const flashoptim_matrix* logits) {
     const int64_t blocks = logits->rows * parts_of(logits->cols, logits->dtype);
     return blocks > fo::kMaxWorkItems / kPartThreads || logits->rows > fo::kMaxWorkItems / 1024 ? FLASHOPTIM_ERR_NUMEL_RANGE : FLASHOPTIM_OK;
@@ -1014,6 +1053,7 @@ int flashoptim_policy_loss(const flashoptim_policy_spec* spec, const flashoptim_
         a.dx = (char*)dlogits->data;
         a.dx_stride = rows > 1 ? dlogits->stride : 0;
     }
+    if (rows > 0 && few_rows(rows, logits->cols, logits->dtype)) return logits->dtype == FLASHOPTIM_FP32 ? launch_few<true>(a, stats, stream) : launch_few<false>(a, stats, stream);
     if (rows > 0 && holds_rows(rows, logits->cols, logits->dtype)) {
         FO_TRY(logits->dtype == FLASHOPTIM_FP32 ? launch_held<true>(a, stream) : launch_held<false>(a, stream));
     } else if (rows > 0) {

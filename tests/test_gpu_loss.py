@@ -168,6 +168,15 @@ def test_policy_loss_over_vocabularies(vocab, dtype):
     policy(Case(5, vocab, dtype, seed=4), in_place=True)
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("rows", [1, 2, 15, 16, 17])
+def test_policy_loss_of_a_few_rows(rows, dtype):
+    # by one workgroup or several, at the lengths of rows where that changes
+    for vocab in (1, 31, 2047, 2048, 2055, 4095, 4096, 4103):
+        for old, kl in ((True, 0.1), (False, None)):
+            policy(Case(rows, vocab, dtype, pad=vocab % 3, seed=20), old=old, kl=kl, weights=kl is None)
+
+
 @pytest.mark.parametrize("old", [False, True])
 @pytest.mark.parametrize("kl", [None, 0.0, 0.1])
 @pytest.mark.parametrize("weights", [False, True])
