@@ -34,7 +34,7 @@ struct Tile {
 };
 // A launch's table.  Of up to kGradSome tensors each lane holds one, fetched once and all together, so that a tile is found in registers; longer ones are
 // searched in memory, one step after the other.  (25 tensors of 250 thousand elements together, searched in memory and held: norm 3.6 us and 2.8, clipping 4.3
-// and 3.8; 20 tensors of 1.5 G elements, norm 447 us and 441.)
+// and 3.8; 21 tensors of 1.5 G elements, norm 447 us and 441.)
 template <int N, bool DST>
 struct Lookup {
     static constexpr bool kHeld = N <= fo::kGradSome;
