@@ -894,9 +894,14 @@ bool holds_rows(int64_t rows, int64_t vocab, int dtype) {
 // 50257 values, one row 7.1 against 6.7, 64 rows 8.3 against 7.3), and as many as there are compute units (256 rows of 128256 15.3 us against 19.1, 128 rows
 // 13.8 against 12.3).
 bool streams_rows(int64_t rows, int64_t vocab, int dtype) { return words(vocab, dtype) <= 4096 || rows >= kUnits; }
-// And by how many wavefronts: few rows by all that a workgroup may have (256 rows of 10000 BF16 values 6.1 -> 5.1 us, of 128256 17.6 -> 15.3), many, or rows of 512
-// words, by eight, so that a unit has several rows.
-int stream_waves(int64_t rows, int64_t vocab, int dtype) { return rows < 2 * kUnits && words(vocab, dtype) > 512 ? 16 : 8; }
+// And by how many wavefronts: few rows by all that a workgroup may have (256 rows of 10000 BF16 values 6.1 -> 5.1 us, of 128256 17.6 -> 15.3).  Many rows by as
+// many as find a part of 512 words for each, since those without one only wait (8192 rows of 4096 BF16 values by 1, 2, 4 and 8 wavefronts 16.0, 18.3, 20.9 and
+// 37.1 us; of 8192 27.4, 25.8, 28.7 and 42.3; of 16384 49.7, 47.4, 45.4 and 50.9; of 24000 71.9, 69.6, 72.1 and 71.1, but 600 of these 18.0, 13.0, 11.1 and 10.5).
+int stream_waves(int64_t rows, int64_t vocab, int dtype) {
+    const int64_t parts = up(words(vocab, dtype), 512);
+    if (rows < 2 * kUnits && parts > 1) return 16;
+    return parts <= 1 ? 1 : parts <= 2 ? 2 : parts <= 4 ? 4 : 8;
+}
 
 // A call's parts in its workspace.
 PartsArgs to_parts(const RowsArgs& a, int dtype, void* workspace) {
@@ -996,7 +1001,13 @@ int flashoptim_token_logprob(const flashoptim_matrix* logits, const int64_t* tok
             hipLaunchKernelGGL((logprob_rows_kernel<decltype(fp32)::value, W>), dim3(a.rows), dim3(W * 64), 0, (hipStream_t)stream, a);
         };
         const auto with = [&](auto fp32) {
-            if (stream_waves(rows, logits->cols, logits->dtype) == 16) launch(fp32, Int<16>{}); else launch(fp32, Int<8>{});
+            switch (stream_waves(rows, logits->cols, logits->dtype)) {
+                case 1: return launch(fp32, Int<1>{});
+                case 2: return launch(fp32, Int<2>{});
+                case 4: return launch(fp32, Int<4>{});
+                case 8: return launch(fp32, Int<8>{});
+                default: launch(fp32, Int<16>{});
+            }
         };
         if (logits->dtype == FLASHOPTIM_FP32) with(std::true_type{}); else with(std::false_type{});
         return fo::hip_status(hipGetLastError());

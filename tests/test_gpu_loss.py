@@ -151,6 +151,17 @@ def test_numbers_of_rows(rows, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("words", [1, 512, 1024, 2048])
+def test_log_probabilities_by_the_length_of_rows(words, dtype):
+    # rows of as many words and of a few values less and more, by one wavefront to sixteen, in calls of few rows and of many
+    size = 8 if dtype == BF16 else 4
+    for rows in (2, 511, 512):
+        for more in (-1, 0, 1, size + 1):
+            c = Case(rows, words * size + more, dtype, pad=more % 4, seed=21)
+            ref, lse = check_logprob(c)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
 @pytest.mark.parametrize("pad,shift", [(1, 0), (3, 1), (8, 8), (0, 3), (5, 7)])
 def test_rows_at_any_address(pad, shift, dtype):
     for vocab in (3, 77, 2051, 20001):
