@@ -352,7 +352,7 @@ __device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& a, const Polic
     if (a.in.ref_logprob) {
         const double d = (double)in.ref - logprob, e = expm1_of(d);
         kl = d < __builtin_inf() ? e - d : d;
-        slope -= (double)a.spec.kl_weight * e;
+        if (a.spec.kl_weight != 0.0f) slope -= (double)a.spec.kl_weight * e;       // (0: watched only, and e may be infinite)
     }
     return {(float)(slope * w * (double)a.spec.grad_scale), surrogate * w, kl * w, blocked ? w : 0.0};
 }
@@ -381,11 +381,11 @@ struct RowsArgs {
     PolicyArgs policy;
 };
 
-// The statistics from the sums of the three terms.
+// The statistics from the sums of the three terms.  (A KL term without weight may be infinite.)
 __device__ __forceinline__ void put_stats(const double (&s)[3], float kl_weight, float* stats) {
 #pragma unroll
     for (int k = 0; k < 3; ++k) stats[1 + k] = (float)s[k];
-    stats[0] = (float)(s[0] + (double)kl_weight * s[1]);
+    stats[0] = (float)(kl_weight != 0.0f ? s[0] + (double)kl_weight * s[1] : s[0]);
 }
 
 // One row to LANES lanes, which hold it: the policy loss and its gradient in one pass over the logits.  What the row's terms are, in lane 0.

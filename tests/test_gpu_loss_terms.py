@@ -1,0 +1,47 @@
+"""Terms of the policy loss that do not count beside infinities: what a term multiplies by 0 is left out of the loss and its gradient, whatever the term itself is.
+By every way in which the loss handles a row.  No tolerances: each call is compared with one that does not have the term, bit for bit."""
+import gc
+
+import pytest
+import torch
+
+from test_gpu_loss import BF16, FP32, Case, memory
+import paper_2602_23349_amd as fo
+
+pytestmark = pytest.mark.gpu
+
+# a few short rows by one workgroup; rows that a wavefront holds, a workgroup of 256, 512 and 1024 lanes; long rows by workgroups that stay; parts
+SHAPES = [(9, 31, FP32), (40, 1000, BF16), (9, 10_003, BF16), (130, 20_003, BF16), (130, 40_001, FP32), (515, 32_773, FP32), (9, 70_001, BF16)]
+
+
+@pytest.fixture(autouse=True)
+def nothing_left_to_collect():
+    gc.collect()
+    yield
+    torch.cuda.empty_cache()
+
+
+def call(c, spec, **kw):
+    stats, logprob = torch.full((4,), 7.0, device="cuda"), torch.full((c.rows,), 7.0, device="cuda")
+    dx = torch.full_like(c.logits, 7.0)
+    fo.policy_loss(spec, c.logits, c.tokens, c.advantages, stats, logprob=logprob, dlogits=dx, workspace=memory(fo.policy_loss_workspace(c.logits)), **kw)
+    return stats, logprob, dx
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", SHAPES)
+def test_a_kl_term_that_is_only_watched(rows, vocab, dtype):
+    c = Case(rows, vocab, dtype, masked=0, seed=40)
+    c.logits[1, c.tokens[1]] = float("-inf")                  # a token of probability 0, to which the reference gives a chance
+    ref = (torch.randn(rows, generator=torch.Generator().manual_seed(vocab)) - 6).cuda()
+    old = ref + 0.3
+    ref[2] = 900.0                                            # so far above that the term overflows
+    spec = fo.PolicyLoss(kl_weight=0.0)
+    for kw in (dict(), dict(old_logprob=old), dict(weights=c.weights + 0.1)):
+        without, with_ref = call(c, spec, **kw), call(c, spec, ref_logprob=ref, **kw)
+        assert bool(torch.isfinite(without[0]).all()) and bool(torch.isfinite(without[2]).all()) and float(without[0][2]) == 0
+        for k in (0, 1, 3):
+            assert torch.equal(with_ref[0][k], without[0][k]), k
+        assert float(with_ref[0][2]) == float("inf")
+        assert torch.equal(with_ref[1], without[1]) and torch.equal(with_ref[2], without[2])
+    # a term with a weight is infinite all the same
+    assert float(call(c, fo.PolicyLoss(kl_weight=0.1), ref_logprob=ref)[0][0]) == float("inf")
