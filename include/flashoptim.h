@@ -452,7 +452,7 @@ int flashoptim_token_logprob_backward(const flashoptim_matrix* logits, const int
 /* policy_loss: the clipped policy loss with a KL term to a reference policy, and its gradient in the same pass over the logits.  By row,
  * with A the advantage and w the weight:
  *   r = exp(logprob - old_logprob)                 (old_logprob NULL: of the policy to itself, r = 1, through which the gradient goes all the same)
- *   surrogate = -min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A)
+ *   surrogate = -min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A)               (A = 0: 0, also where r is infinite)
  *   kl = exp(d) - d - 1,  d = ref_logprob - logprob         (ref_logprob NULL: 0; kl_weight 0: in stats [2] only, whatever it is)
  *   stats [4] = { sum w (surrogate + kl_weight kl),  sum w surrogate,  sum w kl,  sum w [blocked] }     the first is the loss
  *   dlogits = grad_scale * the loss's gradient.  A row is blocked, its surrogate without gradient, where A > 0 and r > 1 + clip_high or

@@ -347,8 +347,9 @@ __device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& a, const Polic
     const double ratio = a.in.old_logprob ? exp_of(logprob - (double)in.old) : logprob == logprob ? 1.0 : logprob;
     const double low = 1.0 - (double)a.spec.clip_low, high = 1.0 + (double)a.spec.clip_high;
     const bool blocked = (adv > 0.0 && ratio > high) || (adv < 0.0 && ratio < low);
-    const double surrogate = blocked ? -adv * (adv > 0.0 ? high : low) : -adv * ratio;
-    double slope = blocked ? 0.0 : -adv * ratio, kl = 0.0;
+    const double gain = adv == 0.0 && ratio == ratio ? 0.0 : adv * ratio;        // (the ratio may be infinite; NaN stays)
+    const double surrogate = blocked ? -adv * (adv > 0.0 ? high : low) : -gain;
+    double slope = blocked ? 0.0 : -gain, kl = 0.0;
     if (a.in.ref_logprob) {
         const double d = (double)in.ref - logprob, e = expm1_of(d);
         kl = d < __builtin_inf() ? e - d : d;

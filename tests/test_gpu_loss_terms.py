@@ -45,3 +45,26 @@ def test_a_kl_term_that_is_only_watched(rows, vocab, dtype):
         assert torch.equal(with_ref[1], without[1]) and torch.equal(with_ref[2], without[2])
     # a term with a weight is infinite all the same
     assert float(call(c, fo.PolicyLoss(kl_weight=0.1), ref_logprob=ref)[0][0]) == float("inf")
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", SHAPES)
+def test_an_advantage_of_0_has_no_surrogate(rows, vocab, dtype):
+    c = Case(rows, vocab, dtype, masked=0, seed=41)
+    c.advantages[1:4] = 0
+    old = (torch.randn(rows, generator=torch.Generator().manual_seed(vocab)) - 6).cuda()
+    ref = old + 0.2
+    old[1], old[2] = float("-inf"), -2000.0                   # ratios that are infinite, by their definition or in FP64
+    w = c.weights + 0.1
+    without = w.clone()
+    without[1:3] = 0
+    got, want = (call(c, fo.PolicyLoss(), old_logprob=old, weights=v) for v in (w, without))
+    assert bool(torch.isfinite(got[0]).all()) and torch.equal(got[0], want[0]) and torch.equal(got[2], want[2])
+    assert bool(torch.isfinite(got[1]).all()) and torch.equal(got[1][3:], want[1][3:])
+    # the KL term is there all the same
+    spec = fo.PolicyLoss(kl_weight=0.1)
+    got, want = call(c, spec, old_logprob=old, ref_logprob=ref, weights=w), call(c, spec, old_logprob=ref, ref_logprob=ref, weights=w)
+    assert torch.equal(got[2][1:3], want[2][1:3]) and bool((got[2][1:3] != 0).any(1).all()) and bool(torch.isfinite(got[0]).all())
+    # and what is no number stays none
+    old[3] = float("nan")
+    got = call(c, fo.PolicyLoss(), old_logprob=old, weights=w)
+    assert bool(torch.isnan(got[0][0])) and bool(torch.isnan(got[2][3]).all())
