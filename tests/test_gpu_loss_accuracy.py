@@ -1,0 +1,82 @@
+"""How near the losses on logits come to their definitions in 64 bits, by bounds that follow the kernels' own sums, with u = 2^-24.
+
+A power of two stands for exp((x - m) / T): the difference is off by u of itself, the product with the factor's two parts by u, so that the power is off by
+2 u |x - m| / T, and by 2 u of its own.  A lane adds up eight values in three roundings (four in two) and at most 16 words of these in as many, in FP32; all else
+is FP64, but a part's sum is brought to another largest value at most HOPS times, each by a power of 2 u, whose exponents add up to |x - m|.  So a value's part
+of the sum is off by (2 |x - m| / T + ADDS) u of itself with ADDS = 2 (1 + HOPS) + 19.  HOPS: the words of a row of 262147 BF16 values lie 4096 or fewer to a pass of a
+workgroup, which makes eight passes, once between its wavefronts, and once more between parts.
+
+The largest value's own part is exact (its power is 1, words that hold a value of some weight are added up in FP64): beside a token that is all but certain only the others' part is off,
+by as much of itself, and FP64 sums of fewer than 1000 additions by 2^-43."""
+import gc
+
+import pytest
+import torch
+
+import loss_reference as R
+from test_gpu_loss import BF16, FP32, Case, check_logprob, forward, memory, policy
+import paper_2602_23349_amd as fo
+
+pytestmark = pytest.mark.gpu
+
+U = R.U
+HOPS = 10
+ADDS = 2 * (1 + HOPS) + 19
+
+
+@pytest.fixture(autouse=True)
+def nothing_left_to_collect():
+    gc.collect()
+    yield
+    torch.cuda.empty_cache()
+
+
+@pytest.fixture
+def tight(monkeypatch):
+    """The bounds of loss_reference.py, 3 sum p |x - m| / T + 2 + 1.5 adds, with the additions that there are."""
+    monkeypatch.setattr(R, "adds", lambda vocab: (ADDS - 2) / 1.5)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("rows,vocab", [(5, 1000), (5, 8192), (5, 50_257), (5, 131_073), (5, 262_147), (300, 4099), (300, 30_001), (260, 70_001)])
+def test_log_probabilities(rows, vocab, dtype, tight):
+    check_logprob(Case(rows, vocab, dtype, temperature=0.7, masked=0.1, seed=50))
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("rows,vocab", [(6, 9), (6, 1000), (6, 8192), (6, 50_257), (6, 262_147), (300, 4099), (300, 30_001), (260, 70_001)])
+def test_tokens_that_are_all_but_certain(rows, vocab, dtype):
+    c = Case(rows, vocab, dtype, masked=0, seed=51, spread=1.0)
+    g = torch.Generator().manual_seed(vocab)
+    row = torch.arange(rows)
+    # ahead of the others by 16 to 36: probabilities of 1 - 10^-2 (of many others) to 1 - 10^-14
+    ahead = 16 + 20 * torch.rand(rows, generator=g)
+    tokens = c.tokens.cpu()
+    x = c.logits.cpu()
+    x[row, tokens] = (x.float().amax(1) + ahead).to(dtype)
+    c.logits.copy_(x)
+    x = x.double()
+    gap = x[row, tokens][:, None] - x
+    other = torch.exp(-gap)
+    other[row, tokens] = 0
+    want = -torch.log1p(other.sum(1))
+    err = U * (other * (2 * gap + ADDS)).sum(1) + 2.0 ** -43
+    wide = torch.full((rows,), 7.0, dtype=torch.float64, device="cuda")
+    fo.token_logprob(c.logits, c.tokens, logprob64=wide, workspace=memory(fo.token_logprob_workspace(c.logits)))
+    R.close(wide, want, err, "logprob64")
+    # the policy loss's own sum, by its shape
+    stats, logprob = torch.empty(4, device="cuda"), torch.empty(rows, device="cuda")
+    fo.policy_loss(fo.PolicyLoss(), c.logits, c.tokens, c.advantages, stats, logprob=logprob, workspace=memory(fo.policy_loss_workspace(c.logits)))
+    R.close(logprob, want, err + U * want.abs(), "logprob")
+
+
+@pytest.mark.parametrize("grad", [True, False])
+@pytest.mark.parametrize("rows,vocab,dtype", [
+    (128, 16_392, BF16), (130, 20_003, BF16), (129, 32_768, BF16), (131, 10_001, FP32),           # rows that 512 lanes hold by 8 words
+    (128, 32_776, BF16), (130, 50_257, BF16), (130, 30_001, FP32),                                # by 16
+    (128, 65_544, BF16), (260, 70_001, BF16), (300, 40_003, FP32), (511, 32_773, FP32),           # that 1024 lanes hold
+])
+def test_the_policy_loss_of_rows_that_a_workgroup_holds(rows, vocab, dtype, grad, tight):
+    policy(Case(rows, vocab, dtype, temperature=0.9, pad=vocab % 3, shift=vocab % 5, masked=0.2, seed=52), grad=grad)
+    if grad:
+        policy(Case(rows, vocab, dtype, masked=0.2, seed=53), old=False, kl=None, in_place=True)
