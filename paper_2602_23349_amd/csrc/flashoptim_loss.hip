@@ -9,6 +9,7 @@
 #include <stdint.h>
 
 #include <cmath>
+#include <limits>
 #include <type_traits>
 
 #include "flashoptim.h"
@@ -960,7 +961,7 @@ Factor factor_of(float temperature) {
     float high = (float)c;
     if ((double)high > c) high = std::nextafter(high, 0.0f);
     const float low = (float)(c - (double)high);
-    return {high, low > 1e-30f ? low : 1e-30f};
+    return {high, low > 0.0f ? low : std::numeric_limits<float>::denorm_min()};       // (of no weight beside high, at any temperature)
 }
 RowsArgs rows_args(const flashoptim_matrix* logits, const int64_t* tokens, float temperature) {
     RowsArgs a = {};

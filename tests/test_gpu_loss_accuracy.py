@@ -80,3 +80,18 @@ def test_the_policy_loss_of_rows_that_a_workgroup_holds(rows, vocab, dtype, grad
     policy(Case(rows, vocab, dtype, temperature=0.9, pad=vocab % 3, shift=vocab % 5, masked=0.2, seed=52), grad=grad)
     if grad:
         policy(Case(rows, vocab, dtype, masked=0.2, seed=53), old=False, kl=None, in_place=True)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("temperature", [1e20, 1e30, 1e36, 1e38])
+@pytest.mark.parametrize("rows,vocab", [(4, 40), (4, 70_001)])
+def test_extreme_temperatures(rows, vocab, temperature, dtype, tight):
+    # they give even a mask of the type's lowest value a chance again
+    c = Case(rows, vocab, dtype, temperature=temperature, masked=0, seed=56)
+    c.logits[:, 7:vocab // 2] = torch.finfo(dtype).min
+    c.logits[1, 9:vocab - 9] = float("-inf")
+    c.tokens.remainder_(7)
+    if temperature == 1e38:
+        c.tokens[0] = 8
+    check_logprob(c)
+    policy(c, scale=1e30)
