@@ -438,8 +438,9 @@ int flashoptim_block_norm_backward(const flashoptim_block_norm_spec* spec, const
  * token_logprob: logprob, lse [rows] and logprob64 [rows], the same as logprob in FP64, for the difference of long sums that a preference
  *   loss is made of.  Each may be NULL (not all, unless rows = 0).
  * token_logprob_backward: dlogits_ij = dlogprob_i / T ([j = t] - exp(logits_ij / T - lse_i)), of the type of logits, from the lse that the forward
- *   call left.  That lse is rounded to FP32 goes into the exponent, so that the probabilities are off by |lse| 2^-24 of themselves; where |lse| is
- *   2^17 or more (logits of the type's lowest value and no others) the gradient is NaN.  (policy_loss, which does not go by lse, has one.)
+ *   call left.  That lse is rounded to FP32 goes into the exponent: the probabilities are off by |lse| 2^-24 of themselves, beside (3 |logits / T - lse| + 5) 2^-24
+ *   by the exponent's own roundings and the forward call's error (T below 2^85); where |lse| is 2^17 or more (logits of the type's lowest value and no
+ *   others) the gradient is NaN.  (policy_loss, which does not go by lse, has one.)
  *   The logits of a row whose dlogprob is 0 are not read; its gradient is 0.  dlogits may be logits' own buffer.
  * workspace: as in the products above, of the bytes that the *_workspace call returns for the same sizes and type.
  * Here and below, buffers that are written overlap no others of the call unless it says so. */

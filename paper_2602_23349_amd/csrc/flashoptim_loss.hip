@@ -666,10 +666,10 @@ struct GradArgs {
     int64_t stride;
     const int64_t* tokens;
     const float *lse, *slope;
-    float scale, c;          // of the slopes
+    float scale, t, c;       // of the slopes; the temperature T, and log2(e) / T
     uint32_t parts;
 };
-constexpr float kMostLse = 131072.0f;
+constexpr float kMostLse = 131072.0f, kMostBase = 0x1p102f;       // (a logit of any size less kMostBase is finite)
 template <bool FP32, int NV>
 __global__ __launch_bounds__(kPartThreads) void gradient_kernel(GradArgs a) {
     const uint32_t row = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
@@ -683,11 +683,18 @@ __global__ __launch_bounds__(kPartThreads) void gradient_kernel(GradArgs a) {
         h.store_zeros(dx);
         return;
     }
-    // (from kMostLse on what FP32 has lost of lse would be more than 1 % of the probabilities, at the type's lowest value all of them)
-    if (token >= a.x.vocab || !(fabsf(a.lse[row]) < kMostLse)) d = __builtin_nanf("");
-    const float shift = a.lse[row] * (float)kLog2e;
+    // (from kMostLse on what FP32 has lost of lse would be up to 0.8 % of the probabilities and more, at the type's lowest value all of them)
+    const float lse = a.lse[row];
+    if (token >= a.x.vocab || !(fabsf(lse) < kMostLse)) d = __builtin_nanf("");
+    // The difference first, as in the sums: x / T - lse = (x - base) / T - rest / T with lse T = base + rest.  (x c - lse log2(e) in FP32 loses as much as lse
+    // itself has lost twice more, by the constants and by the product's rounding.)
+    float base = lse * a.t, shift = fmaf(lse, a.t, -base) * a.c;
+    if (fabsf(base) > kMostBase) {           // (T of 2^85 or more)
+        base = 0.0f;
+        shift = lse * (float)kLog2e;
+    }
     h.load(x);
-    h.store_gradient(dx, token_in(token, a.x.vocab), d, 0.0f, a.c, shift);
+    h.store_gradient(dx, token_in(token, a.x.vocab), d, base, a.c, shift);
 }
 
 // Three sums over a workgroup's rows, and from them the statistics.
@@ -1030,7 +1037,7 @@ int flashoptim_token_logprob_backward(const flashoptim_matrix* logits, const int
     if (!fo::aligned_to(lse, 4) || !fo::aligned_to(dlogprob, 4)) return FLASHOPTIM_ERR_MISALIGNED;
     FO_TRY(check_launch(logits));
     const int vecs = gradient_vecs(logits->rows, logits->cols, logits->dtype);
-    const GradArgs g = {to_dev(logits), (char*)dlogits->data, dlogits->rows > 1 ? dlogits->stride : 0, tokens, lse, dlogprob, 1.0f / temperature,
+    const GradArgs g = {to_dev(logits), (char*)dlogits->data, dlogits->rows > 1 ? dlogits->stride : 0, tokens, lse, dlogprob, 1.0f / temperature, temperature,
                         (float)(kLog2e / (double)temperature), (uint32_t)parts_of(logits->cols, logits->dtype, vecs)};
     const dim3 grid((unsigned)(logits->rows * (int64_t)g.parts)), block(kPartThreads);
     const auto launch = [&](auto fp32, auto nv) {

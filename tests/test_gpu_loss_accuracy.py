@@ -95,3 +95,46 @@ def test_extreme_temperatures(rows, vocab, temperature, dtype, tight):
         c.tokens[0] = 8
     check_logprob(c)
     policy(c, scale=1e30)
+
+
+@pytest.mark.parametrize("temperature", [0.6, 0.7, 0.9, 1.0, 1.3])
+@pytest.mark.parametrize("vocab", [40, 3001])
+def test_the_gradient_from_an_lse(vocab, temperature):
+    # logits far from 0: what FP32 has lost of lse is all that the probabilities may be off by, beside roundings of the exponent itself.  With t = |x / T - lse|:
+    # the difference, the factor and the exponent u t each, the power 2 u, the slope by T, its product and the result 3 u, the forward call's lse as above
+    levels = torch.tensor([0.0, 30.0, -700.0, 1000.0, 5000.0, 20000.0, -60000.0])
+    c = Case(len(levels), vocab, FP32, temperature=temperature, masked=0, seed=54)
+    c.logits += levels.cuda()[:, None]
+    lse = forward(c)[1]
+    d = torch.full_like(c.logits, 7.0)
+    fo.token_logprob_backward(c.logits, c.tokens, lse, torch.ones(c.rows, device="cuda"), d, temperature=temperature)
+    t = float(torch.tensor(temperature, dtype=torch.float32))
+    x = c.logits.double().cpu() / t
+    want_lse = torch.logsumexp(x, 1, keepdim=True)
+    p = torch.exp(x - want_lse)
+    far = (p * (x.amax(1, keepdim=True) - x)).sum(1, keepdim=True)
+    e = U * (want_lse.abs() + 3 * (x - want_lse).abs() + 5 + 2 * far + ADDS)
+    err = p / t * (e + e * e)
+    hit = torch.zeros_like(x).scatter_(1, c.tokens.cpu()[:, None], 1.0)
+    R.close(d, (hit - p) / t, err + 3 * U * hit / t, "dlogits")
+
+
+@pytest.mark.parametrize("temperature", [1e-30, 1e20, 1e27, 1e38])
+def test_the_gradient_from_an_lse_at_extreme_temperatures(temperature):
+    # beside a mask of the type's lowest value, which such temperatures give a chance again; the exponent's roundings are of values that may be as far apart
+    c = Case(4, 300, FP32, temperature=temperature, masked=0, seed=55)
+    if temperature < 1:
+        c.logits *= temperature
+    c.logits[:, 7:90] = torch.finfo(FP32).min
+    lse = forward(c)[1]
+    d = torch.full_like(c.logits, 7.0)
+    fo.token_logprob_backward(c.logits, c.tokens, lse, torch.full((4,), min(temperature, 1e30), device="cuda"), d, temperature=temperature)
+    t = float(torch.tensor(temperature, dtype=torch.float32))
+    slope = float(torch.tensor(min(temperature, 1e30), dtype=torch.float32)) / t
+    x = c.logits.double().cpu() / t
+    want_lse = torch.logsumexp(x, 1, keepdim=True)
+    p = torch.exp(x - want_lse)
+    hit = torch.zeros_like(x).scatter_(1, c.tokens.cpu()[:, None], 1.0)
+    far = (p * (x.amax(1, keepdim=True) - x)).sum(1, keepdim=True)
+    e = U * (3 * want_lse.abs() + 3 * (x - want_lse).abs() + 5 + 2 * far + ADDS)
+    R.close(d, (hit - p) * slope, slope * (p * (e + e * e) + 3 * U * hit) + 2.0 ** -148, "dlogits")
