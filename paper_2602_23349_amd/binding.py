@@ -722,6 +722,8 @@ class GradList:
     """A host array of flashoptim_gradient descriptors, built once and reused: `src` contiguous GPU tensors of one type, bfloat16 or
     float32, `dst` where clip_gradients leaves them (None: in place), of that type or bfloat16."""
 
+    params = None
+
     def __init__(self, src, dst=None):
         self.src, self.dst = list(src), None if dst is None else list(dst)
         if self.dst is not None and len(self.dst) != len(self.src):
@@ -750,7 +752,8 @@ class GradList:
 
     @classmethod
     def of(cls, params):
-        """The gradients of a TensorList as its descriptors have them now, clipped in place."""
+        """The gradients of a TensorList, clipped in place: at each call those that its steps take then, also behind a set_grad (a captured
+        call keeps those that it was captured with).  As for the steps, their memory is the caller's to keep."""
         if any(getattr(b, "grad", None) is not None and not b.grad.is_cuda for b in params.buffers):
             raise ValueError("gradients: tensors on the GPU")
         out = cls([])
@@ -758,9 +761,12 @@ class GradList:
         out.array = (_Gradient * max(out.n, 1))()
         for d, t in zip(out.array, params.array[:params.n]):
             d.src, d.dst, d.numel = t.grad, t.grad, t.numel
-        out.src = params
+        out.src = out.params = params
         out._pack()
         return out
+
+    def follow(self):
+        (_fast or _marshal()).follow(self.args[0], C.addressof(self.params.array), self.n)
 
 
 class ClipFactor:
@@ -781,14 +787,16 @@ def grad_norm_workspace(grads):
     return _size(load_library().flashoptim_grad_norm_workspace(grads.array, grads.n, grads.src_dtype), "flashoptim_grad_norm_workspace")
 
 
-def _same_device(grads, factor):
+def _ready(grads, factor):
+    if grads.params is not None:
+        grads.follow()
     if grads.device not in (None, factor.device):
         raise ValueError("the gradients and the factor lie on different devices")
 
 
 def grad_norm(grads, max_norm, factor, workspace=None, stream=None):
     """factor (ClipFactor) <- the norm of all gradients of a GradList, and max_norm / norm where that is less than 1."""
-    _same_device(grads, factor)
+    _ready(grads, factor)
     status = (_fast or _marshal()).grad_norm(*grads.args, factor.device, max_norm, factor.address, workspace, _handle(stream))
     if status:
         raise FlashOptimError(status, "flashoptim_grad_norm")
@@ -801,7 +809,7 @@ def clip_factor_from_sum(factor, max_norm, stream=None):
 
 def clip_gradients(grads, factor, stream=None):
     """The destinations of a GradList <- its gradients times the factor's scale."""
-    _same_device(grads, factor)
+    _ready(grads, factor)
     status = (_fast or _marshal()).clip(*grads.args, factor.device, factor.address, _handle(stream))
     if status:
         raise FlashOptimError(status, "flashoptim_clip_gradients")

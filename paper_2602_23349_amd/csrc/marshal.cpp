@@ -383,6 +383,17 @@ PyObject* clip(PyObject*, PyObject* const* args, Py_ssize_t n) {
     return status(a, a.failed ? 0 : call_clip(g.list, g.n, g.src, g.dst, factor, stream));
 }
 
+// follow(gradients, tensors, count): each gradient is read and clipped where its tensor's descriptor has it now.
+PyObject* follow(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Args a(args, n, 3);
+    auto* gradients = const_cast<flashoptim_gradient*>(a.address<flashoptim_gradient>());
+    const auto* tensors = a.address<flashoptim_tensor>();
+    const int64_t count = a.integer();
+    if (a.failed) return nullptr;
+    for (int64_t i = 0; i < count; ++i) gradients[i].src = gradients[i].dst = const_cast<void*>((const void*)tensors[i].grad);
+    Py_RETURN_NONE;
+}
+
 // bind(addresses by name, current_stream, current_device)
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (n != 3 || !PyDict_Check(args[0])) {
@@ -426,7 +437,7 @@ PyObject* guarded(PyObject* self, PyObject* const* args, Py_ssize_t n) {
 PyMethodDef methods[] = {FO_METHOD(bind),   FO_METHOD(quantize),        FO_METHOD(dequantize), FO_METHOD(matmul),
                          FO_METHOD(linear), FO_METHOD(linear_backward), FO_METHOD(norm),       FO_METHOD(norm_backward),
                          FO_METHOD(logprob), FO_METHOD(logprob_backward), FO_METHOD(policy), FO_METHOD(preference),
-                         FO_METHOD(grad_norm), FO_METHOD(clip),
+                         FO_METHOD(grad_norm), FO_METHOD(clip), FO_METHOD(follow),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

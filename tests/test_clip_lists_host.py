@@ -1,0 +1,65 @@
+"""Lists of gradients that follow a list of parameters, without a GPU: what a call is given is looked at instead of the call itself."""
+import types
+
+import pytest
+import torch
+
+import paper_2602_23349_amd as fo
+from paper_2602_23349_amd import _marshal as M
+from paper_2602_23349_amd import binding as B
+
+
+class Tensor:
+    """What the binding looks at of a tensor, on a GPU that exists in name only."""
+    dtype = torch.bfloat16
+
+    def __init__(self, address, device=0):
+        self.data_ptr, self.get_device, self.is_cuda = lambda: address, lambda: device, device >= 0
+
+
+class Factor:
+    address = 0x10000
+
+    def __init__(self, device=0):
+        self.device = device
+
+
+def parameters(*grads):
+    fields = ("param", "rho", "m_q", "m_scale", "v_q", "v_scale")
+    return fo.TensorList(types.SimpleNamespace(**{f: None for f in fields}, grad=g, numel=8 + i, lr=0.1, weight_decay=0.0) for i, g in enumerate(grads))
+
+
+@pytest.fixture
+def seen(monkeypatch):
+    """The lists that the calls are given: (src, dst, numel) of each gradient."""
+    lists = []
+
+    def call(address, n, *rest):
+        lists.append([(g.src, g.dst, g.numel) for g in (B._Gradient * n).from_address(address)])
+        return 0
+    monkeypatch.setattr(B, "_fast", types.SimpleNamespace(grad_norm=call, clip=call, follow=M.follow))
+    return lists
+
+
+def test_a_list_follows_the_gradients_of_its_parameters(seen):
+    params = parameters(Tensor(0x1000), Tensor(0x2000), Tensor(0x3000))
+    grads = fo.GradList.of(params)
+    for changed in (None, 1, 0, 1):
+        if changed is not None:
+            params.set_grad(changed, Tensor(0x100000 * (len(seen) + 1)))
+        fo.grad_norm(grads, 1.0, Factor())
+        fo.clip_gradients(grads, Factor())
+        now = [(t.grad, t.grad, t.numel) for t in params.array]
+        assert seen[-2] == seen[-1] == now and now[2] == (0x3000, 0x3000, 10)
+    # one that is taken away is refused by the call, which sees no address
+    params.set_grad(2, None)
+    fo.grad_norm(grads, 1.0, Factor())
+    assert seen[-1][2] == (None, None, 10)
+
+
+def test_a_list_of_tensors_stays_as_it_is(seen):
+    class Whole(Tensor):
+        is_contiguous, numel = (lambda self: True), (lambda self: 8)
+    grads = fo.GradList([Whole(0x1000), Whole(0x2000)])
+    fo.grad_norm(grads, 1.0, Factor())
+    assert seen == [[(0x1000, 0x1000, 8), (0x2000, 0x2000, 8)]]
