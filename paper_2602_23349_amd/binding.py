@@ -280,12 +280,17 @@ class ParamBuffers:
         return out
 
 
+def _device(t):
+    return None if t is None else t.get_device()
+
+
 class TensorList:
     """A host array of flashoptim_tensor descriptors, built once and reused across steps."""
 
     def __init__(self, buffers):
         self.buffers = list(buffers)
         self.n = len(self.buffers)
+        self._lies_on, self._devices = [_device(b.grad) for b in self.buffers], None
         self.array = (_Tensor * max(self.n, 1))()
         for i, b in enumerate(self.buffers):
             d = self.array[i]
@@ -301,11 +306,23 @@ class TensorList:
 
     def set_grad(self, i, grad):
         self.array[i].grad = _ptr(grad)
+        device = _device(grad)
+        if device != self._lies_on[i]:
+            self._lies_on[i], self._devices = device, None
+
+    def grad_device(self):
+        """The device of all gradients, None where there are none.  The steps do not ask for it."""
+        if self._devices is None:
+            self._devices = set(self._lies_on) - {None}
+        if len(self._devices) > 1 or -1 in self._devices:
+            raise ValueError("gradients: tensors on one GPU")
+        return next(iter(self._devices), None)
 
     def slice(self, i):
         """A one-element list viewing tensor i (for per-tensor, gradient-release style calls)."""
         out = TensorList.__new__(TensorList)
         out.buffers, out.n = [self.buffers[i]], 1
+        out._lies_on, out._devices = [self._lies_on[i]], None
         out.array = (_Tensor * 1)()
         C.memmove(out.array, C.byref(self.array[i]), C.sizeof(_Tensor))
         return out
@@ -754,9 +771,8 @@ class GradList:
     def of(cls, params):
         """The gradients of a TensorList, clipped in place: at each call those that its steps take then, also behind a set_grad (a captured
         call keeps those that it was captured with).  As for the steps, their memory is the caller's to keep."""
-        if any(getattr(b, "grad", None) is not None and not b.grad.is_cuda for b in params.buffers):
-            raise ValueError("gradients: tensors on the GPU")
         out = cls([])
+        out.device = params.grad_device()
         out.n = params.n
         out.array = (_Gradient * max(out.n, 1))()
         for d, t in zip(out.array, params.array[:params.n]):
@@ -766,6 +782,7 @@ class GradList:
         return out
 
     def follow(self):
+        self.device = self.params.grad_device()
         (_fast or _marshal()).follow(self.args[0], C.addressof(self.params.array), self.n)
 
 

@@ -63,3 +63,27 @@ def test_a_list_of_tensors_stays_as_it_is(seen):
     grads = fo.GradList([Whole(0x1000), Whole(0x2000)])
     fo.grad_norm(grads, 1.0, Factor())
     assert seen == [[(0x1000, 0x1000, 8), (0x2000, 0x2000, 8)]]
+
+
+def test_parameters_on_another_device_than_the_factor_are_refused(seen):
+    for grads in ((Tensor(0x1000, 1), Tensor(0x2000, 1)), (None, Tensor(0x2000, 1))):
+        followed = fo.GradList.of(parameters(*grads))
+        for call in (lambda: fo.grad_norm(followed, 1.0, Factor()), lambda: fo.clip_gradients(followed, Factor())):
+            with pytest.raises(ValueError):
+                call()
+    for grads in ((Tensor(0x1000), Tensor(0x2000, 1)), (Tensor(0x1000, -1),)):
+        with pytest.raises(ValueError):
+            fo.GradList.of(parameters(*grads))
+    # and where a gradient comes later: from another device, from the host, and back
+    params = parameters(Tensor(0x1000), Tensor(0x2000), None)
+    for of in (params, params.slice(1)):
+        followed, last = fo.GradList.of(of), of.n - 1
+        for device, good in ((0, True), (1, False), (0, True), (-1, False), (0, True)):
+            of.set_grad(last, Tensor(0x4000, device))
+            if good:
+                fo.grad_norm(followed, 1.0, Factor())
+                continue
+            with pytest.raises(ValueError):
+                fo.grad_norm(followed, 1.0, Factor())
+    assert len(seen) == 6
+    fo.grad_norm(fo.GradList.of(parameters()), 1.0, Factor(1))
