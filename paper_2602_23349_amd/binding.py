@@ -386,8 +386,17 @@ def _as_list(tensors):
     return tensors if isinstance(tensors, TensorList) else TensorList(tensors)
 
 
+def _on_current(factor):
+    """(launches go to the current device)"""
+    if factor.device != (_raw_current_device or torch.cuda.current_device)():
+        raise ValueError("the factor lies on another device than the current one")
+
+
 def _clipped(name, tl, hp, clip, stream):
     call = f"flashoptim_{name}_clipped"
+    _on_current(clip)
+    if tl.grad_device() not in (None, clip.device):
+        raise ValueError("the gradients and the factor lie on different devices")
     _check(getattr(load_library(), call)(tl.array, tl.n, hp, clip.address, _stream_handle(stream)), call)
 
 
@@ -821,6 +830,7 @@ def grad_norm(grads, max_norm, factor, workspace=None, stream=None):
 
 def clip_factor_from_sum(factor, max_norm, stream=None):
     """norm and scale of `factor` from its sum_squares as it is now."""
+    _on_current(factor)
     _check(load_library().flashoptim_clip_factor_from_sum(factor.address, max_norm, _stream_handle(stream)), "flashoptim_clip_factor_from_sum")
 
 

@@ -87,3 +87,28 @@ def test_parameters_on_another_device_than_the_factor_are_refused(seen):
                 fo.grad_norm(followed, 1.0, Factor())
     assert len(seen) == 6
     fo.grad_norm(fo.GradList.of(parameters()), 1.0, Factor(1))
+
+
+STEPS = {"adamw_step": (0.9, 0.99, 1e-8, 1), "adamw_step_exact": (0.9, 0.99, 1e-8, 1), "sgd_step": (0.9,), "lion_step": (0.9, 0.99)}
+
+
+def test_a_factor_on_another_device_than_the_current_one_is_refused(monkeypatch):
+    calls = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: calls.append(name) or 0
+    monkeypatch.setattr(B, "load_library", lambda: Library())
+    monkeypatch.setattr(B, "_raw_current_device", lambda: 0)
+    with pytest.raises(ValueError):
+        fo.clip_factor_from_sum(Factor(1), 1.0, stream=0)
+    fo.clip_factor_from_sum(Factor(0), 1.0, stream=0)
+    here, there, mixed = (parameters(*[Tensor(0x1000 * (i + 1), d) for i, d in enumerate(on)]) for on in ((0, 0), (1, 1), (0, 1)))
+    for name, hp in STEPS.items():
+        step = getattr(fo, name)
+        for tensors, factor in ((here, 1), (there, 1), (there, 0), (mixed, 0)):
+            with pytest.raises(ValueError):
+                step(tensors, *hp, stream=0, clip=Factor(factor))
+        step(here, *hp, stream=0, clip=Factor(0))
+        step(there, *hp, stream=0)                                   # without a factor the steps do not ask
+    assert calls == ["flashoptim_clip_factor_from_sum"] + [f"flashoptim_{name}{end}" for name in STEPS for end in ("_clipped", "")]
