@@ -229,6 +229,10 @@ def _stream_handle(stream):
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _current_device():
+    return (_raw_current_device or torch.cuda.current_device)()
+
+
 def _stream(stream):
     return C.c_void_p(_stream_handle(stream))
 
@@ -386,15 +390,16 @@ def _as_list(tensors):
     return tensors if isinstance(tensors, TensorList) else TensorList(tensors)
 
 
-def _on_current(factor):
+def _on_current(factor, stream):
     """(launches go to the current device)"""
-    if factor.device != (_raw_current_device or torch.cuda.current_device)():
+    if factor.device != _current_device():
         raise ValueError("the factor lies on another device than the current one")
+    _check_stream(stream)
 
 
 def _clipped(name, tl, hp, clip, stream):
     call = f"flashoptim_{name}_clipped"
-    _on_current(clip)
+    _on_current(clip, stream)
     if tl.grad_device() not in (None, clip.device):
         raise ValueError("the gradients and the factor lie on different devices")
     _check(getattr(load_library(), call)(tl.array, tl.n, hp, clip.address, _stream_handle(stream)), call)
@@ -568,6 +573,20 @@ def _handle(stream):
     return None if stream is None else _stream_handle(stream)
 
 
+def _check_stream(stream):
+    """(losses, and calls on gradients: their tensors and their stream are the current device's)"""
+    device = getattr(stream, "device_index", None)
+    if device is not None and device != _current_device():
+        raise ValueError("the stream is another device's than the current one")
+
+
+def _handle_here(stream):
+    if stream is None:
+        return None
+    _check_stream(stream)
+    return _stream_handle(stream)
+
+
 class Mx4Tensor:
     """A matrix of rows by cols values in microscaled 4 bits: `codes` [rows, 128 ceil(cols/256)] and `scales`
     [rows, 16 ceil(cols/512)], both uint8, laid out as flashoptim.h describes.  A new one is a matrix of
@@ -693,14 +712,14 @@ def token_logprob_workspace(logits):
 def token_logprob(logits, tokens, logprob=None, lse=None, temperature=1.0, logprob64=None, workspace=None, stream=None):
     """logprob [rows] <- the log-probability of each row's token (int64, negative: the row does not count), logprob64 the same in float64,
     lse <- the log of the row's sum of exponentials, for the backward pass; what is None is left out."""
-    status = (_fast or _marshal()).logprob(logits, tokens, temperature, logprob, logprob64, lse, workspace, _handle(stream))
+    status = (_fast or _marshal()).logprob(logits, tokens, temperature, logprob, logprob64, lse, workspace, _handle_here(stream))
     if status:
         raise FlashOptimError(status, "flashoptim_token_logprob")
 
 
 def token_logprob_backward(logits, tokens, lse, dlogprob, dlogits, temperature=1.0, stream=None):
     """dlogits <- the gradient of the logits (which it may replace in their memory) from that of the log-probabilities."""
-    status = (_fast or _marshal()).logprob_backward(logits, tokens, temperature, lse, dlogprob, dlogits, _handle(stream))
+    status = (_fast or _marshal()).logprob_backward(logits, tokens, temperature, lse, dlogprob, dlogits, _handle_here(stream))
     if status:
         raise FlashOptimError(status, "flashoptim_token_logprob_backward")
 
@@ -722,7 +741,7 @@ def policy_loss(spec, logits, tokens, advantages, stats, old_logprob=None, ref_l
     """stats [4] <- the loss, its surrogate, KL and clipped parts; logprob [rows] and the gradient dlogits (which may replace the logits
     in their memory) where they are not None."""
     status = (_fast or _marshal()).policy(spec.address, logits, tokens, advantages, old_logprob, ref_logprob, weights, stats, logprob, dlogits,
-                                          workspace, _handle(stream))
+                                          workspace, _handle_here(stream))
     if status:
         raise FlashOptimError(status, "flashoptim_policy_loss")
 
@@ -739,7 +758,7 @@ class PreferenceLoss:
 def preference_loss(spec, logprob, offsets, loss, ref_logprob=None, weights=None, margins=None, dlogprob=None, stream=None):
     """loss [1] <- the mean over pairs of sequences, sequence i being the rows offsets[i] .. offsets[i + 1] - 1 of logprob (float32, or
     float64 as token_logprob leaves it in logprob64); margins [pairs] and the gradient dlogprob [rows] where they are not None."""
-    status = (_fast or _marshal()).preference(spec.address, logprob, offsets, loss, ref_logprob, weights, margins, dlogprob, _handle(stream))
+    status = (_fast or _marshal()).preference(spec.address, logprob, offsets, loss, ref_logprob, weights, margins, dlogprob, _handle_here(stream))
     if status:
         raise FlashOptimError(status, "flashoptim_preference_loss")
 
@@ -823,21 +842,21 @@ def _ready(grads, factor):
 def grad_norm(grads, max_norm, factor, workspace=None, stream=None):
     """factor (ClipFactor) <- the norm of all gradients of a GradList, and max_norm / norm where that is less than 1."""
     _ready(grads, factor)
-    status = (_fast or _marshal()).grad_norm(*grads.args, factor.device, max_norm, factor.address, workspace, _handle(stream))
+    status = (_fast or _marshal()).grad_norm(*grads.args, factor.device, max_norm, factor.address, workspace, _handle_here(stream))
     if status:
         raise FlashOptimError(status, "flashoptim_grad_norm")
 
 
 def clip_factor_from_sum(factor, max_norm, stream=None):
     """norm and scale of `factor` from its sum_squares as it is now."""
-    _on_current(factor)
+    _on_current(factor, stream)
     _check(load_library().flashoptim_clip_factor_from_sum(factor.address, max_norm, _stream_handle(stream)), "flashoptim_clip_factor_from_sum")
 
 
 def clip_gradients(grads, factor, stream=None):
     """The destinations of a GradList <- its gradients times the factor's scale."""
     _ready(grads, factor)
-    status = (_fast or _marshal()).clip(*grads.args, factor.device, factor.address, _handle(stream))
+    status = (_fast or _marshal()).clip(*grads.args, factor.device, factor.address, _handle_here(stream))
     if status:
         raise FlashOptimError(status, "flashoptim_clip_gradients")
 

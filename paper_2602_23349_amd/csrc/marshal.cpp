@@ -38,7 +38,7 @@ struct Args {
     PyObject* const* at;
     Py_ssize_t n, i = 0;
     bool failed = false;
-    const bool one_device;               // all tensors lie on one device, that of the current stream where no other is given
+    const bool one_device;               // all tensors lie on one device, the current one
     int64_t device = -1;
 
     Args(PyObject* const* args, Py_ssize_t count, Py_ssize_t expected, bool one_device_ = false) : at(args), n(count), one_device(one_device_) {
@@ -61,8 +61,9 @@ struct Args {
         const at::Tensor* t = &THPVariable_Unpack(o);
         if (!t->is_cuda()) fail(PyExc_ValueError, "%s: not on the GPU", name);
         if (one_device && !failed) {
-            if (device >= 0 && device != t->get_device()) fail(PyExc_ValueError, "%s: on another device than the others", name);
-            device = t->get_device();
+            const int64_t on = t->get_device();      // (may run Python, so ahead of any error)
+            if (device >= 0 && device != on) fail(PyExc_ValueError, "%s: on another device than the others", name);
+            device = on;
         }
         return failed ? nullptr : t;
     }
@@ -129,24 +130,20 @@ struct Args {
         }
         return failed ? nullptr : reinterpret_cast<const T*>((uintptr_t)v);
     }
-    // A stream's handle, or None for the current stream of the current device.
+    // A stream's handle, or None for the current stream of the current device.  A call whose tensors lie on one device runs on that one only.
     void* stream() {
         PyObject* o = next();
         if (failed) return nullptr;
-        if (o != Py_None) {
-            void* v = PyLong_AsVoidPtr(o);
-            failed = PyErr_Occurred() != nullptr;
-            return v;
-        }
-        PyObject* current = PyObject_CallNoArgs(current_device);
+        PyObject* current = o == Py_None || (one_device && device >= 0) ? PyObject_CallNoArgs(current_device) : nullptr;
         if (current && one_device && device >= 0 && PyLong_AsLongLong(current) != device) fail(PyExc_ValueError, "%s", "the tensors lie on another device than the current one");
-        PyObject* handle = current && !failed ? PyObject_CallOneArg(current_stream, current) : nullptr;
+        PyObject* handle = o != Py_None ? Py_NewRef(o) : current && !failed ? PyObject_CallOneArg(current_stream, current) : nullptr;
         Py_XDECREF(current);
         if (!handle) {
             failed = true;
             return nullptr;
         }
         void* v = PyLong_AsVoidPtr(handle);
+        failed = failed || PyErr_Occurred() != nullptr;
         Py_DECREF(handle);
         return v;
     }

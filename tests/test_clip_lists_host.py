@@ -1,8 +1,10 @@
 """Lists of gradients that follow a list of parameters, without a GPU: what a call is given is looked at instead of the call itself."""
+import ctypes as C
 import types
 
 import pytest
 import torch
+from torch._subclasses import FakeTensorMode
 
 import paper_2602_23349_amd as fo
 from paper_2602_23349_amd import _marshal as M
@@ -112,3 +114,66 @@ def test_a_factor_on_another_device_than_the_current_one_is_refused(monkeypatch)
         step(here, *hp, stream=0, clip=Factor(0))
         step(there, *hp, stream=0)                                   # without a factor the steps do not ask
     assert calls == ["flashoptim_clip_factor_from_sum"] + [f"flashoptim_{name}{end}" for name in STEPS for end in ("_clipped", "")]
+
+
+@pytest.fixture
+def marshal(monkeypatch):
+    """The C++ module with the library's entry points, the current device being 0."""
+    names = [n for n in B.EXPORTED_SYMBOLS if n.startswith(("flashoptim_mx4_", "flashoptim_block_norm", "flashoptim_token_logprob", "flashoptim_policy_loss",
+                                                            "flashoptim_preference_loss", "flashoptim_grad_norm", "flashoptim_clip_gradients"))]
+    M.bind({n: C.cast(getattr(fo.load_library(), n), C.c_void_p).value for n in names}, lambda device: 0, lambda: 0)
+    monkeypatch.setattr(B, "_fast", M)
+    monkeypatch.setattr(B, "_raw_current_device", lambda: 0)
+
+
+class Stream:
+    cuda_stream = 0
+
+    def __init__(self, device):
+        self.device_index = device
+
+
+def test_another_device_is_refused_on_a_given_stream_too(marshal):
+    class Whole(Tensor):
+        is_contiguous, numel = (lambda self: True), (lambda self: 8)
+    for device, streams in ((1, (0, Stream(0), Stream(1))), (0, (Stream(1),))):
+        grads, factor = fo.GradList([Whole(0x1000, device)]), Factor(device)
+        for stream in streams:
+            with pytest.raises(ValueError, match="device"):
+                fo.grad_norm(grads, 1.0, factor, stream=stream)
+            with pytest.raises(ValueError, match="device"):
+                fo.clip_gradients(grads, factor, stream=stream)
+            with pytest.raises(ValueError, match="device"):
+                fo.clip_factor_from_sum(factor, 1.0, stream=stream)
+    with pytest.raises(ValueError, match="device"):
+        fo.adamw_step(parameters(Tensor(0x1000)), 0.9, 0.99, 1e-8, 1, stream=Stream(1), clip=Factor(0))
+
+
+@pytest.mark.filterwarnings("ignore")
+def test_logits_on_another_device_are_refused(marshal):
+    # tensors on GPUs that exist in name only: they are refused before anything asks for their memory
+    policy, preference = fo.PolicyLoss(), fo.PreferenceLoss()
+    with FakeTensorMode():
+        def calls(x, tokens, vec, wide, cuts, stream):
+            return [lambda: fo.token_logprob(x, tokens, vec, vec, stream=stream), lambda: fo.token_logprob(x, tokens, logprob64=wide, stream=stream),
+                    lambda: fo.token_logprob_backward(x, tokens, vec, vec, x, stream=stream),
+                    lambda: fo.policy_loss(policy, x, tokens, vec, vec, dlogits=x, stream=stream),
+                    lambda: fo.preference_loss(preference, vec, cuts, vec[:1], stream=stream)]
+        on = [(torch.empty(4, 64, dtype=torch.bfloat16, device=d), torch.zeros(4, dtype=torch.int64, device=d), torch.empty(4, device=d),
+               torch.empty(4, dtype=torch.float64, device=d), torch.zeros(3, dtype=torch.int64, device=d)) for d in ("cuda:0", "cuda:1")]
+        for tensors, streams in ((on[1], (None, 0, Stream(0), Stream(1))), (on[0], (Stream(1),))):
+            for stream in streams:
+                for call in calls(*tensors, stream):
+                    with pytest.raises(ValueError, match="device"):
+                        call()
+        for k in range(5):
+            mixed = [on[1 if i == k else 0][i] for i in range(5)]
+            refused = 0
+            for call in calls(*mixed, 0):
+                try:
+                    call()
+                except ValueError as e:
+                    refused += "device" in str(e)
+                except Exception:                    # (no memory, where all lie on the current device)
+                    pass
+            assert refused == (4, 4, 4, 1, 1)[k], k
