@@ -485,7 +485,8 @@ int flashoptim_policy_loss(const flashoptim_policy_spec* spec, const flashoptim_
  * offsets [2 pairs + 1] INT64, not descending, within [0, rows] (what lies outside is taken as the nearest bound): sequence i is the rows
  * offsets[i] .. offsets[i + 1] - 1, possibly none.  order: sequences 2p and 2p + 1 are the chosen and the rejected one of pair p
  * (FLASHOPTIM_PAIRS_BY_TURNS), or p and pairs + p (FLASHOPTIM_PAIRS_HALVES).  Rows whose weight is 0 do not count, whatever their
- * logprob; weights, ref_logprob NULL: 1, 0.  No pairs: a loss of 0.  beta > 0, 0 <= label_smoothing <= 0.5, which is for SIGMOID only.
+ * logprob; weights, ref_logprob NULL: 1, 0.  (No tokens are seen here: a row of a negative one, which token_logprob leaves a logprob of 0, is a
+ * part of its sequence's gain, 0 - ref_logprob, unless its weight is 0.)  No pairs: a loss of 0.  beta > 0, 0 <= label_smoothing <= 0.5, which is for SIGMOID only.
  * Sums are FP64.  rows < 2^31, pairs < 2^30. */
 enum { FLASHOPTIM_PREFERENCE_SIGMOID = 0, FLASHOPTIM_PREFERENCE_HINGE = 1, FLASHOPTIM_PREFERENCE_SQUARED = 2 };
 enum { FLASHOPTIM_PAIRS_BY_TURNS = 0, FLASHOPTIM_PAIRS_HALVES = 1 };

@@ -757,7 +757,8 @@ class PreferenceLoss:
 
 def preference_loss(spec, logprob, offsets, loss, ref_logprob=None, weights=None, margins=None, dlogprob=None, stream=None):
     """loss [1] <- the mean over pairs of sequences, sequence i being the rows offsets[i] .. offsets[i + 1] - 1 of logprob (float32, or
-    float64 as token_logprob leaves it in logprob64); margins [pairs] and the gradient dlogprob [rows] where they are not None."""
+    float64 as token_logprob leaves it in logprob64); margins [pairs] and the gradient dlogprob [rows] where they are not None.  Rows that do not
+    count, those of negative tokens among them, have the weight 0."""
     status = (_fast or _marshal()).preference(spec.address, logprob, offsets, loss, ref_logprob, weights, margins, dlogprob, _handle_here(stream))
     if status:
         raise FlashOptimError(status, "flashoptim_preference_loss")

@@ -68,3 +68,23 @@ def test_an_advantage_of_0_has_no_surrogate(rows, vocab, dtype):
     old[3] = float("nan")
     got = call(c, fo.PolicyLoss(), old_logprob=old, weights=w)
     assert bool(torch.isnan(got[0][0])) and bool(torch.isnan(got[2][3]).all())
+
+
+def test_rows_of_negative_tokens_have_no_weight_in_a_preference_loss():
+    # it sees no tokens: their logprob of 0 less the reference's is left out by the weight alone
+    c = Case(40, 300, BF16, masked=0.4, seed=42)
+    ref = (torch.randn(40, generator=torch.Generator().manual_seed(1)) - 6).cuda()
+    wide = torch.empty(40, dtype=torch.float64, device="cuda")
+    fo.token_logprob(c.logits, c.tokens, logprob64=wide, workspace=memory(fo.token_logprob_workspace(c.logits)))
+    there = c.tokens >= 0
+    cuts = torch.tensor([0, 9, 20, 33, 40], device="cuda")
+    kept = torch.cat([torch.zeros(1, dtype=torch.int64, device="cuda"), there.long().cumsum(0)])[cuts]
+    spec, loss, margins = fo.PreferenceLoss(), torch.empty(3, device="cuda"), torch.empty(3, 2, device="cuda")
+    slopes, some = torch.empty(40, device="cuda"), torch.empty(int(there.sum()), device="cuda")
+    fo.preference_loss(spec, wide, cuts, loss[:1], ref_logprob=ref, weights=there.float(), margins=margins[0], dlogprob=slopes)
+    fo.preference_loss(spec, wide[there], kept, loss[1:2], ref_logprob=ref[there], margins=margins[1], dlogprob=some)
+    # (the same values in FP64 sums of another order)
+    assert torch.allclose(margins[0], margins[1], rtol=2.0 ** -22, atol=0) and torch.allclose(loss[0], loss[1], rtol=2.0 ** -22, atol=0)
+    assert torch.allclose(slopes[there], some, rtol=2.0 ** -22, atol=0) and not bool(slopes[~there].any())
+    fo.preference_loss(spec, wide, cuts, loss[2:], ref_logprob=ref, margins=margins[2])
+    assert bool(((margins[2] - margins[0]).abs() > 0.1).all())
