@@ -13,13 +13,13 @@ namespace fo {
 constexpr int kGradThreads = 256;
 constexpr int kGradTile = 8192;
 
-// A launch's tensors, as they travel in its arguments.  `first[i]` is tensor i's first tile, counted within the launch; `lack[i]` the elements that its last
-// tile is short of.
+// A launch's tensors, as they travel in its arguments.  `first[i]` is tensor i's first tile, counted within the launch, and behind the last
+// tensor all its tiles; `lack[i]` the elements that its last tile is short of.  What is left of the tables is not used.
 template <int N, bool DST>
 struct GradTable {
     const void* src[N];
     void* dst[DST ? N : 1];
-    uint32_t first[N + 1];      // behind the launch's last tensor, and in what is left of the table: all its tiles
+    uint32_t first[N + 1];
     uint16_t lack[N];
 };
 // As many as the 4 KB of a launch's arguments hold, or few, for which the host has fewer bytes to copy.

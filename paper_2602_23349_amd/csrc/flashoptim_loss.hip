@@ -214,7 +214,8 @@ struct Held {
         }
         return {sum_of_wave(near + (double)sum), most};
     }
-    // Stores -d p, or d (1 - p) for the token, of all that is held: p = 2^((x - base) c - shift).
+    // Stores -d p, or d (1 - p) for the token, of all that is held: p = 2^((x - base) c - shift).  (c is the factor in one part, off by 2^-24 of itself, or 2^-23 where it
+    // is the sums' first part: p is off by as much of |x - base| / T.)
     __device__ __forceinline__ void store_gradient(char* row, int32_t token, float d, float base, float c, float shift) {
         const Pass pass;
         asm volatile("" : "+v"(lane));
@@ -456,7 +457,7 @@ __global__ __launch_bounds__(kFewRows * 64) void policy_few_rows_kernel(RowsArgs
 // LDS holds, are on their way there while this one is worked on and stored, so that the memory is not idle between two rows.  (4096 rows of 128256 BF16 values
 // 440-453 us without, 391-402 with; half as many words ahead 393-403.  Smaller shapes, of which a unit holds two or more rows, are no faster by it, or slower.)
 // A wavefront fetches and reads its own words, so that nothing but the sums is shared.  Vector loads arrive in order: what is needed while the words are on their
-// way comes as scalars or ahead of them, and nothing but the row's own loads is waited for.  What a workgroup leaves for the statistics are
+// way comes as scalars or ahead of them.  A row's start waits for its own loads, and with them (one counter has both) for the stores of the row before.  What a workgroup leaves for the statistics are
 // the sums of its rows' terms (4096 rows of 128256 BF16 values 392.7 us with each row's, 391.3 so; 1001 of 50257 FP32 values 85.1 and 84.6).
 template <bool FP32>
 __global__ __launch_bounds__(1024) void policy_long_rows_kernel(RowsArgs a) {
