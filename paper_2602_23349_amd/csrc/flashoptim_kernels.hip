@@ -986,7 +986,7 @@ struct VariantArgs : TensorArgs<DIRECT, KIND == 0>, KindConsts<KIND> {
     explicit VariantArgs(const StepArgs& a) : TensorArgs<DIRECT, KIND == 0>(a.single), KindConsts<KIND>(a) {}
 };
 // A clipped step's: the word that holds the factor of the gradients.  NaN: the step leaves weights and states as they are.  (Without and with it, us: AdamW on
-// GPT-2's list 244.3 and 245.3, on a Llama layer 427 and 430, Lion 189.0 and 188.6, 334 and 336, SGD 189.6 and 189.4, 332 and 335; gradients clipped in place ahead of the step instead 334 and
+// GPT-2's list 244.3 and 245.3, on a Llama layer 427 and 430, Lion 189.0 and 188.6, 334 and 336; gradients clipped in place ahead of the step instead 334 and
 // 575, 280 and 477.)
 template <int KIND, bool DIRECT, bool M_HAT, bool THROUGH>
 struct ClippedArgs : VariantArgs<KIND, DIRECT, M_HAT, THROUGH> {
